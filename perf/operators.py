@@ -161,13 +161,13 @@ def _chosen(s):
         p = 1.0 / (1.0 + torch.exp(-logits))
     key = p if s["bias"] is None else p + s["bias"]
     ids = torch.sort(key, dim=1, descending=True, stable=True).indices[:, : s["top_k"]]
-    there = key.gather(1, ids) > -math.inf
+    there = key.gather(1, ids) != -math.inf
     if s["active"] is not None:
         there &= s["active"][:, None]
     weights = torch.where(there, p.gather(1, ids), 0.0)
     if s["renormalize"]:
         total = weights.sum(dim=1, keepdim=True)
-        weights = torch.where(total > 0, weights / total, 0.0)
+        weights = torch.where(total == 0, 0.0, weights / total)
     return torch.where(there, ids, -1).int(), weights * s["factor"]
 
 
