@@ -378,6 +378,77 @@ int oz2_host_product_residues(int index, int64_t count, const int32_t* products,
 /* The same as the large tiles take it for inner dimensions up to 1024 (|product| <= 2^24). */
 int oz2_host_short_product_residues(int index, int64_t count, const int32_t* products, uint8_t* res_out);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Products with weights that are held in 4 bits, for few vectors at a time (one token of a decoder to a small batch).
+ *
+ * A matrix W (n x k) is stored as codes of 4 bits with one scale, and if wanted one zero point, for each group of `group` neighbours in
+ * a row:   w_il = s_ig (q_il - z_ig),  g = floor(l / group),  q in 0 .. 15,  z = 8 where there are no zero points.
+ *   codes   row i starts at codes + i ld_codes; its element l is the low (even l) or high (odd l) half of byte floor(l / 2).
+ *           Bytes of a row beyond ceil(k / 2) and the last half byte of an odd k are never used (the former not read).
+ *   scales  element (i, g) is scales[i ld_scales + g], of type scale_type;  zeros (or NULL) likewise, a byte each
+ *   group   32, 64 or a multiple of 128; the last group of a row may be short
+ *   count   matrices in a stack; matrix e starts stride_codes bytes, stride_scales and stride_zeros elements after matrix e - 1
+ * No alignment beyond that of the element types is needed (rows whose codes start at multiples of 16 bytes are read fastest).
+ *
+ * Arithmetic: a product is the sum over groups of s_ig times the sum of (q - z) x over the group, in FP32 throughout; x is taken
+ * exactly whatever its type, and the result is rounded once.  Infinities and NaNs in x or s give what that formula gives.
+ * Results do not depend on timing: equal calls give equal bits. */
+#define OZ2_F32 0
+#define OZ2_BF16 1
+#define OZ2_F16 2
+typedef struct oz2_w4_matrix {
+  int64_t n, k, group;
+  const void* codes;
+  int64_t ld_codes;
+  const void* scales;
+  int64_t ld_scales;
+  const void* zeros;
+  int64_t ld_zeros;
+  int64_t count, stride_codes, stride_scales, stride_zeros;
+  int scale_type;
+} oz2_w4_matrix;
+
+/* Y := alpha W X + beta C with t vectors: X is k x t (leading dimension ldx, type x_type), C and Y are n x t of type y_type; C may be
+ * Y itself (ldc == ldy) and must not overlap it otherwise, and is not read where beta is 0 (then it may be NULL).  alpha == 0
+ * or k == 0 reads neither W nor X.  W describes one matrix (count, strides ignored).  Uses no workspace; may be captured into a graph. */
+int oz2_w4_matvec(const oz2_w4_matrix* W, int64_t t, float alpha, int x_type, const void* X, int64_t ldx, float beta, const void* C,
+                  int64_t ldc, int y_type, void* Y, int64_t ldy, void* stream);
+
+/* A layer of `count` gated experts (count of the three stacks) with its router, for t tokens x (columns of X):
+ *   logits  l_e = sum_i R_ei x_i, in FP32; row e of the router starts at element e ld_router
+ *   scores  p = softmax(l) or 1 / (1 + exp(-l));   keys p_e + bias_e  (bias may be NULL)
+ *   chosen  the top_k experts with the largest keys, in that order, equal keys by the lower index; a key of -infinity is never
+ *           chosen, so a token may have fewer; a NaN counts as the largest, and so reaches y
+ *   weights p of the chosen, divided by their sum where `renormalize` is set (all 0 if that is 0), times factor
+ *   y = sum over the chosen, in order, of  weight * down_e (act(gate_e x) * (up_e x)),   act = silu or gelu (with erf)
+ * gate and up are stacks of f x d, down of d x f.  The inner vectors of f values are kept in FP32. */
+#define OZ2_SCORE_SOFTMAX 0
+#define OZ2_SCORE_SIGMOID 1
+#define OZ2_ACT_SILU 0
+#define OZ2_ACT_GELU 1
+#define OZ2_MOE_MAX_EXPERTS 1024
+#define OZ2_MOE_MAX_TOP_K 32
+#define OZ2_MOE_MAX_TOKENS 4096
+typedef struct oz2_moe_layer {
+  oz2_w4_matrix gate, up, down;
+  const void* router;
+  int64_t ld_router;
+  const float* bias;
+  int router_type, top_k, score, renormalize, activation;
+  float factor;
+} oz2_moe_layer;
+
+/* Workspace that a call with t tokens takes from the registered one; 0 for an invalid layer or t. */
+size_t oz2_w4_moe_workspace_bytes(const oz2_moe_layer* layer, int64_t t);
+
+/* active: NULL, or t bytes; a token with 0 there is left out: its y is 0.  ids (int32) and weights (float), top_k x t without gaps, or
+ * NULL: the chosen experts and their weights, -1 and 0 in places that have none.  X: d x t, Y: d x t, which must not overlap X.
+ * Returns OZ2_ERR_WORKSPACE where the registered workspace (256-byte aligned) is too small. */
+int oz2_w4_moe(const oz2_moe_layer* layer, int64_t t, int x_type, const void* X, int64_t ldx, const uint8_t* active, int y_type, void* Y,
+               int64_t ldy, int32_t* ids, float* weights, void* stream);
+int oz2_context_w4_moe(oz2_context* ctx, const oz2_moe_layer* layer, int64_t t, int x_type, const void* X, int64_t ldx,
+                       const uint8_t* active, int y_type, void* Y, int64_t ldy, int32_t* ids, float* weights, void* stream);
+
 const char* oz2_status_string(int status);
 
 #ifdef __cplusplus

@@ -13,6 +13,7 @@ SYMBOLS = [
     "oz2_context_create", "oz2_context_destroy", "oz2_context_set_workspace", "oz2_context_set", "oz2_context_get",
     "oz2_context_workspace_bytes", "oz2_context_dgemm", "oz2_context_dsyrk", "oz2_context_dtrmm",
     "oz2_set_kblock", "oz2_set_round_sync", "oz2_set_shift_mode", "oz2_set_product_format", "oz2_set_bit_split", "oz2_set_nonfinite_check", "oz2_set_stage_events", "oz2_calibrate_mfma", "oz2_host_kernel_choice", "oz2_host_route", "oz2_host_crt_element", "oz2_host_crt_element_digits", "oz2_host_crt_element_wide_digits", "oz2_host_residues", "oz2_host_product_residues", "oz2_host_short_product_residues", "oz2_status_string",
+    "oz2_w4_matvec", "oz2_w4_moe_workspace_bytes", "oz2_w4_moe", "oz2_context_w4_moe",
 ]
 
 
@@ -80,6 +81,12 @@ def lib():
         L.oz2_host_residues.argtypes = [ci, ci, ctypes.c_double, ci, vp]
         L.oz2_host_product_residues.argtypes = [ci, i64, vp, vp]
         L.oz2_host_short_product_residues.argtypes = [ci, i64, vp, vp]
+        cf = ctypes.c_float
+        L.oz2_w4_matvec.argtypes = [vp, i64, cf, ci, vp, i64, cf, vp, i64, ci, vp, i64, vp]
+        L.oz2_w4_moe_workspace_bytes.restype = ctypes.c_size_t
+        L.oz2_w4_moe_workspace_bytes.argtypes = [vp, i64]
+        L.oz2_w4_moe.argtypes = [vp, i64, ci, vp, i64, vp, ci, vp, i64, vp, vp, vp]
+        L.oz2_context_w4_moe.argtypes = [vp, vp, i64, ci, vp, i64, vp, ci, vp, i64, vp, vp, vp]
         L.oz2_status_string.restype = ctypes.c_char_p
         L.oz2_status_string.argtypes = [ci]
         _lib = L
@@ -361,6 +368,22 @@ class Context:
                                        float(alpha), A_ptr, lda, B_ptr, ldb, num_moduli, _stream_ptr(stream)),
                "oz2_context_dtrmm")
 
+    def allocate_moe_workspace(self, layer, tokens, device="cuda:0"):
+        """A workspace for w4_moe with up to that many tokens; any other that the context had is let go."""
+        import torch
+        nbytes = int(lib().oz2_w4_moe_workspace_bytes(layer.ref, tokens))
+        if nbytes == 0:
+            raise Oz2Error("invalid layer or number of tokens")
+        buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
+        off = (-buf.data_ptr()) % 256
+        _check(lib().oz2_context_set_workspace(self.handle, buf.data_ptr() + off, nbytes), "oz2_context_set_workspace")
+        self.buf = buf
+        return nbytes
+
+    def w4_moe(self, layer, x, active=None, out=None, ids=None, weights=None, stream=None):
+        """(y, ids, weights) of a MoeLayer for x (tokens, d); see w4_moe."""
+        return _w4_moe(lib().oz2_context_w4_moe, "oz2_context_w4_moe", (self.handle,), layer, x, active, out, ids, weights, stream)
+
     def close(self):
         if self.handle:
             lib().oz2_context_destroy(self.handle)
@@ -425,3 +448,147 @@ def dgemm(A, B, num_moduli, C=None, workspace=None):
         workspace = Workspace(m, n, k, num_moduli, device=A.device)
     oz2_dgemm(m, n, k, A.data_ptr(), max(1, m), B.data_ptr(), max(1, k), C.data_ptr(), max(1, m), num_moduli)
     return C
+
+
+OZ2_F32, OZ2_BF16, OZ2_F16 = range(3)
+OZ2_SCORE_SOFTMAX, OZ2_SCORE_SIGMOID = range(2)
+OZ2_ACT_SILU, OZ2_ACT_GELU = range(2)
+
+
+class _W4(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_int64) for f in ("n", "k", "group")] + [("codes", ctypes.c_void_p), ("ld_codes", ctypes.c_int64),
+                ("scales", ctypes.c_void_p), ("ld_scales", ctypes.c_int64), ("zeros", ctypes.c_void_p), ("ld_zeros", ctypes.c_int64)] +
+                [(f, ctypes.c_int64) for f in ("count", "stride_codes", "stride_scales", "stride_zeros")] + [("scale_type", ctypes.c_int)])
+
+
+class _Moe(ctypes.Structure):
+    _fields_ = ([(f, _W4) for f in ("gate", "up", "down")] + [("router", ctypes.c_void_p), ("ld_router", ctypes.c_int64), ("bias", ctypes.c_void_p)] +
+                [(f, ctypes.c_int) for f in ("router_type", "top_k", "score", "renormalize", "activation")] + [("factor", ctypes.c_float)])
+
+
+_types = {}
+
+
+def _type(dtype):
+    if not _types:
+        import torch
+        _types.update({torch.float32: OZ2_F32, torch.bfloat16: OZ2_BF16, torch.float16: OZ2_F16})
+    if dtype not in _types:
+        raise Oz2Error("float32, bfloat16 or float16 wanted, got %s" % dtype)
+    return _types[dtype]
+
+
+def _on_device(device, **tensors):
+    if device.type != "cuda":
+        raise Oz2Error("tensors on the GPU wanted, got %s" % device)
+    for name, v in tensors.items():
+        if v is not None and v.device != device:
+            raise Oz2Error("%s is on %s, not on %s" % (name, v.device, device))
+
+
+class W4Matrix:
+    """A matrix held in 4 bits, or a stack of them (include/oz2.h): codes (.., n, bytes) uint8 with two codes to a byte, scales (.., n, groups)
+    in float32, bfloat16 or float16, zeros (.., n, groups) uint8 or None.  The last dimension of each is without gaps; the object
+    keeps the tensors."""
+
+    def __init__(self, codes, scales, zeros=None, k=None, group=128):
+        import torch
+        parts = [codes, scales] + ([] if zeros is None else [zeros])
+        if codes.dtype != torch.uint8 or (zeros is not None and zeros.dtype != torch.uint8):
+            raise Oz2Error("codes and zeros are uint8")
+        if codes.dim() not in (2, 3) or any(v.dim() != codes.dim() or v.shape[:-1] != codes.shape[:-1] for v in parts):
+            raise Oz2Error("codes, scales and zeros are (n, .) or (count, n, .) alike")
+        if any(v.shape[-1] > 1 and v.stride(-1) != 1 for v in parts):
+            raise Oz2Error("the last dimension of codes, scales and zeros is contiguous")
+        k = 2 * codes.shape[-1] if k is None else int(k)
+        if group < 1 or k < 0 or codes.shape[-1] < (k + 1) // 2 or any(v.shape[-1] < -(-k // group) for v in parts[1:]):
+            raise Oz2Error("codes, scales or zeros have too few columns for k = %d, group = %d" % (k, group))
+        if any(v.device != codes.device for v in parts):
+            raise Oz2Error("codes, scales and zeros are on different devices")
+        self.codes, self.scales, self.zeros = codes, scales, zeros
+        self.n, self.k, self.count, self.device = codes.shape[-2], k, codes.shape[0] if codes.dim() == 3 else 1, codes.device
+        over = [v.stride(0) if v.dim() == 3 else 0 for v in parts] + [0]
+        self.struct = _W4(self.n, k, group, codes.data_ptr(), codes.stride(-2), scales.data_ptr(), scales.stride(-2),
+                          None if zeros is None else zeros.data_ptr(), 0 if zeros is None else zeros.stride(-2), self.count, *over[:3],
+                          _type(scales.dtype))
+        self.ref = ctypes.addressof(self.struct)
+
+
+def _rows(name, x, width):
+    """leading dimension of a (rows, width) tensor whose rows are contiguous"""
+    if x.dim() != 2 or x.shape[1] != width or (width > 1 and x.stride(1) != 1):
+        raise Oz2Error("%s is (tokens, %d) with contiguous rows, got shape %s" % (name, width, tuple(x.shape)))
+    return max(x.stride(0), width)
+
+
+def w4_matvec(W, x, alpha=1.0, beta=0.0, c=None, out=None, stream=None):
+    """alpha W x + beta c for every row of x (tokens, k), as (tokens, n) in the type of `out`, or of x where it is None; c is like the result."""
+    import torch
+    if out is None:
+        out = torch.empty((x.shape[0], W.n), dtype=x.dtype, device=x.device)
+    if not x.is_cuda or W.device != x.device or out.device != x.device or (c is not None and c.device != x.device):
+        _on_device(W.device, x=x, out=out, c=c)
+    ldx, ldy = _rows("x", x, W.k), _rows("out", out, W.n)
+    if out.shape[0] != x.shape[0] or (c is not None and (c.dtype != out.dtype or c.shape[0] != x.shape[0])):
+        raise Oz2Error("x, c and out have the same number of tokens, c and out the same type")
+    if W.count != 1:
+        raise Oz2Error("one matrix wanted, not a stack")
+    rc = lib().oz2_w4_matvec(W.ref, x.shape[0], alpha, _type(x.dtype), x.data_ptr(), ldx, beta, None if c is None else c.data_ptr(),
+                             0 if c is None else _rows("c", c, W.n), _type(out.dtype), out.data_ptr(), ldy, _stream_ptr(stream))
+    _check(rc, "oz2_w4_matvec")
+    return out
+
+
+class MoeLayer:
+    """A layer of gated experts on stacks of W4Matrix (include/oz2.h): router (experts, d), gate and up f x d, down d x f, bias (experts,)
+    float32 or None.  The object keeps the tensors."""
+
+    def __init__(self, router, gate, up, down, top_k, bias=None, score="softmax", renormalize=True, factor=1.0, activation="silu"):
+        import torch
+        if router.dim() != 2 or router.shape != (gate.count, gate.k) or (gate.k > 1 and router.stride(1) != 1):
+            raise Oz2Error("router is (experts, d) = (%d, %d) with contiguous rows" % (gate.count, gate.k))
+        if (up.n, up.k, up.count) != (gate.n, gate.k, gate.count) or (down.n, down.k, down.count) != (gate.k, gate.n, gate.count):
+            raise Oz2Error("gate and up are f x d, down is d x f, each for every expert")
+        if bias is not None and (bias.dtype != torch.float32 or tuple(bias.shape) != (gate.count,) or not bias.is_contiguous()):
+            raise Oz2Error("bias is (experts,) in float32")
+        if any(v.device != gate.device for v in (router, up, down) + (() if bias is None else (bias,))):
+            raise Oz2Error("the parts of the layer are on different devices")
+        self.router, self.gate, self.up, self.down, self.bias = router, gate, up, down, bias
+        self.d, self.top_k, self.device = gate.k, int(top_k), gate.device
+        self.struct = _Moe(gate.struct, up.struct, down.struct, router.data_ptr(), max(router.stride(0), gate.k), None if bias is None else bias.data_ptr(),
+                           _type(router.dtype), self.top_k, ("softmax", "sigmoid").index(score), int(bool(renormalize)),
+                           ("silu", "gelu").index(activation), float(factor))
+        self.ref = ctypes.addressof(self.struct)
+
+
+def _w4_moe(call, name, first, layer, x, active, out, ids, weights, stream):
+    import torch
+    t = x.shape[0]
+    if out is None:
+        out = torch.empty((t, layer.d), dtype=x.dtype, device=x.device)
+    if ids is None:
+        ids = torch.empty((t, layer.top_k), dtype=torch.int32, device=x.device)
+    if weights is None:
+        weights = torch.empty((t, layer.top_k), dtype=torch.float32, device=x.device)
+    _on_device(layer.device, x=x, active=active, out=out, ids=ids, weights=weights)
+    ldx, ldy = _rows("x", x, layer.d), _rows("out", out, layer.d)
+    if out.shape[0] != t:
+        raise Oz2Error("x and out have the same number of tokens")
+    for what, v, dtype in (("ids", ids, torch.int32), ("weights", weights, torch.float32)):
+        if v.dtype != dtype or tuple(v.shape) != (t, layer.top_k) or not v.is_contiguous():
+            raise Oz2Error("%s is (tokens, top_k), %s, without gaps" % (what, dtype))
+    if active is not None and (active.dtype not in (torch.bool, torch.uint8) or tuple(active.shape) != (t,) or not active.is_contiguous()):
+        raise Oz2Error("active is (tokens,), bool or uint8")
+    _check(call(*first, layer.ref, t, _type(x.dtype), x.data_ptr(), ldx, None if active is None else active.data_ptr(), _type(out.dtype),
+                out.data_ptr(), ldy, ids.data_ptr(), weights.data_ptr(), _stream_ptr(stream)), name)
+    return out, ids, weights
+
+
+def w4_moe(layer, x, active=None, out=None, ids=None, weights=None, stream=None):
+    """(y, ids, weights) of a MoeLayer for x (tokens, d), in the workspace that set_workspace registered; tokens whose `active` is 0 get 0."""
+    return _w4_moe(lib().oz2_w4_moe, "oz2_w4_moe", (), layer, x, active, out, ids, weights, stream)
+
+
+def w4_moe_workspace_bytes(layer, tokens):
+    """Bytes that w4_moe takes of the registered workspace; 0 for an invalid layer or number of tokens."""
+    return int(lib().oz2_w4_moe_workspace_bytes(layer.ref, tokens))

@@ -6,6 +6,7 @@
 #include "oz2_bound.h"
 #include "oz2_internal.h"
 #include "oz2_route.h"
+#include "oz2_w4.h"
 
 namespace {
 
@@ -836,6 +837,90 @@ int oz2_host_product_residues(int index, int64_t count, const int32_t* products,
 
 int oz2_host_short_product_residues(int index, int64_t count, const int32_t* products, uint8_t* res_out) {
   return host_product_residues(index, count, products, res_out, oz2_host_short_product_residues_impl);
+}
+
+namespace {
+bool type_ok(int type) { return type == OZ2_F32 || type == OZ2_BF16 || type == OZ2_F16; }
+
+// A matrix (of a stack, if stacks are asked for) that the kernels can read: extents below 2^31, rows that do not overlap.
+bool w4_ok(const oz2_w4_matrix& w, bool stack) {
+  const int64_t lim = ((int64_t)1 << 31) - 65536;
+  if (w.n < 0 || w.k < 0 || w.n >= lim || w.k >= lim) return false;
+  if (w.group != 32 && w.group != 64 && (w.group < 128 || w.group % 128 != 0)) return false;
+  if (!type_ok(w.scale_type)) return false;
+  if (w.n == 0 || w.k == 0) return true;
+  const int64_t bytes = (w.k + 1) / 2, groups = (w.k + w.group - 1) / w.group;
+  if (!w.codes || !w.scales) return false;
+  // one row has no next one, so its pitch says nothing
+  if (w.n > 1 && (w.ld_codes < bytes || w.ld_scales < groups || (w.zeros && w.ld_zeros < groups))) return false;
+  if (!stack) return true;
+  if (w.count < 1) return false;
+  const int64_t rows = w.n - 1;
+  return w.count == 1 || (w.stride_codes >= rows * w.ld_codes + bytes && w.stride_scales >= rows * w.ld_scales + groups &&
+                          (!w.zeros || w.stride_zeros >= rows * w.ld_zeros + groups));
+}
+
+bool moe_ok(const oz2_moe_layer* m) {
+  if (!m || !w4_ok(m->gate, true) || !w4_ok(m->up, true) || !w4_ok(m->down, true)) return false;
+  const int64_t f = m->gate.n, d = m->gate.k, experts = m->gate.count;
+  if (d < 1 || f < 1 || experts < 1 || experts > OZ2_MOE_MAX_EXPERTS) return false;
+  if (m->up.n != f || m->up.k != d || m->up.count != experts) return false;
+  if (m->down.n != d || m->down.k != f || m->down.count != experts) return false;
+  if (!m->router || !type_ok(m->router_type) || (experts > 1 && m->ld_router < d)) return false;
+  if (m->top_k < 1 || m->top_k > OZ2_MOE_MAX_TOP_K || m->top_k > experts) return false;
+  if (m->score != OZ2_SCORE_SOFTMAX && m->score != OZ2_SCORE_SIGMOID) return false;
+  return m->activation == OZ2_ACT_SILU || m->activation == OZ2_ACT_GELU;
+}
+}  // namespace
+
+int oz2_w4_matvec(const oz2_w4_matrix* W, int64_t t, float alpha, int x_type, const void* X, int64_t ldx, float beta, const void* C,
+                  int64_t ldc, int y_type, void* Y, int64_t ldy, void* stream) {
+  if (!W) return -1;
+  oz2_w4_matrix w = *W;
+  if (alpha == 0.f) w.k = 0;
+  if (!w4_ok(w, false)) return -1;
+  if (t < 0 || t > 65535) return -2;
+  if (!type_ok(x_type)) return -4;
+  if (t > 1 && w.k > 0 && ldx < w.k) return -6;
+  if (beta != 0.f && t > 1 && ldc < (w.n > 1 ? w.n : 1)) return -9;
+  if (!type_ok(y_type)) return -10;
+  if (t > 1 && ldy < (w.n > 1 ? w.n : 1)) return -12;
+  if (w.n == 0 || t == 0) return OZ2_OK;
+  if (w.k > 0 && !X) return -5;
+  if (beta != 0.f && !C) return -8;
+  if (!Y) return -11;
+  return oz2_launch_w4_matvec(w, t, alpha, x_type, X, ldx, beta, C, ldc, y_type, Y, ldy, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? OZ2_OK : OZ2_ERR_HIP;
+}
+
+size_t oz2_w4_moe_workspace_bytes(const oz2_moe_layer* layer, int64_t t) {
+  if (!moe_ok(layer) || t < 0 || t > OZ2_MOE_MAX_TOKENS) return 0;
+  return oz2_w4_moe_space(*layer, t ? t : 1);
+}
+
+int oz2_w4_moe(const oz2_moe_layer* layer, int64_t t, int x_type, const void* X, int64_t ldx, const uint8_t* active, int y_type, void* Y,
+               int64_t ldy, int32_t* ids, float* weights, void* stream) {
+  if (!moe_ok(layer)) return -1;
+  if (t < 0 || t > OZ2_MOE_MAX_TOKENS) return -2;
+  if (!type_ok(x_type)) return -3;
+  if (t > 1 && ldx < layer->gate.k) return -5;
+  if (!type_ok(y_type)) return -7;
+  if (t > 1 && ldy < layer->gate.k) return -9;
+  if (t == 0) return OZ2_OK;
+  if (!X) return -4;
+  if (!Y) return -8;
+  State& s = state();
+  std::lock_guard<std::mutex> lock(s.mu);
+  if (!s.ws || s.ws_bytes < oz2_w4_moe_space(*layer, t)) return OZ2_ERR_WORKSPACE;
+  return oz2_launch_w4_moe(*layer, t, x_type, X, ldx, active, y_type, Y, ldy, ids, weights, s.ws, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? OZ2_OK : OZ2_ERR_HIP;
+}
+
+int oz2_context_w4_moe(oz2_context* ctx, const oz2_moe_layer* layer, int64_t t, int x_type, const void* X, int64_t ldx,
+                       const uint8_t* active, int y_type, void* Y, int64_t ldy, int32_t* ids, float* weights, void* stream) {
+  UseContext use(ctx);
+  const int rc = oz2_w4_moe(layer, t, x_type, X, ldx, active, y_type, Y, ldy, ids, weights, stream);
+  return rc < 0 ? rc - 1 : rc;
 }
 
 const char* oz2_status_string(int status) {
