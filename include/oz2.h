@@ -391,7 +391,8 @@ int oz2_host_short_product_residues(int index, int64_t count, const int32_t* pro
  * No alignment beyond that of the element types is needed (rows whose codes start at multiples of 16 bytes are read fastest).
  *
  * Arithmetic: a product is the sum over groups of s_ig times the sum of (q - z) x over the group, in FP32 throughout; x is taken
- * exactly whatever its type, and the result is rounded once.  Infinities and NaNs in x or s give what that formula gives.
+ * exactly whatever its type, and the result is rounded once.  Infinities and NaNs in x give what that formula gives; a scale that is not
+ * finite makes results of its row that are not finite.
  * Results do not depend on timing: equal calls give equal bits. */
 #define OZ2_F32 0
 #define OZ2_BF16 1

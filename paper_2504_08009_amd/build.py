@@ -24,6 +24,8 @@ EXTRA_FLAGS = {
     "oz2_stage3.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "oz2_stage2_tiles.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "oz2_thin.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "oz2_w4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "oz2_w4_moe.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 
 
