@@ -511,31 +511,53 @@ class W4Matrix:
         self.struct = _W4(self.n, k, group, codes.data_ptr(), codes.stride(-2), scales.data_ptr(), scales.stride(-2),
                           None if zeros is None else zeros.data_ptr(), 0 if zeros is None else zeros.stride(-2), self.count, *over[:3],
                           _type(scales.dtype))
-        self.ref = ctypes.addressof(self.struct)
+        self.ref, self.index = ctypes.addressof(self.struct), codes.get_device()
 
 
 def _rows(name, x, width):
     """leading dimension of a (rows, width) tensor whose rows are contiguous"""
-    if x.dim() != 2 or x.shape[1] != width or (width > 1 and x.stride(1) != 1):
+    if x.dim() != 2 or x.size(1) != width or (width > 1 and x.stride(1) != 1):
         raise Oz2Error("%s is (tokens, %d) with contiguous rows, got shape %s" % (name, width, tuple(x.shape)))
     return max(x.stride(0), width)
 
 
+_raw_stream = None
+
+
+def _stream_on(stream, index):
+    """The stream's pointer; without one, that of the current stream of the device.  A call of a few microseconds notices how long this
+    takes: torch.cuda.current_stream() 2.7 us, torch's own accessor of the pointer 0.1."""
+    global _raw_stream
+    if stream is not None:
+        return getattr(stream, "cuda_stream", stream)
+    if _raw_stream is None:
+        import torch
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+    return _raw_stream(index)
+
+
 def w4_matvec(W, x, alpha=1.0, beta=0.0, c=None, out=None, stream=None):
     """alpha W x + beta c for every row of x (tokens, k), as (tokens, n) in the type of `out`, or of x where it is None; c is like the result."""
-    import torch
     if out is None:
-        out = torch.empty((x.shape[0], W.n), dtype=x.dtype, device=x.device)
-    if not x.is_cuda or W.device != x.device or out.device != x.device or (c is not None and c.device != x.device):
-        _on_device(W.device, x=x, out=out, c=c)
-    ldx, ldy = _rows("x", x, W.k), _rows("out", out, W.n)
-    if out.shape[0] != x.shape[0] or (c is not None and (c.dtype != out.dtype or c.shape[0] != x.shape[0])):
-        raise Oz2Error("x, c and out have the same number of tokens, c and out the same type")
+        out = x.new_empty((x.shape[0], W.n))
+    index = x.get_device()
+    if index < 0 or index != W.index or out.get_device() != index:
+        _on_device(W.device, x=x, out=out)
+    ldx, ldy, t = _rows("x", x, W.k), _rows("out", out, W.n), x.size(0)
+    if out.size(0) != t:
+        raise Oz2Error("x and out have the same number of tokens")
     if W.count != 1:
         raise Oz2Error("one matrix wanted, not a stack")
-    rc = lib().oz2_w4_matvec(W.ref, x.shape[0], alpha, _type(x.dtype), x.data_ptr(), ldx, beta, None if c is None else c.data_ptr(),
-                             0 if c is None else _rows("c", c, W.n), _type(out.dtype), out.data_ptr(), ldy, _stream_ptr(stream))
-    _check(rc, "oz2_w4_matvec")
+    c_ptr, ldc, y_type = None, 0, _type(out.dtype)
+    if c is not None:
+        _on_device(W.device, c=c)
+        if c.dtype != out.dtype or c.size(0) != t:
+            raise Oz2Error("c has the type and the number of tokens of the result")
+        c_ptr, ldc = c.data_ptr(), _rows("c", c, W.n)
+    rc = lib().oz2_w4_matvec(W.ref, t, alpha, _type(x.dtype), x.data_ptr(), ldx, beta, c_ptr, ldc, y_type, out.data_ptr(), ldy,
+                             _stream_on(stream, index))
+    if rc:
+        _check(rc, "oz2_w4_matvec")
     return out
 
 
@@ -563,24 +585,31 @@ class MoeLayer:
 
 def _w4_moe(call, name, first, layer, x, active, out, ids, weights, stream):
     import torch
-    t = x.shape[0]
+    t, index = x.shape[0], x.get_device()
     if out is None:
-        out = torch.empty((t, layer.d), dtype=x.dtype, device=x.device)
+        out = x.new_empty((t, layer.d))
     if ids is None:
-        ids = torch.empty((t, layer.top_k), dtype=torch.int32, device=x.device)
+        ids = x.new_empty((t, layer.top_k), dtype=torch.int32)
     if weights is None:
-        weights = torch.empty((t, layer.top_k), dtype=torch.float32, device=x.device)
-    _on_device(layer.device, x=x, active=active, out=out, ids=ids, weights=weights)
+        weights = x.new_empty((t, layer.top_k), dtype=torch.float32)
+    if index < 0 or any(v.get_device() != index for v in (layer.router, out, ids, weights)):
+        _on_device(layer.device, x=x, out=out, ids=ids, weights=weights)
     ldx, ldy = _rows("x", x, layer.d), _rows("out", out, layer.d)
-    if out.shape[0] != t:
+    if out.size(0) != t:
         raise Oz2Error("x and out have the same number of tokens")
     for what, v, dtype in (("ids", ids, torch.int32), ("weights", weights, torch.float32)):
-        if v.dtype != dtype or tuple(v.shape) != (t, layer.top_k) or not v.is_contiguous():
+        if v.dtype != dtype or v.shape != (t, layer.top_k) or not v.is_contiguous():
             raise Oz2Error("%s is (tokens, top_k), %s, without gaps" % (what, dtype))
-    if active is not None and (active.dtype not in (torch.bool, torch.uint8) or tuple(active.shape) != (t,) or not active.is_contiguous()):
-        raise Oz2Error("active is (tokens,), bool or uint8")
-    _check(call(*first, layer.ref, t, _type(x.dtype), x.data_ptr(), ldx, None if active is None else active.data_ptr(), _type(out.dtype),
-                out.data_ptr(), ldy, ids.data_ptr(), weights.data_ptr(), _stream_ptr(stream)), name)
+    mask = None
+    if active is not None:
+        _on_device(layer.device, active=active)
+        if active.dtype not in (torch.bool, torch.uint8) or active.shape != (t,) or not active.is_contiguous():
+            raise Oz2Error("active is (tokens,), bool or uint8")
+        mask = active.data_ptr()
+    rc = call(*first, layer.ref, t, _type(x.dtype), x.data_ptr(), ldx, mask, _type(out.dtype), out.data_ptr(), ldy, ids.data_ptr(), weights.data_ptr(),
+              _stream_on(stream, index))
+    if rc:
+        _check(rc, name)
     return out, ids, weights
 
 

@@ -24,7 +24,9 @@ EXTRA_FLAGS = {
     "oz2_stage3.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "oz2_stage2_tiles.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "oz2_thin.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-    "oz2_w4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "oz2_w4_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "oz2_w4_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "oz2_w4_f16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "oz2_w4_moe.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 

@@ -842,10 +842,9 @@ int oz2_host_short_product_residues(int index, int64_t count, const int32_t* pro
 namespace {
 bool type_ok(int type) { return type == OZ2_F32 || type == OZ2_BF16 || type == OZ2_F16; }
 
-// A matrix (of a stack, if stacks are asked for) that the kernels can read: extents below 2^31, rows that do not overlap.
+// A matrix (of a stack, if stacks are asked for) that the kernels can read: extents that they count in, rows that do not overlap.
 bool w4_ok(const oz2_w4_matrix& w, bool stack) {
-  const int64_t lim = ((int64_t)1 << 31) - 65536;
-  if (w.n < 0 || w.k < 0 || w.n >= lim || w.k >= lim) return false;
+  if (w.n < 0 || w.k < 0 || w.n >= ((int64_t)1 << 31) - 65536 || w.k >= (int64_t)1 << 23) return false;
   if (w.group != 32 && w.group != 64 && (w.group < 128 || w.group % 128 != 0)) return false;
   if (!type_ok(w.scale_type)) return false;
   if (w.n == 0 || w.k == 0) return true;

@@ -48,117 +48,110 @@ struct W4Rows {
   const char* scales;
   const uint8_t* zeros;
   int64_t ld_codes, ld_scales, ld_zeros;
-  int n, k, bytes, blocks, groups;
-  int shift, per_group;  // blocks of a group (where that is 128 or more): 1 << shift, or per_group where shift < 0
-  int scale_type;
+  int n, k, group, bytes, full, groups;  // full: whole blocks
+  unsigned recip, keep;  // group of block b: the upper half of b recip, recip = ceil(2^32 / blocks of a group), or, where that is one, b
 };
 
-// The lane's row of a tile of sixteen, and the registers that a block of it takes.
+// The lane's row of a tile of sixteen, and the registers that a block of it takes.  All loads of a block are made whatever the place: a
+// load that a branch may leave out makes the compiler wait for younger ones.
 struct W4Lane {
   const uint8_t* codes;
   const char* scales;
   const uint8_t* zeros;
 };
 template <int SPB>
+using W4Words = unsigned __attribute__((ext_vector_type(SPB)));
+// Bytes of a block's scales or zero points, of a type that is no wider (else the compiler widens them where the loop turns, and waits
+// for them there).
+template <int BYTES> struct W4Width { typedef w4_u4 type; };
+template <> struct W4Width<8> { typedef W4Words<2> type; };
+template <> struct W4Width<4> { typedef unsigned type; };
+template <> struct W4Width<2> { typedef unsigned short type; };
+template <> struct W4Width<1> { typedef unsigned char type; };
+template <int BYTES>
+__device__ __forceinline__ typename W4Width<BYTES>::type w4_bytes(const void* p) {
+  struct __attribute__((packed, aligned(1))) Any { typename W4Width<BYTES>::type v; };
+  return reinterpret_cast<const Any*>(p)->v;
+}
+template <int BYTES>
+__device__ __forceinline__ unsigned w4_word(typename W4Width<BYTES>::type v, int i) {
+  if constexpr (BYTES > 4) return v[i];
+  else return v;
+}
+template <int SPB, int ST>
 struct W4Regs {
   w4_u4 q;
-  unsigned __attribute__((ext_vector_type(SPB))) s;
-  unsigned z;
+  typename W4Width<SPB * (ST == OZ2_F32 ? 4 : 2)>::type s;  // as they lie in memory
+  typename W4Width<SPB>::type z;  // a byte each
+};
+template <int SPB>
+struct W4Tail {
+  w4_u4 q;
+  int cut;  // bytes by which q begins early
+  W4Words<SPB> s, z;  // one each
 };
 
+template <int ST>
 __device__ __forceinline__ W4Lane w4_lane(const W4Rows& w, int64_t row) {
   row = row < w.n ? row : w.n - 1;  // rows past the end read the last one; nothing is stored of them
   W4Lane l;
-  const int size = w.scale_type == OZ2_F32 ? 4 : 2;
   l.codes = w.codes + row * w.ld_codes + (threadIdx.x % 64 / 16) * 16;
-  l.scales = w.scales + row * w.ld_scales * size;
-  l.zeros = w.zeros ? w.zeros + row * w.ld_zeros : nullptr;
+  l.scales = w.scales + row * w.ld_scales * (ST == OZ2_F32 ? 4 : 2);
+  l.zeros = w.zeros + row * w.ld_zeros;
   return l;
 }
 
-// Block b of the row: 16 bytes of codes for this lane, and the scales and zero points of its segments (a group, or 128 of one).
-// (Values are returned and assigned whole: stores into parts of an array from different branches would put it into memory.)
-__device__ __forceinline__ w4_u4 w4_fetch_codes(const W4Rows& w, const W4Lane& l, int b) {
-  const uint8_t* p = l.codes + (int64_t)b * (kW4Block / 2);
-  if ((b + 1) * (kW4Block / 2) <= w.bytes) {
-    const W4Bytes16 c = *reinterpret_cast<const W4Bytes16*>(p);
-    return w4_u4{c.v[0], c.v[1], c.v[2], c.v[3]};
-  }
-  // the row's last block: no byte past its end
-  const int left = w.bytes - b * (kW4Block / 2) - (threadIdx.x % 64 / 16) * 16;
-  auto word = [&](int i) {
-    unsigned v = 0;
-#pragma unroll
-    for (int j = i; j < i + 4; ++j)
-      if (j < left) v |= (unsigned)p[j] << (8 * (j - i));
-    return v;
-  };
-  return w4_u4{word(0), word(4), word(8), word(12)};
+template <int SPB>
+__device__ __forceinline__ int w4_group(const W4Rows& w, int b) {
+  if constexpr (SPB > 1) return b * SPB;
+  // b below 2^16 and no more blocks in a group than there are blocks: exact, since 2^32 / blocks is exceeded by less than one
+  return (int)(__umulhi((unsigned)b, w.recip) + ((unsigned)b & w.keep));
 }
 
-// As they lie in memory: a word each (f32), or two to a word.
-template <int SPB>
-using W4Scales = unsigned __attribute__((ext_vector_type(SPB)));
-template <int SPB>
-__device__ __forceinline__ W4Scales<SPB> w4_fetch_scales(const W4Rows& w, const W4Lane& l, int g) {
-  auto wide = [&](int i) { return reinterpret_cast<const W4Bytes4*>(l.scales + (int64_t)(g + i) * 4)->v; };
-  auto narrow = [&](int i) { return (unsigned)reinterpret_cast<const W4Bytes2*>(l.scales + (int64_t)(g + i) * 2)->v; };
-  if constexpr (SPB == 1) {
-    return w.scale_type == OZ2_F32 ? wide(0) : narrow(0);
-  } else {
-    const bool whole = g + SPB <= w.groups;
-    if (w.scale_type == OZ2_F32) {
-      if constexpr (SPB == 2) {
-        if (whole) { const W4Bytes8 c = *reinterpret_cast<const W4Bytes8*>(l.scales + (int64_t)g * 4); return W4Scales<2>{c.v[0], c.v[1]}; }
-        return W4Scales<2>{wide(0), 0u};
-      } else {
-        if (whole) { const W4Bytes16 c = *reinterpret_cast<const W4Bytes16*>(l.scales + (int64_t)g * 4); return W4Scales<4>{c.v[0], c.v[1], c.v[2], c.v[3]}; }
-        const int last = w.groups - 1 - g;  // below 3; segments past the last group get a scale of 0
-        return W4Scales<4>{wide(0), last > 0 ? wide(1) : 0u, last > 1 ? wide(2) : 0u, 0u};
-      }
-    }
-    if constexpr (SPB == 2) {
-      return W4Scales<2>{whole ? reinterpret_cast<const W4Bytes4*>(l.scales + (int64_t)g * 2)->v : narrow(0), 0u};
-    } else {
-      if (whole) { const W4Bytes8 c = *reinterpret_cast<const W4Bytes8*>(l.scales + (int64_t)g * 2); return W4Scales<4>{c.v[0], c.v[1], 0u, 0u}; }
-      const int last = w.groups - 1 - g;
-      return W4Scales<4>{narrow(0) | (last > 0 ? narrow(1) << 16 : 0u), last > 1 ? narrow(2) : 0u, 0u, 0u};
-    }
-  }
-}
-
-// A byte each.
-template <int SPB>
-__device__ __forceinline__ unsigned w4_fetch_zeros(const W4Rows& w, const W4Lane& l, int g) {
-  if (!w.zeros) return 0x08080808u;
-  const uint8_t* p = l.zeros + g;
-  if constexpr (SPB == 1) return p[0];
-  if constexpr (SPB == 2) return g + SPB <= w.groups ? reinterpret_cast<const W4Bytes2*>(p)->v : p[0];
-  if (g + SPB <= w.groups) return reinterpret_cast<const W4Bytes4*>(p)->v;
-  const int last = w.groups - 1 - g;
-  return p[0] | (last > 0 ? (unsigned)p[1] << 8 : 0u) | (last > 1 ? (unsigned)p[2] << 16 : 0u);
-}
-
-template <int SPB>
-__device__ __forceinline__ W4Regs<SPB> w4_fetch(const W4Rows& w, const W4Lane& l, int b) {
-  int g;
-  if constexpr (SPB > 1) g = b * SPB;
-  else g = w.shift >= 0 ? b >> w.shift : b / w.per_group;
-  W4Regs<SPB> r;
-  r.q = w4_fetch_codes(w, l, b);
-  r.s = w4_fetch_scales<SPB>(w, l, g);
-  r.z = w4_fetch_zeros<SPB>(w, l, g);
+// Whole block b of the row: 16 bytes of codes for this lane, the scales and zero points of its segments (a group, or 128 of one).
+template <int SPB, int ST, bool ZEROS>
+__device__ __forceinline__ W4Regs<SPB, ST> w4_fetch(const W4Rows& w, const W4Lane& l, int b) {
+  W4Regs<SPB, ST> r;
+  const W4Bytes16 c = *reinterpret_cast<const W4Bytes16*>(l.codes + (int64_t)b * (kW4Block / 2));
+  r.q = w4_u4{c.v[0], c.v[1], c.v[2], c.v[3]};
+  const int g = w4_group<SPB>(w, b);
+  r.s = w4_bytes<SPB * (ST == OZ2_F32 ? 4 : 2)>(l.scales + (int64_t)g * (ST == OZ2_F32 ? 4 : 2));
+  if constexpr (ZEROS) r.z = w4_bytes<SPB>(l.zeros + g);
   return r;
+}
+
+// The block behind the whole ones, of rows of at least 16 bytes.  A lane whose bytes are not all there loads the sixteen that end with the
+// row, and cuts off later what came early; codes past the end may be anything, since x is 0 there.
+template <int SPB, int ST, bool ZEROS>
+__device__ __forceinline__ W4Tail<SPB> w4_fetch_tail(const W4Rows& w, const W4Lane& l) {
+  W4Tail<SPB> r;
+  const int left = w.bytes - w.full * (kW4Block / 2) - threadIdx.x % 64 / 16 * 16;  // bytes from the lane's first on
+  r.cut = left >= 16 || left <= 0 ? 0 : 16 - left;
+  const W4Bytes16 c = *reinterpret_cast<const W4Bytes16*>(left > 0 ? l.codes + (int64_t)w.full * (kW4Block / 2) - r.cut : l.codes - threadIdx.x % 64 / 16 * 16);
+  r.q = w4_u4{c.v[0], c.v[1], c.v[2], c.v[3]};
+  const int g = w4_group<SPB>(w, w.full);
+  w4_each<SPB>([&](auto i) __attribute__((always_inline)) {
+    const int at = min(g + i.value, w.groups - 1);
+    if constexpr (ST == OZ2_F32) r.s[i.value] = reinterpret_cast<const W4Bytes4*>(l.scales + (int64_t)at * 4)->v;
+    else r.s[i.value] = reinterpret_cast<const W4Bytes2*>(l.scales + (int64_t)at * 2)->v;
+    if constexpr (ZEROS) r.z[i.value] = l.zeros[at];
+    else r.z[i.value] = 8u;
+  });
+  return r;
+}
+
+// 16 bytes without the first `cut` (below 16), zeros behind.
+__device__ __forceinline__ w4_u4 w4_cut(w4_u4 v, int cut) {
+  unsigned long long lo = v[0] | (unsigned long long)v[1] << 32, hi = v[2] | (unsigned long long)v[3] << 32;
+  const int bits = 8 * cut;
+  if (bits >= 64) lo = hi >> (bits - 64), hi = 0;
+  else if (bits) lo = lo >> bits | hi << (64 - bits), hi >>= bits;
+  return w4_u4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
 }
 
 __device__ __forceinline__ float w4_decode16(int type, unsigned v) {  // of the lower half
   return type == OZ2_BF16 ? __uint_as_float(v << 16) : (float)__builtin_bit_cast(_Float16, (unsigned short)v);
 }
-template <int SPB>
-__device__ __forceinline__ float w4_scale(int type, const W4Regs<SPB>& r, int seg) {
-  return type == OZ2_F32 ? __uint_as_float(r.s[seg]) : w4_decode16(type, r.s[seg / 2] >> (seg % 2 * 16));
-}
-
 // Eight codes as 16 + q in pairs (0, 4), (1, 5), (2, 6), (3, 7).
 template <int XT>
 __device__ __forceinline__ void w4_unpack(unsigned w, unsigned out[4]) {
@@ -211,10 +204,10 @@ __device__ __forceinline__ int w4_token(int a) { return a / 4 + 4 * (a % 4); }
 
 // One block: the lane's sums (tokens quarter + 4 r, its row) grow by  scale ((16 + q) x - (16 + z) x).
 // x: the lane's token at the block's start, part p at + p part_bytes; sums: of the block's first segment.
-template <int XT, int SPB, int RT>
-__device__ __forceinline__ void w4_block(const W4Rows& w, const W4Regs<SPB>& r, const char* x, int part_bytes, const float* sums, float* sum) {
+template <int XT, int SPB, int RT, class Scale, class Zero>
+__device__ __forceinline__ void w4_block(w4_u4 codes, Scale scale, Zero zero, const char* x, int part_bytes, const float* sums, float* sum) {
   const int quarter = threadIdx.x % 64 / 16;
-  const w4_u4 q = w4_exchange<SPB>(r.q);
+  const w4_u4 q = w4_exchange<SPB>(codes);
   w4_each<SPB>([&](auto index) __attribute__((always_inline)) {
     constexpr int seg = index.value;
     w4_f4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -227,88 +220,123 @@ __device__ __forceinline__ void w4_block(const W4Rows& w, const W4Regs<SPB>& r, 
       for (int p = 0; p < w4_parts<XT>(); ++p)
         acc = w4_mfma<XT>(*reinterpret_cast<const uint4*>(x + p * part_bytes + 2 * w4_inner<SPB>(j, quarter)), b, acc);
     }
-    const float s = w4_scale<SPB>(w.scale_type, r, seg);
-    const float z = kW4Offset + (float)(r.z >> (8 * seg) & 255u);
+    const float s = scale(index), z = kW4Offset + zero(index);
 #pragma unroll
     for (int i = 0; i < RT; ++i) sum[i] = fmaf(s, fmaf(-z, sums[(seg * 4 + quarter) * RT + i], acc[i]), sum[i]);
   });
 }
+template <int XT, int SPB, int ST, bool ZEROS, int RT>
+__device__ __forceinline__ void w4_whole(const W4Regs<SPB, ST>& r, const char* x, int part_bytes, const float* sums, float* sum) {
+  w4_block<XT, SPB, RT>(
+      r.q,
+      [&](auto i) __attribute__((always_inline)) {
+        if constexpr (ST == OZ2_F32) return __uint_as_float(w4_word<SPB * 4>(r.s, i.value));
+        else return w4_decode16(ST, w4_word<SPB * 2>(r.s, i.value / 2) >> (i.value % 2 * 16));
+      },
+      [&](auto i) __attribute__((always_inline)) {
+        if constexpr (ZEROS) return (float)(w4_word<SPB>(r.z, 0) >> (8 * i.value) & 255u);
+        else return 8.f;
+      }, x, part_bytes, sums, sum);
+}
+template <int XT, int SPB, int ST, int RT>
+__device__ __forceinline__ void w4_tail(const W4Rows& w, const W4Tail<SPB>& r, const char* x, int part_bytes, const float* sums, float* sum) {
+  const int g = w4_group<SPB>(w, w.full);
+  w4_block<XT, SPB, RT>(
+      w4_cut(r.q, r.cut),
+      [&](auto i) __attribute__((always_inline)) {  // (0 past the last group: a scale that is not finite must not meet the 0 of x)
+        const float s = ST == OZ2_F32 ? __uint_as_float(r.s[i.value]) : w4_decode16(ST, r.s[i.value]);
+        return g + i.value < w.groups ? s : 0.f;
+      },
+      [&](auto i) __attribute__((always_inline)) { return (float)r.z[i.value]; }, x, part_bytes, sums, sum);
+}
 
 // The same by the formula itself, code by code: for blocks whose x has infinities, NaNs, or values near the end of the range.
-template <int SPB, int RT, class X>
-__device__ __forceinline__ void w4_block_plain(const W4Rows& w, const W4Lane& l, int b, X value, float* sum) {
+template <int SPB, int ST, int RT, class X>
+__device__ __forceinline__ void w4_block_plain(const W4Rows& w, const W4Lane& l, bool zeros, int b, X value, float* sum) {
   const uint8_t* codes = l.codes - (threadIdx.x % 64 / 16) * 16;
   const int end = min(w.k, (b + 1) * kW4Block);
 #pragma unroll 1
   for (int i = b * kW4Block; i < end; ++i) {
     const int q = codes[i / 2] >> (i % 2 * 4) & 15;
-    int g;
-    if (SPB > 1) g = i / (kW4Block / SPB);
-    else g = w.shift >= 0 ? b >> w.shift : b / w.per_group;
-    const float s = w4_load(w.scale_type, l.scales, g);
-    const float v = s * (float)(q - (w.zeros ? (int)l.zeros[g] : 8));
+    const int g = SPB > 1 ? i / (kW4Block / SPB) : w4_group<1>(w, b);
+    const float s = w4_load(ST, l.scales, g);
+    const float v = s * (float)(q - (zeros ? (int)l.zeros[g] : 8));
 #pragma unroll
     for (int r = 0; r < RT; ++r) sum[r] = fmaf(v, value(r, i), sum[r]);
   }
 }
 
-// Brings inner indexes [first, first + length) of `tokens` vectors into LDS (zeros past k); length is a multiple of 128.  Returns
-// whether what this thread saw calls for w4_block_plain.  row(token): element offset of the vector.
-template <int XT, int SPB, int RT, class Row>
-__device__ __forceinline__ bool w4_stage(const void* x, Row row, int tokens, int k, int first, int length, char* lds, int pitch, float* sums,
-                                         int threads) {
-  constexpr int SEG = kW4Block / SPB, P = w4_parts<XT>();
-  bool plain = false;
-  const int eights = length / 8;
-  for (int i = threadIdx.x; i < tokens * eights; i += threads) {
-    const int t = i / eights, at = (i - t * eights) * 8, l = first + at;
-    float v[8];
-    unsigned h[P][8];
-    if constexpr (XT == OZ2_F32) {
-      const float* p = static_cast<const float*>(x) + row(t) + l;
-      if (l + 8 <= k) {
-        const W4Bytes16 a = *reinterpret_cast<const W4Bytes16*>(p), b = *reinterpret_cast<const W4Bytes16*>(p + 4);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(a.v[e]), v[e + 4] = __uint_as_float(b.v[e]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = l + e < k ? p[e] : 0.f;
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {  // cut, not rounded: each part takes the next eight bits, and none can overflow
-        float rest = v[e];
-#pragma unroll
-        for (int c = 0; c < 3; ++c) {
-          h[c][e] = __float_as_uint(rest) >> 16;
-          rest -= __uint_as_float(h[c][e] << 16);
-        }
-      }
-    } else {
-      const uint16_t* p = static_cast<const uint16_t*>(x) + row(t) + l;
-      if (l + 8 <= k) {
-        const W4Bytes16 a = *reinterpret_cast<const W4Bytes16*>(p);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[0][e] = a.v[e / 2] >> (e % 2 * 16) & 0xFFFFu;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[0][e] = l + e < k ? p[e] : 0u;
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = w4_decode16(XT, h[0][e]);
-    }
-#pragma unroll
-    for (int c = 0; c < P; ++c)
-      *reinterpret_cast<uint4*>(lds + (t * P + c) * pitch + 2 * at) =
-          make_uint4(h[c][0] | h[c][4] << 16, h[c][1] | h[c][5] << 16, h[c][2] | h[c][6] << 16, h[c][3] | h[c][7] << 16);
-    float s = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-    float a = ((fabsf(v[0]) + fabsf(v[1])) + (fabsf(v[2]) + fabsf(v[3]))) + ((fabsf(v[4]) + fabsf(v[5])) + (fabsf(v[6]) + fabsf(v[7])));
-    // the threads of a segment are neighbours, and all of them are here: `eights` is a multiple of 16
-#pragma unroll
-    for (int d = 1; d < SEG / 8; d *= 2) s += __shfl_xor(s, d), a += __shfl_xor(a, d);
-    plain |= !(a < kW4Large);
-    if (at % SEG == 0) sums[(at / SEG * 4 + t % 4) * RT + t / 4] = s;
+// Eight values of x on their way into LDS.
+template <int XT>
+struct W4Raw {
+  w4_u4 v[XT == OZ2_F32 ? 2 : 1];
+};
+// How a chunk of x comes into LDS: inner indexes first .. first + length - 1 (a multiple of 128) of `tokens` vectors, zeros past k.  Piece i of
+// the work, eight values of a token, belongs to thread i % threads.
+struct W4Stage {
+  const char* x;
+  int64_t first;
+  int tokens, k, eights;
+};
+// (k is at least 8: where fewer than the 16 bytes of a load are there, it takes the 16 that end with the vector.)
+template <int XT, class Row>
+__device__ __forceinline__ W4Raw<XT> w4_stage_load(const W4Stage& st, Row row, int i) {
+  constexpr int size = XT == OZ2_F32 ? 4 : 2, per = 16 / size;  // values of 16 bytes
+  W4Raw<XT> r;
+  const int t = i / st.eights, l = (int)st.first + (i - t * st.eights) * 8;
+  const char* p = st.x + row(t) * size;
+  w4_each<8 / per>([&](auto h) __attribute__((always_inline)) {
+    const W4Bytes16 c = *reinterpret_cast<const W4Bytes16*>(p + (int64_t)min(l + h.value * per, st.k - per) * size);
+    r.v[h.value] = w4_u4{c.v[0], c.v[1], c.v[2], c.v[3]};
+  });
+  return r;
+}
+// Value of the lane across in a pair, four, eight or sixteen lanes whose halves hold one value each (a pair: its two lanes).
+template <int STEP>
+__device__ __forceinline__ float w4_partner(float v) {
+  constexpr int ctrl = STEP == 0 ? 0xB1 : STEP == 1 ? 0x4E : STEP == 2 ? 0x141 : 0x140;  // quad permutations, mirrors of 8 and 16 lanes
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), ctrl, 0xF, 0xF, true));
+}
+// Writes a piece and (with its neighbours) the sums over its segment.  Returns whether the values call for w4_block_plain.
+template <int XT, int SPB, int RT>
+__device__ __forceinline__ bool w4_stage_store(const W4Stage& st, W4Raw<XT> r, int i, char* lds, int pitch, float* sums) {
+  constexpr int SEG = kW4Block / SPB, P = w4_parts<XT>(), size = XT == OZ2_F32 ? 4 : 2, per = 16 / size;
+  const int t = i / st.eights, at = (i - t * st.eights) * 8;
+  if ((int)st.first + at + 8 > st.k) {
+    w4_each<8 / per>([&](auto h) __attribute__((always_inline)) {
+      const int there = st.k - ((int)st.first + at + h.value * per);
+      r.v[h.value] = there <= 0 ? w4_u4{0, 0, 0, 0} : there < per ? w4_cut(r.v[h.value], (per - there) * size) : r.v[h.value];
+    });
   }
-  return plain;
+  float v[8];
+  unsigned h[P][8];
+  if constexpr (XT == OZ2_F32) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {  // cut, not rounded: each part takes the next eight bits, and none can overflow
+      float rest = v[e] = __uint_as_float(r.v[e / 4][e % 4]);
+#pragma unroll
+      for (int c = 0; c < 3; ++c) {
+        h[c][e] = __float_as_uint(rest) >> 16;
+        rest -= __uint_as_float(h[c][e] << 16);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      h[0][e] = r.v[0][e / 2] >> (e % 2 * 16) & 0xFFFFu;
+      v[e] = w4_decode16(XT, h[0][e]);
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < P; ++c)
+    *reinterpret_cast<uint4*>(lds + (t * P + c) * pitch + 2 * at) =
+        make_uint4(h[c][0] | h[c][4] << 16, h[c][1] | h[c][5] << 16, h[c][2] | h[c][6] << 16, h[c][3] | h[c][7] << 16);
+  float s = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+  float a = ((fabsf(v[0]) + fabsf(v[1])) + (fabsf(v[2]) + fabsf(v[3]))) + ((fabsf(v[4]) + fabsf(v[5])) + (fabsf(v[6]) + fabsf(v[7])));
+  // the threads of a segment are neighbours, and all of them are here: the pieces of a token are a multiple of 16
+  w4_each<SPB == 4 ? 2 : SPB == 2 ? 3 : 4>([&](auto step) __attribute__((always_inline)) { s += w4_partner<step.value>(s), a += w4_partner<step.value>(a); });
+  if (at % SEG == 0) sums[(at / SEG * 4 + t % 4) * RT + t / 4] = s;
+  return !(a < kW4Large);
 }
 
 #endif
