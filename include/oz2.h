@@ -386,7 +386,7 @@ int oz2_host_short_product_residues(int index, int64_t count, const int32_t* pro
  *   codes   row i starts at codes + i ld_codes; its element l is the low (even l) or high (odd l) half of byte floor(l / 2).
  *           Bytes of a row beyond ceil(k / 2) and the last half byte of an odd k are never used (the former not read).
  *   scales  element (i, g) is scales[i ld_scales + g], of type scale_type;  zeros (or NULL) likewise, a byte each
- *   group   32, 64 or a multiple of 128; the last group of a row may be short
+ *   group   32, 64 or a multiple of 128; the last group of a row may be short;  k is below 2^23
  *   count   matrices in a stack; matrix e starts stride_codes bytes, stride_scales and stride_zeros elements after matrix e - 1
  * No alignment beyond that of the element types is needed (rows whose codes start at multiples of 16 bytes are read fastest).
  *
@@ -422,7 +422,8 @@ int oz2_w4_matvec(const oz2_w4_matrix* W, int64_t t, float alpha, int x_type, co
  *           chosen, so a token may have fewer; a NaN counts as the largest, and so reaches y
  *   weights p of the chosen, divided by their sum where `renormalize` is set (all 0 if that is 0), times factor
  *   y = sum over the chosen, in order, of  weight * down_e (act(gate_e x) * (up_e x)),   act = silu or gelu (with erf)
- * gate and up are stacks of f x d, down of d x f.  The inner vectors of f values are kept in FP32. */
+ * gate and up are stacks of f x d, down of d x f; gate and up are alike in group, type of the scales and whether they have zero points.
+ * The inner vectors of f values are kept in FP32. */
 #define OZ2_SCORE_SOFTMAX 0
 #define OZ2_SCORE_SIGMOID 1
 #define OZ2_ACT_SILU 0

@@ -27,7 +27,6 @@ EXTRA_FLAGS = {
     "oz2_w4_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "oz2_w4_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "oz2_w4_f16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-    "oz2_w4_moe.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 
 

@@ -864,6 +864,7 @@ bool moe_ok(const oz2_moe_layer* m) {
   const int64_t f = m->gate.n, d = m->gate.k, experts = m->gate.count;
   if (d < 1 || f < 1 || experts < 1 || experts > OZ2_MOE_MAX_EXPERTS) return false;
   if (m->up.n != f || m->up.k != d || m->up.count != experts) return false;
+  if (m->up.group != m->gate.group || m->up.scale_type != m->gate.scale_type || !m->up.zeros != !m->gate.zeros) return false;
   if (m->down.n != d || m->down.k != f || m->down.count != experts) return false;
   if (!m->router || !type_ok(m->router_type) || (experts > 1 && m->ld_router < d)) return false;
   if (m->top_k < 1 || m->top_k > OZ2_MOE_MAX_TOP_K || m->top_k > experts) return false;

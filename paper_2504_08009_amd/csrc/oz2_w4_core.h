@@ -36,7 +36,7 @@ struct __attribute__((packed, aligned(1))) W4Bytes2 { unsigned short v; };
 
 constexpr int kW4Block = 128;  // inner indexes that a wave takes at a time: 16 bytes of codes a lane
 constexpr float kW4Offset = 16.f;
-constexpr float kW4Large = 1e36f;  // sums of |x| over a group from here on are not trusted to 31 sum |x| in FP32
+constexpr float kW4Large = 1e34f;  // where sums of |x| over a few values get there, 31 sum |x| over a group might leave the range of FP32
 
 // 16-bit floats a value of x is made of
 template <int XT>
@@ -152,16 +152,37 @@ __device__ __forceinline__ w4_u4 w4_cut(w4_u4 v, int cut) {
 __device__ __forceinline__ float w4_decode16(int type, unsigned v) {  // of the lower half
   return type == OZ2_BF16 ? __uint_as_float(v << 16) : (float)__builtin_bit_cast(_Float16, (unsigned short)v);
 }
-// Eight codes as 16 + q in pairs (0, 4), (1, 5), (2, 6), (3, 7).
+// Eight codes as 16 + q in pairs (0, 4), (1, 5), (2, 6), (3, 7).  The constants come from registers, one of them from a vector register:
+// then the and and the or are one instruction, which takes no literals.
 template <int XT>
 __device__ __forceinline__ void w4_unpack(unsigned w, unsigned out[4]) {
+  unsigned m = XT == OZ2_F16 ? 0x03C003C0u : 0x00780078u, c = XT == OZ2_F16 ? 0x4C004C00u : 0x41804180u;
+  asm("" : "+s"(m));
+  asm("" : "+v"(c));
   if constexpr (XT == OZ2_F16) {
-    constexpr unsigned m = 0x03C003C0u, c = 0x4C004C00u;
     out[0] = (w << 6 & m) | c, out[1] = (w << 2 & m) | c, out[2] = (w >> 2 & m) | c, out[3] = (w >> 6 & m) | c;
   } else {
-    constexpr unsigned m = 0x00780078u, c = 0x41804180u;
     out[0] = (w << 3 & m) | c, out[1] = (w >> 1 & m) | c, out[2] = (w >> 5 & m) | c, out[3] = (w >> 9 & m) | c;
   }
+}
+
+// Eight 16-bit floats: their order as that of the pairs above, their sum, and that of their sizes.
+__device__ __forceinline__ w4_u4 w4_pairs(w4_u4 v) {
+  return w4_u4{__builtin_amdgcn_perm(v[2], v[0], 0x05040100u), __builtin_amdgcn_perm(v[2], v[0], 0x07060302u),
+               __builtin_amdgcn_perm(v[3], v[1], 0x05040100u), __builtin_amdgcn_perm(v[3], v[1], 0x07060302u)};
+}
+typedef __bf16 w4_bf2 __attribute__((ext_vector_type(2)));
+typedef _Float16 w4_h2 __attribute__((ext_vector_type(2)));
+template <int XT>
+__device__ __forceinline__ float w4_dot2(unsigned a, unsigned b, float c) {
+  if constexpr (XT == OZ2_F16) return __builtin_amdgcn_fdot2(__builtin_bit_cast(w4_h2, a), __builtin_bit_cast(w4_h2, b), c, false);
+  else return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(w4_bf2, a), __builtin_bit_cast(w4_bf2, b), c, false);
+}
+template <int XT>
+__device__ __forceinline__ void w4_sums(w4_u4 v, float& s, float& a) {
+  constexpr unsigned one = XT == OZ2_F16 ? 0x3C003C00u : 0x3F803F80u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s = w4_dot2<XT>(v[i], one, s), a = w4_dot2<XT>(v[i] & 0x7FFF7FFFu, one, a);
 }
 
 template <int XT>
@@ -308,33 +329,34 @@ __device__ __forceinline__ bool w4_stage_store(const W4Stage& st, W4Raw<XT> r, i
       r.v[h.value] = there <= 0 ? w4_u4{0, 0, 0, 0} : there < per ? w4_cut(r.v[h.value], (per - there) * size) : r.v[h.value];
     });
   }
-  float v[8];
-  unsigned h[P][8];
+  float s, a;
+  char* to = lds + t * P * pitch + 2 * at;
   if constexpr (XT == OZ2_F32) {
+    float v[8];
+    unsigned h[P][8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {  // cut, not rounded: each part takes the next eight bits, and none can overflow
       float rest = v[e] = __uint_as_float(r.v[e / 4][e % 4]);
 #pragma unroll
       for (int c = 0; c < 3; ++c) {
-        h[c][e] = __float_as_uint(rest) >> 16;
-        rest -= __uint_as_float(h[c][e] << 16);
+        h[c][e] = __float_as_uint(rest);
+        rest -= __uint_as_float(h[c][e] & 0xFFFF0000u);
       }
     }
+#pragma unroll
+    for (int c = 0; c < P; ++c)
+      *reinterpret_cast<w4_u4*>(to + c * pitch) =
+          w4_u4{__builtin_amdgcn_perm(h[c][4], h[c][0], 0x07060302u), __builtin_amdgcn_perm(h[c][5], h[c][1], 0x07060302u),
+                __builtin_amdgcn_perm(h[c][6], h[c][2], 0x07060302u), __builtin_amdgcn_perm(h[c][7], h[c][3], 0x07060302u)};
+    s = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    a = ((fabsf(v[0]) + fabsf(v[1])) + (fabsf(v[2]) + fabsf(v[3]))) + ((fabsf(v[4]) + fabsf(v[5])) + (fabsf(v[6]) + fabsf(v[7])));
   } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      h[0][e] = r.v[0][e / 2] >> (e % 2 * 16) & 0xFFFFu;
-      v[e] = w4_decode16(XT, h[0][e]);
-    }
+    s = a = 0.f;
+    w4_sums<XT>(r.v[0], s, a);
+    *reinterpret_cast<w4_u4*>(to) = w4_pairs(r.v[0]);
   }
-#pragma unroll
-  for (int c = 0; c < P; ++c)
-    *reinterpret_cast<uint4*>(lds + (t * P + c) * pitch + 2 * at) =
-        make_uint4(h[c][0] | h[c][4] << 16, h[c][1] | h[c][5] << 16, h[c][2] | h[c][6] << 16, h[c][3] | h[c][7] << 16);
-  float s = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-  float a = ((fabsf(v[0]) + fabsf(v[1])) + (fabsf(v[2]) + fabsf(v[3]))) + ((fabsf(v[4]) + fabsf(v[5])) + (fabsf(v[6]) + fabsf(v[7])));
   // the threads of a segment are neighbours, and all of them are here: the pieces of a token are a multiple of 16
-  w4_each<SPB == 4 ? 2 : SPB == 2 ? 3 : 4>([&](auto step) __attribute__((always_inline)) { s += w4_partner<step.value>(s), a += w4_partner<step.value>(a); });
+  w4_each<SPB == 4 ? 2 : SPB == 2 ? 3 : 4>([&](auto step) __attribute__((always_inline)) { s += w4_partner<step.value>(s); });
   if (at % SEG == 0) sums[(at / SEG * 4 + t % 4) * RT + t / 4] = s;
   return !(a < kW4Large);
 }

@@ -17,6 +17,7 @@ struct W4Call {
 };
 template <int XT>
 hipError_t oz2_w4_matvec_of(const W4Call& a, int64_t group);
+int oz2_w4_compute_units();
 
 #ifdef __HIPCC__
 namespace {
@@ -151,21 +152,15 @@ __global__ void __launch_bounds__(64 * kWaves) w4_vector_kernel(W4Rows w, int sp
   const int split = 1 << split_log, s = wave & (split - 1), per = kWaves >> split_log;
   const int batches = (w.n + 3) / 4, step = gridDim.x * per, first = blockIdx.x * per;
   const int unit = s * 64 + lane;
-  const W4Place at[1] = {w4_place(w, unit)};
-  const bool ragged[1] = {__ballot(at[0].cut != 0) != 0};
-  W4Rows4<XT, T, 1, ST, ZEROS> rows;
+  const W4Place at = w4_place(w, unit);
+  const bool ragged = __ballot(at.cut != 0) != 0;
+  W4Rows4<XT, T, ST, ZEROS> rows;
   int b = first + (wave >> split_log);
-  rows.fetch(w, w.codes, w.scales, w.zeros, b * 4, at);
-  W4X<XT> kept[T][1];
-  bool plain = false;
-  {
-    w4_u4 raw[T][XT == OZ2_F32 ? 8 : 4];
-#pragma unroll
-    for (int t = 0; t < T; ++t) w4_load_x<XT>(x + t * ldx * (XT == OZ2_F32 ? 4 : 2), w.k, unit, raw[t]);
-#pragma unroll
-    for (int t = 0; t < T; ++t) kept[t][0] = w4_keep_x<XT>(w.k, unit, raw[t], plain);
-  }
-  plain = __ballot(plain) != 0;
+  auto row_of = [&](int batch) { return [&, batch](int i) { return w4_row<ST>(w, batch * 4 + i); }; };
+  auto vector = [&](int t) { return x + t * ldx * (XT == OZ2_F32 ? 4 : 2); };
+  rows.fetch(row_of(b), at);
+  W4X<XT> kept[T];
+  const unsigned plain = w4_take_x<XT, T>(w.k, unit, vector, kept);
   auto finish = [&](int64_t row, int t, float v) {
     float u = alpha * v;
     if (beta != 0.f) u = fmaf(beta, w4_load(y_type, c, t * ldc + row), u);
@@ -174,9 +169,9 @@ __global__ void __launch_bounds__(64 * kWaves) w4_vector_kernel(W4Rows w, int sp
   const int rounds = (batches - first + step - 1) / step;  // of the workgroup: its first wave has the most
   for (int i = 0; i < rounds; ++i, b += step) {
     float sum[4][T];
-    if (plain) rows.multiply_plain(w, w.codes, w.scales, w.zeros, b * 4, x, ldx, unit, sum);
-    else rows.multiply(at, kept, ragged, sum);
-    if (i + 1 < rounds) rows.fetch(w, w.codes, w.scales, w.zeros, (b + step) * 4, at);
+    rows.multiply(at, kept, ragged, sum);
+    if (plain) rows.multiply_plain(plain, w.k, w.group, row_of(b), vector, unit, sum);
+    if (i + 1 < rounds) rows.fetch(row_of(b + step), at);
     float v[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) v[t] = w4_sum4(sum[0][t], sum[1][t], sum[2][t], sum[3][t]);
@@ -200,21 +195,13 @@ __global__ void __launch_bounds__(64 * kWaves) w4_vector_kernel(W4Rows w, int sp
   }
 }
 
-inline int compute_units() {
-  static const int cus = [] {
-    int device = 0, n = 0;
-    return hipGetDevice(&device) == hipSuccess && hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, device) == hipSuccess && n > 0 ? n : 256;
-  }();
-  return cus;
-}
-
 template <int XT, int T, int ST, bool ZEROS>
 hipError_t launch_vector(const W4Call& a) {
   int split_log = 0;
   while ((kW4Span << split_log) < a.w.k) ++split_log;
   const int per = kWaves >> split_log, batches = (a.w.n + 3) / 4;
   // three workgroups a compute unit fit; each has x in its registers and walks as many batches as all others
-  const int most = compute_units() * 3, needed = (batches + per - 1) / per, rounds = (needed + most - 1) / most, grid = (needed + rounds - 1) / rounds;
+  const int most = oz2_w4_compute_units() * 3, needed = (batches + per - 1) / per, rounds = (needed + most - 1) / most, grid = (needed + rounds - 1) / rounds;
   hipLaunchKernelGGL((w4_vector_kernel<XT, T, ST, ZEROS>), dim3(grid), dim3(64 * kWaves), 0, a.st, a.w, split_log, a.alpha,
                      static_cast<const char*>(a.x), a.ldx, a.beta, a.c, a.ldc, a.y_type, a.y, a.ldy);
   return hipGetLastError();

@@ -1,5 +1,9 @@
 // A layer of gated experts whose weights are held in 4 bits, with its router, for a few tokens (oz2_w4_moe).
-#include "oz2_w4.h"
+#include "oz2_w4_moe.h"
+
+extern template hipError_t oz2_moe_gate_up<OZ2_F32>(const MoeCall&, int);
+extern template hipError_t oz2_moe_gate_up<OZ2_BF16>(const MoeCall&, int);
+extern template hipError_t oz2_moe_gate_up<OZ2_F16>(const MoeCall&, int);
 
 namespace {
 
@@ -7,6 +11,42 @@ __device__ __forceinline__ float wave_sum(float v) {
   for (int d = 32; d; d /= 2) v += __shfl_xor(v, d);
   return v;
 }
+
+// Logits of four tokens for an expert a wave: eight values of its router's row at a time and lane.
+__device__ __forceinline__ void load_eight(int type, const char* p, int64_t i, int left, float out[8]) {
+  if (left >= 8) {
+    const int size = type == OZ2_F32 ? 4 : 2;
+    const w4_u4 a = w4_bytes<16>(p + i * size), b = type == OZ2_F32 ? w4_bytes<16>(p + (i + 4) * size) : w4_u4{0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      out[e] = type == OZ2_F32 ? __uint_as_float(e < 4 ? a[e % 4] : b[e % 4]) : w4_decode16(type, a[e / 2] >> (e % 2 * 16) & 0xFFFFu);
+  } else {
+    for (int e = 0; e < 8; ++e) out[e] = e < left ? w4_load(type, p, i + e) : 0.f;
+  }
+}
+__global__ void __launch_bounds__(256) moe_router_kernel(const char* router, int router_type, int64_t ld_router, int x_type, MoeCall c) {
+  const int e = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x % 64, first = blockIdx.y * 4, tokens = min(4, c.t - first);
+  if (e >= c.experts) return;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int i = lane * 8; i < c.d; i += 512) {
+    float r[8], x[8];
+    load_eight(router_type, router, e * ld_router + i, c.d - i, r);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      if (t >= tokens) continue;
+      load_eight(x_type, c.x, (first + t) * c.ldx + i, c.d - i, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[t] = fmaf(r[j], x[j], sum[t]);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const float v = wave_sum(sum[t]);
+    if (lane == 0 && t < tokens) c.logits[(int64_t)(first + t) * c.experts + e] = v;
+  }
+}
+
+// The kernels below serve layers whose vectors are too short or too long for those of the other files.
 
 // One wave a logit.
 __global__ void __launch_bounds__(256) moe_logits_kernel(oz2_moe_layer m, int x_type, const char* x, int64_t ldx, float* logits) {
@@ -93,36 +133,79 @@ __global__ void __launch_bounds__(256) moe_outer_kernel(oz2_moe_layer m, const i
 }
 
 struct Space {
-  size_t logits, ids, weights, h, total;
+  size_t logits, ids, weights, chosen, h, part, total;
 };
 Space space(const oz2_moe_layer& m, int64_t t) {
   Space s;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
-  s.logits = take((size_t)t * m.gate.count * 4);
-  s.ids = take((size_t)t * m.top_k * 4);
-  s.weights = take((size_t)t * m.top_k * 4);
-  s.h = take((size_t)t * m.top_k * m.gate.n * 4);
+  const size_t at_once = t < kMoeTokens ? t : kMoeTokens, places = at_once * m.top_k;
+  s.logits = take(at_once * m.gate.count * 4);
+  s.ids = take(places * 4);
+  s.weights = take(places * 4);
+  s.chosen = take((2 + 3 * (size_t)kMoePlaces) * 4);
+  s.h = take(places * m.gate.n * 4);
+  s.part = take(places * m.down.n * 4);
   s.total = at;
   return s;
 }
 
 }  // namespace
 
+int oz2_w4_compute_units() {
+  static const int cus = [] {
+    int device = 0, n = 0;
+    return hipGetDevice(&device) == hipSuccess && hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, device) == hipSuccess && n > 0 ? n : 256;
+  }();
+  return cus;
+}
+
 size_t oz2_w4_moe_space(const oz2_moe_layer& m, int64_t t) { return space(m, t).total; }
 
 hipError_t oz2_launch_w4_moe(const oz2_moe_layer& m, int64_t t, int x_type, const void* x, int64_t ldx, const uint8_t* active, int y_type,
                              void* y, int64_t ldy, int32_t* ids, float* weights, char* ws, hipStream_t st) {
   const Space s = space(m, t);
-  float* logits = reinterpret_cast<float*>(ws + s.logits);
-  float* h = reinterpret_cast<float*>(ws + s.h);
-  if (!ids) ids = reinterpret_cast<int32_t*>(ws + s.ids);
-  if (!weights) weights = reinterpret_cast<float*>(ws + s.weights);
-  const char* xp = static_cast<const char*>(x);
-  hipLaunchKernelGGL(moe_logits_kernel, dim3((unsigned)((m.gate.count + 3) / 4), (unsigned)t), dim3(256), 0, st, m, x_type, xp, ldx, logits);
-  hipLaunchKernelGGL(moe_choose_kernel, dim3((unsigned)((t + 63) / 64)), dim3(64), 0, st, m, t, active, logits, ids, weights);
-  hipLaunchKernelGGL(moe_inner_kernel, dim3((unsigned)((m.gate.n + 3) / 4), (unsigned)(t * m.top_k)), dim3(256), 0, st, m, x_type, xp, ldx, ids, h);
-  hipLaunchKernelGGL(moe_outer_kernel, dim3((unsigned)((m.down.n + 3) / 4), (unsigned)t), dim3(256), 0, st, m, ids, weights, h, y_type,
-                     static_cast<char*>(y), ldy);
-  return hipGetLastError();
+  const int64_t d = m.gate.k, f = m.gate.n;
+  const int x_size = x_type == OZ2_F32 ? 4 : 2, y_size = y_type == OZ2_F32 ? 4 : 2;
+  for (int64_t first = 0; first < t; first += kMoeTokens) {
+    MoeCall c;
+    c.t = (int)(t - first < kMoeTokens ? t - first : kMoeTokens);
+    c.d = (int)d, c.f = (int)f, c.experts = (int)m.gate.count, c.top_k = m.top_k;
+    c.score = m.score, c.renormalize = m.renormalize, c.activation = m.activation, c.factor = m.factor, c.bias = m.bias;
+    c.active = active ? active + first : nullptr;
+    c.x = static_cast<const char*>(x) + first * ldx * x_size, c.ldx = ldx;
+    const oz2_w4_matrix* of[3] = {&m.gate, &m.up, &m.down};
+    W4Rows* rows[3] = {&c.gate, &c.up, &c.down};
+    for (int i = 0; i < 3; ++i) {
+      *rows[i] = oz2_w4_rows(*of[i]);
+      c.code_strides[i] = of[i]->stride_codes, c.scale_strides[i] = of[i]->stride_scales * (of[i]->scale_type == OZ2_F32 ? 4 : 2);
+      c.zero_strides[i] = of[i]->stride_zeros;
+    }
+    c.y_type = y_type, c.y = static_cast<char*>(y) + first * ldy * y_size, c.ldy = ldy;
+    c.logits = reinterpret_cast<float*>(ws + s.logits);
+    c.ids = ids ? ids + first * m.top_k : reinterpret_cast<int32_t*>(ws + s.ids);
+    c.weights = weights ? weights + first * m.top_k : reinterpret_cast<float*>(ws + s.weights);
+    c.chosen = reinterpret_cast<int*>(ws + s.chosen);
+    c.h = reinterpret_cast<float*>(ws + s.h), c.part = reinterpret_cast<float*>(ws + s.part);
+    c.st = st;
+    // rows of 16 bytes of codes or more, and spans of 2048 for at most eight waves
+    if (d < kW4Unit || f < kW4Unit || d > kW4Span * 8 || f > kW4Span * 8) {
+      hipLaunchKernelGGL(moe_logits_kernel, dim3((unsigned)((c.experts + 3) / 4), c.t), dim3(256), 0, st, m, x_type, c.x, ldx, c.logits);
+      hipLaunchKernelGGL(moe_choose_kernel, dim3(1), dim3(64), 0, st, m, c.t, c.active, c.logits, c.ids, c.weights);
+      hipLaunchKernelGGL(moe_inner_kernel, dim3((unsigned)((f + 3) / 4), c.t * c.top_k), dim3(256), 0, st, m, x_type, c.x, ldx, c.ids, c.h);
+      hipLaunchKernelGGL(moe_outer_kernel, dim3((unsigned)((d + 3) / 4), c.t), dim3(256), 0, st, m, c.ids, c.weights, c.h, y_type, c.y, ldy);
+      if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+      continue;
+    }
+    hipLaunchKernelGGL(moe_router_kernel, dim3((c.experts + 3) / 4, (c.t + 3) / 4), dim3(256), 0, st, static_cast<const char*>(m.router), m.router_type,
+                       m.ld_router, x_type, c);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess)
+      e = x_type == OZ2_F32    ? oz2_moe_gate_up<OZ2_F32>(c, m.gate.scale_type)
+          : x_type == OZ2_BF16 ? oz2_moe_gate_up<OZ2_BF16>(c, m.gate.scale_type)
+                               : oz2_moe_gate_up<OZ2_F16>(c, m.gate.scale_type);
+    if (e == hipSuccess) e = oz2_moe_down(c, m.down.scale_type);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }

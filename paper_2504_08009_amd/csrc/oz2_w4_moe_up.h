@@ -1,0 +1,172 @@
+// Choice of the experts and their first products: h = act(gate x) * (up x) for every place.
+#ifndef OZ2_W4_MOE_UP_H
+#define OZ2_W4_MOE_UP_H
+
+#include "oz2_w4_moe.h"
+
+#ifdef __HIPCC__
+namespace {
+
+// Largest of the wave's keys, and the smallest index that has it.
+__device__ __forceinline__ void moe_best(float& key, int& index) {
+#pragma unroll
+  for (int d = 32; d; d /= 2) {
+    const float k = __shfl_xor(key, d);
+    const int i = __shfl_xor(index, d);
+    if (k > key || (k == key && i < index)) key = k, index = i;
+  }
+}
+
+// Experts and weights of one token, by one wave; ids (LDS) gets -1 where there is none.  A lane holds the experts lane, lane + 64, ...
+template <int V>
+__device__ __forceinline__ void moe_choose(const MoeCall& c, int token, short* ids, float* weights) {
+  const int lane = threadIdx.x % 64;
+  const float* logits = c.logits + (int64_t)token * c.experts;
+  float p[V], key[V], high = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int e = lane + 64 * i;
+    p[i] = e < c.experts ? logits[e] : -INFINITY;
+    high = fmaxf(high, p[i]);
+  }
+  if (c.score == OZ2_SCORE_SOFTMAX) {
+    float total = 0.f;
+    for (int d = 32; d; d /= 2) high = fmaxf(high, __shfl_xor(high, d));
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      p[i] = lane + 64 * i < c.experts ? expf(p[i] - high) : 0.f;
+      total += p[i];
+    }
+    for (int d = 32; d; d /= 2) total += __shfl_xor(total, d);
+#pragma unroll
+    for (int i = 0; i < V; ++i) p[i] /= total;
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) p[i] = 1.f / (1.f + expf(-p[i]));
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int e = lane + 64 * i;
+    key[i] = e < c.experts ? p[i] + (c.bias ? c.bias[e] : 0.f) : -INFINITY;
+    if (key[i] != key[i]) key[i] = INFINITY;
+  }
+  const bool active = !c.active || c.active[token];
+  float sum = 0.f, mine = 0.f;  // (lane j keeps the j-th weight)
+  for (int j = 0; j < c.top_k; ++j) {
+    float best = -INFINITY;
+    int id = c.experts;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (key[i] > best) best = key[i], id = lane + 64 * i;
+    moe_best(best, id);
+    const bool there = best > -INFINITY && active;
+    float w = 0.f;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (lane + 64 * i == id) w = p[i], key[i] = -INFINITY;
+    w = there ? __shfl(w, id % 64) : 0.f;
+    sum += w;
+    if (lane == j) mine = w;
+    if (lane == 0) ids[token * c.top_k + j] = there ? id : -1;
+  }
+  if (c.renormalize) mine = sum == 0.f ? 0.f : mine / sum;
+  if (lane < c.top_k) weights[token * c.top_k + lane] = mine * c.factor;
+}
+
+// Every workgroup makes the choice for itself, which is cheaper than a launch in between; the first one leaves it for the launches behind.
+__device__ __forceinline__ void moe_route(const MoeCall& c, Chosen& chosen, short* ids, float* weights, int* count) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+  const int places = c.t * c.top_k;
+  for (int e = threadIdx.x; e < c.experts; e += 64 * kMoeWaves) count[e] = 0;
+  for (int token = wave; token < c.t; token += kMoeWaves) {
+    if (c.experts <= 64) moe_choose<1>(c, token, ids, weights);
+    else if (c.experts <= 128) moe_choose<2>(c, token, ids, weights);
+    else if (c.experts <= 256) moe_choose<4>(c, token, ids, weights);
+    else moe_choose<16>(c, token, ids, weights);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < places; i += 64 * kMoeWaves)
+    if (ids[i] >= 0) atomicAdd(&count[ids[i]], 1);
+  __syncthreads();
+  if (wave == 0) {  // experts that have places, and where these begin
+    int found = 0, at = 0;
+    for (int e = 0; e < c.experts; e += 64) {
+      const int n = e + lane < c.experts ? count[e + lane] : 0;
+      int before = n;
+      for (int d = 1; d < 64; d *= 2) {
+        const int other = __shfl_up(before, d);
+        if (lane >= d) before += other;
+      }
+      const unsigned long long mask = __ballot(n > 0);
+      if (n) {
+        const int i = found + __popcll(mask & ((1ull << lane) - 1));
+        chosen.expert[i] = e + lane;
+        chosen.first[i] = at + before - n;
+        count[e + lane] = at + before - n;  // from here on: where its next place goes
+      }
+      found += __popcll(mask);
+      at += __shfl(before, 63);
+    }
+    if (lane == 0) chosen.count = found, chosen.first[found] = at;
+  }
+  __syncthreads();
+  // (the order of an expert's places changes no result: each is summed by itself)
+  for (int i = threadIdx.x; i < places; i += 64 * kMoeWaves)
+    if (ids[i] >= 0) chosen.place[atomicAdd(&count[ids[i]], 1)] = i;
+  __syncthreads();
+  if (blockIdx.x) return;
+  for (int i = threadIdx.x; i < places; i += 64 * kMoeWaves) c.ids[i] = ids[i], c.weights[i] = weights[i];
+  int* to = c.chosen;
+  const int n = chosen.count;
+  if (threadIdx.x == 0) to[0] = n;
+  for (int i = threadIdx.x; i <= n; i += 64 * kMoeWaves) to[1 + i] = chosen.first[i];
+  for (int i = threadIdx.x; i < n; i += 64 * kMoeWaves) to[2 + kMoePlaces + i] = chosen.expert[i];
+  for (int i = threadIdx.x; i < chosen.first[n]; i += 64 * kMoeWaves) to[2 + 2 * kMoePlaces + i] = chosen.place[i];
+}
+
+template <int XT, int T, int ST, bool ZEROS>
+__global__ void __launch_bounds__(64 * kMoeWaves) moe_up_kernel(MoeCall c, int split_log) {
+  __shared__ Chosen chosen;
+  __shared__ short ids[kMoePlaces];
+  __shared__ float weights[kMoePlaces];
+  __shared__ int count[OZ2_MOE_MAX_EXPERTS];
+  __shared__ float part[2][kMoeRounds][kMoeWaves][4][T];
+  moe_route(c, chosen, ids, weights, count);
+  struct Two { W4Rows gate, up; };
+  moe_products<XT, T, ST, ZEROS>(
+      chosen, c.d, c.f, 2, split_log, c.gate, part,
+      [&](int64_t e) {
+        return Two{w4_of_stack(c.gate, e, c.code_strides[0], c.scale_strides[0], c.zero_strides[0]),
+                   w4_of_stack(c.up, e, c.code_strides[1], c.scale_strides[1], c.zero_strides[1])};
+      },
+      [&](const Two& m, int row, int i) { return w4_row<ST>(i < 2 ? m.gate : m.up, row + i % 2); },
+      [&](int place) { return c.x + place / c.top_k * c.ldx * (XT == OZ2_F32 ? 4 : 2); },
+      [&](int place, int row, const float* u) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (row + i < c.f) {
+            const float g = u[i];
+            const float a = c.activation == OZ2_ACT_SILU ? g / (1.f + expf(-g)) : 0.5f * g * (1.f + erff(g * 0.70710678f));
+            c.h[(int64_t)place * c.f + row + i] = a * u[2 + i];
+          }
+      });
+}
+
+template <int XT, int T, int ST>
+hipError_t launch_up(const MoeCall& c) {
+  const dim3 grid(oz2_w4_compute_units() * 2), block(64 * kMoeWaves);
+  if (c.gate.zeros) hipLaunchKernelGGL((moe_up_kernel<XT, T, ST, true>), grid, block, 0, c.st, c, moe_split(c.d));
+  else hipLaunchKernelGGL((moe_up_kernel<XT, T, ST, false>), grid, block, 0, c.st, c, moe_split(c.d));
+  return hipGetLastError();
+}
+
+}  // namespace
+
+template <int XT>
+hipError_t oz2_moe_gate_up(const MoeCall& c, int scale_type) {
+  if (c.t == 1)
+    return scale_type == OZ2_F32 ? launch_up<XT, 1, OZ2_F32>(c) : scale_type == OZ2_BF16 ? launch_up<XT, 1, OZ2_BF16>(c) : launch_up<XT, 1, OZ2_F16>(c);
+  return scale_type == OZ2_F32 ? launch_up<XT, 2, OZ2_F32>(c) : scale_type == OZ2_BF16 ? launch_up<XT, 2, OZ2_BF16>(c) : launch_up<XT, 2, OZ2_F16>(c);
+}
+#endif
+#endif

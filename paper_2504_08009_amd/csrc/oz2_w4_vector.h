@@ -11,9 +11,6 @@
 constexpr int kW4Unit = 32;                 // inner indexes of a lane
 constexpr int kW4Span = 64 * kW4Unit;       // of a wave
 
-typedef __bf16 w4_bf2 __attribute__((ext_vector_type(2)));
-typedef _Float16 w4_h2 __attribute__((ext_vector_type(2)));
-
 // A lane's 32 values of x (pairs in the order of w4_unpack, or FP32), their sum, and where it finds the codes and scales of a row.
 template <int XT>
 struct W4X {
@@ -63,16 +60,10 @@ __device__ __forceinline__ W4X<XT> w4_keep_x(int k, int unit, w4_u4 raw[XT == OZ
         s += __uint_as_float(raw[j][e]), a += fabsf(__uint_as_float(raw[j][e]));
       }
     } else {
+      w4_sums<XT>(raw[j], s, a);
+      const w4_u4 p = w4_pairs(raw[j]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float lo = w4_decode16(XT, raw[j][e] & 0xFFFFu), hi = w4_decode16(XT, raw[j][e] >> 16);
-        s += lo + hi, a += fabsf(lo) + fabsf(hi);
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {  // (0, 4), (1, 5), (2, 6), (3, 7)
-        const unsigned lo = raw[j][e / 2], hi = raw[j][2 + e / 2];
-        x.v[4 * j + e] = e % 2 ? (lo >> 16) | (hi & 0xFFFF0000u) : (lo & 0xFFFFu) | hi << 16;
-      }
+      for (int e = 0; e < 4; ++e) x.v[4 * j + e] = p[e];
     }
   }
   x.sum = s;
@@ -81,8 +72,8 @@ __device__ __forceinline__ W4X<XT> w4_keep_x(int k, int unit, w4_u4 raw[XT == OZ
 }
 
 // sum of (16 + q) x (16-bit x) or q x (FP32 x) over the lane's codes, for T vectors at once
-template <int XT, int T, int NC>
-__device__ __forceinline__ void w4_dot(w4_u4 codes, const W4X<XT> (&x)[T][NC], int c, float out[T]) {
+template <int XT, int T>
+__device__ __forceinline__ void w4_dot(w4_u4 codes, const W4X<XT> (&x)[T], float (&out)[T]) {
   float a[T][2];
 #pragma unroll
   for (int t = 0; t < T; ++t) a[t][0] = a[t][1] = 0.f;
@@ -95,8 +86,8 @@ __device__ __forceinline__ void w4_dot(w4_u4 codes, const W4X<XT> (&x)[T][NC], i
         const float q = (float)(even >> (8 * e) & 255u), r = (float)(odd >> (8 * e) & 255u);
 #pragma unroll
         for (int t = 0; t < T; ++t) {
-          a[t][0] = fmaf(q, __uint_as_float(x[t][c].v[8 * j + 2 * e]), a[t][0]);
-          a[t][1] = fmaf(r, __uint_as_float(x[t][c].v[8 * j + 2 * e + 1]), a[t][1]);
+          a[t][0] = fmaf(q, __uint_as_float(x[t].v[8 * j + 2 * e]), a[t][0]);
+          a[t][1] = fmaf(r, __uint_as_float(x[t].v[8 * j + 2 * e + 1]), a[t][1]);
         }
       }
     } else {
@@ -106,10 +97,7 @@ __device__ __forceinline__ void w4_dot(w4_u4 codes, const W4X<XT> (&x)[T][NC], i
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int t = 0; t < T; ++t) {
-          if constexpr (XT == OZ2_BF16)
-            a[t][e % 2] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(w4_bf2, b[e]), __builtin_bit_cast(w4_bf2, x[t][c].v[4 * j + e]), a[t][e % 2], false);
-          else
-            a[t][e % 2] = __builtin_amdgcn_fdot2(__builtin_bit_cast(w4_h2, b[e]), __builtin_bit_cast(w4_h2, x[t][c].v[4 * j + e]), a[t][e % 2], false);
+          a[t][e % 2] = w4_dot2<XT>(b[e], x[t].v[4 * j + e], a[t][e % 2]);
         }
     }
   }
@@ -117,16 +105,27 @@ __device__ __forceinline__ void w4_dot(w4_u4 codes, const W4X<XT> (&x)[T][NC], i
   for (int t = 0; t < T; ++t) out[t] = a[t][0] + a[t][1];
 }
 
-// The same for the row, straight from memory, with s (q - z) x one by one: for x with infinities, NaNs or values near the end of the range.
+// A row of codes, its scales and its zero points.
+struct W4Row {
+  const uint8_t* codes;
+  const char* scales;
+  const uint8_t* zeros;
+};
+template <int ST>
+__device__ __forceinline__ W4Row w4_row(const W4Rows& w, int row) {
+  const int64_t n = min(row, w.n - 1);
+  return {w.codes + n * w.ld_codes, w.scales + n * w.ld_scales * (ST == OZ2_F32 ? 4 : 2), w.zeros + n * w.ld_zeros};
+}
+
+// The lane's sum of s (q - z) x straight from memory, one by one: for x with infinities, NaNs or values near the end of the range.
 template <int XT, int ST, bool ZEROS>
-__device__ __forceinline__ float w4_unit_plain(const W4Rows& w, const uint8_t* codes, const char* scales, const uint8_t* zeros, int64_t row, const char* x,
-                                               int unit) {
-  const int end = min((unit + 1) * kW4Unit, w.k), g = unit / (w.group / kW4Unit);
+__device__ __forceinline__ float w4_unit_plain(int k, int group, W4Row row, const char* x, int unit) {
+  const int end = min((unit + 1) * kW4Unit, k), g = unit / (group / kW4Unit);
   float sum = 0.f;
 #pragma unroll 1
   for (int i = unit * kW4Unit; i < end; ++i) {
-    const int q = codes[row * w.ld_codes + i / 2] >> (i % 2 * 4) & 15;
-    sum = fmaf(w4_load(ST, scales, row * w.ld_scales + g) * (float)(q - (ZEROS ? (int)zeros[row * w.ld_zeros + g] : 8)), w4_load(XT, x, i), sum);
+    const int q = row.codes[i / 2] >> (i % 2 * 4) & 15;
+    sum = fmaf(w4_load(ST, row.scales, g) * (float)(q - (ZEROS ? (int)row.zeros[g] : 8)), w4_load(XT, x, i), sum);
   }
   return sum;
 }
@@ -145,62 +144,69 @@ __device__ __forceinline__ float w4_sum4(float a, float b, float c, float d) {
   return v;
 }
 
-// Four rows (from `row`, those past the end repeat the last) times T vectors, the inner indexes of this wave's NC spans; x as kept.
-// All loads first: R * NC of 16 bytes a lane are in flight.
-template <int XT, int T, int NC, int ST, bool ZEROS>
+// Four rows times T vectors, a span of the inner indexes; x as kept.  All loads come first: 4 KiB a wave in flight.
+template <int XT, int T, int ST, bool ZEROS>
 struct W4Rows4 {
-  W4Regs<1, ST> r[4][NC];
+  W4Regs<1, ST> r[4];
 
-  __device__ __forceinline__ void fetch(const W4Rows& w, const uint8_t* codes, const char* scales, const uint8_t* zeros, int row, const W4Place (&at)[NC]) {
+  template <class Row>
+  __device__ __forceinline__ void fetch(Row row, W4Place at) {
     constexpr int size = ST == OZ2_F32 ? 4 : 2;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int64_t n = min(row + i, w.n - 1);
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        r[i][c].q = w4_bytes<16>(codes + n * w.ld_codes + at[c].codes);
-        r[i][c].s = w4_bytes<size>(scales + n * w.ld_scales * size + at[c].group * size);
-        if constexpr (ZEROS) r[i][c].z = zeros[n * w.ld_zeros + at[c].group];
-      }
+      const W4Row p = row(i);
+      r[i].q = w4_bytes<16>(p.codes + at.codes);
+      r[i].s = w4_bytes<size>(p.scales + at.group * size);
+      if constexpr (ZEROS) r[i].z = p.zeros[at.group];
     }
   }
 
   // sum[i][t] of the lane
-  __device__ __forceinline__ void multiply(const W4Place (&at)[NC], const W4X<XT> (&x)[T][NC], const bool (&ragged)[NC], float (&sum)[4][T]) {
+  __device__ __forceinline__ void multiply(W4Place at, const W4X<XT> (&x)[T], bool ragged, float (&sum)[4][T]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+      w4_u4 q = r[i].q;
+      if (ragged) q = w4_cut(q, at.cut);
+      float s, z = 8.f, p[T];
+      if constexpr (ST == OZ2_F32) s = __uint_as_float(r[i].s);
+      else s = w4_decode16(ST, r[i].s);
+      if constexpr (ZEROS) z = (float)r[i].z;
+      w4_dot<XT, T>(q, x, p);
 #pragma unroll
-      for (int t = 0; t < T; ++t) sum[i][t] = 0.f;
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        w4_u4 q = r[i][c].q;
-        if (ragged[c]) q = w4_cut(q, at[c].cut);
-        float s, z = 8.f;
-        if constexpr (ST == OZ2_F32) s = __uint_as_float(r[i][c].s);
-        else s = w4_decode16(ST, r[i][c].s);
-        if constexpr (ZEROS) z = (float)r[i][c].z;
-        float p[T];
-        w4_dot<XT, T, NC>(q, x, c, p);
-#pragma unroll
-        for (int t = 0; t < T; ++t) sum[i][t] = fmaf(s, fmaf(-(XT == OZ2_F32 ? z : z + kW4Offset), x[t][c].sum, p[t]), sum[i][t]);
-      }
+      for (int t = 0; t < T; ++t) sum[i][t] = s * fmaf(-(XT == OZ2_F32 ? z : z + kW4Offset), x[t].sum, p[t]);
     }
   }
 
-  __device__ __forceinline__ void multiply_plain(const W4Rows& w, const uint8_t* codes, const char* scales, const uint8_t* zeros, int row, const char* x,
-                                                 int64_t ldx, int unit, float (&sum)[4][T]) {
+  // The sums of the vectors in `which` again (no other's: what one vector holds changes no bit of another's result).
+  template <class Row, class X>
+  __device__ __forceinline__ void multiply_plain(unsigned which, int k, int group, Row row, X x, int unit, float (&sum)[4][T]) {
 #pragma unroll 1
     for (int j = 0; j < 4 * T; ++j) {
-      float v = 0.f;
-#pragma unroll 1
-      for (int c = 0; c < NC; ++c)
-        v += w4_unit_plain<XT, ST, ZEROS>(w, codes, scales, zeros, min(row + j / T, w.n - 1), x + j % T * ldx * (XT == OZ2_F32 ? 4 : 2), unit + 64 * c);
+      if (!(which >> (j % T) & 1)) continue;
+      const float v = w4_unit_plain<XT, ST, ZEROS>(k, group, row(j / T), x(j % T), unit);
       w4_each<4 * T>([&](auto i) __attribute__((always_inline)) {
         if (j == i.value) sum[i.value / T][i.value % T] = v;
       });
     }
   }
 };
+
+// T vectors of a span, from memory into registers; returns a bit for each vector whose values call for multiply_plain.  x(t): start of vector t.
+template <int XT, int T, class X>
+__device__ __forceinline__ unsigned w4_take_x(int k, int unit, X x, W4X<XT> (&kept)[T]) {
+  w4_u4 raw[T][XT == OZ2_F32 ? 8 : 4];
+  unsigned which = 0;
+  asm volatile("" : "+v"(unit));  // else, in a loop, all that follows from it is kept in registers
+#pragma unroll
+  for (int t = 0; t < T; ++t) w4_load_x<XT>(x(t), k, unit, raw[t]);
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    bool plain = false;
+    kept[t] = w4_keep_x<XT>(k, unit, raw[t], plain);
+    which |= (unsigned)(__ballot(plain) != 0) << t;
+  }
+  return which;
+}
 
 #endif
 #endif
