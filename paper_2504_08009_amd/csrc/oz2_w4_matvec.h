@@ -154,9 +154,9 @@ __global__ void __launch_bounds__(64 * kWaves) w4_vector_kernel(W4Rows w, int sp
   const int unit = s * 64 + lane;
   const W4Place at = w4_place(w, unit);
   const bool ragged = __ballot(at.cut != 0) != 0;
-  W4Rows4<XT, T, ST, ZEROS> rows;
+  W4Rows4<XT, T, ST, ZEROS, 1> rows;
   int b = first + (wave >> split_log);
-  auto row_of = [&](int batch) { return [&, batch](int i) { return w4_row<ST>(w, batch * 4 + i); }; };
+  auto row_of = [&](int batch) { return [&, batch](int i) { return w4_row<ST, 1>(w, batch * 4, i); }; };
   auto vector = [&](int t) { return x + t * ldx * (XT == OZ2_F32 ? 4 : 2); };
   rows.fetch(row_of(b), at);
   W4X<XT> kept[T];
@@ -174,7 +174,11 @@ __global__ void __launch_bounds__(64 * kWaves) w4_vector_kernel(W4Rows w, int sp
     if (i + 1 < rounds) rows.fetch(row_of(b + step), at);
     float v[T];
 #pragma unroll
-    for (int t = 0; t < T; ++t) v[t] = w4_sum4(sum[0][t], sum[1][t], sum[2][t], sum[3][t]);
+    for (int t = 0; t < T; ++t) {
+      float one[1];
+      w4_sum4<1>(sum[0][t], sum[1][t], sum[2][t], sum[3][t], one);
+      v[t] = one[0];
+    }
     const int t = lane % 16;
     if (split == 1) {
       const int64_t row = (int64_t)b * 4 + lane / 16;

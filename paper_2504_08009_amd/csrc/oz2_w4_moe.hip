@@ -12,38 +12,55 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
-// Logits of four tokens for an expert a wave: eight values of its router's row at a time and lane.
-__device__ __forceinline__ void load_eight(int type, const char* p, int64_t i, int left, float out[8]) {
+// Logits of four tokens for an expert: a workgroup, whose waves share the inner dimension; a lane takes eight values of each at a time.
+template <int TYPE>
+__device__ __forceinline__ void load_eight(const char* p, int64_t i, int left, float (&out)[8]) {
+  constexpr int size = TYPE == OZ2_F32 ? 4 : 2;
   if (left >= 8) {
-    const int size = type == OZ2_F32 ? 4 : 2;
-    const w4_u4 a = w4_bytes<16>(p + i * size), b = type == OZ2_F32 ? w4_bytes<16>(p + (i + 4) * size) : w4_u4{0, 0, 0, 0};
+    w4_u4 a = w4_bytes<16>(p + i * size), b = a;
+    if constexpr (TYPE == OZ2_F32) b = w4_bytes<16>(p + (i + 4) * size);
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      out[e] = type == OZ2_F32 ? __uint_as_float(e < 4 ? a[e % 4] : b[e % 4]) : w4_decode16(type, a[e / 2] >> (e % 2 * 16) & 0xFFFFu);
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (TYPE == OZ2_F32) out[e] = __uint_as_float(e < 4 ? a[e % 4] : b[e % 4]);
+      else out[e] = w4_decode16(TYPE, a[e / 2] >> (e % 2 * 16) & 0xFFFFu);
+    }
   } else {
-    for (int e = 0; e < 8; ++e) out[e] = e < left ? w4_load(type, p, i + e) : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) out[e] = e < left ? w4_load(TYPE, p, i + e) : 0.f;
   }
 }
-__global__ void __launch_bounds__(256) moe_router_kernel(const char* router, int router_type, int64_t ld_router, int x_type, MoeCall c) {
-  const int e = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x % 64, first = blockIdx.y * 4, tokens = min(4, c.t - first);
-  if (e >= c.experts) return;
+template <int RT, int XT>
+__global__ void __launch_bounds__(256) moe_router_kernel(const char* router, int64_t ld_router, MoeCall c) {
+  __shared__ float part[4][4];
+  const int e = blockIdx.x, wave = threadIdx.x / 64, lane = threadIdx.x % 64, first = blockIdx.y * 4, tokens = min(4, c.t - first);
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int i = lane * 8; i < c.d; i += 512) {
-    float r[8], x[8];
-    load_eight(router_type, router, e * ld_router + i, c.d - i, r);
+#pragma unroll 2
+  for (int i = threadIdx.x * 8; i < c.d; i += 2048) {
+    float r[8], x[4][8];
+    load_eight<RT>(router, e * ld_router + i, c.d - i, r);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      if (t >= tokens) continue;
-      load_eight(x_type, c.x, (first + t) * c.ldx + i, c.d - i, x);
+    for (int t = 0; t < 4; ++t) load_eight<XT>(c.x, (first + min(t, tokens - 1)) * c.ldx + i, c.d - i, x[t]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum[t] = fmaf(r[j], x[j], sum[t]);
-    }
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[t] = fmaf(r[j], x[t][j], sum[t]);
   }
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const float v = wave_sum(sum[t]);
-    if (lane == 0 && t < tokens) c.logits[(int64_t)(first + t) * c.experts + e] = v;
-  }
+  for (int t = 0; t < 4; ++t) sum[t] = wave_sum(sum[t]);
+  if (lane == 0)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) part[wave][t] = sum[t];
+  __syncthreads();
+  if (threadIdx.x < tokens)
+    c.logits[(int64_t)(first + threadIdx.x) * c.experts + e] = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
+}
+template <int RT>
+void launch_router(const oz2_moe_layer& m, int x_type, const MoeCall& c) {
+  const dim3 grid(c.experts, (c.t + 3) / 4), block(256);
+  const char* r = static_cast<const char*>(m.router);
+  if (x_type == OZ2_F32) hipLaunchKernelGGL((moe_router_kernel<RT, OZ2_F32>), grid, block, 0, c.st, r, m.ld_router, c);
+  else if (x_type == OZ2_BF16) hipLaunchKernelGGL((moe_router_kernel<RT, OZ2_BF16>), grid, block, 0, c.st, r, m.ld_router, c);
+  else hipLaunchKernelGGL((moe_router_kernel<RT, OZ2_F16>), grid, block, 0, c.st, r, m.ld_router, c);
 }
 
 // The kernels below serve layers whose vectors are too short or too long for those of the other files.
@@ -187,9 +204,10 @@ hipError_t oz2_launch_w4_moe(const oz2_moe_layer& m, int64_t t, int x_type, cons
     c.weights = weights ? weights + first * m.top_k : reinterpret_cast<float*>(ws + s.weights);
     c.chosen = reinterpret_cast<int*>(ws + s.chosen);
     c.h = reinterpret_cast<float*>(ws + s.h), c.part = reinterpret_cast<float*>(ws + s.part);
+    c.pairs = 2 * c.t * c.top_k > c.experts;
     c.st = st;
-    // rows of 16 bytes of codes or more, and spans of 2048 for at most eight waves
-    if (d < kW4Unit || f < kW4Unit || d > kW4Span * 8 || f > kW4Span * 8) {
+    // rows of 16 bytes of codes or more, and spans of 2048 for the waves of a workgroup
+    if (d < kW4Unit || f < kW4Unit || d > kMoeLongest || f > kMoeLongest) {
       hipLaunchKernelGGL(moe_logits_kernel, dim3((unsigned)((c.experts + 3) / 4), c.t), dim3(256), 0, st, m, x_type, c.x, ldx, c.logits);
       hipLaunchKernelGGL(moe_choose_kernel, dim3(1), dim3(64), 0, st, m, c.t, c.active, c.logits, c.ids, c.weights);
       hipLaunchKernelGGL(moe_inner_kernel, dim3((unsigned)((f + 3) / 4), c.t * c.top_k), dim3(256), 0, st, m, x_type, c.x, ldx, c.ids, c.h);
@@ -197,8 +215,9 @@ hipError_t oz2_launch_w4_moe(const oz2_moe_layer& m, int64_t t, int x_type, cons
       if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
       continue;
     }
-    hipLaunchKernelGGL(moe_router_kernel, dim3((c.experts + 3) / 4, (c.t + 3) / 4), dim3(256), 0, st, static_cast<const char*>(m.router), m.router_type,
-                       m.ld_router, x_type, c);
+    if (m.router_type == OZ2_F32) launch_router<OZ2_F32>(m, x_type, c);
+    else if (m.router_type == OZ2_BF16) launch_router<OZ2_BF16>(m, x_type, c);
+    else launch_router<OZ2_F16>(m, x_type, c);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess)
       e = x_type == OZ2_F32    ? oz2_moe_gate_up<OZ2_F32>(c, m.gate.scale_type)

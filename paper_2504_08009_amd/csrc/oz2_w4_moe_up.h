@@ -5,19 +5,32 @@
 #include "oz2_w4_moe.h"
 
 #ifdef __HIPCC__
+#ifndef MOE_UP_WAVES
+#define MOE_UP_WAVES 4
+#endif
+#ifndef MOE_UP_GRID
+#define MOE_UP_GRID 4
+#endif
 namespace {
 
-// Largest of the wave's keys, and the smallest index that has it.
-__device__ __forceinline__ void moe_best(float& key, int& index) {
-#pragma unroll
-  for (int d = 32; d; d /= 2) {
-    const float k = __shfl_xor(key, d);
-    const int i = __shfl_xor(index, d);
-    if (k > key || (k == key && i < index)) key = k, index = i;
-  }
+// Over the wave, in every lane.
+__device__ __forceinline__ float wave_max(float v) {
+  typedef unsigned u2 __attribute__((ext_vector_type(2)));
+  auto larger = [](u2 r) { return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])); };
+  v = fmaxf(v, w4_partner<0>(v)), v = fmaxf(v, w4_partner<1>(v)), v = fmaxf(v, w4_partner<2>(v)), v = fmaxf(v, w4_partner<3>(v));
+  v = larger(__builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+  return larger(__builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  typedef unsigned u2 __attribute__((ext_vector_type(2)));
+  auto both = [](u2 r) { return __uint_as_float(r[0]) + __uint_as_float(r[1]); };
+  v += w4_partner<0>(v), v += w4_partner<1>(v), v += w4_partner<2>(v), v += w4_partner<3>(v);
+  v = both(__builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+  return both(__builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
 }
 
-// Experts and weights of one token, by one wave; ids (LDS) gets -1 where there is none.  A lane holds the experts lane, lane + 64, ...
+// Experts and weights of one token, by one wave; ids (LDS) gets -1 where there is none.  A lane holds V neighbouring experts, so that the
+// first lane with the largest key has the lowest index that has it.
 template <int V>
 __device__ __forceinline__ void moe_choose(const MoeCall& c, int token, short* ids, float* weights) {
   const int lane = threadIdx.x % 64;
@@ -25,19 +38,20 @@ __device__ __forceinline__ void moe_choose(const MoeCall& c, int token, short* i
   float p[V], key[V], high = -INFINITY;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int e = lane + 64 * i;
+    const int e = lane * V + i;
     p[i] = e < c.experts ? logits[e] : -INFINITY;
+    key[i] = e < c.experts && c.bias ? c.bias[e] : 0.f;
     high = fmaxf(high, p[i]);
   }
   if (c.score == OZ2_SCORE_SOFTMAX) {
     float total = 0.f;
-    for (int d = 32; d; d /= 2) high = fmaxf(high, __shfl_xor(high, d));
+    high = wave_max(high);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      p[i] = lane + 64 * i < c.experts ? expf(p[i] - high) : 0.f;
+      p[i] = lane * V + i < c.experts ? expf(p[i] - high) : 0.f;
       total += p[i];
     }
-    for (int d = 32; d; d /= 2) total += __shfl_xor(total, d);
+    total = wave_sum(total);
 #pragma unroll
     for (int i = 0; i < V; ++i) p[i] /= total;
   } else {
@@ -46,31 +60,37 @@ __device__ __forceinline__ void moe_choose(const MoeCall& c, int token, short* i
   }
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int e = lane + 64 * i;
-    key[i] = e < c.experts ? p[i] + (c.bias ? c.bias[e] : 0.f) : -INFINITY;
+    key[i] = lane * V + i < c.experts ? p[i] + key[i] : -INFINITY;
     if (key[i] != key[i]) key[i] = INFINITY;
   }
   const bool active = !c.active || c.active[token];
-  float sum = 0.f, mine = 0.f;  // (lane j keeps the j-th weight)
+  float sum = 0.f, mine = 0.f;  // (lane j keeps the j-th)
+  int id = -1;
   for (int j = 0; j < c.top_k; ++j) {
-    float best = -INFINITY;
-    int id = c.experts;
+    float best = key[0];
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (key[i] > best) best = key[i], id = lane + 64 * i;
-    moe_best(best, id);
-    const bool there = best > -INFINITY && active;
+    for (int i = 1; i < V; ++i) best = fmaxf(best, key[i]);
+    const float most = wave_max(best);
+    if (!active || !(most > -INFINITY)) break;
+    const int winner = __ffsll(__ballot(best == most)) - 1;
     float w = 0.f;
+    int which = -1;
+#pragma unroll
+    for (int i = V - 1; i >= 0; --i)
+      if (key[i] == most) w = p[i], which = i;
+    w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), winner));
+    which = __builtin_amdgcn_readlane(which, winner);
 #pragma unroll
     for (int i = 0; i < V; ++i)
-      if (lane + 64 * i == id) w = p[i], key[i] = -INFINITY;
-    w = there ? __shfl(w, id % 64) : 0.f;
+      if (lane == winner && i == which) key[i] = -INFINITY;
     sum += w;
-    if (lane == j) mine = w;
-    if (lane == 0) ids[token * c.top_k + j] = there ? id : -1;
+    if (lane == j) mine = w, id = winner * V + which;
   }
   if (c.renormalize) mine = sum == 0.f ? 0.f : mine / sum;
-  if (lane < c.top_k) weights[token * c.top_k + lane] = mine * c.factor;
+  if (lane < c.top_k) {
+    ids[token * c.top_k + lane] = id;
+    weights[token * c.top_k + lane] = mine * c.factor;
+  }
 }
 
 // Every workgroup makes the choice for itself, which is cheaper than a launch in between; the first one leaves it for the launches behind.
@@ -124,47 +144,51 @@ __device__ __forceinline__ void moe_route(const MoeCall& c, Chosen& chosen, shor
   for (int i = threadIdx.x; i < chosen.first[n]; i += 64 * kMoeWaves) to[2 + 2 * kMoePlaces + i] = chosen.place[i];
 }
 
-template <int XT, int T, int ST, bool ZEROS>
-__global__ void __launch_bounds__(64 * kMoeWaves) moe_up_kernel(MoeCall c, int split_log) {
+template <int XT, int T, int ST, bool ZEROS, int FOLD>
+__global__ void __launch_bounds__(64 * kMoeWaves, MOE_UP_WAVES) moe_up_kernel(MoeCall c, int split_log) {
   __shared__ Chosen chosen;
   __shared__ short ids[kMoePlaces];
   __shared__ float weights[kMoePlaces];
   __shared__ int count[OZ2_MOE_MAX_EXPERTS];
-  __shared__ float part[2][kMoeRounds][kMoeWaves][4][T];
+  __shared__ float part[2][kMoeRounds][kMoeWaves][4 * FOLD][T];
   moe_route(c, chosen, ids, weights, count);
   struct Two { W4Rows gate, up; };
-  moe_products<XT, T, ST, ZEROS>(
+  moe_products<XT, T, ST, ZEROS, FOLD>(
       chosen, c.d, c.f, 2, split_log, c.gate, part,
       [&](int64_t e) {
         return Two{w4_of_stack(c.gate, e, c.code_strides[0], c.scale_strides[0], c.zero_strides[0]),
                    w4_of_stack(c.up, e, c.code_strides[1], c.scale_strides[1], c.zero_strides[1])};
       },
-      [&](const Two& m, int row, int i) { return w4_row<ST>(i < 2 ? m.gate : m.up, row + i % 2); },
+      [&](const Two& m, int row, int i) { return w4_row<ST, FOLD>(i < 2 ? m.gate : m.up, row, i % 2); },
       [&](int place) { return c.x + place / c.top_k * c.ldx * (XT == OZ2_F32 ? 4 : 2); },
       [&](int place, int row, const float* u) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 2 * FOLD; ++i)
           if (row + i < c.f) {
             const float g = u[i];
             const float a = c.activation == OZ2_ACT_SILU ? g / (1.f + expf(-g)) : 0.5f * g * (1.f + erff(g * 0.70710678f));
-            c.h[(int64_t)place * c.f + row + i] = a * u[2 + i];
+            c.h[(int64_t)place * c.f + row + i] = a * u[2 * FOLD + i];
           }
       });
 }
 
+template <int XT, int T, int ST, bool ZEROS>
+hipError_t launch_up(const MoeCall& c) {
+  const dim3 grid(oz2_w4_compute_units() * MOE_UP_GRID), block(64 * kMoeWaves);
+  if (moe_fold(c.gate) && moe_fold(c.up)) hipLaunchKernelGGL((moe_up_kernel<XT, T, ST, ZEROS, 2>), grid, block, 0, c.st, c, 0);
+  else hipLaunchKernelGGL((moe_up_kernel<XT, T, ST, ZEROS, 1>), grid, block, 0, c.st, c, moe_split(c.d));
+  return hipGetLastError();
+}
 template <int XT, int T, int ST>
 hipError_t launch_up(const MoeCall& c) {
-  const dim3 grid(oz2_w4_compute_units() * 2), block(64 * kMoeWaves);
-  if (c.gate.zeros) hipLaunchKernelGGL((moe_up_kernel<XT, T, ST, true>), grid, block, 0, c.st, c, moe_split(c.d));
-  else hipLaunchKernelGGL((moe_up_kernel<XT, T, ST, false>), grid, block, 0, c.st, c, moe_split(c.d));
-  return hipGetLastError();
+  return c.gate.zeros ? launch_up<XT, T, ST, true>(c) : launch_up<XT, T, ST, false>(c);
 }
 
 }  // namespace
 
 template <int XT>
 hipError_t oz2_moe_gate_up(const MoeCall& c, int scale_type) {
-  if (c.t == 1)
+  if (!c.pairs)
     return scale_type == OZ2_F32 ? launch_up<XT, 1, OZ2_F32>(c) : scale_type == OZ2_BF16 ? launch_up<XT, 1, OZ2_BF16>(c) : launch_up<XT, 1, OZ2_F16>(c);
   return scale_type == OZ2_F32 ? launch_up<XT, 2, OZ2_F32>(c) : scale_type == OZ2_BF16 ? launch_up<XT, 2, OZ2_BF16>(c) : launch_up<XT, 2, OZ2_F16>(c);
 }

@@ -17,14 +17,18 @@ struct W4X {
   unsigned v[XT == OZ2_F32 ? 32 : 16];
   float sum;
 };
+// (Unsigned: the offset of a load from a row's start, which is in scalar registers.)
 struct W4Place {
-  int codes, cut;  // bytes from the row's start; bytes that come early (the lane in which the row ends loads the last 16)
-  int group;
+  unsigned codes, group;  // bytes from the row's start; of the scale
+  int cut;                // bytes that come early (the lane in which the row ends loads the last 16)
 };
+// Vectors of up to 1024 take half a wave: its halves then hold rows of their own (FOLD 2), and a batch of four loads has eight rows,
+// row 2 i + (lane / 32) in load i.
+constexpr int kW4Short = 1024;
 
 __device__ __forceinline__ W4Place w4_place(const W4Rows& w, int unit) {
   const int left = w.bytes - unit * (kW4Unit / 2);
-  W4Place p = {0, 0, 0};  // (past the end: the row's first bytes, whose x is 0)
+  W4Place p = {0u, 0u, 0};  // (past the end: the row's first bytes, whose x is 0)
   if (left > 0) {
     p.cut = left < 16 ? 16 - left : 0;
     p.codes = unit * (kW4Unit / 2) - p.cut;
@@ -37,7 +41,7 @@ template <int XT>
 __device__ __forceinline__ void w4_load_x(const char* x, int k, int unit, w4_u4 raw[XT == OZ2_F32 ? 8 : 4]) {
   constexpr int size = XT == OZ2_F32 ? 4 : 2, per = 16 / size;
 #pragma unroll
-  for (int j = 0; j < kW4Unit / per; ++j) raw[j] = w4_bytes<16>(x + (int64_t)min(unit * kW4Unit + j * per, k - per) * size);
+  for (int j = 0; j < kW4Unit / per; ++j) raw[j] = w4_bytes<16>(x + (unsigned)(min(unit * kW4Unit + j * per, k - per) * size));
 }
 template <int XT>
 __device__ __forceinline__ W4X<XT> w4_keep_x(int k, int unit, w4_u4 raw[XT == OZ2_F32 ? 8 : 4], bool& plain) {
@@ -48,6 +52,7 @@ __device__ __forceinline__ W4X<XT> w4_keep_x(int k, int unit, w4_u4 raw[XT == OZ
     for (int j = 0; j < kW4Unit / per; ++j) {
       const int there = k - (unit * kW4Unit + j * per);
       raw[j] = there <= 0 ? w4_u4{0, 0, 0, 0} : there < per ? w4_cut(raw[j], (per - there) * size) : raw[j];
+      __builtin_amdgcn_sched_barrier(0);  // one after the other: together they take many registers
     }
   }
   float s = 0.f, a = 0.f;
@@ -110,11 +115,25 @@ struct W4Row {
   const uint8_t* codes;
   const char* scales;
   const uint8_t* zeros;
+  int codes2, scales2, zeros2;  // FOLD 2: from the first half's row to the second's
+  __device__ __forceinline__ W4Row of_half(bool second) const {
+    if (!second) return *this;
+    return {codes + codes2, scales + scales2, zeros + zeros2, 0, 0, 0};
+  }
 };
+// Load `i` of a batch from row `first` on: row first + i (FOLD 1), or rows first + 2 i and the one behind (FOLD 2); rows past the end are
+// the last.  The second of two rows is `other` rows behind.
 template <int ST>
 __device__ __forceinline__ W4Row w4_row(const W4Rows& w, int row) {
   const int64_t n = min(row, w.n - 1);
   return {w.codes + n * w.ld_codes, w.scales + n * w.ld_scales * (ST == OZ2_F32 ? 4 : 2), w.zeros + n * w.ld_zeros};
+}
+template <int ST, int FOLD>
+__device__ __forceinline__ W4Row w4_row(const W4Rows& w, int first, int i) {
+  W4Row r = w4_row<ST>(w, first + FOLD * i);
+  r.codes2 = r.scales2 = r.zeros2 = 0;
+  if (FOLD == 2 && first + 2 * i + 1 < w.n) r.codes2 = (int)w.ld_codes, r.scales2 = (int)w.ld_scales * (ST == OZ2_F32 ? 4 : 2), r.zeros2 = (int)w.ld_zeros;
+  return r;
 }
 
 // The lane's sum of s (q - z) x straight from memory, one by one: for x with infinities, NaNs or values near the end of the range.
@@ -130,34 +149,41 @@ __device__ __forceinline__ float w4_unit_plain(int k, int group, W4Row row, cons
   return sum;
 }
 
-// Sums of four values over the wave: lane l gets that of value l / 16.
-__device__ __forceinline__ float w4_sum4(float a, float b, float c, float d) {
+// Sums of the four loads' values: of a batch's rows, lane 16 j (FOLD 1) holds row j; lanes 32 j and 32 j + 16 (FOLD 2) hold, in v[0] rows j and
+// 2 + j, in v[1] rows 4 + j and 6 + j, and so do the 15 lanes behind each.
+template <int FOLD>
+__device__ __forceinline__ int w4_row_of_lane(int i) {
+  const int lane = threadIdx.x % 64;
+  return FOLD == 1 ? lane / 16 : 4 * i + lane / 32 + lane / 16 % 2 * 2;
+}
+template <int FOLD>
+__device__ __forceinline__ void w4_sum4(float a, float b, float c, float d, float (&v)[FOLD]) {
   typedef unsigned u2 __attribute__((ext_vector_type(2)));
-  auto pair32 = [](float p, float q) {
-    const u2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(p), __float_as_uint(q), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  };
-  const float p = pair32(a, c), q = pair32(b, d);
-  const u2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(p), __float_as_uint(q), false, false);
-  float v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  v += w4_partner<0>(v), v += w4_partner<1>(v), v += w4_partner<2>(v), v += w4_partner<3>(v);
-  return v;
+  auto swapped = [](u2 r) { return __uint_as_float(r[0]) + __uint_as_float(r[1]); };
+  auto pair32 = [&](float p, float q) { return swapped(__builtin_amdgcn_permlane32_swap(__float_as_uint(p), __float_as_uint(q), false, false)); };
+  auto pair16 = [&](float p, float q) { return swapped(__builtin_amdgcn_permlane16_swap(__float_as_uint(p), __float_as_uint(q), false, false)); };
+  if constexpr (FOLD == 1) v[0] = pair16(pair32(a, c), pair32(b, d));
+  else v[0] = pair16(a, b), v[1] = pair16(c, d);
+#pragma unroll
+  for (int i = 0; i < FOLD; ++i) v[i] += w4_partner<0>(v[i]), v[i] += w4_partner<1>(v[i]), v[i] += w4_partner<2>(v[i]), v[i] += w4_partner<3>(v[i]);
 }
 
-// Four rows times T vectors, a span of the inner indexes; x as kept.  All loads come first: 4 KiB a wave in flight.
-template <int XT, int T, int ST, bool ZEROS>
+// Four loads of rows times T vectors, a span of the inner indexes; x as kept.  All loads come first: 4 KiB a wave in flight.
+template <int XT, int T, int ST, bool ZEROS, int FOLD>
 struct W4Rows4 {
   W4Regs<1, ST> r[4];
 
   template <class Row>
   __device__ __forceinline__ void fetch(Row row, W4Place at) {
-    constexpr int size = ST == OZ2_F32 ? 4 : 2;
+    unsigned codes = at.codes, scale = at.group * (ST == OZ2_F32 ? 4 : 2), zero = at.group;
+    asm volatile("" : "+v"(codes), "+v"(scale), "+v"(zero));  // (32 bits here: a loop would keep them widened, and add the row's address to that)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const W4Row p = row(i);
-      r[i].q = w4_bytes<16>(p.codes + at.codes);
-      r[i].s = w4_bytes<size>(p.scales + at.group * size);
-      if constexpr (ZEROS) r[i].z = p.zeros[at.group];
+      const bool second = FOLD == 2 && threadIdx.x % 64 >= 32;
+      r[i].q = w4_bytes<16>(p.codes + (codes + (unsigned)(second ? p.codes2 : 0)));
+      r[i].s = w4_bytes<ST == OZ2_F32 ? 4 : 2>(p.scales + (scale + (unsigned)(second ? p.scales2 : 0)));
+      if constexpr (ZEROS) r[i].z = p.zeros[zero + (unsigned)(second ? p.zeros2 : 0)];
     }
   }
 
@@ -183,7 +209,7 @@ struct W4Rows4 {
 #pragma unroll 1
     for (int j = 0; j < 4 * T; ++j) {
       if (!(which >> (j % T) & 1)) continue;
-      const float v = w4_unit_plain<XT, ST, ZEROS>(k, group, row(j / T), x(j % T), unit);
+      const float v = w4_unit_plain<XT, ST, ZEROS>(k, group, row(j / T).of_half(FOLD == 2 && threadIdx.x % 64 >= 32), x(j % T), unit);
       w4_each<4 * T>([&](auto i) __attribute__((always_inline)) {
         if (j == i.value) sum[i.value / T][i.value % T] = v;
       });
