@@ -7,21 +7,23 @@ extern template hipError_t oz2_w4_matvec_of<OZ2_F16>(const W4Call&, int64_t);
 
 namespace {
 
-// Rows of a few bytes, which the loads of the matrix-core kernel do not fit: one wave a row and vector.
-__global__ void __launch_bounds__(256) w4_short_rows_kernel(oz2_w4_matrix w, float alpha, int x_type, const char* x, int64_t ldx, float beta,
-                                                            const char* c, int64_t ldc, int y_type, char* y, int64_t ldy) {
+// What the loads of the other kernels do not fit: rows of a few bytes, or further apart than they count.  One wave a row and vector.
+__global__ void __launch_bounds__(256) w4_simple_kernel(oz2_w4_matrix w, float alpha, int x_type, const char* x, int64_t ldx, float beta,
+                                                        const char* c, int64_t ldc, int y_type, char* y, int64_t ldy) {
   const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64, col = blockIdx.y;
-  const int l = threadIdx.x % 64;
+  const int lane = threadIdx.x % 64;
   if (row >= w.n) return;
+  const uint8_t* codes = static_cast<const uint8_t*>(w.codes) + row * w.ld_codes;
   float sum = 0.f;
-  if (l < w.k) {  // (a single group: k is below 32)
-    const int q = static_cast<const uint8_t*>(w.codes)[row * w.ld_codes + l / 2] >> (l % 2 * 4) & 15;
-    const int z = w.zeros ? static_cast<const uint8_t*>(w.zeros)[row * w.ld_zeros] : 8;
-    sum = (float)(q - z) * w4_load(x_type, x, col * ldx + l);
+  for (int64_t l = lane; l < w.k; l += 64) {
+    const int q = codes[l / 2] >> (l % 2 * 4) & 15;
+    const int64_t g = l / w.group;
+    const int z = w.zeros ? static_cast<const uint8_t*>(w.zeros)[row * w.ld_zeros + g] : 8;
+    sum = fmaf(w4_load(w.scale_type, w.scales, row * w.ld_scales + g) * (float)(q - z), w4_load(x_type, x, col * ldx + l), sum);
   }
   for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
-  if (l) return;
-  float v = w.k ? alpha * (w4_load(w.scale_type, w.scales, row * w.ld_scales) * sum) : 0.f;
+  if (lane) return;
+  float v = w.k ? alpha * sum : 0.f;
   if (beta != 0.f) v = fmaf(beta, w4_load(y_type, c, col * ldc + row), v);
   w4_store(y_type, y, col * ldy + row, v);
 }
@@ -48,12 +50,12 @@ W4Rows oz2_w4_rows(const oz2_w4_matrix& m) {
 
 hipError_t oz2_launch_w4_matvec(const oz2_w4_matrix& m, int64_t t, float alpha, int x_type, const void* x, int64_t ldx, float beta,
                                 const void* c, int64_t ldc, int y_type, void* y, int64_t ldy, hipStream_t st) {
-  if (m.k < 32) {
-    hipLaunchKernelGGL(w4_short_rows_kernel, dim3((unsigned)((m.n + 3) / 4), (unsigned)t), dim3(256), 0, st, m, alpha, x_type,
+  const W4Call a = {oz2_w4_rows(m), m.scale_type, (int)t, alpha, beta, x, c, ldx, ldc, ldy, y_type, y, st};
+  if (m.k < 32 || !w4_tile_fits(a.w)) {
+    hipLaunchKernelGGL(w4_simple_kernel, dim3((unsigned)((m.n + 3) / 4), (unsigned)t), dim3(256), 0, st, m, alpha, x_type,
                        static_cast<const char*>(x), ldx, beta, static_cast<const char*>(c), ldc, y_type, static_cast<char*>(y), ldy);
     return hipGetLastError();
   }
-  const W4Call a = {oz2_w4_rows(m), m.scale_type, (int)t, alpha, beta, x, c, ldx, ldc, ldy, y_type, y, st};
   return x_type == OZ2_F32    ? oz2_w4_matvec_of<OZ2_F32>(a, m.group)
          : x_type == OZ2_BF16 ? oz2_w4_matvec_of<OZ2_BF16>(a, m.group)
                               : oz2_w4_matvec_of<OZ2_F16>(a, m.group);

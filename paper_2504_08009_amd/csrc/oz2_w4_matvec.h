@@ -2,6 +2,7 @@
 #ifndef OZ2_W4_MATVEC_H
 #define OZ2_W4_MATVEC_H
 
+#include "oz2_w4_tile.h"
 #include "oz2_w4_vector.h"
 
 struct W4Call {
@@ -22,100 +23,74 @@ int oz2_w4_compute_units();
 #ifdef __HIPCC__
 namespace {
 
-#ifndef W4_WANT
-#define W4_WANT 2048
+#ifndef W4_TILE_WAVES
+#define W4_TILE_WAVES 1
 #endif
 constexpr int kWaves = 8;
-constexpr int kLds = 64 * 1024;
+constexpr int kLds = 156 * 1024;
 
-// How a launch cuts the inner dimension: `split` waves share a tile of sixteen rows, wave s of them takes blocks s, s + split, ... of every chunk;
-// x is brought into LDS a chunk of blocks at a time.
+// How a launch of tiles cuts the inner dimension: `split` waves share two tiles of sixteen rows, wave s of them takes runs of blocks s, s + split, ... of
+// every chunk; x is brought into LDS a chunk of blocks at a time.
 struct Cut {
-  int split_log, chunk, chunks, pitch, sums_at, flags_at, reduce_at;
+  int split_log, waves, chunk, chunks, pitch, sums_at, flags_at, reduce_at;  // waves: of a workgroup
 };
 
-template <int XT, int SPB, int RT, int ST, bool ZEROS>
-__global__ void __launch_bounds__(64 * kWaves) w4_matvec_kernel(W4Rows w, Cut cut, int t, float alpha, const void* x, int64_t ldx, float beta,
-                                                                const void* c, int64_t ldc, int y_type, void* y, int64_t ldy) {
-#ifndef W4_U
-#define W4_U 4
-#endif
-  constexpr int U = W4_U;  // blocks of a wave in flight
-  constexpr int PIECES = RT == 1 ? 2 : 4;  // pieces of x of a thread in flight
+template <int XT, int SPB, int RT, bool WIDE, bool ZEROS>
+__global__ void __launch_bounds__(64 * kWaves, W4_TILE_WAVES) w4_tile_kernel(W4Rows w, int scale_type, Cut cut, int t, float alpha, const char* x, int64_t ldx, float beta,
+                                                              const void* c, int64_t ldc, int y_type, void* y, int64_t ldy) {
   extern __shared__ char lds[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   const int split = 1 << cut.split_log, s = wave & (split - 1);
-  const int64_t tile = (int64_t)blockIdx.x * (kWaves >> cut.split_log) + (wave >> cut.split_log);
-  const int64_t row = tile * 16 + lane % 16;
+  const int64_t pair = (int64_t)blockIdx.x * (cut.waves >> cut.split_log) + (wave >> cut.split_log);
+  const bool in = pair * 32 < w.n;
+  const int row[2] = {(int)(in ? pair * 32 : 0), (int)(in ? min(pair * 32 + 16, (int64_t)w.n - 1) : 0)};
+  const W4Rows both[2] = {w, w};
   const int first = blockIdx.y * 4 * RT, tokens = min(4 * RT, t - first);
-  const W4Lane l = w4_lane<ST>(w, row);
   float* sums = reinterpret_cast<float*>(lds + cut.sums_at);
   unsigned* flags = reinterpret_cast<unsigned*>(lds + cut.flags_at);
   const char* lane_x = lds + min(w4_token<RT>(lane % 16), tokens - 1) * w4_parts<XT>() * cut.pitch;
   auto row_of = [&](int token) { return (first + token) * ldx; };
-  const bool in = tile * 16 < w.n;
-  float sum[RT];
+  W4Two<XT, SPB, RT, WIDE, ZEROS> two;
+  two.init(scale_type);
+  two.tile[0].init(w, row[0]), two.tile[1].init(w, row[1]);
+  float sum[2][RT];
 #pragma unroll
-  for (int r = 0; r < RT; ++r) sum[r] = 0.f;
-
-  // Chunks, and blocks inside one, are walked from a place of its own for every workgroup and tile: rows lie whole pages apart as a rule, and
-  // where all waves stand at the same inner index, they ask the same few memory channels.
+  for (int r = 0; r < RT; ++r) sum[0][r] = sum[1][r] = 0.f;
+  // Chunks are walked from a place of its own for every workgroup: rows lie whole pages apart as a rule, and where all stand at the same inner
+  // index, they ask the same few memory channels.
   int at = cut.chunks > 1 ? blockIdx.x % cut.chunks : 0;
   for (int done = 0; done < cut.chunks; ++done) {
-    const int start = at * cut.chunk, whole = min(cut.chunk, w.full - start);  // (whole blocks: 0 or more)
+    const int start = at * cut.chunk, end = min(start + cut.chunk, w.full);  // of whole blocks (none: end <= start)
     const bool last = at == cut.chunks - 1, ragged = last && w.full * kW4Block < w.k;
-    const int count = in ? (whole - s + split - 1) >> cut.split_log : 0;  // whole blocks of this wave
-    const int turn = count > 1 ? (int)((unsigned)tile * 4 % (unsigned)count) : 0;
-    auto block = [&](int i) {
-      i = min(i, count - 1) + turn;
-      return start + s + ((i < count ? i : i - count) << cut.split_log);
-    };
-    const W4Stage stage = {static_cast<const char*>(x), (int64_t)start * kW4Block, tokens, w.k, (whole + ragged) * (kW4Block / 8)};
-    const int pieces = tokens * stage.eights;
-    W4Regs<SPB, ST> regs[U];
-    W4Tail<SPB> tail;
-    if (count)
-      w4_each<U>([&](auto u) __attribute__((always_inline)) { regs[u.value] = w4_fetch<SPB, ST, ZEROS>(w, l, block(u.value)); });
-    const bool tail_here = ragged && in && (whole & (split - 1)) == s;
-    if (tail_here) tail = w4_fetch_tail<SPB, ST, ZEROS>(w, l);
     if (done) __syncthreads();
-    bool plain = false;
-#pragma unroll 1
-    for (int piece = threadIdx.x; piece < pieces; piece += PIECES * 64 * kWaves) {
-      W4Raw<XT> raw[PIECES];
-      w4_each<PIECES>([&](auto i) __attribute__((always_inline)) {
-        raw[i.value] = w4_stage_load<XT>(stage, row_of, min(piece + i.value * 64 * kWaves, pieces - 1));
-      });
-      w4_each<PIECES>([&](auto i) __attribute__((always_inline)) {
-        if (piece + i.value * 64 * kWaves < pieces)
-          plain |= w4_stage_store<XT, SPB, RT>(stage, raw[i.value], piece + i.value * 64 * kWaves, lds, cut.pitch, sums);
-      });
-    }
-    const bool any = __ballot(plain) != 0;
-    if (lane == 0) flags[wave] = any;
+    const unsigned mine = w4_stage<XT, SPB, RT>(x, row_of, tokens, w.k, start, end - start + ragged, lds, cut.pitch, sums, 64 * cut.waves);
+    if (lane == 0) flags[wave] = mine;
     __syncthreads();
-    unsigned seen = 0;
+    unsigned which = 0;
+    for (int i = 0; i < cut.waves; ++i) which |= flags[i];
+    which = __builtin_amdgcn_readfirstlane(which);
+    if (in) {
+      float before[2][RT];
+      if (which)
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) seen |= flags[i];
-    if (__builtin_amdgcn_readfirstlane(seen)) {
-#pragma unroll 1
-      for (int i = 0; i < count + tail_here; ++i)
-        w4_block_plain<SPB, ST, RT>(w, l, ZEROS, i < count ? block(i) : w.full, [&](int r, int k) {
+        for (int r = 0; r < RT; ++r) before[0][r] = sum[0][r], before[1][r] = sum[1][r];
+      const int first_run = start / kW4Run + s, runs = (end + kW4Run - 1) / kW4Run;
+      two.multiply(w, first_run, split, (runs - first_run + split - 1) >> cut.split_log, end, start, lane_x, cut.pitch, sums, sum);
+      const bool tail = ragged && s == ((end - start) / kW4Run & (split - 1));
+      if (tail) {
+        const int b = w.full - start;
+        two.multiply_tail(both, row, lane_x + b * kW4Block * 2, cut.pitch, sums + b * SPB * 4 * RT, sum);
+      }
+      if (which) {  // these tokens' sums again (and no other's: what one holds changes no bit of another's result)
+        auto value = [&](int r, int k) {
           const int token = lane / 16 + 4 * r;
           return token < tokens ? w4_load(XT, x, row_of(token) + k) : 0.f;
-        }, sum);
-    } else {
-#pragma unroll 1
-      for (int i = 0; i < count; i += U)
-        w4_each<U>([&](auto u) __attribute__((always_inline)) {
-          const int b = block(i + u.value) - start;
-          if (i + u.value < count)
-            w4_whole<XT, SPB, ST, ZEROS, RT>(regs[u.value], lane_x + b * kW4Block * 2, cut.pitch, sums + b * SPB * 4 * RT, sum);
-          regs[u.value] = w4_fetch<SPB, ST, ZEROS>(w, l, block(i + u.value + U));
-        });
-      if (tail_here) {
-        const int b = w.full - start;
-        w4_tail<XT, SPB, ST, RT>(w, tail, lane_x + b * kW4Block * 2, cut.pitch, sums + b * SPB * 4 * RT, sum);
+        };
+        for (int b = start; b < end + ragged; ++b)
+          if (b == w.full ? tail : (b / kW4Run & (split - 1)) == (first_run & (split - 1))) two.block_plain(both, row, b, value, before);
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+          if (which >> (lane / 16 + 4 * r) & 1) sum[0][r] = before[0][r], sum[1][r] = before[1][r];
       }
     }
     at = last ? 0 : at + 1;
@@ -123,21 +98,21 @@ __global__ void __launch_bounds__(64 * kWaves) w4_matvec_kernel(W4Rows w, Cut cu
   if (split > 1) {
     float* part = reinterpret_cast<float*>(lds + cut.reduce_at) + lane;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) part[(wave * RT + r) * 64] = sum[r];
+    for (int r = 0; r < 2 * RT; ++r) part[(wave * 2 * RT + r) * 64] = sum[r / RT][r % RT];
     __syncthreads();
     if (s) return;
     for (int i = 1; i < split; ++i)
 #pragma unroll
-      for (int r = 0; r < RT; ++r) sum[r] += part[((wave + i) * RT + r) * 64];
+      for (int r = 0; r < 2 * RT; ++r) sum[r / RT][r % RT] += part[((wave + i) * 2 * RT + r) * 64];
   }
-  if (row >= w.n) return;
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    const int token = lane / 16 + 4 * r;
-    if (token >= tokens) continue;
-    float v = cut.chunks ? alpha * sum[r] : 0.f;
-    if (beta != 0.f) v = fmaf(beta, w4_load(y_type, c, (first + token) * ldc + row), v);
-    w4_store(y_type, y, (first + token) * ldy + row, v);
+  for (int i = 0; i < 2 * RT; ++i) {
+    const int token = lane / 16 + 4 * (i % RT);
+    const int64_t to = pair * 32 + i / RT * 16 + lane % 16;
+    if (token >= tokens || to >= w.n) continue;
+    float v = alpha * sum[i / RT][i % RT];
+    if (beta != 0.f) v = fmaf(beta, w4_load(y_type, c, (first + token) * ldc + to), v);
+    w4_store(y_type, y, (first + token) * ldy + to, v);
   }
 }
 
@@ -211,54 +186,64 @@ hipError_t launch_vector(const W4Call& a) {
   return hipGetLastError();
 }
 
-template <int XT, int SPB, int RT, int ST, bool ZEROS>
-hipError_t launch(const W4Call& a) {
+template <int XT, int SPB, int RT, bool WIDE, bool ZEROS>
+hipError_t launch_tile(const W4Call& a) {
   constexpr int P = w4_parts<XT>();
   const int tokens = a.t < 4 * RT ? a.t : 4 * RT;
-  const int64_t tiles = (a.w.n + 15) / 16;
-  const int blocks = (int)((a.w.k + (int64_t)kW4Block - 1) / kW4Block);
+  const int64_t pairs = (a.w.n + 31) / 32;
+  const int blocks = (a.w.k + kW4Block - 1) / kW4Block;
+  const int cus = oz2_w4_compute_units();
   Cut cut;
   cut.split_log = 0;
-  while (cut.split_log < 3 && (tiles << cut.split_log) < W4_WANT && (2 << cut.split_log) <= blocks) ++cut.split_log;
+  while (cut.split_log < 3 && (pairs << cut.split_log) < 8 * cus && (kW4Run << cut.split_log) < blocks) ++cut.split_log;
   auto lay = [&](int chunk) {
     cut.chunk = chunk;
     cut.pitch = chunk * kW4Block * 2 + 16;
     cut.sums_at = tokens * P * cut.pitch;
     cut.flags_at = cut.sums_at + chunk * SPB * 4 * RT * 4;
     cut.reduce_at = cut.flags_at + kWaves * 4;
-    return cut.reduce_at + (cut.split_log ? kWaves * RT * 64 * 4 : 0);
+    return cut.reduce_at + (cut.split_log ? kWaves * 2 * RT * 64 * 4 : 0);
   };
-  int lds = lay(blocks > 0 ? blocks : 1);
-  if (lds > kLds) {  // not in one piece: as many blocks for each wave of a tile as fit, fewer waves a tile where that is none
-    while (lay(1 << cut.split_log) > kLds) --cut.split_log;
+  int lds = lay(blocks);
+  if (lds > kLds) {  // not in one piece: as many runs for each wave of a pair as fit, fewer waves a pair where that is none
+    while (cut.split_log && lay(kW4Run << cut.split_log) > kLds) --cut.split_log;
     int each = 1;
-    while (lay((each + 1) << cut.split_log) <= kLds) ++each;
-    lds = lay(each << cut.split_log);
+    while (lay((each + 1) * kW4Run << cut.split_log) <= kLds) ++each;
+    lds = lay(each * kW4Run << cut.split_log);
   }
   cut.chunks = (blocks + cut.chunk - 1) / cut.chunk;
-  const int per = kWaves >> cut.split_log;
-  hipLaunchKernelGGL((w4_matvec_kernel<XT, SPB, RT, ST, ZEROS>), dim3((unsigned)((tiles + per - 1) / per), (unsigned)((a.t + 4 * RT - 1) / (4 * RT))),
-                     dim3(64 * kWaves), lds, a.st, a.w, cut, a.t, a.alpha, a.x, a.ldx, a.beta, a.c, a.ldc, a.y_type, a.y, a.ldy);
+  // pairs of tiles that a workgroup takes: as many as still leave every compute unit one
+  int per = 1;
+  while ((per * 2 << cut.split_log) <= kWaves && pairs >= 2 * per * cus) per *= 2;
+  cut.waves = per << cut.split_log;
+  static const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void*>(&w4_tile_kernel<XT, SPB, RT, WIDE, ZEROS>),
+                                                    hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+  if (set != hipSuccess) return set;
+  hipLaunchKernelGGL((w4_tile_kernel<XT, SPB, RT, WIDE, ZEROS>), dim3((unsigned)((pairs + per - 1) / per), (unsigned)((a.t + 4 * RT - 1) / (4 * RT))),
+                     dim3(64 * cut.waves), lds, a.st, a.w, a.scale_type, cut, a.t, a.alpha, static_cast<const char*>(a.x), a.ldx, a.beta, a.c, a.ldc, a.y_type,
+                     a.y, a.ldy);
   return hipGetLastError();
 }
 
-// f(type of the scales, whether there are zero points), as constants
-template <class F>
-hipError_t by_scales(const W4Call& a, F f) {
-  auto zeros = [&](auto st) { return a.w.zeros ? f(st, W4Index<1>{}) : f(st, W4Index<0>{}); };
-  return a.scale_type == OZ2_F32 ? zeros(W4Index<OZ2_F32>{}) : a.scale_type == OZ2_BF16 ? zeros(W4Index<OZ2_BF16>{}) : zeros(W4Index<OZ2_F16>{});
-}
 template <int XT, int SPB, int RT>
-hipError_t launch_tile(const W4Call& a) {
-  return by_scales(a, [&](auto st, auto zeros) { return launch<XT, SPB, RT, decltype(st)::value, decltype(zeros)::value>(a); });
+hipError_t launch_scales(const W4Call& a) {
+  if (a.scale_type == OZ2_F32) return a.w.zeros ? launch_tile<XT, SPB, RT, true, true>(a) : launch_tile<XT, SPB, RT, true, false>(a);
+  return a.w.zeros ? launch_tile<XT, SPB, RT, false, true>(a) : launch_tile<XT, SPB, RT, false, false>(a);
 }
 template <int XT, int SPB>
 hipError_t launch_tokens(const W4Call& a) {
-  return a.t <= 4 ? launch_tile<XT, SPB, 1>(a) : launch_tile<XT, SPB, 4>(a);
+  return a.t <= 4 ? launch_scales<XT, SPB, 1>(a) : launch_scales<XT, SPB, 4>(a);
+}
+
+template <int XT, int T, bool ZEROS>
+hipError_t launch_rows(const W4Call& a) {
+  return a.scale_type == OZ2_F32    ? launch_vector<XT, T, OZ2_F32, ZEROS>(a)
+         : a.scale_type == OZ2_BF16 ? launch_vector<XT, T, OZ2_BF16, ZEROS>(a)
+                                    : launch_vector<XT, T, OZ2_F16, ZEROS>(a);
 }
 template <int XT, int T>
 hipError_t launch_rows(const W4Call& a) {
-  return by_scales(a, [&](auto st, auto zeros) { return launch_vector<XT, T, decltype(st)::value, decltype(zeros)::value>(a); });
+  return a.w.zeros ? launch_rows<XT, T, true>(a) : launch_rows<XT, T, false>(a);
 }
 
 }  // namespace
