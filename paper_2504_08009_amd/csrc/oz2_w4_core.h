@@ -217,149 +217,17 @@ __device__ __forceinline__ int w4_inner(int j, int quarter) {
   else return 32 * j + 8 * quarter;
 }
 
-// x in LDS.  A token's values lie in rows of `pitch` bytes for each of its parts, eight at a time in the order of w4_unpack's pairs; the sums
-// over segments lie by segment, then by token.  Row a of the matrix cores' tile is token a / 4 + 4 (a % 4), so that with
-// few tokens only the first result registers of a lane count (RT: 1, 2 or 4 for up to 4, 8 or 16 tokens).
+// x in LDS.  A token's values lie in rows of `pitch` bytes for each of its parts, eight at a time in the order of w4_unpack's pairs.  Row a of the
+// matrix cores' tile is token a / 4 + 4 (a % 4), so that with few tokens only the first result registers of a lane count (RT: 1 or 4
+// for up to 4 or 16 tokens).
 template <int RT>
 __device__ __forceinline__ int w4_token(int a) { return a / 4 + 4 * (a % 4); }
 
-// One block: the lane's sums (tokens quarter + 4 r, its row) grow by  scale ((16 + q) x - (16 + z) x).
-// x: the lane's token at the block's start, part p at + p part_bytes; sums: of the block's first segment.
-template <int XT, int SPB, int RT, class Scale, class Zero>
-__device__ __forceinline__ void w4_block(w4_u4 codes, Scale scale, Zero zero, const char* x, int part_bytes, const float* sums, float* sum) {
-  const int quarter = threadIdx.x % 64 / 16;
-  const w4_u4 q = w4_exchange<SPB>(codes);
-  w4_each<SPB>([&](auto index) __attribute__((always_inline)) {
-    constexpr int seg = index.value;
-    w4_f4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 4 / SPB; ++i) {
-      const int j = seg * (4 / SPB) + i;
-      unsigned b[4];
-      w4_unpack<XT>(q[w4_register<SPB>(j)], b);
-#pragma unroll
-      for (int p = 0; p < w4_parts<XT>(); ++p)
-        acc = w4_mfma<XT>(*reinterpret_cast<const uint4*>(x + p * part_bytes + 2 * w4_inner<SPB>(j, quarter)), b, acc);
-    }
-    const float s = scale(index), z = kW4Offset + zero(index);
-#pragma unroll
-    for (int i = 0; i < RT; ++i) sum[i] = fmaf(s, fmaf(-z, sums[(seg * 4 + quarter) * RT + i], acc[i]), sum[i]);
-  });
-}
-template <int XT, int SPB, int ST, bool ZEROS, int RT>
-__device__ __forceinline__ void w4_whole(const W4Regs<SPB, ST>& r, const char* x, int part_bytes, const float* sums, float* sum) {
-  w4_block<XT, SPB, RT>(
-      r.q,
-      [&](auto i) __attribute__((always_inline)) {
-        if constexpr (ST == OZ2_F32) return __uint_as_float(w4_word<SPB * 4>(r.s, i.value));
-        else return w4_decode16(ST, w4_word<SPB * 2>(r.s, i.value / 2) >> (i.value % 2 * 16));
-      },
-      [&](auto i) __attribute__((always_inline)) {
-        if constexpr (ZEROS) return (float)(w4_word<SPB>(r.z, 0) >> (8 * i.value) & 255u);
-        else return 8.f;
-      }, x, part_bytes, sums, sum);
-}
-template <int XT, int SPB, int ST, int RT>
-__device__ __forceinline__ void w4_tail(const W4Rows& w, const W4Tail<SPB>& r, const char* x, int part_bytes, const float* sums, float* sum) {
-  const int g = w4_group<SPB>(w, w.full);
-  w4_block<XT, SPB, RT>(
-      w4_cut(r.q, r.cut),
-      [&](auto i) __attribute__((always_inline)) {  // (0 past the last group: a scale that is not finite must not meet the 0 of x)
-        const float s = ST == OZ2_F32 ? __uint_as_float(r.s[i.value]) : w4_decode16(ST, r.s[i.value]);
-        return g + i.value < w.groups ? s : 0.f;
-      },
-      [&](auto i) __attribute__((always_inline)) { return (float)r.z[i.value]; }, x, part_bytes, sums, sum);
-}
-
-// The same by the formula itself, code by code: for blocks whose x has infinities, NaNs, or values near the end of the range.
-template <int SPB, int ST, int RT, class X>
-__device__ __forceinline__ void w4_block_plain(const W4Rows& w, const W4Lane& l, bool zeros, int b, X value, float* sum) {
-  const uint8_t* codes = l.codes - (threadIdx.x % 64 / 16) * 16;
-  const int end = min(w.k, (b + 1) * kW4Block);
-#pragma unroll 1
-  for (int i = b * kW4Block; i < end; ++i) {
-    const int q = codes[i / 2] >> (i % 2 * 4) & 15;
-    const int g = SPB > 1 ? i / (kW4Block / SPB) : w4_group<1>(w, b);
-    const float s = w4_load(ST, l.scales, g);
-    const float v = s * (float)(q - (zeros ? (int)l.zeros[g] : 8));
-#pragma unroll
-    for (int r = 0; r < RT; ++r) sum[r] = fmaf(v, value(r, i), sum[r]);
-  }
-}
-
-// Eight values of x on their way into LDS.
-template <int XT>
-struct W4Raw {
-  w4_u4 v[XT == OZ2_F32 ? 2 : 1];
-};
-// How a chunk of x comes into LDS: inner indexes first .. first + length - 1 (a multiple of 128) of `tokens` vectors, zeros past k.  Piece i of
-// the work, eight values of a token, belongs to thread i % threads.
-struct W4Stage {
-  const char* x;
-  int64_t first;
-  int tokens, k, eights;
-};
-// (k is at least 8: where fewer than the 16 bytes of a load are there, it takes the 16 that end with the vector.)
-template <int XT, class Row>
-__device__ __forceinline__ W4Raw<XT> w4_stage_load(const W4Stage& st, Row row, int i) {
-  constexpr int size = XT == OZ2_F32 ? 4 : 2, per = 16 / size;  // values of 16 bytes
-  W4Raw<XT> r;
-  const int t = i / st.eights, l = (int)st.first + (i - t * st.eights) * 8;
-  const char* p = st.x + row(t) * size;
-  w4_each<8 / per>([&](auto h) __attribute__((always_inline)) {
-    const W4Bytes16 c = *reinterpret_cast<const W4Bytes16*>(p + (int64_t)min(l + h.value * per, st.k - per) * size);
-    r.v[h.value] = w4_u4{c.v[0], c.v[1], c.v[2], c.v[3]};
-  });
-  return r;
-}
 // Value of the lane across in a pair, four, eight or sixteen lanes whose halves hold one value each (a pair: its two lanes).
 template <int STEP>
 __device__ __forceinline__ float w4_partner(float v) {
   constexpr int ctrl = STEP == 0 ? 0xB1 : STEP == 1 ? 0x4E : STEP == 2 ? 0x141 : 0x140;  // quad permutations, mirrors of 8 and 16 lanes
   return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), ctrl, 0xF, 0xF, true));
 }
-// Writes a piece and (with its neighbours) the sums over its segment.  Returns whether the values call for w4_block_plain.
-template <int XT, int SPB, int RT>
-__device__ __forceinline__ bool w4_stage_store(const W4Stage& st, W4Raw<XT> r, int i, char* lds, int pitch, float* sums) {
-  constexpr int SEG = kW4Block / SPB, P = w4_parts<XT>(), size = XT == OZ2_F32 ? 4 : 2, per = 16 / size;
-  const int t = i / st.eights, at = (i - t * st.eights) * 8;
-  if ((int)st.first + at + 8 > st.k) {
-    w4_each<8 / per>([&](auto h) __attribute__((always_inline)) {
-      const int there = st.k - ((int)st.first + at + h.value * per);
-      r.v[h.value] = there <= 0 ? w4_u4{0, 0, 0, 0} : there < per ? w4_cut(r.v[h.value], (per - there) * size) : r.v[h.value];
-    });
-  }
-  float s, a;
-  char* to = lds + t * P * pitch + 2 * at;
-  if constexpr (XT == OZ2_F32) {
-    float v[8];
-    unsigned h[P][8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {  // cut, not rounded: each part takes the next eight bits, and none can overflow
-      float rest = v[e] = __uint_as_float(r.v[e / 4][e % 4]);
-#pragma unroll
-      for (int c = 0; c < 3; ++c) {
-        h[c][e] = __float_as_uint(rest);
-        rest -= __uint_as_float(h[c][e] & 0xFFFF0000u);
-      }
-    }
-#pragma unroll
-    for (int c = 0; c < P; ++c)
-      *reinterpret_cast<w4_u4*>(to + c * pitch) =
-          w4_u4{__builtin_amdgcn_perm(h[c][4], h[c][0], 0x07060302u), __builtin_amdgcn_perm(h[c][5], h[c][1], 0x07060302u),
-                __builtin_amdgcn_perm(h[c][6], h[c][2], 0x07060302u), __builtin_amdgcn_perm(h[c][7], h[c][3], 0x07060302u)};
-    s = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-    a = ((fabsf(v[0]) + fabsf(v[1])) + (fabsf(v[2]) + fabsf(v[3]))) + ((fabsf(v[4]) + fabsf(v[5])) + (fabsf(v[6]) + fabsf(v[7])));
-  } else {
-    s = a = 0.f;
-    w4_sums<XT>(r.v[0], s, a);
-    *reinterpret_cast<w4_u4*>(to) = w4_pairs(r.v[0]);
-  }
-  // the threads of a segment are neighbours, and all of them are here: the pieces of a token are a multiple of 16
-  w4_each<SPB == 4 ? 2 : SPB == 2 ? 3 : 4>([&](auto step) __attribute__((always_inline)) { s += w4_partner<step.value>(s); });
-  if (at % SEG == 0) sums[(at / SEG * 4 + t % 4) * RT + t / 4] = s;
-  return !(a < kW4Large);
-}
-
 #endif
 #endif

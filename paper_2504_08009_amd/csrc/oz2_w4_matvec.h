@@ -32,7 +32,7 @@ constexpr int kLds = 156 * 1024;
 // How a launch of tiles cuts the inner dimension: `split` waves share two tiles of sixteen rows, wave s of them takes runs of blocks s, s + split, ... of
 // every chunk; x is brought into LDS a chunk of blocks at a time.
 struct Cut {
-  int split_log, waves, chunk, chunks, pitch, sums_at, flags_at, reduce_at;  // waves: of a workgroup
+  int split_log, waves, chunk, chunks, pitch, reduce_at;  // waves: of a workgroup
 };
 
 template <int XT, int SPB, int RT, bool WIDE, bool ZEROS>
@@ -46,13 +46,12 @@ __global__ void __launch_bounds__(64 * kWaves, W4_TILE_WAVES) w4_tile_kernel(W4R
   const int row[2] = {(int)(in ? pair * 32 : 0), (int)(in ? min(pair * 32 + 16, (int64_t)w.n - 1) : 0)};
   const W4Rows both[2] = {w, w};
   const int first = blockIdx.y * 4 * RT, tokens = min(4 * RT, t - first);
-  float* sums = reinterpret_cast<float*>(lds + cut.sums_at);
-  unsigned* flags = reinterpret_cast<unsigned*>(lds + cut.flags_at);
   const char* lane_x = lds + min(w4_token<RT>(lane % 16), tokens - 1) * w4_parts<XT>() * cut.pitch;
   auto row_of = [&](int token) { return (first + token) * ldx; };
   W4Two<XT, SPB, RT, WIDE, ZEROS> two;
   two.init(scale_type);
   two.tile[0].init(w, row[0]), two.tile[1].init(w, row[1]);
+  const int owner = w.full / kW4Run & (split - 1);  // of the block behind the whole ones
   float sum[2][RT];
 #pragma unroll
   for (int r = 0; r < RT; ++r) sum[0][r] = sum[1][r] = 0.f;
@@ -62,38 +61,35 @@ __global__ void __launch_bounds__(64 * kWaves, W4_TILE_WAVES) w4_tile_kernel(W4R
   for (int done = 0; done < cut.chunks; ++done) {
     const int start = at * cut.chunk, end = min(start + cut.chunk, w.full);  // of whole blocks (none: end <= start)
     const bool last = at == cut.chunks - 1, ragged = last && w.full * kW4Block < w.k;
+    const int first_run = start / kW4Run + s, runs = (end + kW4Run - 1) / kW4Run;
+    typename W4Two<XT, SPB, RT, WIDE, ZEROS>::Ahead ahead;
+    if (w.full) two.begin(w, first_run, end, ahead);
     if (done) __syncthreads();
-    const unsigned mine = w4_stage<XT, SPB, RT>(x, row_of, tokens, w.k, start, end - start + ragged, lds, cut.pitch, sums, 64 * cut.waves);
-    if (lane == 0) flags[wave] = mine;
+    w4_stage<XT>(x, row_of, tokens, w.k, start, end - start + ragged, lds, cut.pitch, 64 * cut.waves);
     __syncthreads();
-    unsigned which = 0;
-    for (int i = 0; i < cut.waves; ++i) which |= flags[i];
-    which = __builtin_amdgcn_readfirstlane(which);
     if (in) {
-      float before[2][RT];
-      if (which)
-#pragma unroll
-        for (int r = 0; r < RT; ++r) before[0][r] = sum[0][r], before[1][r] = sum[1][r];
-      const int first_run = start / kW4Run + s, runs = (end + kW4Run - 1) / kW4Run;
-      two.multiply(w, first_run, split, (runs - first_run + split - 1) >> cut.split_log, end, start, lane_x, cut.pitch, sums, sum);
-      const bool tail = ragged && s == ((end - start) / kW4Run & (split - 1));
-      if (tail) {
-        const int b = w.full - start;
-        two.multiply_tail(both, row, lane_x + b * kW4Block * 2, cut.pitch, sums + b * SPB * 4 * RT, sum);
-      }
-      if (which) {  // these tokens' sums again (and no other's: what one holds changes no bit of another's result)
-        auto value = [&](int r, int k) {
-          const int token = lane / 16 + 4 * r;
-          return token < tokens ? w4_load(XT, x, row_of(token) + k) : 0.f;
-        };
-        for (int b = start; b < end + ragged; ++b)
-          if (b == w.full ? tail : (b / kW4Run & (split - 1)) == (first_run & (split - 1))) two.block_plain(both, row, b, value, before);
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-          if (which >> (lane / 16 + 4 * r) & 1) sum[0][r] = before[0][r], sum[1][r] = before[1][r];
-      }
+      two.multiply(w, first_run, split, (runs - first_run + split - 1) >> cut.split_log, end, start, ahead, lane_x, cut.pitch, sum);
+      if (ragged && s == owner) two.multiply_tail(both, row, lane_x + (w.full - start) * kW4Block * 2, cut.pitch, sum);
     }
     at = last ? 0 : at + 1;
+  }
+  bool again = false;
+#pragma unroll
+  for (int r = 0; r < 2 * RT; ++r) again |= !(fabsf(sum[r / RT][r % RT]) < INFINITY) && lane / 16 + 4 * (r % RT) < tokens;
+  if (in && __ballot(again)) {
+    float plain[2][RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) plain[0][r] = plain[1][r] = 0.f;
+#pragma unroll 1
+    for (int b = 0; b <= w.full; ++b)
+      if (b == w.full ? s == owner : (b / kW4Run & (split - 1)) == s)
+        two.block_plain(both, row, b, [&](int r, int k) {
+          const int token = lane / 16 + 4 * r;
+          return token < tokens ? w4_load(XT, x, row_of(token) + k) : 0.f;
+        }, plain);
+#pragma unroll
+    for (int r = 0; r < 2 * RT; ++r)
+      if (!(fabsf(sum[r / RT][r % RT]) < INFINITY)) sum[r / RT][r % RT] = plain[r / RT][r % RT];
   }
   if (split > 1) {
     float* part = reinterpret_cast<float*>(lds + cut.reduce_at) + lane;
@@ -199,9 +195,7 @@ hipError_t launch_tile(const W4Call& a) {
   auto lay = [&](int chunk) {
     cut.chunk = chunk;
     cut.pitch = chunk * kW4Block * 2 + 16;
-    cut.sums_at = tokens * P * cut.pitch;
-    cut.flags_at = cut.sums_at + chunk * SPB * 4 * RT * 4;
-    cut.reduce_at = cut.flags_at + kWaves * 4;
+    cut.reduce_at = tokens * P * cut.pitch;
     return cut.reduce_at + (cut.split_log ? kWaves * 2 * RT * 64 * 4 : 0);
   };
   int lds = lay(blocks);

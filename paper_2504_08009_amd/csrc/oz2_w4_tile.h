@@ -77,11 +77,13 @@ struct W4Two {
 
   // sum[t] += the tiles' products for one block.  q: codes as the matrix cores take them; scale(t, segment), zero(t, segment).
   template <class Scale, class Zero>
-  __device__ __forceinline__ void block(const w4_u4 (&q)[2], Scale scale, Zero zero, const char* x, int part_bytes, const float* sums, float (&sum)[2][RT]) const {
+  __device__ __forceinline__ void block(const w4_u4 (&q)[2], Scale scale, Zero zero, const char* x, int part_bytes, float (&sum)[2][RT]) const {
     const int quarter = threadIdx.x % 64 / 16;
+    constexpr unsigned one = XT == OZ2_F16 ? 0x3C003C00u : 0x3F803F80u;
+    const unsigned ones[4] = {one, one, one, one};
     w4_each<SPB>([&](auto index) __attribute__((always_inline)) {
       constexpr int seg = index.value;
-      w4_f4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      w4_f4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, of_x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < 4 / SPB; ++i) {
         const int j = seg * (4 / SPB) + i;
@@ -93,11 +95,9 @@ struct W4Two {
           const uint4 v = *reinterpret_cast<const uint4*>(x + p * part_bytes + 2 * w4_inner<SPB>(j, quarter));
           acc[0] = w4_mfma<XT>(v, b[0], acc[0]);
           acc[1] = w4_mfma<XT>(v, b[1], acc[1]);
+          of_x = w4_mfma<XT>(v, ones, of_x);  // sum of x, as each lane wants it
         }
       }
-      float of_x[RT];
-#pragma unroll
-      for (int i = 0; i < RT; ++i) of_x[i] = sums[(seg * 4 + quarter) * RT + i];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const float s = scale(t, index), z = kW4Offset + zero(t, index);
@@ -107,16 +107,23 @@ struct W4Two {
     });
   }
 
-  // Runs first, first + stride, ... (`count` of them) of the whole blocks below `end`.  x, sums: of block `origin`.
-  __device__ __forceinline__ void multiply(const W4Rows& w, int first, int stride, int count, int end, int origin, const char* x, int part_bytes,
-                                           const float* sums, float (&sum)[2][RT]) const {
-    if (count <= 0) return;
+  // Loads of a first run, ahead of whatever has to be done before its products.  There is a whole block.
+  struct Ahead {
     w4_u4 ring[kW4Run][2];
-    W4RunScales<SPB, WIDE> now = scales(w, first), next;
+    W4RunScales<SPB, WIDE> now;
+  };
+  __device__ __forceinline__ void begin(const W4Rows& w, int first, int end, Ahead& a) const {
+    a.now = scales(w, first);
     w4_each<kW4Run>([&](auto u) __attribute__((always_inline)) {
-      const int b = min(first * kW4Run + u.value, end - 1);
-      ring[u.value][0] = codes(0, b), ring[u.value][1] = codes(1, b);
+      const int b = max(min(first * kW4Run + u.value, end - 1), 0);
+      a.ring[u.value][0] = codes(0, b), a.ring[u.value][1] = codes(1, b);
     });
+  }
+  // Runs first, first + stride, ... (`count` of them) of the whole blocks below `end`.  x: of block `origin`.
+  __device__ __forceinline__ void multiply(const W4Rows& w, int first, int stride, int count, int end, int origin, Ahead& ahead, const char* x, int part_bytes,
+                                           float (&sum)[2][RT]) const {
+    w4_u4 (&ring)[kW4Run][2] = ahead.ring;
+    W4RunScales<SPB, WIDE> now = ahead.now, next;
 #pragma unroll 1
     for (int i = 0; i < count; ++i) {
       const int run = first + i * stride, then = i + 1 < count ? run + stride : run;
@@ -150,7 +157,7 @@ struct W4Two {
                 if constexpr (ZEROS) return (float)(z[t] >> (8 * seg.value) & 255u);
                 else return 8.f;
               },
-              x + (b - origin) * kW4Block * 2, part_bytes, sums + (b - origin) * SPB * 4 * RT, sum);
+              x + (b - origin) * kW4Block * 2, part_bytes, sum);
         }
         const int f = min(then * kW4Run + u.value, end - 1);
         ring[u.value][0] = codes(0, f), ring[u.value][1] = codes(1, f);
@@ -160,7 +167,7 @@ struct W4Two {
   }
 
   // The block behind the whole ones; row[t]: the tiles' first rows.
-  __device__ __forceinline__ void multiply_tail(const W4Rows (&w)[2], const int (&row)[2], const char* x, int part_bytes, const float* sums, float (&sum)[2][RT]) const {
+  __device__ __forceinline__ void multiply_tail(const W4Rows (&w)[2], const int (&row)[2], const char* x, int part_bytes, float (&sum)[2][RT]) const {
     constexpr int ST = WIDE ? OZ2_F32 : OZ2_BF16;  // (16 bits are decoded here)
     W4Tail<SPB> r[2];
     w4_u4 q[2];
@@ -175,10 +182,11 @@ struct W4Two {
           const float s = WIDE ? __uint_as_float(r[t].s[i.value]) : decode(r[t].s[i.value]);
           return g + i.value < w[0].groups ? s : 0.f;
         },
-        [&](int t, auto i) __attribute__((always_inline)) { return (float)r[t].z[i.value]; }, x, part_bytes, sums, sum);
+        [&](int t, auto i) __attribute__((always_inline)) { return (float)r[t].z[i.value]; }, x, part_bytes, sum);
   }
 
-  // The sums over block b of the tokens in `which`, by the formula itself.  value(r, k): x of the lane's token quarter + 4 r.
+  // The sums over block b by the formula itself: for x with infinities, NaNs or values near the end of the range, from which the
+  // products above make sums that are not finite, and only from these.  value(r, k): x of the lane's token quarter + 4 r.
   template <class X>
   __device__ __forceinline__ void block_plain(const W4Rows (&w)[2], const int (&row)[2], int b, X value, float (&sum)[2][RT]) const {
     const int end = min(w[0].k, (b + 1) * kW4Block);
@@ -198,27 +206,54 @@ struct W4Two {
   }
 };
 
-// Brings blocks start .. start + length - 1 of x into LDS, by all threads of a workgroup, between two barriers of the caller's.  Returns a bit for each
-// token whose values call for block_plain, of what the wave saw.
-template <int XT, int SPB, int RT, class Row>
-__device__ __forceinline__ unsigned w4_stage(const char* x, Row row, int tokens, int k, int start, int length, char* lds, int pitch, float* sums, int threads) {
-  constexpr int PIECES = 4;  // of a thread in flight
-  const W4Stage stage = {x, (int64_t)start * kW4Block, tokens, k, length * (kW4Block / 8)};
-  const int pieces = tokens * stage.eights;
-  unsigned seen = 0;
+// Brings blocks start .. start + length - 1 of x into LDS, zeros past k, by all threads of a workgroup, between two barriers of the caller's.  A thread
+// takes eight values of several tokens at a time.  row(token): element offset of the vector; k is at least 8.
+template <int XT, class Row>
+__device__ __forceinline__ void w4_stage(const char* x, Row row, int tokens, int k, int start, int length, char* lds, int pitch, int threads) {
+  constexpr int PIECES = XT == OZ2_F32 ? 4 : 8, P = w4_parts<XT>(), size = XT == OZ2_F32 ? 4 : 2, per = 16 / size;  // 128 bytes of a thread in flight
 #pragma unroll 1
-  for (int piece = threadIdx.x; piece < pieces; piece += PIECES * threads) {
-    W4Raw<XT> raw[PIECES];
-    w4_each<PIECES>([&](auto i) __attribute__((always_inline)) { raw[i.value] = w4_stage_load<XT>(stage, row, min(piece + i.value * threads, pieces - 1)); });
-    w4_each<PIECES>([&](auto i) __attribute__((always_inline)) {
-      const int at = piece + i.value * threads;
-      if (at < pieces) seen |= (unsigned)w4_stage_store<XT, SPB, RT>(stage, raw[i.value], at, lds, pitch, sums) << (at / stage.eights);
-    });
+  for (int e = threadIdx.x; e < length * (kW4Block / 8); e += threads) {
+    const int at = start * kW4Block + e * 8;
+#pragma unroll 1
+    for (int t = 0; t < tokens; t += PIECES) {
+      w4_u4 raw[PIECES][8 / per];
+      w4_each<PIECES>([&](auto i) __attribute__((always_inline)) {
+        const char* p = x + row(min(t + i.value, tokens - 1)) * size;
+        w4_each<8 / per>([&](auto h) __attribute__((always_inline)) { raw[i.value][h.value] = w4_bytes<16>(p + w4_narrow(min(at + h.value * per, k - per) * size)); });
+      });
+      if (at + 8 > k)  // the 16 bytes that end with the vector, or nothing
+        w4_each<PIECES>([&](auto i) __attribute__((always_inline)) {
+          w4_each<8 / per>([&](auto h) __attribute__((always_inline)) {
+            const int there = k - (at + h.value * per);
+            w4_u4& v = raw[i.value][h.value];
+            v = there <= 0 ? w4_u4{0, 0, 0, 0} : there < per ? w4_cut(v, (per - there) * size) : v;
+          });
+        });
+      w4_each<PIECES>([&](auto i) __attribute__((always_inline)) {
+        if (t + i.value >= tokens) return;
+        char* to = lds + (t + i.value) * P * pitch + 16 * e;
+        if constexpr (XT == OZ2_F32) {
+          unsigned h[P][8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {  // cut, not rounded: each part takes the next eight bits, and none can overflow
+            float rest = __uint_as_float(raw[i.value][j / 4][j % 4]);
+#pragma unroll
+            for (int c = 0; c < P; ++c) {
+              h[c][j] = __float_as_uint(rest);
+              rest -= __uint_as_float(h[c][j] & 0xFFFF0000u);
+            }
+          }
+#pragma unroll
+          for (int c = 0; c < P; ++c)
+            *reinterpret_cast<w4_u4*>(to + c * pitch) =
+                w4_u4{__builtin_amdgcn_perm(h[c][4], h[c][0], 0x07060302u), __builtin_amdgcn_perm(h[c][5], h[c][1], 0x07060302u),
+                      __builtin_amdgcn_perm(h[c][6], h[c][2], 0x07060302u), __builtin_amdgcn_perm(h[c][7], h[c][3], 0x07060302u)};
+        } else {
+          *reinterpret_cast<w4_u4*>(to) = w4_pairs(raw[i.value][0]);
+        }
+      });
+    }
   }
-  unsigned which = 0;
-  if (__ballot(seen != 0))
-    for (int t = 0; t < 4 * RT; ++t) which |= (unsigned)(__ballot(seen >> t & 1) != 0) << t;
-  return which;
 }
 
 #endif
