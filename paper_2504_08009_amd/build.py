@@ -27,6 +27,10 @@ EXTRA_FLAGS = {
     "oz2_w4_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "oz2_w4_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "oz2_w4_f16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "oz2_w4_moe_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "oz2_w4_moe_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "oz2_w4_moe_f16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "oz2_w4_moe_down.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 
 

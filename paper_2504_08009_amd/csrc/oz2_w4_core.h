@@ -220,8 +220,15 @@ __device__ __forceinline__ int w4_inner(int j, int quarter) {
 // x in LDS.  A token's values lie in rows of `pitch` bytes for each of its parts, eight at a time in the order of w4_unpack's pairs.  Row a of the
 // matrix cores' tile is token a / 4 + 4 (a % 4), so that with few tokens only the first result registers of a lane count (RT: 1 or 4
 // for up to 4 or 16 tokens).
-template <int RT>
-__device__ __forceinline__ int w4_token(int a) { return a / 4 + 4 * (a % 4); }
+// Where row a of the tile reads from: its token, or, for rows without one, whose results nobody looks at, what lies 16 bytes further for each.  The sixteen
+// rows of a quarter then read from sixteen places of the banks; when they read a token's place together, a read takes ten times as long
+// (1 KiB in about 60 cycles).  Nothing is read past kW4Slack bytes behind the last token.
+constexpr int kW4Slack = 16 * 16 * 3;
+template <int PARTS>
+__device__ __forceinline__ int w4_row_of_x(int a, int tokens, int pitch) {
+  const int t = a / 4 + 4 * (a % 4), last = tokens - 1;
+  return t < tokens ? t * PARTS * pitch : last * PARTS * pitch + (t - last) * PARTS * 16;
+}
 
 // Value of the lane across in a pair, four, eight or sixteen lanes whose halves hold one value each (a pair: its two lanes).
 template <int STEP>

@@ -38,7 +38,7 @@ struct Cut {
 template <int XT, int SPB, int RT, bool WIDE, bool ZEROS>
 __global__ void __launch_bounds__(64 * kWaves, W4_TILE_WAVES) w4_tile_kernel(W4Rows w, int scale_type, Cut cut, int t, float alpha, const char* x, int64_t ldx, float beta,
                                                               const void* c, int64_t ldc, int y_type, void* y, int64_t ldy) {
-  extern __shared__ char lds[];
+  extern __shared__ __attribute__((aligned(16))) char lds[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   const int split = 1 << cut.split_log, s = wave & (split - 1);
   const int64_t pair = (int64_t)blockIdx.x * (cut.waves >> cut.split_log) + (wave >> cut.split_log);
@@ -46,29 +46,28 @@ __global__ void __launch_bounds__(64 * kWaves, W4_TILE_WAVES) w4_tile_kernel(W4R
   const int row[2] = {(int)(in ? pair * 32 : 0), (int)(in ? min(pair * 32 + 16, (int64_t)w.n - 1) : 0)};
   const W4Rows both[2] = {w, w};
   const int first = blockIdx.y * 4 * RT, tokens = min(4 * RT, t - first);
-  const char* lane_x = lds + min(w4_token<RT>(lane % 16), tokens - 1) * w4_parts<XT>() * cut.pitch;
+  const char* lane_x = lds + w4_row_of_x<w4_parts<XT>()>(lane % 16, tokens, cut.pitch);
   auto row_of = [&](int token) { return (first + token) * ldx; };
   W4Two<XT, SPB, RT, WIDE, ZEROS> two;
-  two.init(scale_type);
-  two.tile[0].init(w, row[0]), two.tile[1].init(w, row[1]);
+  two.init(both, row, scale_type);
   const int owner = w.full / kW4Run & (split - 1);  // of the block behind the whole ones
   float sum[2][RT];
 #pragma unroll
   for (int r = 0; r < RT; ++r) sum[0][r] = sum[1][r] = 0.f;
-  // Chunks are walked from a place of its own for every workgroup: rows lie whole pages apart as a rule, and where all stand at the same inner
-  // index, they ask the same few memory channels.
+  // Chunks too are walked from a place of its own for every workgroup.
   int at = cut.chunks > 1 ? blockIdx.x % cut.chunks : 0;
   for (int done = 0; done < cut.chunks; ++done) {
     const int start = at * cut.chunk, end = min(start + cut.chunk, w.full);  // of whole blocks (none: end <= start)
     const bool last = at == cut.chunks - 1, ragged = last && w.full * kW4Block < w.k;
     const int first_run = start / kW4Run + s, runs = (end + kW4Run - 1) / kW4Run;
     typename W4Two<XT, SPB, RT, WIDE, ZEROS>::Ahead ahead;
-    if (w.full) two.begin(w, first_run, end, ahead);
+    const typename W4Two<XT, SPB, RT, WIDE, ZEROS>::Walk walk(first_run, split, (runs - first_run + split - 1) >> cut.split_log, end, (unsigned)pair);
+    if (w.full) two.begin(w, walk, ahead);
     if (done) __syncthreads();
-    w4_stage<XT>(x, row_of, tokens, w.k, start, end - start + ragged, lds, cut.pitch, 64 * cut.waves);
+    w4_stage<XT>([&](int token) { return x + row_of(token) * (XT == OZ2_F32 ? 4 : 2); }, tokens, w.k, start, end - start + ragged, lds, cut.pitch, 64 * cut.waves);
     __syncthreads();
     if (in) {
-      two.multiply(w, first_run, split, (runs - first_run + split - 1) >> cut.split_log, end, start, ahead, lane_x, cut.pitch, sum);
+      two.multiply(w, walk, start, ahead, lane_x, cut.pitch, sum);
       if (ragged && s == owner) two.multiply_tail(both, row, lane_x + (w.full - start) * kW4Block * 2, cut.pitch, sum);
     }
     at = last ? 0 : at + 1;
@@ -195,7 +194,7 @@ hipError_t launch_tile(const W4Call& a) {
   auto lay = [&](int chunk) {
     cut.chunk = chunk;
     cut.pitch = chunk * kW4Block * 2 + 16;
-    cut.reduce_at = tokens * P * cut.pitch;
+    cut.reduce_at = tokens * P * cut.pitch + kW4Slack;
     return cut.reduce_at + (cut.split_log ? kWaves * 2 * RT * 64 * 4 : 0);
   };
   int lds = lay(blocks);

@@ -3,6 +3,7 @@
 #ifndef OZ2_W4_MOE_H
 #define OZ2_W4_MOE_H
 
+#include "oz2_w4_tile.h"
 #include "oz2_w4_vector.h"
 
 constexpr int kMoeTokens = 32;                               // of a sequence of launches; more tokens take several
@@ -28,14 +29,15 @@ struct MoeCall {
   float* h;         // f x places
   float* part;      // d x places: products of the down matrices times the weights
   int* chosen;      // of the layer's experts: number that somebody chose, then each with its first entry in `list`, then the places by expert
-  int pairs;        // 1: two tokens of an expert at a time, 0: one
+  int tiles;        // vectors of an expert at a time: 1, by the vector units, or 4 or 16, by the matrix cores
+  int direct;       // the second products of a token's places are summed where they are formed
   hipStream_t st;
 };
 
 W4Rows oz2_w4_rows(const oz2_w4_matrix& m);
 template <int XT>
-hipError_t oz2_moe_gate_up(const MoeCall& c, int scale_type);
-hipError_t oz2_moe_down(const MoeCall& c, int scale_type);
+hipError_t oz2_moe_gate_up(const MoeCall& c, const oz2_w4_matrix& gate);
+hipError_t oz2_moe_down(const MoeCall& c, const oz2_w4_matrix& down);
 int oz2_w4_compute_units();
 
 #ifdef __HIPCC__
@@ -52,8 +54,21 @@ struct Chosen {
   short place[kMoePlaces];
 };
 
-struct MoeItem {
-  int expert, first, places, row;
+// How the experts' batches (or groups of rows) are dealt out: items of up to kMoeRounds neighbouring ones, neighbouring items to neighbouring workgroups,
+// which then read neighbouring memory (where each has an even share of its own, all read a fixed distance apart, and 32
+// tokens through 128 experts of 4096 x 2048 take 864 in the place of 632 us).  The size of an item is that with which the busiest
+// workgroup has the least to do, `cost` batches beside its own for an item.
+struct Items {
+  int rounds, of_expert, all;
+  __device__ __forceinline__ Items(int experts, int batches, int cost) {
+    int least = 0x7FFFFFFF;
+    rounds = of_expert = all = 0;
+    for (int r = 1; r <= kMoeRounds; ++r) {
+      const int n = (batches + r - 1) / r, load = (experts * n + (int)gridDim.x - 1) / (int)gridDim.x * (r + cost);
+      if (load < least) least = load, rounds = r, of_expert = n;
+    }
+    all = experts * of_expert;
+  }
 };
 
 __device__ __forceinline__ W4Rows w4_of_stack(W4Rows w, int64_t e, int64_t codes, int64_t scales, int64_t zeros) {
@@ -61,8 +76,7 @@ __device__ __forceinline__ W4Rows w4_of_stack(W4Rows w, int64_t e, int64_t codes
   return w;
 }
 
-// Rows of experts times the places that chose them.  A workgroup takes an item (an expert and up to kMoeRounds batches of its rows) after the other;
-// a batch is four loads of rows for each `1 << split_log` waves, `loads` of which (4, or 2 beside 2 of a second matrix) are of one matrix.
+// Rows of experts times the places that chose them.  A batch is four loads of rows for each `1 << split_log` waves, `loads` of which (4, or 2 beside 2 of a second matrix) are of one matrix.
 // row(expert's matrices, row, i): the i-th load of the batch from that row; x(place): vector; out(place, row, sums): called by one
 // thread with the sums of the batch's 4 FOLD rows.
 template <int XT, int T, int ST, bool ZEROS, int FOLD, class Matrix, class Row, class X, class Out>
@@ -75,18 +89,15 @@ __device__ __forceinline__ void moe_products(const Chosen& chosen, int k, int ro
   const bool ragged = __ballot(at.cut != 0) != 0;
   auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
   const int count = uniform(chosen.count);
-  // as many rounds as leave every workgroup one item, if that can be
-  const int batches = (rows + rows_of_batch * per - 1) / (rows_of_batch * per);
-  const int rounds = max(1, min(kMoeRounds, (batches * count + (int)gridDim.x - 1) / (int)gridDim.x));
-  const int chunks = (batches + rounds - 1) / rounds;
+  const int batches = (rows + rows_of_batch * per - 1) / (rows_of_batch * per);  // of an expert
   int flip = 0;
-  for (int item = blockIdx.x; item < count * chunks; item += gridDim.x) {
-    const int a = item / chunks, chunk = item - a * chunks;
+  const Items items(count, batches, 2);
+  for (int item = blockIdx.x; item < items.all; item += gridDim.x) {  // (an expert's second and later places find the codes in the caches)
+    const int a = item / items.of_expert, b = (item - a * items.of_expert) * items.rounds, turns = min(items.rounds, batches - b);
     const int first = uniform(chosen.first[a]), places = uniform(chosen.first[a + 1]) - first;
     const auto m = matrix((int64_t)uniform(chosen.expert[a]));
-    const int start = chunk * rounds * per, turns = min(rounds, batches - chunk * rounds);
     auto rows_at = [&](int i) {
-      const int row = (start + i * per + group) * rows_of_batch;
+      const int row = ((b + i) * per + group) * rows_of_batch;
       return [&, row](int j) { return row_of(m, row, j); };
     };
     for (int p = 0; p < places; p += T) {
@@ -113,15 +124,93 @@ __device__ __forceinline__ void moe_products(const Chosen& chosen, int k, int ro
       for (int j = threadIdx.x; j < turns * per * T; j += 64 * kMoeWaves) {
         const int t = j % T, g = j / T % per, i = j / T / per;
         if (p + t >= places) continue;
-        float u[4 * FOLD];
+        float v[4 * FOLD];
 #pragma unroll
-        for (int n = 0; n < 4 * FOLD; ++n) u[n] = part[flip][i][g * split][n][t];
+        for (int n = 0; n < 4 * FOLD; ++n) v[n] = part[flip][i][g * split][n][t];
         for (int q = 1; q < split; ++q)
 #pragma unroll
-          for (int n = 0; n < 4 * FOLD; ++n) u[n] += part[flip][i][g * split + q][n][t];
-        out(chosen.place[first + p + t], (start + i * per + g) * rows_of_batch, u);
+          for (int n = 0; n < 4 * FOLD; ++n) v[n] += part[flip][i][g * split + q][n][t];
+        out(chosen.place[first + p + t], ((b + i) * per + g) * rows_of_batch, v);
       }
       flip ^= 1;
+    }
+  }
+}
+
+// The same on the matrix cores: a wave takes two tiles of sixteen rows, of one matrix or of two, for up to 4 RT places at a time, a workgroup
+// rows_of_wave rows for each of its waves.  tile(expert's matrices, t): the matrix of tile t; row(first, t): its first row; out(place, row, sum0,
+// sum1): called by the lane that has the sums of row `row` of either tile.
+// x of a workgroup, so that three fit a compute unit.  It holds a run of blocks of 16 vectors in 16 bits, or of 12 in FP32.
+constexpr int kMoeLds = 44 * 1024;
+static_assert(kMoeLds - kW4Slack >= 12 * 3 * (kW4Run * kW4Block * 2 + 16) && kMoeLds - kW4Slack >= 16 * (kW4Run * kW4Block * 2 + 16), "a run");
+
+template <int XT, int SPB, int RT, bool WIDE, bool ZEROS, class Matrix, class Tile, class First, class X, class Out>
+__device__ __forceinline__ void moe_tiles(const Chosen& chosen, int k, int rows, int rows_of_wave, int scale_type, char* lds, Matrix matrix, Tile tile, First first_row,
+                                          X vector, Out out) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+  auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  const int count = uniform(chosen.count), blocks = (k + kW4Block - 1) / kW4Block, full = k / kW4Block;
+  const int groups = (rows + rows_of_wave * kMoeWaves - 1) / (rows_of_wave * kMoeWaves);
+  W4Two<XT, SPB, RT, WIDE, ZEROS> two;
+  const Items items(count, groups, 0);
+  for (int item = blockIdx.x; item < items.all; item += gridDim.x) {
+    const int a = item / items.of_expert, g = (item - a * items.of_expert) * items.rounds, here = min(items.rounds, groups - g);
+    const int first = uniform(chosen.first[a]), places = uniform(chosen.first[a + 1]) - first;
+    const auto m = matrix((int64_t)uniform(chosen.expert[a]));
+    const W4Rows w[2] = {tile(m, 0), tile(m, 1)};
+    constexpr int most = RT == 4 && w4_parts<XT>() == 3 ? 12 : 4 * RT;
+    for (int p = 0; p < places; p += most) {
+      const int tokens = min(most, places - p);
+      auto x_of = [&](int t) { return vector(uniform(chosen.place[first + p + t])); };
+      // blocks of x at a time: all, or runs that fit
+      int chunk = min(blocks, ((kMoeLds - kW4Slack) / (tokens * w4_parts<XT>()) - 16) / (kW4Block * 2));
+      if (chunk < blocks) chunk = chunk / kW4Run * kW4Run;
+      const int chunks = (blocks + chunk - 1) / chunk, pitch = chunk * kW4Block * 2 + 16;
+      const char* lane_x = lds + w4_row_of_x<w4_parts<XT>()>(lane % 16, tokens, pitch);
+      for (int r = 0; r < here; ++r) {
+        const int row = ((g + r) * kMoeWaves + wave) * rows_of_wave;  // (past the end: the last rows again, not stored)
+        const int at[2] = {min(first_row(row, 0), w[0].n - 1), min(first_row(row, 1), w[1].n - 1)};
+        two.init(w, at, scale_type);
+        float sum[2][RT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) sum[0][i] = sum[1][i] = 0.f;
+        for (int j = 0; j < chunks; ++j) {
+          const int start = j * chunk, end = min(start + chunk, full);
+          const bool ragged = j == chunks - 1 && full * kW4Block < k;
+          typename W4Two<XT, SPB, RT, WIDE, ZEROS>::Ahead ahead;
+          const typename W4Two<XT, SPB, RT, WIDE, ZEROS>::Walk walk(start / kW4Run, 1, (end - start + kW4Run - 1) / kW4Run, end, blockIdx.x * kMoeWaves + wave);
+          if (full) two.begin(w[0], walk, ahead);
+          if (chunks > 1 || r == 0) {
+            __syncthreads();
+            w4_stage<XT>(x_of, tokens, k, start, end - start + ragged, lds, pitch, 64 * kMoeWaves);
+            __syncthreads();
+          }
+          two.multiply(w[0], walk, start, ahead, lane_x, pitch, sum);
+          if (ragged) two.multiply_tail(w, at, lane_x + (full - start) * kW4Block * 2, pitch, sum);
+        }
+        bool again = false;
+#pragma unroll
+        for (int i = 0; i < RT; ++i) again |= !(fabsf(sum[0][i]) < INFINITY && fabsf(sum[1][i]) < INFINITY) && lane / 16 + 4 * i < tokens;
+        if (__ballot(again)) {
+          float plain[2][RT];
+#pragma unroll
+          for (int i = 0; i < RT; ++i) plain[0][i] = plain[1][i] = 0.f;
+#pragma unroll 1
+          for (int b = 0; b < blocks; ++b)
+            two.block_plain(w, at, b, [&](int i, int l) {
+              const int token = min(lane / 16 + 4 * i, tokens - 1);
+              return w4_load(XT, vector(chosen.place[first + p + token]), l);
+            }, plain);
+#pragma unroll
+          for (int i = 0; i < 2 * RT; ++i)
+            if (!(fabsf(sum[i / RT][i % RT]) < INFINITY)) sum[i / RT][i % RT] = plain[i / RT][i % RT];
+        }
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+          const int token = lane / 16 + 4 * i;
+          if (token < tokens) out(chosen.place[first + p + token], row + lane % 16, sum[0][i], sum[1][i]);
+        }
+      }
     }
   }
 }

@@ -1,9 +1,9 @@
 // A layer of gated experts whose weights are held in 4 bits, with its router, for a few tokens (oz2_w4_moe).
 #include "oz2_w4_moe.h"
 
-extern template hipError_t oz2_moe_gate_up<OZ2_F32>(const MoeCall&, int);
-extern template hipError_t oz2_moe_gate_up<OZ2_BF16>(const MoeCall&, int);
-extern template hipError_t oz2_moe_gate_up<OZ2_F16>(const MoeCall&, int);
+extern template hipError_t oz2_moe_gate_up<OZ2_F32>(const MoeCall&, const oz2_w4_matrix&);
+extern template hipError_t oz2_moe_gate_up<OZ2_BF16>(const MoeCall&, const oz2_w4_matrix&);
+extern template hipError_t oz2_moe_gate_up<OZ2_F16>(const MoeCall&, const oz2_w4_matrix&);
 
 namespace {
 
@@ -204,7 +204,13 @@ hipError_t oz2_launch_w4_moe(const oz2_moe_layer& m, int64_t t, int x_type, cons
     c.weights = weights ? weights + first * m.top_k : reinterpret_cast<float*>(ws + s.weights);
     c.chosen = reinterpret_cast<int*>(ws + s.chosen);
     c.h = reinterpret_cast<float*>(ws + s.h), c.part = reinterpret_cast<float*>(ws + s.part);
-    c.pairs = 2 * c.t * c.top_k > c.experts;
+    // More than one token for an expert on the average: the matrix cores.  Of layers of 4096 x 2048 to 2048 x 1024, us without / with them:
+    // load 0.5 (8 tokens, 4 of 60 experts, FP32) 56 / 51, 1 (3 tokens, 3 of 9, 1000 x 777) 33 / 43, 1 (16, 8 of 128) 339 / 343, 1.5 (16, 6 of 64)
+    // 142 / 107, 2 (32, 8 of 128) 657 / 556, 2 (8, 2 of 8) 60 / 78, 4 (32, 8 of 64) 222 / 121, 16 (32, 4 of 8) 307 / 127.
+    const bool near = w4_tile_fits(c.gate) && w4_tile_fits(c.up) && w4_tile_fits(c.down);
+    c.tiles = !near || c.t * c.top_k <= c.experts ? 1 : c.t * c.top_k <= 2 * c.experts ? 4 : 16;
+    // Hardly an expert with two tokens: each token's second products are summed where they are formed.
+    c.direct = c.t == 1 || 2 * c.t * c.top_k <= c.experts;
     c.st = st;
     // rows of 16 bytes of codes or more, and spans of 2048 for the waves of a workgroup
     if (d < kW4Unit || f < kW4Unit || d > kMoeLongest || f > kMoeLongest) {
@@ -220,10 +226,10 @@ hipError_t oz2_launch_w4_moe(const oz2_moe_layer& m, int64_t t, int x_type, cons
     else launch_router<OZ2_F16>(m, x_type, c);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess)
-      e = x_type == OZ2_F32    ? oz2_moe_gate_up<OZ2_F32>(c, m.gate.scale_type)
-          : x_type == OZ2_BF16 ? oz2_moe_gate_up<OZ2_BF16>(c, m.gate.scale_type)
-                               : oz2_moe_gate_up<OZ2_F16>(c, m.gate.scale_type);
-    if (e == hipSuccess) e = oz2_moe_down(c, m.down.scale_type);
+      e = x_type == OZ2_F32    ? oz2_moe_gate_up<OZ2_F32>(c, m.gate)
+          : x_type == OZ2_BF16 ? oz2_moe_gate_up<OZ2_BF16>(c, m.gate)
+                               : oz2_moe_gate_up<OZ2_F16>(c, m.gate);
+    if (e == hipSuccess) e = oz2_moe_down(c, m.down);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

@@ -1,4 +1,4 @@
 // First products of a layer of experts for tokens in BF16.
 #include "oz2_w4_moe_up.h"
 
-template hipError_t oz2_moe_gate_up<OZ2_BF16>(const MoeCall&, int);
+template hipError_t oz2_moe_gate_up<OZ2_BF16>(const MoeCall&, const oz2_w4_matrix&);

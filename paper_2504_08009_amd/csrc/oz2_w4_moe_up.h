@@ -5,12 +5,6 @@
 #include "oz2_w4_moe.h"
 
 #ifdef __HIPCC__
-#ifndef MOE_UP_WAVES
-#define MOE_UP_WAVES 4
-#endif
-#ifndef MOE_UP_GRID
-#define MOE_UP_GRID 4
-#endif
 namespace {
 
 // Over the wave, in every lane.
@@ -97,13 +91,31 @@ __device__ __forceinline__ void moe_choose(const MoeCall& c, int token, short* i
 __device__ __forceinline__ void moe_route(const MoeCall& c, Chosen& chosen, short* ids, float* weights, int* count) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   const int places = c.t * c.top_k;
-  for (int e = threadIdx.x; e < c.experts; e += 64 * kMoeWaves) count[e] = 0;
-  for (int token = wave; token < c.t; token += kMoeWaves) {
+  auto choose = [&](int token) {
     if (c.experts <= 64) moe_choose<1>(c, token, ids, weights);
     else if (c.experts <= 128) moe_choose<2>(c, token, ids, weights);
     else if (c.experts <= 256) moe_choose<4>(c, token, ids, weights);
     else moe_choose<16>(c, token, ids, weights);
+  };
+  if (c.t == 1) {  // every place has an expert of its own, and those without one come last
+    if (wave == 0) {
+      choose(0);
+      const int id = lane < c.top_k ? ids[lane] : -1, n = __popcll(__ballot(id >= 0));
+      if (id >= 0) chosen.expert[lane] = id, chosen.place[lane] = lane;
+      if (lane <= n) chosen.first[lane] = lane;
+      if (lane == 0) chosen.count = n;
+      if (blockIdx.x == 0) {
+        if (lane < c.top_k) c.ids[lane] = id, c.weights[lane] = weights[lane];
+        if (lane == 0) c.chosen[0] = n;
+        if (lane <= n) c.chosen[1 + lane] = lane;
+        if (id >= 0) c.chosen[2 + kMoePlaces + lane] = id, c.chosen[2 + 2 * kMoePlaces + lane] = lane;
+      }
+    }
+    __syncthreads();
+    return;
   }
+  for (int e = threadIdx.x; e < c.experts; e += 64 * kMoeWaves) count[e] = 0;
+  for (int token = wave; token < c.t; token += kMoeWaves) choose(token);
   __syncthreads();
   for (int i = threadIdx.x; i < places; i += 64 * kMoeWaves)
     if (ids[i] >= 0) atomicAdd(&count[ids[i]], 1);
@@ -144,53 +156,93 @@ __device__ __forceinline__ void moe_route(const MoeCall& c, Chosen& chosen, shor
   for (int i = threadIdx.x; i < chosen.first[n]; i += 64 * kMoeWaves) to[2 + 2 * kMoePlaces + i] = chosen.place[i];
 }
 
-template <int XT, int T, int ST, bool ZEROS, int FOLD>
-__global__ void __launch_bounds__(64 * kMoeWaves, MOE_UP_WAVES) moe_up_kernel(MoeCall c, int split_log) {
+struct GateUp {
+  W4Rows gate, up;
+};
+__device__ __forceinline__ GateUp moe_gate_up_of(const MoeCall& c, int64_t e) {
+  return {w4_of_stack(c.gate, e, c.code_strides[0], c.scale_strides[0], c.zero_strides[0]),
+          w4_of_stack(c.up, e, c.code_strides[1], c.scale_strides[1], c.zero_strides[1])};
+}
+__device__ __forceinline__ void moe_inner(const MoeCall& c, int place, int row, float g, float u) {
+  if (row >= c.f) return;
+  const float a = c.activation == OZ2_ACT_SILU ? g / (1.f + expf(-g)) : 0.5f * g * (1.f + erff(g * 0.70710678f));
+  c.h[(int64_t)place * c.f + row] = a * u;
+}
+
+// One place of an expert at a time, by the vector units.
+template <int XT, int ST, bool ZEROS, int FOLD>
+__global__ void __launch_bounds__(64 * kMoeWaves, 4) moe_up_kernel(MoeCall c, int split_log) {
   __shared__ Chosen chosen;
   __shared__ short ids[kMoePlaces];
   __shared__ float weights[kMoePlaces];
   __shared__ int count[OZ2_MOE_MAX_EXPERTS];
-  __shared__ float part[2][kMoeRounds][kMoeWaves][4 * FOLD][T];
+  __shared__ float part[2][kMoeRounds][kMoeWaves][4 * FOLD][1];
   moe_route(c, chosen, ids, weights, count);
-  struct Two { W4Rows gate, up; };
-  moe_products<XT, T, ST, ZEROS, FOLD>(
-      chosen, c.d, c.f, 2, split_log, c.gate, part,
-      [&](int64_t e) {
-        return Two{w4_of_stack(c.gate, e, c.code_strides[0], c.scale_strides[0], c.zero_strides[0]),
-                   w4_of_stack(c.up, e, c.code_strides[1], c.scale_strides[1], c.zero_strides[1])};
-      },
-      [&](const Two& m, int row, int i) { return w4_row<ST, FOLD>(i < 2 ? m.gate : m.up, row, i % 2); },
+  moe_products<XT, 1, ST, ZEROS, FOLD>(
+      chosen, c.d, c.f, 2, split_log, c.gate, part, [&](int64_t e) { return moe_gate_up_of(c, e); },
+      [&](const GateUp& m, int row, int i) { return w4_row<ST, FOLD>(i < 2 ? m.gate : m.up, row, i % 2); },
       [&](int place) { return c.x + place / c.top_k * c.ldx * (XT == OZ2_F32 ? 4 : 2); },
       [&](int place, int row, const float* u) {
 #pragma unroll
-        for (int i = 0; i < 2 * FOLD; ++i)
-          if (row + i < c.f) {
-            const float g = u[i];
-            const float a = c.activation == OZ2_ACT_SILU ? g / (1.f + expf(-g)) : 0.5f * g * (1.f + erff(g * 0.70710678f));
-            c.h[(int64_t)place * c.f + row + i] = a * u[2 * FOLD + i];
-          }
+        for (int i = 0; i < 2 * FOLD; ++i) moe_inner(c, place, row + i, u[i], u[2 * FOLD + i]);
       });
 }
 
-template <int XT, int T, int ST, bool ZEROS>
+// Several, by the matrix cores: a tile of either matrix.
+template <int XT, int SPB, int RT, bool WIDE, bool ZEROS>
+__global__ void __launch_bounds__(64 * kMoeWaves, 3) moe_up_tiles_kernel(MoeCall c, int scale_type) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  __shared__ Chosen chosen;
+  {  // (the choice is done with its own arrays before x is brought in)
+    short* ids = reinterpret_cast<short*>(lds);
+    float* weights = reinterpret_cast<float*>(ids + kMoePlaces);
+    moe_route(c, chosen, ids, weights, reinterpret_cast<int*>(weights + kMoePlaces));
+    __syncthreads();
+  }
+  moe_tiles<XT, SPB, RT, WIDE, ZEROS>(
+      chosen, c.d, c.f, 16, scale_type, lds, [&](int64_t e) { return moe_gate_up_of(c, e); },
+      [](const GateUp& m, int t) { return t ? m.up : m.gate; }, [](int row, int) { return row; },
+      [&](int place) { return c.x + place / c.top_k * c.ldx * (XT == OZ2_F32 ? 4 : 2); },
+      [&](int place, int row, float g, float u) { moe_inner(c, place, row, g, u); });
+}
+
+template <int XT, int ST>
 hipError_t launch_up(const MoeCall& c) {
-  const dim3 grid(oz2_w4_compute_units() * MOE_UP_GRID), block(64 * kMoeWaves);
-  if (moe_fold(c.gate) && moe_fold(c.up)) hipLaunchKernelGGL((moe_up_kernel<XT, T, ST, ZEROS, 2>), grid, block, 0, c.st, c, 0);
-  else hipLaunchKernelGGL((moe_up_kernel<XT, T, ST, ZEROS, 1>), grid, block, 0, c.st, c, moe_split(c.d));
+  const dim3 grid(oz2_w4_compute_units() * 4), block(64 * kMoeWaves);
+  const bool fold = moe_fold(c.gate) && moe_fold(c.up);
+  const int split = fold ? 0 : moe_split(c.d);
+  if (c.gate.zeros) {
+    if (fold) hipLaunchKernelGGL((moe_up_kernel<XT, ST, true, 2>), grid, block, 0, c.st, c, split);
+    else hipLaunchKernelGGL((moe_up_kernel<XT, ST, true, 1>), grid, block, 0, c.st, c, split);
+  } else {
+    if (fold) hipLaunchKernelGGL((moe_up_kernel<XT, ST, false, 2>), grid, block, 0, c.st, c, split);
+    else hipLaunchKernelGGL((moe_up_kernel<XT, ST, false, 1>), grid, block, 0, c.st, c, split);
+  }
   return hipGetLastError();
 }
-template <int XT, int T, int ST>
-hipError_t launch_up(const MoeCall& c) {
-  return c.gate.zeros ? launch_up<XT, T, ST, true>(c) : launch_up<XT, T, ST, false>(c);
+
+template <int XT, int SPB, int RT, bool WIDE, bool ZEROS>
+hipError_t launch_up_tiles(const MoeCall& c, int scale_type) {
+  hipLaunchKernelGGL((moe_up_tiles_kernel<XT, SPB, RT, WIDE, ZEROS>), dim3(oz2_w4_compute_units() * 3), dim3(64 * kMoeWaves), kMoeLds + kMoeWaves * 2 * 2 * RT * 64 * 4, c.st, c, scale_type);
+  return hipGetLastError();
+}
+template <int XT, int SPB, int RT>
+hipError_t launch_up_tiles(const MoeCall& c, int scale_type) {
+  if (scale_type == OZ2_F32) return c.gate.zeros ? launch_up_tiles<XT, SPB, RT, true, true>(c, scale_type) : launch_up_tiles<XT, SPB, RT, true, false>(c, scale_type);
+  return c.gate.zeros ? launch_up_tiles<XT, SPB, RT, false, true>(c, scale_type) : launch_up_tiles<XT, SPB, RT, false, false>(c, scale_type);
+}
+template <int XT, int SPB>
+hipError_t launch_up_tiles(const MoeCall& c, int scale_type) {
+  return c.tiles == 4 ? launch_up_tiles<XT, SPB, 1>(c, scale_type) : launch_up_tiles<XT, SPB, 4>(c, scale_type);
 }
 
 }  // namespace
 
 template <int XT>
-hipError_t oz2_moe_gate_up(const MoeCall& c, int scale_type) {
-  if (!c.pairs)
-    return scale_type == OZ2_F32 ? launch_up<XT, 1, OZ2_F32>(c) : scale_type == OZ2_BF16 ? launch_up<XT, 1, OZ2_BF16>(c) : launch_up<XT, 1, OZ2_F16>(c);
-  return scale_type == OZ2_F32 ? launch_up<XT, 2, OZ2_F32>(c) : scale_type == OZ2_BF16 ? launch_up<XT, 2, OZ2_BF16>(c) : launch_up<XT, 2, OZ2_F16>(c);
+hipError_t oz2_moe_gate_up(const MoeCall& c, const oz2_w4_matrix& gate) {
+  const int type = gate.scale_type;
+  if (c.tiles == 1) return type == OZ2_F32 ? launch_up<XT, OZ2_F32>(c) : type == OZ2_BF16 ? launch_up<XT, OZ2_BF16>(c) : launch_up<XT, OZ2_F16>(c);
+  return gate.group == 32 ? launch_up_tiles<XT, 4>(c, type) : gate.group == 64 ? launch_up_tiles<XT, 2>(c, type) : launch_up_tiles<XT, 1>(c, type);
 }
 #endif
 #endif

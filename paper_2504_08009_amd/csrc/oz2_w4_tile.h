@@ -1,8 +1,10 @@
 // Two tiles of sixteen rows held in 4 bits times up to sixteen vectors, by one wave on the matrix cores.  Both tiles meet the same
 // fragments of x, read from LDS once for the two.
 //
-// Four neighbouring lanes load 64 bytes of a row in one access; where each lane loads from a row of its own, as the matrix cores want their operand,
-// the vector cache is asked 64 times for a load and sets the pace (65536 x 8192 with one vector: 3.6 TB/s).  The words then change lanes.
+// Four neighbouring lanes load 64 bytes of a row, eight of them two lines' worth of two blocks; where each lane loads from a row of its own, as the matrix
+// cores want their operand, the vector cache is asked 64 times for a load and sets the pace.  The words then change lanes and
+// registers: inside four lanes by selecting from the neighbour's, across sixteen and 32 by swapping registers' halves.  (Through LDS, with
+// ds_bpermute, a KiB of codes took 165 cycles of it, four times what the memory takes to bring it.)
 #ifndef OZ2_W4_TILE_H
 #define OZ2_W4_TILE_H
 
@@ -10,34 +12,13 @@
 
 #ifdef __HIPCC__
 
-constexpr int kW4Run = 4;  // blocks whose scales a wave loads together, a block a lane of four, and that it has in flight
+constexpr int kW4Run = 2;   // blocks that a wave loads together
+constexpr int kW4Ahead = 2; // runs in flight
 
-// A tile as a launch sees it: its first row, and the lane's row (lane / 4) from there.
-template <bool WIDE, bool ZEROS>
-struct W4Tile {
-  const uint8_t* codes;
-  const char* scales;
-  const uint8_t* zeros;
-  unsigned codes_at, scales_at, zeros_at;
-
-  __device__ __forceinline__ void init(const W4Rows& w, int row) {
-    const int lane = threadIdx.x % 64, first = min(row, w.n - 1), mine = min(lane / 4, w.n - 1 - first);
-    codes = w.codes + first * w.ld_codes, scales = w.scales + first * w.ld_scales * (WIDE ? 4 : 2), zeros = w.zeros + first * w.ld_zeros;
-    codes_at = (unsigned)(mine * (int)w.ld_codes + lane % 4 * 16);
-    scales_at = (unsigned)(mine * (int)w.ld_scales * (WIDE ? 4 : 2));
-    zeros_at = (unsigned)(mine * (int)w.ld_zeros);
-  }
-};
-inline bool w4_tile_fits(const W4Rows& w) {  // sixteen rows lie within 32 bits
+inline bool w4_tile_fits(const W4Rows& w) {  // a lane's rows lie within 32 bits of each other
   constexpr int64_t far = (int64_t)1 << 25;
   return w.ld_codes < far && w.ld_scales < far && w.ld_zeros < far;
 }
-
-template <int SPB, bool WIDE>
-struct W4RunScales {
-  typename W4Width<SPB * (WIDE ? 4 : 2)>::type s[2];
-  typename W4Width<SPB>::type z[2];
-};
 
 // 32 bits that a loop must not keep widened, for the sake of loads with a scalar base
 __device__ __forceinline__ unsigned w4_narrow(unsigned v) {
@@ -47,39 +28,95 @@ __device__ __forceinline__ unsigned w4_narrow(unsigned v) {
 
 template <int XT, int SPB, int RT, bool WIDE, bool ZEROS>
 struct W4Two {
-  W4Tile<WIDE, ZEROS> tile[2];
-  int half;  // whether 16-bit scales are f16
-  int from, from_scale;  // lanes (times 4) whose codes, and whose scales of a run's first block, this lane takes
+  // Where a lane loads from.  Codes: load j takes row 4 (lane / 4 % 4) + j of tile lane / 16 % 2, chunk lane % 4 of block lane / 32 of the run;
+  // scales: row lane % 16 of that tile and block.
+  const uint8_t* codes;
+  const char* scales;
+  const uint8_t* zeros;
+  int step[3];  // from the lane's first row to the others (fewer at the end of the matrix: the last one again)
+  int half;     // whether 16-bit scales are f16
 
-  __device__ __forceinline__ void init(int scale_type) {
-    const int lane = threadIdx.x % 64;
+  __device__ __forceinline__ void init(const W4Rows (&w)[2], const int (&row)[2], int scale_type) {
+    const int lane = threadIdx.x % 64, t = lane / 16 % 2;
     half = scale_type == OZ2_F16;
-    from = (lane % 16 * 4 + lane / 16) * 4, from_scale = lane % 16 * 16;
-  }
-  __device__ __forceinline__ w4_u4 codes(int t, int block) const {
-    return w4_bytes<16>(tile[t].codes + (int64_t)block * (kW4Block / 2) + w4_narrow(tile[t].codes_at));
-  }
-  __device__ __forceinline__ W4RunScales<SPB, WIDE> scales(const W4Rows& w, int run) const {
-    constexpr int size = WIDE ? 4 : 2;
-    W4RunScales<SPB, WIDE> r;
-    const unsigned g = w4_group<SPB>(w, min(run * kW4Run + (int)(threadIdx.x % 4), w.full - 1));
+    const W4Rows& m = w[0];  // (both are alike but for their addresses)
+    const int n = m.n - 1, first = min((t ? row[1] : row[0]) + lane / 4 % 4 * 4, n), mine = min((t ? row[1] : row[0]) + lane % 16, n);
+    codes = (t ? w[1].codes : w[0].codes) + first * (t ? w[1].ld_codes : w[0].ld_codes) + lane % 4 * 16;
+    scales = (t ? w[1].scales : w[0].scales) + mine * (t ? w[1].ld_scales : w[0].ld_scales) * (WIDE ? 4 : 2);
+    zeros = (t ? w[1].zeros : w[0].zeros) + mine * (t ? w[1].ld_zeros : w[0].ld_zeros);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      r.s[t] = w4_bytes<SPB * size>(tile[t].scales + w4_narrow(tile[t].scales_at + g * size));
-      if constexpr (ZEROS) r.z[t] = w4_bytes<SPB>(tile[t].zeros + w4_narrow(tile[t].zeros_at + g));
-    }
+    for (int j = 0; j < 3; ++j) step[j] = min(j + 1, n - first) * (int)(t ? w[1].ld_codes : w[0].ld_codes);
+  }
+  struct Run {
+    w4_u4 q[4];
+    typename W4Width<SPB * (WIDE ? 4 : 2)>::type s;
+    typename W4Width<SPB>::type z;
+  };
+  // The run's blocks below `end`; of those past it, the one before it.
+  __device__ __forceinline__ Run fetch(const W4Rows& w, int run, int end) const {
+    constexpr int size = WIDE ? 4 : 2;
+    Run r;
+    const int b = min(run * kW4Run + (int)(threadIdx.x % 64 / 32), end - 1);
+    const unsigned at = b * (kW4Block / 2), g = w4_group<SPB>(w, b);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r.q[j] = w4_bytes<16>(codes + (unsigned)(at + (j ? step[j ? j - 1 : 0] : 0)));
+    r.s = w4_bytes<SPB * size>(scales + g * size);
+    if constexpr (ZEROS) r.z = w4_bytes<SPB>(zeros + g);
     return r;
   }
   __device__ __forceinline__ float decode(unsigned v) const {
     const float b = __uint_as_float(v << 16), h = (float)__builtin_bit_cast(_Float16, (unsigned short)v);
     return half ? h : b;
   }
+  // Register j of lane i for register i of lane j, of every four lanes: two exchanges, of which each result is one instruction, the lane's own
+  // value or its neighbour's by a mask.  (The waits are those between a vector instruction and one that reads its result from another lane.)
+  static __device__ __forceinline__ void turn_four(unsigned& a, unsigned& b, unsigned& c, unsigned& d) {
+    unsigned p, q, r, s;
+    asm("s_nop 1\n\t"
+        "s_mov_b64 vcc, %8\n\t"
+        "v_cndmask_b32_dpp %1, %4, %5, vcc quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf\n\t"
+        "v_cndmask_b32_dpp %3, %6, %7, vcc quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf\n\t"
+        "s_not_b64 vcc, vcc\n\t"
+        "v_cndmask_b32_dpp %0, %5, %4, vcc quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf\n\t"
+        "v_cndmask_b32_dpp %2, %7, %6, vcc quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf\n\t"
+        "s_mov_b64 vcc, %9\n\t"
+        "v_cndmask_b32_dpp %6, %0, %2, vcc quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf\n\t"
+        "v_cndmask_b32_dpp %7, %1, %3, vcc quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf\n\t"
+        "s_not_b64 vcc, vcc\n\t"
+        "v_cndmask_b32_dpp %4, %2, %0, vcc quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf\n\t"
+        "v_cndmask_b32_dpp %5, %3, %1, vcc quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf\n\t"
+        : "=&v"(p), "=&v"(q), "=&v"(r), "=&v"(s), "+v"(a), "+v"(b), "+v"(c), "+v"(d)
+        : "s"(0xAAAAAAAAAAAAAAAAull), "s"(0xCCCCCCCCCCCCCCCCull)
+        : "vcc", "scc");
+  }
+  // out[2 block + tile]: codes as the matrix cores take them
+  static __device__ __forceinline__ void turn(const Run& r, w4_u4 (&out)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      unsigned v[4] = {r.q[0][j], r.q[1][j], r.q[2][j], r.q[3][j]};
+      turn_four(v[0], v[1], v[2], v[3]);
+      const w4_u4 u = w4_exchange<4>(w4_u4{v[0], v[1], v[2], v[3]});
+#pragma unroll
+      for (int i = 0; i < 4; ++i) out[i][j] = u[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = w4_exchange<SPB>(out[i]);
+  }
+  // out[2 block + tile]: the value of the lane's row
+  static __device__ __forceinline__ void spread(float f, float (&out)[4]) {
+    const unsigned v = __float_as_uint(f);
+    typedef unsigned u2 __attribute__((ext_vector_type(2)));
+    const u2 r = __builtin_amdgcn_permlane16_swap(v, v, false, false);  // tile 0's, tile 1's in the sixteens of either block's 32
+    const u2 a = __builtin_amdgcn_permlane32_swap(r[0], r[0], false, false), b = __builtin_amdgcn_permlane32_swap(r[1], r[1], false, false);
+    out[0] = __uint_as_float(a[0]), out[1] = __uint_as_float(b[0]), out[2] = __uint_as_float(a[1]), out[3] = __uint_as_float(b[1]);
+  }
 
   // sum[t] += the tiles' products for one block.  q: codes as the matrix cores take them; scale(t, segment), zero(t, segment).
   template <class Scale, class Zero>
   __device__ __forceinline__ void block(const w4_u4 (&q)[2], Scale scale, Zero zero, const char* x, int part_bytes, float (&sum)[2][RT]) const {
     const int quarter = threadIdx.x % 64 / 16;
-    constexpr unsigned one = XT == OZ2_F16 ? 0x3C003C00u : 0x3F803F80u;
+    // sum (16 + q) x - 24 sum x comes out of the matrix cores where there are no zero points, else sum (16 + q) x and sum x
+    constexpr unsigned one = ZEROS ? (XT == OZ2_F16 ? 0x3C003C00u : 0x3F803F80u) : (XT == OZ2_F16 ? 0xCE00CE00u : 0xC1C0C1C0u);
     const unsigned ones[4] = {one, one, one, one};
     w4_each<SPB>([&](auto index) __attribute__((always_inline)) {
       constexpr int seg = index.value;
@@ -93,77 +130,68 @@ struct W4Two {
 #pragma unroll
         for (int p = 0; p < w4_parts<XT>(); ++p) {
           const uint4 v = *reinterpret_cast<const uint4*>(x + p * part_bytes + 2 * w4_inner<SPB>(j, quarter));
+          of_x = w4_mfma<XT>(v, ones, of_x);
           acc[0] = w4_mfma<XT>(v, b[0], acc[0]);
           acc[1] = w4_mfma<XT>(v, b[1], acc[1]);
-          of_x = w4_mfma<XT>(v, ones, of_x);  // sum of x, as each lane wants it
         }
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const float s = scale(t, index), z = kW4Offset + zero(t, index);
+        const float s = scale(t, index);
 #pragma unroll
-        for (int i = 0; i < RT; ++i) sum[t][i] = fmaf(s, fmaf(-z, of_x[i], acc[t][i]), sum[t][i]);
+        for (int i = 0; i < RT; ++i) {
+          const float v = ZEROS ? fmaf(-(kW4Offset + zero(t, index)), of_x[i], acc[t][i]) : acc[t][i] + of_x[i];
+          sum[t][i] = fmaf(s, v, sum[t][i]);
+        }
       }
     });
   }
 
-  // Loads of a first run, ahead of whatever has to be done before its products.  There is a whole block.
-  struct Ahead {
-    w4_u4 ring[kW4Run][2];
-    W4RunScales<SPB, WIDE> now;
-  };
-  __device__ __forceinline__ void begin(const W4Rows& w, int first, int end, Ahead& a) const {
-    a.now = scales(w, first);
-    w4_each<kW4Run>([&](auto u) __attribute__((always_inline)) {
-      const int b = max(min(first * kW4Run + u.value, end - 1), 0);
-      a.ring[u.value][0] = codes(0, b), a.ring[u.value][1] = codes(1, b);
-    });
-  }
-  // Runs first, first + stride, ... (`count` of them) of the whole blocks below `end`.  x: of block `origin`.
-  __device__ __forceinline__ void multiply(const W4Rows& w, int first, int stride, int count, int end, int origin, Ahead& ahead, const char* x, int part_bytes,
-                                           float (&sum)[2][RT]) const {
-    w4_u4 (&ring)[kW4Run][2] = ahead.ring;
-    W4RunScales<SPB, WIDE> now = ahead.now, next;
-#pragma unroll 1
-    for (int i = 0; i < count; ++i) {
-      const int run = first + i * stride, then = i + 1 < count ? run + stride : run;
-      next = scales(w, then);
-      w4_each<kW4Run>([&](auto u) __attribute__((always_inline)) {
-        const int b = run * kW4Run + u.value;
-        if (b < end) {
-          w4_u4 q[2];
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) q[t][j] = __builtin_amdgcn_ds_bpermute(from, ring[u.value][t][j]);
-            q[t] = w4_exchange<SPB>(q[t]);
-          }
-          constexpr int words = (SPB * (WIDE ? 4 : 2) + 3) / 4;
-          unsigned s[2][words], z[2];
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-#pragma unroll
-            for (int j = 0; j < words; ++j)
-              s[t][j] = __builtin_amdgcn_ds_bpermute(from_scale + 4 * u.value, w4_word<SPB * (WIDE ? 4 : 2)>(now.s[t], j));
-            if constexpr (ZEROS) z[t] = __builtin_amdgcn_ds_bpermute(from_scale + 4 * u.value, w4_word<SPB>(now.z[t], 0));
-          }
-          block(
-              q,
-              [&](int t, auto seg) __attribute__((always_inline)) {
-                if constexpr (WIDE) return __uint_as_float(s[t][seg.value]);
-                else return decode(s[t][seg.value / 2] >> (seg.value % 2 * 16));
-              },
-              [&](int t, auto seg) __attribute__((always_inline)) {
-                if constexpr (ZEROS) return (float)(z[t] >> (8 * seg.value) & 255u);
-                else return 8.f;
-              },
-              x + (b - origin) * kW4Block * 2, part_bytes, sum);
-        }
-        const int f = min(then * kW4Run + u.value, end - 1);
-        ring[u.value][0] = codes(0, f), ring[u.value][1] = codes(1, f);
-      });
-      now = next;
+  // What a wave walks: runs first, first + stride, ... (`count` of them) of the whole blocks below `end`, from the `turn`-th on and round.  Each wave
+  // begins at a place of its own: rows lie whole pages apart as a rule, and where all stand at the same inner index, they ask the same few memory channels.
+  struct Walk {
+    int first, stride, count, end, turn;
+    __device__ __forceinline__ Walk(int first, int stride, int count, int end, unsigned who)
+        : first(first), stride(stride), count(count), end(end), turn(count > 1 ? who % (unsigned)count : 0) {}
+    __device__ __forceinline__ int run(int i) const {  // (past the last: the last again)
+      i = max(min(i, count - 1), 0) + turn;
+      return first + (i < count || count < 1 ? i : i - count) * stride;
     }
+  };
+  // Loads of the first runs, ahead of whatever has to be done before their products.
+  struct Ahead {
+    Run run[kW4Ahead];
+  };
+  __device__ __forceinline__ void begin(const W4Rows& w, const Walk& walk, Ahead& a) const {
+    w4_each<kW4Ahead>([&](auto i) __attribute__((always_inline)) { a.run[i.value] = fetch(w, walk.run(i.value), max(walk.end, 1)); });
+  }
+  // x: of block `origin`.
+  __device__ __forceinline__ void multiply(const W4Rows& w, const Walk& walk, int origin, Ahead& ahead, const char* x, int part_bytes, float (&sum)[2][RT]) const {
+#pragma unroll 1
+    for (int i = 0; i < walk.count; i += kW4Ahead)
+      w4_each<kW4Ahead>([&](auto a) __attribute__((always_inline)) {
+        const int at = i + a.value, run = walk.run(at);
+        w4_u4 q[4];
+        float s[SPB][4], z[SPB][4];
+        turn(ahead.run[a.value], q);
+        w4_each<SPB>([&](auto j) __attribute__((always_inline)) {  // (decoded where they were loaded, once, and not where they are used)
+          const auto& r = ahead.run[a.value];
+          if constexpr (WIDE) spread(__uint_as_float(w4_word<SPB * 4>(r.s, j.value)), s[j.value]);
+          else spread(decode(w4_word<SPB * 2>(r.s, j.value / 2) >> (j.value % 2 * 16)), s[j.value]);
+          if constexpr (ZEROS) spread((float)(w4_word<SPB>(r.z, 0) >> (8 * j.value) & 255u), z[j.value]);
+        });
+        ahead.run[a.value] = fetch(w, walk.run(at + kW4Ahead), walk.end);
+        w4_each<kW4Run>([&](auto u) __attribute__((always_inline)) {
+          const int b = run * kW4Run + u.value;
+          if (at < walk.count && b < walk.end) {
+            const w4_u4 codes_of[2] = {q[2 * u.value], q[2 * u.value + 1]};
+            block(
+                codes_of, [&](int t, auto seg) __attribute__((always_inline)) { return s[seg.value][2 * u.value + t]; },
+                [&](int t, auto seg) __attribute__((always_inline)) { return z[seg.value][2 * u.value + t]; },
+                x + (b - origin) * kW4Block * 2, part_bytes, sum);
+          }
+        });
+      });
   }
 
   // The block behind the whole ones; row[t]: the tiles' first rows.
@@ -207,9 +235,9 @@ struct W4Two {
 };
 
 // Brings blocks start .. start + length - 1 of x into LDS, zeros past k, by all threads of a workgroup, between two barriers of the caller's.  A thread
-// takes eight values of several tokens at a time.  row(token): element offset of the vector; k is at least 8.
-template <int XT, class Row>
-__device__ __forceinline__ void w4_stage(const char* x, Row row, int tokens, int k, int start, int length, char* lds, int pitch, int threads) {
+// takes eight values of several tokens at a time.  vector(token): its start; k is at least 8.
+template <int XT, class X>
+__device__ __forceinline__ void w4_stage(X vector, int tokens, int k, int start, int length, char* lds, int pitch, int threads) {
   constexpr int PIECES = XT == OZ2_F32 ? 4 : 8, P = w4_parts<XT>(), size = XT == OZ2_F32 ? 4 : 2, per = 16 / size;  // 128 bytes of a thread in flight
 #pragma unroll 1
   for (int e = threadIdx.x; e < length * (kW4Block / 8); e += threads) {
@@ -218,7 +246,7 @@ __device__ __forceinline__ void w4_stage(const char* x, Row row, int tokens, int
     for (int t = 0; t < tokens; t += PIECES) {
       w4_u4 raw[PIECES][8 / per];
       w4_each<PIECES>([&](auto i) __attribute__((always_inline)) {
-        const char* p = x + row(min(t + i.value, tokens - 1)) * size;
+        const char* p = vector(min(t + i.value, tokens - 1));
         w4_each<8 / per>([&](auto h) __attribute__((always_inline)) { raw[i.value][h.value] = w4_bytes<16>(p + w4_narrow(min(at + h.value * per, k - per) * size)); });
       });
       if (at + 8 > k)  // the 16 bytes that end with the vector, or nothing
