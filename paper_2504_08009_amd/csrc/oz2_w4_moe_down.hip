@@ -33,12 +33,14 @@ __global__ void __launch_bounds__(64 * kMoeWaves, 4) moe_down_kernel(MoeCall c, 
       });
 }
 
-// A batch of rows for all places of a token, and their sum.  Groups of `1 << split_log` waves take every per-th place each.
+// A batch of rows for all places of a token, and their sum.  Groups of `1 << split_log` waves take every per-th place each: eight waves, so that
+// most tokens' places are all in flight.
+constexpr int kDirectWaves = 8;
 template <int ST, bool ZEROS, int FOLD>
-__global__ void __launch_bounds__(64 * kMoeWaves, 4) moe_down_direct_kernel(MoeCall c, int split_log) {
-  __shared__ float part[kMoeWaves][4 * FOLD];
+__global__ void __launch_bounds__(64 * kDirectWaves, 4) moe_down_direct_kernel(MoeCall c, int split_log) {
+  __shared__ float part[kDirectWaves][4 * FOLD];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, token = blockIdx.y;
-  const int split = 1 << split_log, group = wave >> split_log, per = kMoeWaves >> split_log;
+  const int split = 1 << split_log, group = wave >> split_log, per = kDirectWaves >> split_log;
   const int unit = FOLD == 2 ? lane % 32 : (wave & (split - 1)) * 64 + lane, row = blockIdx.x * 4 * FOLD;
   const W4Place at = w4_place(c.down, unit);
   const bool ragged = __ballot(at.cut != 0) != 0;
@@ -70,7 +72,7 @@ __global__ void __launch_bounds__(64 * kMoeWaves, 4) moe_down_direct_kernel(MoeC
   if (threadIdx.x >= 4 * FOLD || row + (int)threadIdx.x >= c.d) return;
   float v = 0.f;
 #pragma unroll
-  for (int q = 0; q < kMoeWaves; ++q) v += part[q][threadIdx.x];
+  for (int q = 0; q < kDirectWaves; ++q) v += part[q][threadIdx.x];
   w4_store(c.y_type, c.y, token * c.ldy + row + threadIdx.x, v);
 }
 
@@ -102,9 +104,8 @@ __global__ void __launch_bounds__(256) moe_sum_kernel(MoeCall c) {
 
 template <int ST, bool ZEROS, int FOLD>
 void launch_down(const MoeCall& c, int split) {
-  const dim3 block(64 * kMoeWaves);
-  if (c.direct) hipLaunchKernelGGL((moe_down_direct_kernel<ST, ZEROS, FOLD>), dim3((c.d + 4 * FOLD - 1) / (4 * FOLD), c.t), block, 0, c.st, c, split);
-  else hipLaunchKernelGGL((moe_down_kernel<ST, ZEROS, FOLD>), dim3(oz2_w4_compute_units() * 4), block, 0, c.st, c, split);
+  if (c.direct) hipLaunchKernelGGL((moe_down_direct_kernel<ST, ZEROS, FOLD>), dim3((c.d + 4 * FOLD - 1) / (4 * FOLD), c.t), dim3(64 * kDirectWaves), 0, c.st, c, split);
+  else hipLaunchKernelGGL((moe_down_kernel<ST, ZEROS, FOLD>), dim3(oz2_w4_compute_units() * 4), dim3(64 * kMoeWaves), 0, c.st, c, split);
 }
 template <int ST, bool ZEROS>
 void launch_down(const MoeCall& c) {

@@ -201,6 +201,68 @@ def test_matvec_with_values_at_the_ends_of_the_range():
     close(oz.w4_matvec(small, gx), x @ w.w.T * 2.0 ** -20, w.depth * U * (np.abs(x) @ w.size.T) * 2.0 ** -20, "f32")
 
 
+@pytest.mark.parametrize("t,n,k", [(1, 40, 1500), (2, 40, 1500), (3, 40, 700), (9, 40, 700), (1, 40, 40)])
+def test_matvec_keeps_the_smallest_half_precision_values(t, n, k):
+    """subnormal f16 values of x are values"""
+    rng = np.random.default_rng(31 + t)
+    w = Weights(rng, (), n, k, 32, True)
+    x, gx = rounded(rng.standard_normal((t, k)) * 2.0 ** -20, "f16")
+    assert np.abs(x).max() < 2.0 ** -14
+    close(oz.w4_matvec(w.gpu, gx, out=torch.empty((t, n), device="cuda")), x @ w.w.T, w.depth * U * (np.abs(x) @ w.size.T), "f32")
+
+
+@pytest.mark.parametrize("x_type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("k,group", [(1024, 64), (1100, 32), (2048, 128), (2050, 128), (5000, 64), (16384, 1024), (16390, 128)])
+@pytest.mark.parametrize("t", [1, 2, 3, 6])
+def test_matvec_at_the_ends_of_its_kernels_ranges(x_type, k, group, t):
+    rng = np.random.default_rng(k + t)
+    n = 37
+    w = Weights(rng, (), n, k, group, k % 4 == 0, x_type)
+    x, gx = rounded(rng.standard_normal((t, k)), x_type)
+    close(oz.w4_matvec(w.gpu, gx, out=torch.empty((t, n), device="cuda")), x @ w.w.T, w.depth * U * (np.abs(x) @ w.size.T), "f32")
+
+
+@pytest.mark.parametrize("t", [1, 2, 4, 16])
+def test_matvec_of_many_rows(t):
+    """more rows than one round of the workgroups takes, and a last batch that is not whole"""
+    rng = np.random.default_rng(32 + t)
+    n, k = 60001, 1056
+    codes = torch.from_numpy(rng.integers(0, 256, (n, k // 2), dtype=np.uint8)).cuda()
+    scales = torch.rand((n, k // 32), device="cuda", generator=torch.Generator("cuda").manual_seed(1)) + 0.5
+    x, gx = rounded(rng.standard_normal((t, k)), "bf16")
+    y = oz.w4_matvec(oz.W4Matrix(codes, scales, group=32), gx, out=torch.empty((t, n), device="cuda"))
+    q = torch.stack((codes & 15, codes >> 4), dim=-1).flatten(1).double() - 8
+    w = q * scales.double().repeat_interleave(32, dim=1)
+    tol = (2 * 32 + 33 + 32) * U * (gx.double().abs() @ (scales.double() * 40).repeat_interleave(32, dim=1).t()) + 1e-30
+    assert bool(((y.double() - gx.double() @ w.t()).abs() <= tol * (1 + U)).all())
+
+
+def test_matvec_vectors_do_not_touch_each_other():
+    """what one vector holds changes no bit of another's result"""
+    rng = np.random.default_rng(33)
+    for t, n, k in [(2, 50, 1500), (4, 50, 700), (11, 50, 900), (20, 50, 300)]:
+        w = Weights(rng, (), n, k, 64, True)
+        x, gx = rounded(rng.standard_normal((t, k)), "f32")
+        clean = oz.w4_matvec(w.gpu, gx)
+        gx[1, [0, k - 1]] = torch.tensor([float("inf"), float("nan")], device="cuda")
+        got = oz.w4_matvec(w.gpu, gx)
+        keep = [i for i in range(t) if i != 1]
+        assert torch.equal(got[keep], clean[keep]) and bool(got[1].isnan().all())
+
+
+def test_matvec_with_a_scale_that_is_not_finite():
+    rng = np.random.default_rng(34)
+    for t, k in [(1, 1300), (3, 650), (1, 30)]:
+        w = Weights(rng, (), 40, k, 32, False)
+        w.gpu.scales[7, 0] = float("inf")
+        w.gpu.scales[11, -1] = float("nan")
+        x, gx = rounded(rng.standard_normal((t, k)) + 3, "bf16")
+        y = oz.w4_matvec(w.gpu, gx, out=torch.empty((t, 40), device="cuda"))
+        bad = torch.zeros(40, dtype=torch.bool, device="cuda")
+        bad[[7, 11]] = True
+        assert not bool(y[:, bad].isfinite().any()) and bool(y[:, ~bad].isfinite().all())
+
+
 def test_matvec_beyond_32_bits_of_offset():
     """rows, and vectors, more than 2^32 bytes apart"""
     rng = np.random.default_rng(7)
@@ -346,6 +408,22 @@ MOE = [  # t, experts, top_k, d, f, group, x, result, more
 ]
 
 
+MOE += [  # loads from below a half to many tokens an expert, one span and several, chunks of x that LDS holds in pieces
+    (8, 64, 2, 1400, 1100, 64, "f16", "f32", dict(scales="f16", zeros=False)),
+    (4, 32, 4, 2100, 700, 32, "bf16", "f32", {}),
+    (9, 9, 1, 1100, 2200, 128, "f32", "f32", dict(zeros=False)),
+    (12, 8, 2, 640, 512, 32, "bf16", "f32", dict(scales="bf16", zeros=False)),
+    (31, 4, 3, 1030, 520, 64, "f32", "f32", {}),
+    (32, 4, 4, 4200, 300, 128, "bf16", "f32", dict(scales="bf16")),
+    (24, 3, 2, 300, 4100, 128, "f16", "f32", {}),
+    (35, 2, 2, 3000, 96, 32, "f32", "f32", dict(activation="gelu")),
+    (1, 5, 2, 33, 8192, 32, "bf16", "f32", {}),
+    (2, 4, 2, 8200, 40, 128, "bf16", "f32", {}),
+    (3, 4, 3, 31, 100, 32, "f32", "f32", {}),
+    (3, 4, 3, 100, 31, 32, "f32", "f32", {}),
+]
+
+
 @pytest.mark.parametrize("case", MOE, ids=lambda c: "-".join(map(str, c[:8])) + "-".join(c[8]))
 def test_moe(case):
     t, experts, top_k, d, f, group, x_type, y_type, more = case
@@ -436,6 +514,19 @@ def test_moe_with_scores_of_zero_and_nans():
     sigmoid.gpu.router.copy_(torch.from_numpy(r))
     got = call(sigmoid, rounded(np.eye(64)[:1], "f32")[1])
     assert got[2].cpu().tolist() == [[0.0, 0.0]] and bool((got[0] == 0).all())
+
+
+def test_moe_tokens_do_not_touch_each_other():
+    """an infinity in one token, however many share its experts, changes no bit of the others' results"""
+    rng = np.random.default_rng(35)
+    for t, experts, top_k, d, f in [(5, 40, 2, 130, 90), (6, 4, 2, 300, 200), (30, 3, 2, 260, 150)]:
+        layer = Layer(rng, experts, top_k, d, f)
+        x, gx = tokens(rng, layer, t, "f32")
+        clean = [v.clone() for v in call(layer, gx)]
+        gx[2, 5] = float("inf")
+        got = call(layer, gx)
+        keep = [i for i in range(t) if i != 2]
+        assert all(torch.equal(a[keep], b[keep]) for a, b in zip(got, clean)) and not bool(got[0][2].isfinite().any())
 
 
 def test_moe_with_gaps_and_another_stream_and_small_pieces():
