@@ -29,10 +29,12 @@ __device__ __forceinline__ void w4_each(F f) {
   }
 }
 
-struct __attribute__((packed, aligned(1))) W4Bytes16 { unsigned v[4]; };
-struct __attribute__((packed, aligned(1))) W4Bytes8 { unsigned v[2]; };
-struct __attribute__((packed, aligned(1))) W4Bytes4 { unsigned v; };
-struct __attribute__((packed, aligned(1))) W4Bytes2 { unsigned short v; };
+// threadIdx.x, anew: what follows from it is not kept in registers over the loops around.
+__device__ __forceinline__ int w4_thread() {
+  int i = threadIdx.x;
+  asm volatile("" : "+v"(i));
+  return i;
+}
 
 constexpr int kW4Block = 128;  // inner indexes that a wave takes at a time: 16 bytes of codes a lane
 constexpr float kW4Offset = 16.f;
@@ -95,7 +97,7 @@ template <int ST>
 __device__ __forceinline__ W4Lane w4_lane(const W4Rows& w, int64_t row) {
   row = row < w.n ? row : w.n - 1;  // rows past the end read the last one; nothing is stored of them
   W4Lane l;
-  l.codes = w.codes + row * w.ld_codes + (threadIdx.x % 64 / 16) * 16;
+  l.codes = w.codes + row * w.ld_codes + w4_thread() % 64 / 16 * 16;
   l.scales = w.scales + row * w.ld_scales * (ST == OZ2_F32 ? 4 : 2);
   l.zeros = w.zeros + row * w.ld_zeros;
   return l;
@@ -108,32 +110,20 @@ __device__ __forceinline__ int w4_group(const W4Rows& w, int b) {
   return (int)(__umulhi((unsigned)b, w.recip) + ((unsigned)b & w.keep));
 }
 
-// Whole block b of the row: 16 bytes of codes for this lane, the scales and zero points of its segments (a group, or 128 of one).
-template <int SPB, int ST, bool ZEROS>
-__device__ __forceinline__ W4Regs<SPB, ST> w4_fetch(const W4Rows& w, const W4Lane& l, int b) {
-  W4Regs<SPB, ST> r;
-  const W4Bytes16 c = *reinterpret_cast<const W4Bytes16*>(l.codes + (int64_t)b * (kW4Block / 2));
-  r.q = w4_u4{c.v[0], c.v[1], c.v[2], c.v[3]};
-  const int g = w4_group<SPB>(w, b);
-  r.s = w4_bytes<SPB * (ST == OZ2_F32 ? 4 : 2)>(l.scales + (int64_t)g * (ST == OZ2_F32 ? 4 : 2));
-  if constexpr (ZEROS) r.z = w4_bytes<SPB>(l.zeros + g);
-  return r;
-}
-
 // The block behind the whole ones, of rows of at least 16 bytes.  A lane whose bytes are not all there loads the sixteen that end with the
 // row, and cuts off later what came early; codes past the end may be anything, since x is 0 there.
 template <int SPB, int ST, bool ZEROS>
 __device__ __forceinline__ W4Tail<SPB> w4_fetch_tail(const W4Rows& w, const W4Lane& l) {
   W4Tail<SPB> r;
-  const int left = w.bytes - w.full * (kW4Block / 2) - threadIdx.x % 64 / 16 * 16;  // bytes from the lane's first on
+  const int quarter = w4_thread() % 64 / 16;
+  const int left = w.bytes - w.full * (kW4Block / 2) - quarter * 16;  // bytes from the lane's first on
   r.cut = left >= 16 || left <= 0 ? 0 : 16 - left;
-  const W4Bytes16 c = *reinterpret_cast<const W4Bytes16*>(left > 0 ? l.codes + (int64_t)w.full * (kW4Block / 2) - r.cut : l.codes - threadIdx.x % 64 / 16 * 16);
-  r.q = w4_u4{c.v[0], c.v[1], c.v[2], c.v[3]};
+  r.q = w4_bytes<16>(left > 0 ? l.codes + (int64_t)w.full * (kW4Block / 2) - r.cut : l.codes - quarter * 16);
   const int g = w4_group<SPB>(w, w.full);
   w4_each<SPB>([&](auto i) __attribute__((always_inline)) {
     const int at = min(g + i.value, w.groups - 1);
-    if constexpr (ST == OZ2_F32) r.s[i.value] = reinterpret_cast<const W4Bytes4*>(l.scales + (int64_t)at * 4)->v;
-    else r.s[i.value] = reinterpret_cast<const W4Bytes2*>(l.scales + (int64_t)at * 2)->v;
+    if constexpr (ST == OZ2_F32) r.s[i.value] = w4_bytes<4>(l.scales + (int64_t)at * 4);
+    else r.s[i.value] = w4_bytes<2>(l.scales + (int64_t)at * 2);
     if constexpr (ZEROS) r.z[i.value] = l.zeros[at];
     else r.z[i.value] = 8u;
   });
@@ -220,14 +210,10 @@ __device__ __forceinline__ int w4_inner(int j, int quarter) {
 // x in LDS.  A token's values lie in rows of `pitch` bytes for each of its parts, eight at a time in the order of w4_unpack's pairs.  Row a of the
 // matrix cores' tile is token a / 4 + 4 (a % 4), so that with few tokens only the first result registers of a lane count (RT: 1 or 4
 // for up to 4 or 16 tokens).
-// Where row a of the tile reads from: its token, or, for rows without one, whose results nobody looks at, what lies 16 bytes further for each.  The sixteen
-// rows of a quarter then read from sixteen places of the banks; when they read a token's place together, a read takes ten times as long
-// (1 KiB in about 60 cycles).  Nothing is read past kW4Slack bytes behind the last token.
-constexpr int kW4Slack = 16 * 16 * 3;
+// Row a without a token reads the last one's, and nobody looks at its results.  (The rows of a quarter that read one place together cost nothing.)
 template <int PARTS>
 __device__ __forceinline__ int w4_row_of_x(int a, int tokens, int pitch) {
-  const int t = a / 4 + 4 * (a % 4), last = tokens - 1;
-  return t < tokens ? t * PARTS * pitch : last * PARTS * pitch + (t - last) * PARTS * 16;
+  return min(a / 4 + 4 * (a % 4), tokens - 1) * PARTS * pitch;
 }
 
 // Value of the lane across in a pair, four, eight or sixteen lanes whose halves hold one value each (a pair: its two lanes).

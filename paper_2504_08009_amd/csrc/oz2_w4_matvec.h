@@ -23,9 +23,6 @@ int oz2_w4_compute_units();
 #ifdef __HIPCC__
 namespace {
 
-#ifndef W4_TILE_WAVES
-#define W4_TILE_WAVES 1
-#endif
 constexpr int kWaves = 8;
 constexpr int kLds = 156 * 1024;
 
@@ -36,7 +33,7 @@ struct Cut {
 };
 
 template <int XT, int SPB, int RT, bool WIDE, bool ZEROS>
-__global__ void __launch_bounds__(64 * kWaves, W4_TILE_WAVES) w4_tile_kernel(W4Rows w, int scale_type, Cut cut, int t, float alpha, const char* x, int64_t ldx, float beta,
+__global__ void __launch_bounds__(64 * kWaves) w4_tile_kernel(W4Rows w, int scale_type, Cut cut, int t, float alpha, const char* x, int64_t ldx, float beta,
                                                               const void* c, int64_t ldc, int y_type, void* y, int64_t ldy) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
@@ -194,7 +191,7 @@ hipError_t launch_tile(const W4Call& a) {
   auto lay = [&](int chunk) {
     cut.chunk = chunk;
     cut.pitch = chunk * kW4Block * 2 + 16;
-    cut.reduce_at = tokens * P * cut.pitch + kW4Slack;
+    cut.reduce_at = tokens * P * cut.pitch;
     return cut.reduce_at + (cut.split_log ? kWaves * 2 * RT * 64 * 4 : 0);
   };
   int lds = lay(blocks);

@@ -79,9 +79,9 @@ __device__ __forceinline__ W4Rows w4_of_stack(W4Rows w, int64_t e, int64_t codes
 // Rows of experts times the places that chose them.  A batch is four loads of rows for each `1 << split_log` waves, `loads` of which (4, or 2 beside 2 of a second matrix) are of one matrix.
 // row(expert's matrices, row, i): the i-th load of the batch from that row; x(place): vector; out(place, row, sums): called by one
 // thread with the sums of the batch's 4 FOLD rows.
-template <int XT, int T, int ST, bool ZEROS, int FOLD, class Matrix, class Row, class X, class Out>
+template <int XT, int ST, bool ZEROS, int FOLD, class Matrix, class Row, class X, class Out>
 __device__ __forceinline__ void moe_products(const Chosen& chosen, int k, int rows, int loads, int split_log, const W4Rows& shape,
-                                             float (*part)[kMoeRounds][kMoeWaves][4 * FOLD][T], Matrix matrix, Row row_of, X vector, Out out) {
+                                             float (*part)[kMoeRounds][kMoeWaves][4 * FOLD], Matrix matrix, Row row_of, X vector, Out out) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   const int split = 1 << split_log, s = wave & (split - 1), group = wave >> split_log, per = kMoeWaves >> split_log;
   const int unit = FOLD == 2 ? lane % 32 : s * 64 + lane, rows_of_batch = loads * FOLD;
@@ -100,37 +100,33 @@ __device__ __forceinline__ void moe_products(const Chosen& chosen, int k, int ro
       const int row = ((b + i) * per + group) * rows_of_batch;
       return [&, row](int j) { return row_of(m, row, j); };
     };
-    for (int p = 0; p < places; p += T) {
-      auto x_at = [&](int t) { return vector(uniform(chosen.place[first + min(p + t, places - 1)])); };
-      W4Rows4<XT, T, ST, ZEROS, FOLD> r;
+    for (int p = 0; p < places; ++p) {
+      auto x_at = [&](int) { return vector(uniform(chosen.place[first + p])); };
+      W4Rows4<XT, 1, ST, ZEROS, FOLD> r;
       r.fetch(rows_at(0), at);
-      W4X<XT> kept[T];
-      const unsigned plain = w4_take_x<XT, T>(k, unit, x_at, kept);
+      W4X<XT> kept[1];
+      const unsigned plain = w4_take_x<XT, 1>(k, unit, x_at, kept);
       for (int i = 0; i < turns; ++i) {
-        float sum[4][T];
+        float sum[4][1];
         r.multiply(at, kept, ragged, sum);
         if (plain) r.multiply_plain(plain, k, shape.group, rows_at(i), x_at, unit, sum);
         if (i + 1 < turns) r.fetch(rows_at(i + 1), at);
+        float v[FOLD];
+        w4_sum4<FOLD>(sum[0][0], sum[1][0], sum[2][0], sum[3][0], v);
+        if (lane % 16 == 0)
 #pragma unroll
-        for (int t = 0; t < T; ++t) {
-          float v[FOLD];
-          w4_sum4<FOLD>(sum[0][t], sum[1][t], sum[2][t], sum[3][t], v);
-          if (lane % 16 == 0)
-#pragma unroll
-            for (int j = 0; j < FOLD; ++j) part[flip][i][wave][w4_row_of_lane<FOLD>(j)][t] = v[j];
-        }
+          for (int j = 0; j < FOLD; ++j) part[flip][i][wave][w4_row_of_lane<FOLD>(j)] = v[j];
       }
       __syncthreads();
-      for (int j = threadIdx.x; j < turns * per * T; j += 64 * kMoeWaves) {
-        const int t = j % T, g = j / T % per, i = j / T / per;
-        if (p + t >= places) continue;
+      for (int j = threadIdx.x; j < turns * per; j += 64 * kMoeWaves) {
+        const int g = j % per, i = j / per;
         float v[4 * FOLD];
 #pragma unroll
-        for (int n = 0; n < 4 * FOLD; ++n) v[n] = part[flip][i][g * split][n][t];
+        for (int n = 0; n < 4 * FOLD; ++n) v[n] = part[flip][i][g * split][n];
         for (int q = 1; q < split; ++q)
 #pragma unroll
-          for (int n = 0; n < 4 * FOLD; ++n) v[n] += part[flip][i][g * split + q][n][t];
-        out(chosen.place[first + p + t], ((b + i) * per + g) * rows_of_batch, v);
+          for (int n = 0; n < 4 * FOLD; ++n) v[n] += part[flip][i][g * split + q][n];
+        out(chosen.place[first + p], ((b + i) * per + g) * rows_of_batch, v);
       }
       flip ^= 1;
     }
@@ -140,14 +136,17 @@ __device__ __forceinline__ void moe_products(const Chosen& chosen, int k, int ro
 // The same on the matrix cores: a wave takes two tiles of sixteen rows, of one matrix or of two, for up to 4 RT places at a time, a workgroup
 // rows_of_wave rows for each of its waves.  tile(expert's matrices, t): the matrix of tile t; row(first, t): its first row; out(place, row, sum0,
 // sum1): called by the lane that has the sums of row `row` of either tile.
-// x of a workgroup, so that three fit a compute unit.  It holds a run of blocks of 16 vectors in 16 bits, or of 12 in FP32.
-constexpr int kMoeLds = 44 * 1024;
-static_assert(kMoeLds - kW4Slack >= 12 * 3 * (kW4Run * kW4Block * 2 + 16) && kMoeLds - kW4Slack >= 16 * (kW4Run * kW4Block * 2 + 16), "a run");
+// Three workgroups fit a compute unit by their registers, and x of each, so that they fit by LDS too (two: 16 tokens through 6 of 64 experts of
+// 2048 x 1408 take 104 in the place of 86 us; four of them, with up to 4 vectors, 91).  It holds a run of blocks at least.
+constexpr int kMoeFit = 3, kMoeLds = 44 * 1024;
+template <int XT, int RT>
+constexpr int moe_most() { return RT == 4 && w4_parts<XT>() == 3 ? 12 : 4 * RT; }  // places at a time
+static_assert(kMoeLds >= 12 * 3 * (kW4Run * kW4Block * 2 + 16) && kMoeLds >= 16 * (kW4Run * kW4Block * 2 + 16), "a run");
 
 template <int XT, int SPB, int RT, bool WIDE, bool ZEROS, class Matrix, class Tile, class First, class X, class Out>
 __device__ __forceinline__ void moe_tiles(const Chosen& chosen, int k, int rows, int rows_of_wave, int scale_type, char* lds, Matrix matrix, Tile tile, First first_row,
                                           X vector, Out out) {
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
   const int count = uniform(chosen.count), blocks = (k + kW4Block - 1) / kW4Block, full = k / kW4Block;
   const int groups = (rows + rows_of_wave * kMoeWaves - 1) / (rows_of_wave * kMoeWaves);
@@ -158,15 +157,15 @@ __device__ __forceinline__ void moe_tiles(const Chosen& chosen, int k, int rows,
     const int first = uniform(chosen.first[a]), places = uniform(chosen.first[a + 1]) - first;
     const auto m = matrix((int64_t)uniform(chosen.expert[a]));
     const W4Rows w[2] = {tile(m, 0), tile(m, 1)};
-    constexpr int most = RT == 4 && w4_parts<XT>() == 3 ? 12 : 4 * RT;
+    constexpr int most = moe_most<XT, RT>();
     for (int p = 0; p < places; p += most) {
       const int tokens = min(most, places - p);
       auto x_of = [&](int t) { return vector(uniform(chosen.place[first + p + t])); };
       // blocks of x at a time: all, or runs that fit
-      int chunk = min(blocks, ((kMoeLds - kW4Slack) / (tokens * w4_parts<XT>()) - 16) / (kW4Block * 2));
+      int chunk = min(blocks, (kMoeLds / (tokens * w4_parts<XT>()) - 16) / (kW4Block * 2));
       if (chunk < blocks) chunk = chunk / kW4Run * kW4Run;
       const int chunks = (blocks + chunk - 1) / chunk, pitch = chunk * kW4Block * 2 + 16;
-      const char* lane_x = lds + w4_row_of_x<w4_parts<XT>()>(lane % 16, tokens, pitch);
+      const char* lane_x = lds + w4_row_of_x<w4_parts<XT>()>(w4_thread() % 16, tokens, pitch);
       for (int r = 0; r < here; ++r) {
         const int row = ((g + r) * kMoeWaves + wave) * rows_of_wave;  // (past the end: the last rows again, not stored)
         const int at[2] = {min(first_row(row, 0), w[0].n - 1), min(first_row(row, 1), w[1].n - 1)};
@@ -188,6 +187,7 @@ __device__ __forceinline__ void moe_tiles(const Chosen& chosen, int k, int rows,
           two.multiply(w[0], walk, start, ahead, lane_x, pitch, sum);
           if (ragged) two.multiply_tail(w, at, lane_x + (full - start) * kW4Block * 2, pitch, sum);
         }
+        const int lane = w4_thread() % 64;
         bool again = false;
 #pragma unroll
         for (int i = 0; i < RT; ++i) again |= !(fabsf(sum[0][i]) < INFINITY && fabsf(sum[1][i]) < INFINITY) && lane / 16 + 4 * i < tokens;

@@ -1,6 +1,8 @@
 // A layer of gated experts whose weights are held in 4 bits, with its router, for a few tokens (oz2_w4_moe).
 #include "oz2_w4_moe.h"
 
+#include <algorithm>
+
 extern template hipError_t oz2_moe_gate_up<OZ2_F32>(const MoeCall&, const oz2_w4_matrix&);
 extern template hipError_t oz2_moe_gate_up<OZ2_BF16>(const MoeCall&, const oz2_w4_matrix&);
 extern template hipError_t oz2_moe_gate_up<OZ2_F16>(const MoeCall&, const oz2_w4_matrix&);
@@ -204,13 +206,19 @@ hipError_t oz2_launch_w4_moe(const oz2_moe_layer& m, int64_t t, int x_type, cons
     c.weights = weights ? weights + first * m.top_k : reinterpret_cast<float*>(ws + s.weights);
     c.chosen = reinterpret_cast<int*>(ws + s.chosen);
     c.h = reinterpret_cast<float*>(ws + s.h), c.part = reinterpret_cast<float*>(ws + s.part);
-    // More than one token for an expert on the average: the matrix cores.  Of layers of 4096 x 2048 to 2048 x 1024, us without / with them:
-    // load 0.5 (8 tokens, 4 of 60 experts, FP32) 56 / 51, 1 (3 tokens, 3 of 9, 1000 x 777) 33 / 43, 1 (16, 8 of 128) 339 / 343, 1.5 (16, 6 of 64)
-    // 142 / 107, 2 (32, 8 of 128) 657 / 556, 2 (8, 2 of 8) 60 / 78, 4 (32, 8 of 64) 222 / 121, 16 (32, 4 of 8) 307 / 127.
+    // Matrix cores or vector units.  Above two tokens for an expert on the average: the matrix cores, up to 16 (FP32: 12) at a time.  From a half to two, up
+    // to 4 at a time, and only where every compute unit gets a workgroup of either product: a wave that has 32 rows to itself takes long.  Layers
+    // of D x F, us by the vector units / the matrix cores:
+    //   load 0.53 (8 tokens, 4 of 60 experts, 2048 x 1024, FP32) 54 / 49, 0.75 (12, 4 of 64, 2048 x 2048) 96 / 80, 1 (16, 8 of 128, 4096 x 2048)
+    //   339 / 267, 1.5 (16, 6 of 64, 2048 x 1408) 142 / 88, 2 (32, 8 of 128, 4096 x 2048) 657 / 376, 2.9 (23, 2 of 16, 3000 x 1500) 144 / 83,
+    //   4 (32, 8 of 64, 2048 x 1024) 222 / 90, 16 (32, 4 of 8, 4096 x 2048) 307 / 126;
+    //   few workgroups: 1 (2, 2 of 4, 4096 x 2048) 32 / 48, 1 (8, 1 of 8, 1000 x 4096) 34 / 53, 2 (8, 2 of 8, 2048 x 4096) 60 / 76.
     const bool near = w4_tile_fits(c.gate) && w4_tile_fits(c.up) && w4_tile_fits(c.down);
-    c.tiles = !near || c.t * c.top_k <= c.experts ? 1 : c.t * c.top_k <= 2 * c.experts ? 4 : 16;
+    const int places = c.t * c.top_k, of_expert = std::min((c.f + 63) / 64, (c.d + 127) / 128);
+    const bool filled = std::min(places, c.experts) * of_expert >= oz2_w4_compute_units();
+    c.tiles = !near || 2 * places <= c.experts ? 1 : places > 2 * c.experts ? 16 : filled ? 4 : 1;
     // Hardly an expert with two tokens: each token's second products are summed where they are formed.
-    c.direct = c.t == 1 || 2 * c.t * c.top_k <= c.experts;
+    c.direct = c.t == 1 || 2 * places <= c.experts;
     c.st = st;
     // rows of 16 bytes of codes or more, and spans of 2048 for the waves of a workgroup
     if (d < kW4Unit || f < kW4Unit || d > kMoeLongest || f > kMoeLongest) {

@@ -19,9 +19,9 @@ __device__ __forceinline__ W4Rows moe_down_of(const MoeCall& c, int64_t e) {
 template <int ST, bool ZEROS, int FOLD>
 __global__ void __launch_bounds__(64 * kMoeWaves, 4) moe_down_kernel(MoeCall c, int split_log) {
   __shared__ Chosen chosen;
-  __shared__ float part[2][kMoeRounds][kMoeWaves][4 * FOLD][1];
+  __shared__ float part[2][kMoeRounds][kMoeWaves][4 * FOLD];
   moe_chosen(c, chosen);
-  moe_products<OZ2_F32, 1, ST, ZEROS, FOLD>(
+  moe_products<OZ2_F32, ST, ZEROS, FOLD>(
       chosen, c.f, c.d, 4, split_log, c.down, part, [&](int64_t e) { return moe_down_of(c, e); },
       [&](const W4Rows& m, int row, int i) { return w4_row<ST, FOLD>(m, row, i); },
       [&](int place) { return reinterpret_cast<const char*>(c.h + (int64_t)place * c.f); },
@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(64 * kDirectWaves, 4) moe_down_direct_kernel(M
 }
 
 template <int SPB, int RT, bool WIDE, bool ZEROS>
-__global__ void __launch_bounds__(64 * kMoeWaves, 3) moe_down_tiles_kernel(MoeCall c, int scale_type) {
+__global__ void __launch_bounds__(64 * kMoeWaves, kMoeFit) moe_down_tiles_kernel(MoeCall c, int scale_type) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ Chosen chosen;
   moe_chosen(c, chosen);
@@ -118,7 +118,7 @@ void launch_down(const MoeCall& c) {
 }
 template <int SPB, int RT, bool WIDE, bool ZEROS>
 void launch_down_tiles(const MoeCall& c, int scale_type) {
-  hipLaunchKernelGGL((moe_down_tiles_kernel<SPB, RT, WIDE, ZEROS>), dim3(oz2_w4_compute_units() * 3), dim3(64 * kMoeWaves), kMoeLds + kMoeWaves * 2 * 2 * RT * 64 * 4, c.st, c, scale_type);
+  hipLaunchKernelGGL((moe_down_tiles_kernel<SPB, RT, WIDE, ZEROS>), dim3(oz2_w4_compute_units() * kMoeFit), dim3(64 * kMoeWaves), kMoeLds, c.st, c, scale_type);
 }
 template <int SPB, int RT>
 void launch_down_tiles(const MoeCall& c, int scale_type) {

@@ -176,9 +176,9 @@ __global__ void __launch_bounds__(64 * kMoeWaves, 4) moe_up_kernel(MoeCall c, in
   __shared__ short ids[kMoePlaces];
   __shared__ float weights[kMoePlaces];
   __shared__ int count[OZ2_MOE_MAX_EXPERTS];
-  __shared__ float part[2][kMoeRounds][kMoeWaves][4 * FOLD][1];
+  __shared__ float part[2][kMoeRounds][kMoeWaves][4 * FOLD];
   moe_route(c, chosen, ids, weights, count);
-  moe_products<XT, 1, ST, ZEROS, FOLD>(
+  moe_products<XT, ST, ZEROS, FOLD>(
       chosen, c.d, c.f, 2, split_log, c.gate, part, [&](int64_t e) { return moe_gate_up_of(c, e); },
       [&](const GateUp& m, int row, int i) { return w4_row<ST, FOLD>(i < 2 ? m.gate : m.up, row, i % 2); },
       [&](int place) { return c.x + place / c.top_k * c.ldx * (XT == OZ2_F32 ? 4 : 2); },
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(64 * kMoeWaves, 4) moe_up_kernel(MoeCall c, in
 
 // Several, by the matrix cores: a tile of either matrix.
 template <int XT, int SPB, int RT, bool WIDE, bool ZEROS>
-__global__ void __launch_bounds__(64 * kMoeWaves, 3) moe_up_tiles_kernel(MoeCall c, int scale_type) {
+__global__ void __launch_bounds__(64 * kMoeWaves, kMoeFit) moe_up_tiles_kernel(MoeCall c, int scale_type) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ Chosen chosen;
   {  // (the choice is done with its own arrays before x is brought in)
@@ -223,7 +223,7 @@ hipError_t launch_up(const MoeCall& c) {
 
 template <int XT, int SPB, int RT, bool WIDE, bool ZEROS>
 hipError_t launch_up_tiles(const MoeCall& c, int scale_type) {
-  hipLaunchKernelGGL((moe_up_tiles_kernel<XT, SPB, RT, WIDE, ZEROS>), dim3(oz2_w4_compute_units() * 3), dim3(64 * kMoeWaves), kMoeLds + kMoeWaves * 2 * 2 * RT * 64 * 4, c.st, c, scale_type);
+  hipLaunchKernelGGL((moe_up_tiles_kernel<XT, SPB, RT, WIDE, ZEROS>), dim3(oz2_w4_compute_units() * kMoeFit), dim3(64 * kMoeWaves), kMoeLds, c.st, c, scale_type);
   return hipGetLastError();
 }
 template <int XT, int SPB, int RT>

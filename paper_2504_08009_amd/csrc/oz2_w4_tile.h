@@ -3,8 +3,8 @@
 //
 // Four neighbouring lanes load 64 bytes of a row, eight of them two lines' worth of two blocks; where each lane loads from a row of its own, as the matrix
 // cores want their operand, the vector cache is asked 64 times for a load and sets the pace.  The words then change lanes and
-// registers: inside four lanes by selecting from the neighbour's, across sixteen and 32 by swapping registers' halves.  (Through LDS, with
-// ds_bpermute, a KiB of codes took 165 cycles of it, four times what the memory takes to bring it.)
+// registers: inside four lanes by selecting from the neighbour's, across sixteen and 32 by swapping registers' halves, so that LDS
+// is left to x.
 #ifndef OZ2_W4_TILE_H
 #define OZ2_W4_TILE_H
 
@@ -37,7 +37,7 @@ struct W4Two {
   int half;     // whether 16-bit scales are f16
 
   __device__ __forceinline__ void init(const W4Rows (&w)[2], const int (&row)[2], int scale_type) {
-    const int lane = threadIdx.x % 64, t = lane / 16 % 2;
+    const int lane = w4_thread() % 64, t = lane / 16 % 2;
     half = scale_type == OZ2_F16;
     const W4Rows& m = w[0];  // (both are alike but for their addresses)
     const int n = m.n - 1, first = min((t ? row[1] : row[0]) + lane / 4 % 4 * 4, n), mine = min((t ? row[1] : row[0]) + lane % 16, n);
@@ -200,7 +200,7 @@ struct W4Two {
     W4Tail<SPB> r[2];
     w4_u4 q[2];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) r[t] = w4_fetch_tail<SPB, ST, ZEROS>(w[t], w4_lane<ST>(w[t], row[t] + threadIdx.x % 16));
+    for (int t = 0; t < 2; ++t) r[t] = w4_fetch_tail<SPB, ST, ZEROS>(w[t], w4_lane<ST>(w[t], row[t] + w4_thread() % 16));
 #pragma unroll
     for (int t = 0; t < 2; ++t) q[t] = w4_exchange<SPB>(w4_cut(r[t].q, r[t].cut));
     const int g = w4_group<SPB>(w[0], w[0].full);
@@ -220,7 +220,7 @@ struct W4Two {
     const int end = min(w[0].k, (b + 1) * kW4Block);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const W4Lane l = w4_lane<WIDE ? OZ2_F32 : OZ2_BF16>(w[t], row[t] + threadIdx.x % 16);
+      const W4Lane l = w4_lane<WIDE ? OZ2_F32 : OZ2_BF16>(w[t], row[t] + w4_thread() % 16);
       const uint8_t* code = l.codes - threadIdx.x % 64 / 16 * 16;
 #pragma unroll 1
       for (int i = b * kW4Block; i < end; ++i) {
@@ -240,7 +240,7 @@ template <int XT, class X>
 __device__ __forceinline__ void w4_stage(X vector, int tokens, int k, int start, int length, char* lds, int pitch, int threads) {
   constexpr int PIECES = XT == OZ2_F32 ? 4 : 8, P = w4_parts<XT>(), size = XT == OZ2_F32 ? 4 : 2, per = 16 / size;  // 128 bytes of a thread in flight
 #pragma unroll 1
-  for (int e = threadIdx.x; e < length * (kW4Block / 8); e += threads) {
+  for (int e = w4_thread(); e < length * (kW4Block / 8); e += threads) {
     const int at = start * kW4Block + e * 8;
 #pragma unroll 1
     for (int t = 0; t < tokens; t += PIECES) {
