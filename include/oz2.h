@@ -421,7 +421,8 @@ int oz2_w4_matvec(const oz2_w4_matrix* W, int64_t t, float alpha, int x_type, co
  *   chosen  the top_k experts with the largest keys, in that order, equal keys by the lower index; a key of -infinity is never
  *           chosen, so a token may have fewer; a NaN counts as the largest, and so reaches y
  *   weights p of the chosen, divided by their sum where `renormalize` is set (all 0 if that is 0), times factor
- *   y = sum over the chosen, in order, of  weight * down_e (act(gate_e x) * (up_e x)),   act = silu or gelu (with erf)
+ *   y = sum over the chosen of  weight * down_e (act(gate_e x) * (up_e x)),   act = silu or gelu (with erf), in an order that depends
+ *           on the sizes alone
  * gate and up are stacks of f x d, down of d x f; gate and up are alike in group, type of the scales and whether they have zero points.
  * The inner vectors of f values are kept in FP32. */
 #define OZ2_SCORE_SOFTMAX 0

@@ -33,43 +33,46 @@ __global__ void __launch_bounds__(64 * kMoeWaves, 4) moe_down_kernel(MoeCall c, 
       });
 }
 
-// A batch of rows for all places of a token, and their sum.  Groups of `1 << split_log` waves take every per-th place each: eight waves, so that
-// most tokens' places are all in flight.
+// BATCHES batches of rows for all places of a token, and their sums.  Groups of `1 << split_log` waves take every per-th place each: eight waves, so that
+// most tokens' places are all in flight.  A lane brings 128 bytes of h for the 64 of codes in a batch's four loads: two batches where there are still four
+// workgroups a compute unit: 4 tokens through 6 of 64 experts of 4096 x 1024 in half precision 60 -> 55 us, 8 through 4 of 128 of 2048 x 2048 85 -> 75.
 constexpr int kDirectWaves = 8;
-template <int ST, bool ZEROS, int FOLD>
+template <int ST, bool ZEROS, int FOLD, int BATCHES>
 __global__ void __launch_bounds__(64 * kDirectWaves, 4) moe_down_direct_kernel(MoeCall c, int split_log) {
-  __shared__ float part[kDirectWaves][4 * FOLD];
+  constexpr int ROWS = 4 * FOLD;
+  __shared__ float part[kDirectWaves][BATCHES * ROWS];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, token = blockIdx.y;
   const int split = 1 << split_log, group = wave >> split_log, per = kDirectWaves >> split_log;
-  const int unit = FOLD == 2 ? lane % 32 : (wave & (split - 1)) * 64 + lane, row = blockIdx.x * 4 * FOLD;
+  const int unit = FOLD == 2 ? lane % 32 : (wave & (split - 1)) * 64 + lane, row = blockIdx.x * BATCHES * ROWS;
   const W4Place at = w4_place(c.down, unit);
   const bool ragged = __ballot(at.cut != 0) != 0;
-  float mine[FOLD];
+  float mine[BATCHES][FOLD];
 #pragma unroll
-  for (int i = 0; i < FOLD; ++i) mine[i] = 0.f;
+  for (int i = 0; i < BATCHES * FOLD; ++i) mine[i / FOLD][i % FOLD] = 0.f;
   for (int j = group; j < c.top_k; j += per) {
     const int place = token * c.top_k + j, e = __builtin_amdgcn_readfirstlane(c.ids[place]);
     if (e < 0) break;  // (and so are those behind)
     const float weight = c.weights[place];
     const W4Rows m = moe_down_of(c, e);
-    auto row_of = [&](int i) { return w4_row<ST, FOLD>(m, row, i); };
     auto vector = [&](int) { return reinterpret_cast<const char*>(c.h + (int64_t)place * c.f); };
-    W4Rows4<OZ2_F32, 1, ST, ZEROS, FOLD> r;
-    r.fetch(row_of, at);
+    W4Rows4<OZ2_F32, 1, ST, ZEROS, FOLD> r[BATCHES];
+    w4_each<BATCHES>([&](auto b) __attribute__((always_inline)) { r[b.value].fetch([&](int i) { return w4_row<ST, FOLD>(m, row + b.value * ROWS, i); }, at); });
     W4X<OZ2_F32> kept[1];
-    float sum[4][1], v[FOLD];
     const unsigned plain = w4_take_x<OZ2_F32, 1>(c.f, unit, vector, kept);
-    r.multiply(at, kept, ragged, sum);
-    if (plain) r.multiply_plain(plain, c.f, c.down.group, row_of, vector, unit, sum);
-    w4_sum4<FOLD>(sum[0][0], sum[1][0], sum[2][0], sum[3][0], v);
+    w4_each<BATCHES>([&](auto b) __attribute__((always_inline)) {
+      float sum[4][1], v[FOLD];
+      r[b.value].multiply(at, kept, ragged, sum);
+      if (plain) r[b.value].multiply_plain(plain, c.f, c.down.group, [&](int i) { return w4_row<ST, FOLD>(m, row + b.value * ROWS, i); }, vector, unit, sum);
+      w4_sum4<FOLD>(sum[0][0], sum[1][0], sum[2][0], sum[3][0], v);
 #pragma unroll
-    for (int i = 0; i < FOLD; ++i) mine[i] = fmaf(weight, v[i], mine[i]);
+      for (int i = 0; i < FOLD; ++i) mine[b.value][i] = fmaf(weight, v[i], mine[b.value][i]);
+    });
   }
   if (lane % 16 == 0)
 #pragma unroll
-    for (int i = 0; i < FOLD; ++i) part[wave][w4_row_of_lane<FOLD>(i)] = mine[i];
+    for (int i = 0; i < BATCHES * FOLD; ++i) part[wave][i / FOLD * ROWS + w4_row_of_lane<FOLD>(i % FOLD)] = mine[i / FOLD][i % FOLD];
   __syncthreads();
-  if (threadIdx.x >= 4 * FOLD || row + (int)threadIdx.x >= c.d) return;
+  if (threadIdx.x >= BATCHES * ROWS || row + (int)threadIdx.x >= c.d) return;
   float v = 0.f;
 #pragma unroll
   for (int q = 0; q < kDirectWaves; ++q) v += part[q][threadIdx.x];
@@ -102,10 +105,16 @@ __global__ void __launch_bounds__(256) moe_sum_kernel(MoeCall c) {
   w4_store(c.y_type, c.y, t * c.ldy + i, v);
 }
 
+template <int ST, bool ZEROS, int FOLD, int BATCHES>
+void launch_direct(const MoeCall& c, int split) {
+  constexpr int rows = BATCHES * 4 * FOLD;
+  hipLaunchKernelGGL((moe_down_direct_kernel<ST, ZEROS, FOLD, BATCHES>), dim3((c.d + rows - 1) / rows, c.t), dim3(64 * kDirectWaves), 0, c.st, c, split);
+}
 template <int ST, bool ZEROS, int FOLD>
 void launch_down(const MoeCall& c, int split) {
-  if (c.direct) hipLaunchKernelGGL((moe_down_direct_kernel<ST, ZEROS, FOLD>), dim3((c.d + 4 * FOLD - 1) / (4 * FOLD), c.t), dim3(64 * kDirectWaves), 0, c.st, c, split);
-  else hipLaunchKernelGGL((moe_down_kernel<ST, ZEROS, FOLD>), dim3(oz2_w4_compute_units() * 4), dim3(64 * kMoeWaves), 0, c.st, c, split);
+  if (!c.direct) hipLaunchKernelGGL((moe_down_kernel<ST, ZEROS, FOLD>), dim3(oz2_w4_compute_units() * 4), dim3(64 * kMoeWaves), 0, c.st, c, split);
+  else if ((int64_t)c.d * c.t < (int64_t)oz2_w4_compute_units() * 4 * 8 * FOLD) launch_direct<ST, ZEROS, FOLD, 1>(c, split);
+  else launch_direct<ST, ZEROS, FOLD, 2>(c, split);
 }
 template <int ST, bool ZEROS>
 void launch_down(const MoeCall& c) {

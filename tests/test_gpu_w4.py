@@ -421,6 +421,9 @@ MOE += [  # loads from below a half to many tokens an expert, one span and sever
     (2, 4, 2, 8200, 40, 128, "bf16", "f32", {}),
     (3, 4, 3, 31, 100, 32, "f32", "f32", {}),
     (3, 4, 3, 100, 31, 32, "f32", "f32", {}),
+    (3, 13, 2, 5555, 100, 32, "f32", "f32", {}),
+    (2, 5, 1, 4101, 1030, 64, "bf16", "f32", dict(scales="bf16", zeros=False)),
+    (1, 3, 3, 8192, 1030, 128, "f16", "f32", {}),
 ]
 
 
