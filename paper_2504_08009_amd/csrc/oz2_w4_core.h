@@ -1,11 +1,11 @@
-// What the products with weights held in 4 bits share: sixteen rows of a matrix times up to sixteen vectors, by one wave.
+// What the products with weights held in 4 bits share: how a matrix looks to a launch, how codes become operands, the ends of rows.
 //
-// A group's sum of (q - z) x is formed on the matrix cores.  A code is put into the upper mantissa bits of a 16-bit float whose exponent
-// makes it 16 + q exactly (one shift, one and-or for two codes; q in the lower bits would be 128 + q, which cancels three more bits), x
-// is taken as it is (bf16, f16) or as the three bf16 values that make it up exactly (f32), and
-//   sum (q - z) x = sum (16 + q) x - (16 + z) sum x
-// with the sums of x per group formed once, where x is brought into LDS.  Products of these are exact in FP32, in which everything is summed.
-// The scale multiplies a group's sum, so that nothing is rounded to 16 bits before the result.
+// A group's sum of (q - z) x is formed from 16-bit floats.  A code is put into the upper mantissa bits of one whose exponent makes it 16 + q
+// exactly (one shift, one and-or for two codes; q in the lower bits would be 128 + q, which cancels three more bits), x is taken as it is
+// (bf16, f16) or as the three bf16 values that make it up exactly (f32), and
+//   sum (q - z) x = sum (16 + q) x - (16 + z) sum x.
+// Products of these are exact in FP32, in which everything is summed.  The scale multiplies a group's sum, so that nothing is rounded to
+// 16 bits before the result.
 #ifndef OZ2_W4_CORE_H
 #define OZ2_W4_CORE_H
 
