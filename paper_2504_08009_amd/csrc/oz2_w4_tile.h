@@ -74,7 +74,8 @@ struct W4Two {
     return half ? h : b;
   }
   // Register j of lane i for register i of lane j, of every four lanes: two exchanges, of which each result is one instruction, the lane's own
-  // value or its neighbour's by a mask.  (The waits are those between a vector instruction and one that reads its result from another lane.)
+  // value or its neighbour's by a mask.  The waits are those between a vector instruction and one that reads its result from another lane: before
+  // the first, for what the compiler puts ahead, and behind the last, for what it puts there (it counts nothing in here as such a writer).
   static __device__ __forceinline__ void turn_four(unsigned& a, unsigned& b, unsigned& c, unsigned& d) {
     unsigned p, q, r, s;
     asm("s_nop 1\n\t"
@@ -90,6 +91,7 @@ struct W4Two {
         "s_not_b64 vcc, vcc\n\t"
         "v_cndmask_b32_dpp %4, %2, %0, vcc quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf\n\t"
         "v_cndmask_b32_dpp %5, %3, %1, vcc quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf\n\t"
+        "s_nop 1\n\t"
         : "=&v"(p), "=&v"(q), "=&v"(r), "=&v"(s), "+v"(a), "+v"(b), "+v"(c), "+v"(d)
         : "s"(0xAAAAAAAAAAAAAAAAull), "s"(0xCCCCCCCCCCCCCCCCull)
         : "vcc", "scc");
