@@ -160,7 +160,8 @@ __device__ __forceinline__ void moe_tiles(const Chosen& chosen, int k, int rows,
   for (int item = blockIdx.x; item < items.all; item += gridDim.x) {
     const int a = item / items.of_expert, g = (item - a * items.of_expert) * items.rounds, here = min(items.rounds, groups - g);
     const int first = uniform(chosen.first[a]), places = uniform(chosen.first[a + 1]) - first;
-    const auto m = matrix((int64_t)uniform(chosen.expert[a]));
+    const int expert = uniform(chosen.expert[a]);
+    const auto m = matrix((int64_t)expert);
     const W4Rows w[2] = {tile(m, 0), tile(m, 1)};
     constexpr int most = moe_most<XT, RT>();
     for (int p = 0; p < places; p += most) {
@@ -182,7 +183,9 @@ __device__ __forceinline__ void moe_tiles(const Chosen& chosen, int k, int rows,
           const int start = j * chunk, end = min(start + chunk, full);
           const bool ragged = j == chunks - 1 && full * kW4Block < k;
           typename W4Two<XT, SPB, RT, WIDE, ZEROS>::Ahead ahead;
-          const typename W4Two<XT, SPB, RT, WIDE, ZEROS>::Walk walk(start / kW4Run, 1, (end - start + kW4Run - 1) / kW4Run, end, blockIdx.x * kMoeWaves + wave);
+          // (begins where expert and rows say: which workgroup has them depends on what others have chosen)
+          const typename W4Two<XT, SPB, RT, WIDE, ZEROS>::Walk walk(start / kW4Run, 1, (end - start + kW4Run - 1) / kW4Run, end,
+                                                                    (unsigned)((expert * groups + g + r) * kMoeWaves + wave));
           if (full) two.begin(w[0], walk, ahead);
           if (chunks > 1 || r == 0) {
             __syncthreads();
