@@ -149,13 +149,18 @@ constexpr int moe_most() { return RT == 4 && w4_parts<XT>() == 3 ? 12 : 4 * RT; 
 static_assert(kMoeLds >= 12 * 3 * (kW4Run * kW4Block * 2 + 16) && kMoeLds >= 16 * (kW4Run * kW4Block * 2 + 16), "a run");
 
 template <int XT, int SPB, int RT, bool WIDE, bool ZEROS, class Matrix, class Tile, class First, class X, class Out>
-__device__ __forceinline__ void moe_tiles(const Chosen& chosen, int k, int rows, int rows_of_wave, int scale_type, char* lds, Matrix matrix, Tile tile, First first_row,
-                                          X vector, Out out) {
+__device__ __forceinline__ void moe_tiles(const Chosen& chosen, int tokens_of_call, int k, int rows, int rows_of_wave, int scale_type, char* lds, Matrix matrix, Tile tile,
+                                          First first_row, X vector, Out out) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
   const int count = uniform(chosen.count), blocks = (k + kW4Block - 1) / kW4Block, full = k / kW4Block;
   const int groups = (rows + rows_of_wave * kMoeWaves - 1) / (rows_of_wave * kMoeWaves);
   W4Two<XT, SPB, RT, WIDE, ZEROS> two;
+  // Whether x is one piece for every lot that a call of this size can have (a token has an expert once).  Where it is not, the chunks differ with the
+  // lot, which follows from what the other tokens have chosen, and the runs are taken in ascending order, the same for all chunks.
+  constexpr int most = moe_most<XT, RT>();
+  auto fit = [](int tokens) { return (kMoeLds / (tokens * w4_parts<XT>()) - 16) / (kW4Block * 2); };
+  const bool whole = blocks <= fit(min(most, tokens_of_call));
   const Items items(count, groups, 0);
   for (int item = blockIdx.x; item < items.all; item += gridDim.x) {
     const int a = item / items.of_expert, g = (item - a * items.of_expert) * items.rounds, here = min(items.rounds, groups - g);
@@ -163,12 +168,11 @@ __device__ __forceinline__ void moe_tiles(const Chosen& chosen, int k, int rows,
     const int expert = uniform(chosen.expert[a]);
     const auto m = matrix((int64_t)expert);
     const W4Rows w[2] = {tile(m, 0), tile(m, 1)};
-    constexpr int most = moe_most<XT, RT>();
     for (int p = 0; p < places; p += most) {
       const int tokens = min(most, places - p);
       auto x_of = [&](int t) { return vector(uniform(chosen.place[first + p + t])); };
       // blocks of x at a time: all, or runs that fit
-      int chunk = min(blocks, (kMoeLds / (tokens * w4_parts<XT>()) - 16) / (kW4Block * 2));
+      int chunk = min(blocks, fit(tokens));
       if (chunk < blocks) chunk = chunk / kW4Run * kW4Run;
       const int chunks = (blocks + chunk - 1) / chunk, pitch = chunk * kW4Block * 2 + 16;
       const char* lane_x = lds + w4_row_of_x<w4_parts<XT>()>(w4_thread() % 16, tokens, pitch);
@@ -183,9 +187,9 @@ __device__ __forceinline__ void moe_tiles(const Chosen& chosen, int k, int rows,
           const int start = j * chunk, end = min(start + chunk, full);
           const bool ragged = j == chunks - 1 && full * kW4Block < k;
           typename W4Two<XT, SPB, RT, WIDE, ZEROS>::Ahead ahead;
-          // (begins where expert and rows say: which workgroup has them depends on what others have chosen)
+          // (begins where expert and rows say: which workgroup has them depends on what others have chosen as well)
           const typename W4Two<XT, SPB, RT, WIDE, ZEROS>::Walk walk(start / kW4Run, 1, (end - start + kW4Run - 1) / kW4Run, end,
-                                                                    (unsigned)((expert * groups + g + r) * kMoeWaves + wave));
+                                                                    whole ? (unsigned)((expert * groups + g + r) * kMoeWaves + wave) : 0u);
           if (full) two.begin(w[0], walk, ahead);
           if (chunks > 1 || r == 0) {
             __syncthreads();

@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(64 * kMoeWaves, kMoeFit) moe_down_tiles_kernel
   __shared__ Chosen chosen;
   moe_chosen(c, chosen);
   moe_tiles<OZ2_F32, SPB, RT, WIDE, ZEROS>(
-      chosen, c.f, c.d, 32, scale_type, lds, [&](int64_t e) { return moe_down_of(c, e); }, [](const W4Rows& m, int) { return m; },
+      chosen, c.t, c.f, c.d, 32, scale_type, lds, [&](int64_t e) { return moe_down_of(c, e); }, [](const W4Rows& m, int) { return m; },
       [](int row, int t) { return row + 16 * t; }, [&](int place) { return reinterpret_cast<const char*>(c.h + (int64_t)place * c.f); },
       [&](int place, int row, float u0, float u1) {
         const float weight = c.weights[place];

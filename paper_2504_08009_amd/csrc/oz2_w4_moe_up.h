@@ -142,7 +142,7 @@ __device__ __forceinline__ void moe_route(const MoeCall& c, Chosen& chosen, shor
     if (lane == 0) chosen.count = found, chosen.first[found] = at;
   }
   __syncthreads();
-  // (the order of an expert's places changes no result: each is summed by itself)
+  // (the order of an expert's places, which timing decides, changes no result: each is summed by itself, in an order that those beside it do not touch)
   for (int i = threadIdx.x; i < places; i += 64 * kMoeWaves)
     if (ids[i] >= 0) chosen.place[atomicAdd(&count[ids[i]], 1)] = i;
   __syncthreads();
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(64 * kMoeWaves, kMoeFit) moe_up_tiles_kernel(M
     __syncthreads();
   }
   moe_tiles<XT, SPB, RT, WIDE, ZEROS>(
-      chosen, c.d, c.f, 16, scale_type, lds, [&](int64_t e) { return moe_gate_up_of(c, e); },
+      chosen, c.t, c.d, c.f, 16, scale_type, lds, [&](int64_t e) { return moe_gate_up_of(c, e); },
       [](const GateUp& m, int t) { return t ? m.up : m.gate; }, [](int row, int) { return row; },
       [&](int place) { return c.x + place / c.top_k * c.ldx * (XT == OZ2_F32 ? 4 : 2); },
       [&](int place, int row, float g, float u) { moe_inner(c, place, row, g, u); });

@@ -1,5 +1,5 @@
 """Layers of experts on the matrix cores: the order of a token's sums follows from the sizes of the call alone, so what other tokens choose
-changes no bit of its result.  Inner dimensions here are several runs of blocks long."""
+changes no bit of its result, and equal calls give equal bits.  Inner dimensions here are several runs of blocks and several chunks long."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -70,3 +70,29 @@ def test_the_rank_of_an_expert_among_the_chosen_changes_nothing(t, experts, x_ty
     choices = [(1 + 2 * i % others, 1 + (2 * i + 1) % others) for i in range(t)]
     x = tokens_of(gen, choices, experts, 1300, x_type)
     same_but_for(2, layer, x, (0, choices[2][1]))
+
+
+@pytest.mark.parametrize("x_type", ["bf16", "f32"])
+@pytest.mark.parametrize("t,experts,sharing,d,f", [(30, 4, 29, 1408, 1400), (32, 48, 9, 1300, 2100)])
+def test_how_many_tokens_share_an_expert_changes_nothing(t, experts, sharing, d, f, x_type):
+    """`sharing` tokens have the same two experts, in several lots of as many as the matrix cores take at a time; without one of them, each behind it is
+    one place further ahead.  The chosen experts are the same."""
+    print(t, experts, sharing, d, f, x_type, flush=True)
+    gen = torch.Generator("cuda").manual_seed(42)
+    layer = layer_of(gen, experts, 2, d, f, 128)
+    rest = [e for e in range(experts) if e not in (1, 2)]
+    choices = [(1, 2) if i < sharing else (rest[2 * i % len(rest)], rest[(2 * i + 1) % len(rest)]) for i in range(t)]
+    x = tokens_of(gen, choices, experts, d, x_type)
+    same_but_for(0, layer, x, choices[sharing])
+
+
+@pytest.mark.parametrize("x_type", ["bf16", "f32"])
+def test_equal_calls_give_equal_bits_where_many_tokens_share_an_expert(x_type):
+    """more places than a wave deals out at a time"""
+    gen = torch.Generator("cuda").manual_seed(43)
+    layer = layer_of(gen, 5, 4, 1408, 1400, 128)
+    choices = [[(i + j) % 5 for j in range(4)] for i in range(32)]
+    x = tokens_of(gen, choices, 5, 1408, x_type)
+    first = [v.clone() for v in call(layer, x)]
+    for _ in range(20):
+        assert all(torch.equal(a, b) for a, b in zip(call(layer, x), first))
