@@ -515,10 +515,15 @@ class W4Matrix:
 
 
 def _rows(name, x, width):
-    """leading dimension of a (rows, width) tensor whose rows are contiguous"""
+    """leading dimension of a two-dimensional tensor with rows of that width, which are contiguous and do not overlap (an expanded one's do)"""
     if x.dim() != 2 or x.size(1) != width or (width > 1 and x.stride(1) != 1):
-        raise Oz2Error("%s is (tokens, %d) with contiguous rows, got shape %s" % (name, width, tuple(x.shape)))
-    return max(x.stride(0), width)
+        raise Oz2Error("%s is two-dimensional with contiguous rows of %d, got shape %s" % (name, width, tuple(x.shape)))
+    pitch = x.stride(0)
+    if pitch >= width:
+        return pitch
+    if x.size(0) > 1:
+        raise Oz2Error("the rows of %s overlap: %d wide, %d apart (an expanded tensor: pass a copy)" % (name, width, pitch))
+    return width  # (of one row, or none)
 
 
 _raw_stream = None
@@ -569,6 +574,7 @@ class MoeLayer:
         import torch
         if router.dim() != 2 or router.shape != (gate.count, gate.k) or (gate.k > 1 and router.stride(1) != 1):
             raise Oz2Error("router is (experts, d) = (%d, %d) with contiguous rows" % (gate.count, gate.k))
+        ld_router = _rows("router", router, gate.k)
         if (up.n, up.k, up.count) != (gate.n, gate.k, gate.count) or (down.n, down.k, down.count) != (gate.k, gate.n, gate.count):
             raise Oz2Error("gate and up are f x d, down is d x f, each for every expert")
         if bias is not None and (bias.dtype != torch.float32 or tuple(bias.shape) != (gate.count,) or not bias.is_contiguous()):
@@ -577,7 +583,7 @@ class MoeLayer:
             raise Oz2Error("the parts of the layer are on different devices")
         self.router, self.gate, self.up, self.down, self.bias = router, gate, up, down, bias
         self.d, self.top_k, self.device = gate.k, int(top_k), gate.device
-        self.struct = _Moe(gate.struct, up.struct, down.struct, router.data_ptr(), max(router.stride(0), gate.k), None if bias is None else bias.data_ptr(),
+        self.struct = _Moe(gate.struct, up.struct, down.struct, router.data_ptr(), ld_router, None if bias is None else bias.data_ptr(),
                            _type(router.dtype), self.top_k, ("softmax", "sigmoid").index(score), int(bool(renormalize)),
                            ("silu", "gelu").index(activation), float(factor))
         self.ref = ctypes.addressof(self.struct)
