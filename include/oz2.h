@@ -410,8 +410,9 @@ typedef struct oz2_w4_matrix {
 } oz2_w4_matrix;
 
 /* Y := alpha W X + beta C with t vectors: X is k x t (leading dimension ldx, type x_type), C and Y are n x t of type y_type; C may be
- * Y itself (ldc == ldy) and must not overlap it otherwise, and is not read where beta is 0 (then it may be NULL).  alpha == 0
- * or k == 0 reads neither W nor X.  W describes one matrix (count, strides ignored).  Uses no workspace; may be captured into a graph. */
+ * Y itself (ldc == ldy), and is not read where beta is 0 (then it may be NULL).  alpha == 0 or k == 0 reads neither W nor X.  Y shares no
+ * byte with what is read of X, nor, but for Y itself, of C: calls with such overlaps return -11 and -8 (rows may lie between each other's).
+ * W describes one matrix (count, strides ignored).  Uses no workspace; may be captured into a graph. */
 int oz2_w4_matvec(const oz2_w4_matrix* W, int64_t t, float alpha, int x_type, const void* X, int64_t ldx, float beta, const void* C,
                   int64_t ldc, int y_type, void* Y, int64_t ldy, void* stream);
 
@@ -445,7 +446,8 @@ typedef struct oz2_moe_layer {
 size_t oz2_w4_moe_workspace_bytes(const oz2_moe_layer* layer, int64_t t);
 
 /* active: NULL, or t bytes; a token with 0 there is left out: its y is 0.  ids (int32) and weights (float), top_k x t without gaps, or
- * NULL: the chosen experts and their weights, -1 and 0 in places that have none.  X: d x t, Y: d x t, which must not overlap X.
+ * NULL: the chosen experts and their weights, -1 and 0 in places that have none.  X: d x t, Y: d x t, which is X itself (one size of their types,
+ * ldx == ldy) or shares no byte with it (else -8).
  * Returns OZ2_ERR_WORKSPACE where the registered workspace (256-byte aligned) is too small. */
 int oz2_w4_moe(const oz2_moe_layer* layer, int64_t t, int x_type, const void* X, int64_t ldx, const uint8_t* active, int y_type, void* Y,
                int64_t ldy, int32_t* ids, float* weights, void* stream);

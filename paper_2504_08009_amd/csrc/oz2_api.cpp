@@ -859,6 +859,23 @@ bool w4_ok(const oz2_w4_matrix& w, bool stack) {
                           (!w.zeros || w.stride_zeros >= rows * w.ld_zeros + groups));
 }
 
+int64_t size_of(int type) { return type == OZ2_F32 ? 4 : 2; }
+
+// Whether any byte of `rows` rows of width_a bytes, pitch_a apart, belongs to as many of width_b, pitch_b apart; all four as checked.  Rows that lie
+// between each other's do not meet.
+bool rows_meet(const void* a, int64_t width_a, int64_t pitch_a, const void* b, int64_t width_b, int64_t pitch_b, int64_t rows) {
+  if (rows == 1) pitch_a = pitch_b = 0;
+  const int64_t start = (int64_t)((uintptr_t)b - (uintptr_t)a), far = (int64_t)1 << 46;  // (further apart no memory is; rows are below 2^16)
+  if (pitch_a >= far || pitch_b >= far) return false;
+  if (start >= (rows - 1) * pitch_a + width_a || start + (rows - 1) * pitch_b + width_b <= 0) return false;
+  for (int64_t i = 0; i < rows; ++i) {
+    const int64_t after = i * pitch_a - start - width_b, before = i * pitch_a + width_a - start;  // a row of b that meets row i begins between these
+    const int64_t j = after < 0 ? 0 : pitch_b ? after / pitch_b + 1 : rows;
+    if (j < rows && j * pitch_b < before) return true;
+  }
+  return false;
+}
+
 bool moe_ok(const oz2_moe_layer* m) {
   if (!m || !w4_ok(m->gate, true) || !w4_ok(m->up, true) || !w4_ok(m->down, true)) return false;
   const int64_t f = m->gate.n, d = m->gate.k, experts = m->gate.count;
@@ -889,6 +906,9 @@ int oz2_w4_matvec(const oz2_w4_matrix* W, int64_t t, float alpha, int x_type, co
   if (w.k > 0 && !X) return -5;
   if (beta != 0.f && !C) return -8;
   if (!Y) return -11;
+  const int64_t xs = size_of(x_type), ys = size_of(y_type);
+  if (beta != 0.f && !(C == Y && (t == 1 || ldc == ldy)) && rows_meet(C, w.n * ys, ldc * ys, Y, w.n * ys, ldy * ys, t)) return -8;
+  if (w.k > 0 && rows_meet(X, w.k * xs, ldx * xs, Y, w.n * ys, ldy * ys, t)) return -11;
   return oz2_launch_w4_matvec(w, t, alpha, x_type, X, ldx, beta, C, ldc, y_type, Y, ldy, static_cast<hipStream_t>(stream)) == hipSuccess
              ? OZ2_OK : OZ2_ERR_HIP;
 }
@@ -909,6 +929,9 @@ int oz2_w4_moe(const oz2_moe_layer* layer, int64_t t, int x_type, const void* X,
   if (t == 0) return OZ2_OK;
   if (!X) return -4;
   if (!Y) return -8;
+  // (a token's own x may become its y: it is read before the launch that writes y, and no later piece of the call has it)
+  const int64_t d = layer->gate.k, xs = size_of(x_type), ys = size_of(y_type);
+  if (!(X == Y && xs == ys && (t == 1 || ldx == ldy)) && rows_meet(X, d * xs, ldx * xs, Y, d * ys, ldy * ys, t)) return -8;
   State& s = state();
   std::lock_guard<std::mutex> lock(s.mu);
   if (!s.ws || s.ws_bytes < oz2_w4_moe_space(*layer, t)) return OZ2_ERR_WORKSPACE;

@@ -31,3 +31,25 @@ def test_expanded_tensors():
             bad()
     # one row is a row, however it came about
     assert torch.equal(oz.w4_matvec(w, x[0].expand(1, 256), beta=1.0, c=c[0].expand(1, 96)), oz.w4_matvec(w, x[:1], beta=1.0, c=c[:1]))
+
+
+def test_results_over_what_is_read():
+    """refused where they would be; in the place of a residual and of a layer's tokens they are what they are elsewhere"""
+    w, x = matrix(256, 256), torch.randn((5, 256), device="cuda")
+    want, before = oz.w4_matvec(w, x), x.clone()
+    for bad in (lambda: oz.w4_matvec(w, x, out=x), lambda: oz.w4_matvec(w, x[:4], out=x[1:]), lambda: oz.w4_matvec(w, x[:2], beta=1.0, c=x[2:4], out=x[3:])):
+        with pytest.raises(oz.Oz2Error):
+            bad()
+    assert torch.equal(x, before)
+    both = torch.zeros((5, 600), device="cuda")
+    both[:, :256] = x
+    assert torch.equal(oz.w4_matvec(w, both[:, :256], out=both[:, 256:512]), want)
+    assert torch.equal(oz.w4_matvec(w, both[:, :256], beta=1.0, c=both[:, 256:512], out=both[:, 256:512]), oz.w4_matvec(w, x, beta=1.0, c=want))
+    moe, ctx = layer(), oz.Context()
+    ctx.allocate_moe_workspace(moe, 70)
+    x = torch.randn((70, 256), device="cuda")
+    want = ctx.w4_moe(moe, x)[0].clone()
+    with pytest.raises(oz.Oz2Error):
+        ctx.w4_moe(moe, x[:60], out=x[10:])
+    ctx.w4_moe(moe, x, out=x)
+    assert torch.equal(x, want)
