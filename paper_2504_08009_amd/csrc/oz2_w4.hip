@@ -7,25 +7,28 @@ extern template hipError_t oz2_w4_matvec_of<OZ2_F16>(const W4Call&, int64_t);
 
 namespace {
 
-// What the loads of the other kernels do not fit: rows of a few bytes, or further apart than they count.  One wave a row and vector.
+// What the loads of the other kernels do not fit: rows of a few bytes, or further apart than they count.  One wave a row and vector, and the rows a grid
+// behind it: a launch has fewer than 2^32 threads in a dimension, a matrix up to 2^31 rows.
+constexpr int64_t kSimpleGroups = 1 << 22;
 __global__ void __launch_bounds__(256) w4_simple_kernel(oz2_w4_matrix w, float alpha, int x_type, const char* x, int64_t ldx, float beta,
                                                         const char* c, int64_t ldc, int y_type, char* y, int64_t ldy) {
-  const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64, col = blockIdx.y;
+  const int64_t col = blockIdx.y;
   const int lane = threadIdx.x % 64;
-  if (row >= w.n) return;
-  const uint8_t* codes = static_cast<const uint8_t*>(w.codes) + row * w.ld_codes;
-  float sum = 0.f;
-  for (int64_t l = lane; l < w.k; l += 64) {
-    const int q = codes[l / 2] >> (l % 2 * 4) & 15;
-    const int64_t g = l / w.group;
-    const int z = w.zeros ? static_cast<const uint8_t*>(w.zeros)[row * w.ld_zeros + g] : 8;
-    sum = fmaf(w4_load(w.scale_type, w.scales, row * w.ld_scales + g) * (float)(q - z), w4_load(x_type, x, col * ldx + l), sum);
+  for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; row < w.n; row += (int64_t)gridDim.x * 4) {
+    const uint8_t* codes = static_cast<const uint8_t*>(w.codes) + row * w.ld_codes;
+    float sum = 0.f;
+    for (int64_t l = lane; l < w.k; l += 64) {
+      const int q = codes[l / 2] >> (l % 2 * 4) & 15;
+      const int64_t g = l / w.group;
+      const int z = w.zeros ? static_cast<const uint8_t*>(w.zeros)[row * w.ld_zeros + g] : 8;
+      sum = fmaf(w4_load(w.scale_type, w.scales, row * w.ld_scales + g) * (float)(q - z), w4_load(x_type, x, col * ldx + l), sum);
+    }
+    for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
+    if (lane) continue;
+    float v = w.k ? alpha * sum : 0.f;
+    if (beta != 0.f) v = fmaf(beta, w4_load(y_type, c, col * ldc + row), v);
+    w4_store(y_type, y, col * ldy + row, v);
   }
-  for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
-  if (lane) return;
-  float v = w.k ? alpha * sum : 0.f;
-  if (beta != 0.f) v = fmaf(beta, w4_load(y_type, c, col * ldc + row), v);
-  w4_store(y_type, y, col * ldy + row, v);
 }
 
 }  // namespace
@@ -52,7 +55,8 @@ hipError_t oz2_launch_w4_matvec(const oz2_w4_matrix& m, int64_t t, float alpha, 
                                 const void* c, int64_t ldc, int y_type, void* y, int64_t ldy, hipStream_t st) {
   const W4Call a = {oz2_w4_rows(m), m.scale_type, (int)t, alpha, beta, x, c, ldx, ldc, ldy, y_type, y, st};
   if (m.k < 32 || !w4_tile_fits(a.w)) {
-    hipLaunchKernelGGL(w4_simple_kernel, dim3((unsigned)((m.n + 3) / 4), (unsigned)t), dim3(256), 0, st, m, alpha, x_type,
+    const int64_t groups = (m.n + 3) / 4;
+    hipLaunchKernelGGL(w4_simple_kernel, dim3((unsigned)(groups < kSimpleGroups ? groups : kSimpleGroups), (unsigned)t), dim3(256), 0, st, m, alpha, x_type,
                        static_cast<const char*>(x), ldx, beta, static_cast<const char*>(c), ldc, y_type, static_cast<char*>(y), ldy);
     return hipGetLastError();
   }
