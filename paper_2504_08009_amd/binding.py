@@ -541,10 +541,24 @@ def _stream_on(stream, index):
     return _raw_stream(index)
 
 
+def _new(x, shape, dtype, stream):
+    """A tensor for results of a call on that stream (None: the current one).  It belongs to it: memory that the current stream has given back may still
+    be written by what is pending there."""
+    if stream is None or x.get_device() < 0:
+        return x.new_empty(shape, dtype=dtype)
+    import torch
+    if not hasattr(stream, "cuda_stream"):
+        pointer = getattr(stream, "value", stream)
+        stream = torch.cuda.ExternalStream(pointer, device=x.device) if pointer else torch.cuda.default_stream(x.device)
+    with torch.cuda.stream(stream):
+        return x.new_empty(shape, dtype=dtype)
+
+
 def w4_matvec(W, x, alpha=1.0, beta=0.0, c=None, out=None, stream=None):
-    """alpha W x + beta c for every row of x (tokens, k), as (tokens, n) in the type of `out`, or of x where it is None; c is like the result."""
+    """alpha W x + beta c for every row of x (tokens, k), as (tokens, n) in the type of `out`, or of x where it is None; c is like the result.
+    A result that is made here belongs to the stream of the call."""
     if out is None:
-        out = x.new_empty((x.shape[0], W.n))
+        out = _new(x, (x.shape[0], W.n), x.dtype, stream)
     index = x.get_device()
     if index < 0 or index != W.index or out.get_device() != index:
         _on_device(W.device, x=x, out=out)
@@ -593,11 +607,11 @@ def _w4_moe(call, name, first, layer, x, active, out, ids, weights, stream):
     import torch
     t, index = x.shape[0], x.get_device()
     if out is None:
-        out = x.new_empty((t, layer.d))
+        out = _new(x, (t, layer.d), x.dtype, stream)
     if ids is None:
-        ids = x.new_empty((t, layer.top_k), dtype=torch.int32)
+        ids = _new(x, (t, layer.top_k), torch.int32, stream)
     if weights is None:
-        weights = x.new_empty((t, layer.top_k), dtype=torch.float32)
+        weights = _new(x, (t, layer.top_k), torch.float32, stream)
     if index < 0 or any(v.get_device() != index for v in (layer.router, out, ids, weights)):
         _on_device(layer.device, x=x, out=out, ids=ids, weights=weights)
     ldx, ldy = _rows("x", x, layer.d), _rows("out", out, layer.d)
