@@ -526,19 +526,20 @@ def _rows(name, x, width):
     return width  # (of one row, or none)
 
 
-_raw_stream = None
+_raw_stream = _current_device = None
 
 
 def _stream_on(stream, index):
-    """The stream's pointer; without one, that of the current stream of the device.  A call of a few microseconds notices how long this
-    takes: torch.cuda.current_stream() 2.7 us, torch's own accessor of the pointer 0.1."""
-    global _raw_stream
-    if stream is not None:
-        return getattr(stream, "cuda_stream", stream)
-    if _raw_stream is None:
+    """The stream's pointer; without one, that of the current stream of the device, which has to be the current one: kernels are launched there.
+    A call of a few microseconds notices how long this takes: torch.cuda.current_stream() 2.7 us, torch's own accessor of the pointer 0.1."""
+    global _raw_stream, _current_device
+    if _current_device is None:
         import torch
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
-    return _raw_stream(index)
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    if _current_device() != index:
+        raise Oz2Error("the tensors are on cuda:%d, the current device is cuda:%d" % (index, _current_device()))
+    return _raw_stream(index) if stream is None else getattr(stream, "cuda_stream", stream)
 
 
 def _new(x, shape, dtype, stream):

@@ -41,3 +41,12 @@ def test_expanded_weights_are_refused():
     for w in (oz.W4Matrix(codes[:1].expand(8, 50), scales, group=32), oz.W4Matrix(codes, scales[:1].expand(8, 4), group=32),
               oz.W4Matrix(codes, scales, torch.zeros((1, 4), dtype=torch.uint8).expand(8, 4), group=32)):
         assert oz.lib().oz2_w4_matvec(ctypes.addressof(w.struct), 1, 1.0, 0, 4096, 100, 0.0, None, 0, 0, 4096, 8, None) == -1
+
+
+def test_tensors_on_another_device_than_the_current_one_are_refused(monkeypatch):
+    monkeypatch.setattr(binding, "_current_device", lambda: 1, raising=False)
+    monkeypatch.setattr(binding, "_raw_stream", lambda index: 4096 + index)
+    assert binding._stream_on(None, 1) == 4097 and binding._stream_on(77, 1) == 77
+    for stream in (None, 77):
+        with pytest.raises(oz.Oz2Error, match="cuda:0.*cuda:1"):
+            binding._stream_on(stream, 0)
