@@ -526,6 +526,12 @@ def _rows(name, x, width):
     return width  # (of one row, or none)
 
 
+def _refuse_gradient():
+    import torch
+    if torch.is_grad_enabled():
+        raise Oz2Error("a tensor requires a gradient, which these products do not form: call them under torch.no_grad(), or with detached tensors")
+
+
 _raw_stream = _current_device = None
 
 
@@ -557,7 +563,9 @@ def _new(x, shape, dtype, stream):
 
 def w4_matvec(W, x, alpha=1.0, beta=0.0, c=None, out=None, stream=None):
     """alpha W x + beta c for every row of x (tokens, k), as (tokens, n) in the type of `out`, or of x where it is None; c is like the result.
-    A result that is made here belongs to the stream of the call."""
+    A result that is made here belongs to the stream of the call.  There is no gradient: tensors that require one are refused where one would be recorded."""
+    if x.requires_grad or W.scales.requires_grad or (c is not None and c.requires_grad) or (out is not None and out.requires_grad):
+        _refuse_gradient()
     if out is None:
         out = _new(x, (x.shape[0], W.n), x.dtype, stream)
     index = x.get_device()
@@ -597,6 +605,7 @@ class MoeLayer:
         if any(v.device != gate.device for v in (router, up, down) + (() if bias is None else (bias,))):
             raise Oz2Error("the parts of the layer are on different devices")
         self.router, self.gate, self.up, self.down, self.bias = router, gate, up, down, bias
+        self.with_gradient = tuple(v for v in (router, bias, gate.scales, up.scales, down.scales) if v is not None)
         self.d, self.top_k, self.device = gate.k, int(top_k), gate.device
         self.struct = _Moe(gate.struct, up.struct, down.struct, router.data_ptr(), ld_router, None if bias is None else bias.data_ptr(),
                            _type(router.dtype), self.top_k, ("softmax", "sigmoid").index(score), int(bool(renormalize)),
@@ -607,6 +616,8 @@ class MoeLayer:
 def _w4_moe(call, name, first, layer, x, active, out, ids, weights, stream):
     import torch
     t, index = x.shape[0], x.get_device()
+    if any(v is not None and v.requires_grad for v in (x, out, weights, *layer.with_gradient)):
+        _refuse_gradient()
     if out is None:
         out = _new(x, (t, layer.d), x.dtype, stream)
     if ids is None:
@@ -635,7 +646,8 @@ def _w4_moe(call, name, first, layer, x, active, out, ids, weights, stream):
 
 
 def w4_moe(layer, x, active=None, out=None, ids=None, weights=None, stream=None):
-    """(y, ids, weights) of a MoeLayer for x (tokens, d), in the workspace that set_workspace registered; tokens whose `active` is 0 get 0."""
+    """(y, ids, weights) of a MoeLayer for x (tokens, d), in the workspace that set_workspace registered; tokens whose `active` is 0 get 0.
+    Streams and gradients as for w4_matvec."""
     return _w4_moe(lib().oz2_w4_moe, "oz2_w4_moe", (), layer, x, active, out, ids, weights, stream)
 
 

@@ -50,3 +50,22 @@ def test_tensors_on_another_device_than_the_current_one_are_refused(monkeypatch)
     for stream in (None, 77):
         with pytest.raises(oz.Oz2Error, match="cuda:0.*cuda:1"):
             binding._stream_on(stream, 0)
+
+
+def test_tensors_that_require_a_gradient_are_refused():
+    """in grad mode, where a graph would be recorded; otherwise the call goes on to its next check, which here is that of the device"""
+    w, x, c = stack(1, 60, 100), torch.zeros((2, 100)), torch.zeros((2, 60))
+    layer = oz.MoeLayer(torch.zeros((4, 100)), stack(4, 60, 100), stack(4, 60, 100), stack(4, 100, 60), 2, bias=torch.zeros(4))
+    calls = [(x, lambda: oz.w4_matvec(w, x)), (c, lambda: oz.w4_matvec(w, x, beta=1.0, c=c)), (c, lambda: oz.w4_matvec(w, x, out=c)),
+             (w.scales, lambda: oz.w4_matvec(w, x))]
+    calls += [(v, lambda: oz.w4_moe(layer, x)) for v in (x, layer.router, layer.bias, layer.gate.scales, layer.up.scales, layer.down.scales)]
+    for v, call in calls:
+        with pytest.raises(oz.Oz2Error, match="on the GPU"):
+            call()
+        v.requires_grad_(True)
+        with pytest.raises(oz.Oz2Error, match="gradient"):
+            call()
+        for mode in (torch.no_grad, torch.inference_mode):
+            with mode(), pytest.raises(oz.Oz2Error, match="on the GPU"):
+                call()
+        v.requires_grad_(False)
