@@ -516,12 +516,13 @@ class W4Matrix:
 
 def _rows(name, x, width):
     """leading dimension of a two-dimensional tensor with rows of that width, which are contiguous and do not overlap (an expanded one's do)"""
-    if x.dim() != 2 or x.size(1) != width or (width > 1 and x.stride(1) != 1):
-        raise Oz2Error("%s is two-dimensional with contiguous rows of %d, got shape %s" % (name, width, tuple(x.shape)))
-    pitch = x.stride(0)
+    shape, strides = x.shape, x.stride()  # (whole: each single one asked for costs as much)
+    if len(shape) != 2 or shape[1] != width or (width > 1 and strides[1] != 1):
+        raise Oz2Error("%s is two-dimensional with contiguous rows of %d, got shape %s" % (name, width, tuple(shape)))
+    pitch = strides[0]
     if pitch >= width:
         return pitch
-    if x.size(0) > 1:
+    if shape[0] > 1:
         raise Oz2Error("the rows of %s overlap: %d wide, %d apart (an expanded tensor: pass a copy)" % (name, width, pitch))
     return width  # (of one row, or none)
 
