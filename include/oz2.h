@@ -391,8 +391,10 @@ int oz2_host_short_product_residues(int index, int64_t count, const int32_t* pro
  * No alignment beyond that of the element types is needed (rows whose codes start at multiples of 16 bytes are read fastest).
  *
  * Arithmetic: a product is the sum over groups of s_ig times the sum of (q - z) x over the group, in FP32 throughout; x is taken
- * exactly whatever its type, and the result is rounded once.  Infinities and NaNs in x give what that formula gives; a scale that is not
- * finite makes results of its row that are not finite.
+ * exactly whatever its type, and the result is rounded once.  A group's sum is formed as that of (16 + q) x, or of q x, less a multiple
+ * of the sum of x: its error is of the order of 2^-24 times the sum of (16 + q + z) |x|, which with FP32 results can be several
+ * times that of a direct sum.  Infinities and NaNs in x give what the formula gives; a scale that is not finite makes
+ * results of its row that are not finite.
  * Results do not depend on timing: equal calls give equal bits. */
 #define OZ2_F32 0
 #define OZ2_BF16 1
@@ -412,7 +414,8 @@ typedef struct oz2_w4_matrix {
 /* Y := alpha W X + beta C with t vectors: X is k x t (leading dimension ldx, type x_type), C and Y are n x t of type y_type; C may be
  * Y itself (ldc == ldy), and is not read where beta is 0 (then it may be NULL).  alpha == 0 or k == 0 reads neither W nor X.  Y shares no
  * byte with what is read of X, nor, but for Y itself, of C: calls with such overlaps return -11 and -8 (rows may lie between each other's).
- * W describes one matrix (count, strides ignored).  Uses no workspace; may be captured into a graph. */
+ * W describes one matrix (count, strides ignored).  Uses no workspace; may be captured into a graph.  Meant for few vectors: W is read
+ * once for every sixteen. */
 int oz2_w4_matvec(const oz2_w4_matrix* W, int64_t t, float alpha, int x_type, const void* X, int64_t ldx, float beta, const void* C,
                   int64_t ldc, int y_type, void* Y, int64_t ldy, void* stream);
 
@@ -425,7 +428,8 @@ int oz2_w4_matvec(const oz2_w4_matrix* W, int64_t t, float alpha, int x_type, co
  *   y = sum over the chosen of  weight * down_e (act(gate_e x) * (up_e x)),   act = silu or gelu (with erf), in an order that depends
  *           on the sizes alone
  * gate and up are stacks of f x d, down of d x f; gate and up are alike in group, type of the scales and whether they have zero points.
- * The inner vectors of f values are kept in FP32. */
+ * The inner vectors of f values are kept in FP32.  Meant for few tokens: 32 at a time are taken through the layer, and read the weights of their experts
+ * again.  Layers with d or f below 32 or above 8192 go through plain kernels that read them for every token and expert, at a fraction of the speed. */
 #define OZ2_SCORE_SOFTMAX 0
 #define OZ2_SCORE_SIGMOID 1
 #define OZ2_ACT_SILU 0

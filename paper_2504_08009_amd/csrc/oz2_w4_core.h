@@ -5,7 +5,8 @@
 // (bf16, f16) or as the three bf16 values that make it up exactly (f32), and
 //   sum (q - z) x = sum (16 + q) x - (16 + z) sum x.
 // Products of these are exact in FP32, in which everything is summed.  The scale multiplies a group's sum, so that nothing is rounded to
-// 16 bits before the result.
+// 16 bits before the result.  The difference cancels: its error is that of sums of (16 + q) |x| and (16 + z) |x|, which in an FP32 result can be several times
+// that of a sum of (q - z) x; a 16-bit result does not show it.
 #ifndef OZ2_W4_CORE_H
 #define OZ2_W4_CORE_H
 

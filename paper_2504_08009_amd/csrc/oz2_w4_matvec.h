@@ -171,7 +171,9 @@ hipError_t launch_vector(const W4Call& a) {
   int split_log = 0;
   while ((kW4Span << split_log) < a.w.k) ++split_log;
   const int per = kWaves >> split_log, batches = (a.w.n + 3) / 4;
-  // three workgroups a compute unit fit; each has x in its registers and walks as many batches as all others
+  // Three workgroups a compute unit, each with x in its registers, which walk as many batches as all others.  Three fit with one 16-bit vector and no
+  // zero points (76 registers); two with zero points, two 16-bit vectors or one FP32 vector (83 to 111) and one with two FP32 vectors (155 to 159):
+  // there the last ones begin when the first are done.
   const int most = oz2_w4_compute_units() * 3, needed = (batches + per - 1) / per, rounds = (needed + most - 1) / most, grid = (needed + rounds - 1) / rounds;
   hipLaunchKernelGGL((w4_vector_kernel<XT, T, ST, ZEROS>), dim3(grid), dim3(64 * kWaves), 0, a.st, a.w, split_log, a.alpha,
                      static_cast<const char*>(a.x), a.ldx, a.beta, a.c, a.ldc, a.y_type, a.y, a.ldy);

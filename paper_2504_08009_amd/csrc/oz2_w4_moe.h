@@ -3,8 +3,8 @@
 //
 // Three launches (router; choice, gate and up; down with the sum over a token's experts) where an expert has a token at the most as a rule, four (the
 // sum in its own) where several share its weights, which are then read once for up to sixteen.  One token through 8 of 128 experts of
-// 2048 x 1024: 20.8 us = 3.8 + 11 + 6 for 26 MB, each launch at its own latency; 4 tokens, 6 of 64 of 4096 x 1024: 55 us = 7 + 29 + 20
-// for 140 MB; 16, 6 of 64 of 2048 x 1408: 84 us = 5 + 44 + 34 + 4 for 210 MB.
+// 2048 x 1024: 20.8 us = 3.8 + 11 + 6 for 26 MB, each launch at its own latency; 4 tokens, 6 of 64 of 4096 x 1024: 56 us = 6 + 29 + 20
+// for 140 MB; 16, 6 of 64 of 2048 x 1408: 86 us = 5 + 45 + 35 + 4 for 210 MB.
 #ifndef OZ2_W4_MOE_H
 #define OZ2_W4_MOE_H
 

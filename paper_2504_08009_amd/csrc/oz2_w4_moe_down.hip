@@ -36,6 +36,7 @@ __global__ void __launch_bounds__(64 * kMoeWaves, 4) moe_down_kernel(MoeCall c, 
 // BATCHES batches of rows for all places of a token, and their sums.  Groups of `1 << split_log` waves take every per-th place each: eight waves, so that
 // most tokens' places are all in flight.  A lane brings 128 bytes of h for the 64 of codes in a batch's four loads: two batches where there are still four
 // workgroups a compute unit: 4 tokens through 6 of 64 experts of 4096 x 1024 in half precision 60 -> 55 us, 8 through 4 of 128 of 2048 x 2048 85 -> 75.
+// (With zero points and two rows a load the compiler keeps 48 bytes a lane of it in scratch memory.)
 constexpr int kDirectWaves = 8;
 template <int ST, bool ZEROS, int FOLD, int BATCHES>
 __global__ void __launch_bounds__(64 * kDirectWaves, 4) moe_down_direct_kernel(MoeCall c, int split_log) {

@@ -3,8 +3,8 @@
 // as well, with an operand of equal values.
 //
 // Bound, at the sizes measured, by what comes before and after a wave's few blocks (x into LDS, the first loads' way, sums over the waves)
-// and by the instructions that turn codes into operands, not by bytes: 8192 x 8192 with 16 vectors takes 18.6 us for 35 MB (1.9 TB/s), the
-// experts of 32 tokens, 8 of 128 of 4096 x 2048, 440 us for 1.58 GB (3.6 TB/s).
+// and by the instructions that turn codes into operands, not by bytes: 8192 x 8192 with 16 vectors takes 18.7 us for 35 MB (1.9 TB/s), the
+// experts of 32 tokens, 8 of 128 of 4096 x 2048, 437 us for 1.58 GB (3.6 TB/s).
 //
 // Four neighbouring lanes load 64 bytes of a row, eight of them two lines' worth of two blocks; where each lane loads from a row of its own, as the matrix
 // cores want their operand, the vector cache is asked 64 times for a load and sets the pace.  The words then change lanes and

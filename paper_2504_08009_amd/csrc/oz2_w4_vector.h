@@ -3,7 +3,7 @@
 // one group, so that its sum needs one scale.  The sum of (q - z) x is that of (16 + q) x less (16 + z) times the sum of x (FP32 x: of q x less z times it),
 // which the lane forms once.
 //
-// Bound by reading the codes: 65536 x 8192 with one vector takes 54 us, 5.6 TB/s of the 5.9 that reading alone reaches.  Smaller products take
+// Bound by reading the codes: 65536 x 8192 with one vector takes 53 us, 5.7 TB/s of the 5.9 that reading alone reaches.  Smaller products take
 // a launch's time and one trip to memory: 4096 x 4096 4.8 us for 8.7 MB, 16384 x 4096 in half precision 9.4 us for 37 MB.
 #ifndef OZ2_W4_VECTOR_H
 #define OZ2_W4_VECTOR_H
