@@ -458,6 +458,97 @@ int oz2_w4_moe(const oz2_moe_layer* layer, int64_t t, int x_type, const void* X,
 int oz2_context_w4_moe(oz2_context* ctx, const oz2_moe_layer* layer, int64_t t, int x_type, const void* X, int64_t ldx,
                        const uint8_t* active, int y_type, void* Y, int64_t ldy, int32_t* ids, float* weights, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Attention, for whoever answers with a model: over whole prompts, and over a paged cache of keys and values held in 4 bits.
+ *
+ * Rows of heads: element (token, head, d) of a tensor is data[token ld_token + head ld_head + d], of type `type` (OZ2_F32, OZ2_BF16, OZ2_F16);
+ * strides may be any that keep rows apart, and need no alignment beyond the type's (multiples of 16 bytes are read fastest).
+ * Tokens of several sequences are packed: sequence s has the rows cu[s] .. cu[s + 1] - 1 (cu: sequences + 1 int32 on the device, ascending from 0; what
+ * lies outside 0 .. tokens is cut off).  Rows behind the last sequence are left as they were.  `heads` query heads share `kv_heads` heads of keys and values
+ * in order: query head h reads kv head h / (heads / kv_heads).
+ * Sums, maxima and sums of exponentials are FP32; results are rounded once to their type.  A row that sees no key, or none with a score above
+ * -infinity, is 0; a NaN among the scores that it sees makes it NaN.  What a row does not see never reaches it, whatever it holds.  Equal calls give equal bits. */
+typedef struct oz2_rows {
+  void* data;
+  int64_t ld_token, ld_head;
+  int type;
+} oz2_rows;
+#define OZ2_ATTENTION_MAX_DIM 256
+
+/* out_i := sum_j p_ij v_j,  p_i = softmax over j of  scale q_i k_j,  over the tokens j of i's own sequence, up to i itself if causal != 0.
+ * q, out: tokens x heads x dim; k, v: tokens x kv_heads x dim, of q's type; dim <= OZ2_ATTENTION_MAX_DIM.  For 16-bit types p is rounded to that type before
+ * it meets v (its sum is taken of what it was rounded to).  out shares no byte with q, k or v.  Uses no workspace; may be captured. */
+int oz2_attention(int64_t tokens, int64_t sequences, const int32_t* cu, int64_t heads, int64_t kv_heads, int64_t dim, float scale, int causal,
+                  const oz2_rows* q, const oz2_rows* k, const oz2_rows* v, const oz2_rows* out, void* stream);
+
+/* A cache: pages of page_size places (a multiple of 16), each place with a key and a value of dim codes (dim a multiple of 8, <= 256) for every kv head:
+ *   x_d = s c_d + o,  c in 0 .. 15, one pair (s, o) of FP16 for each key and each value
+ *   codes   byte floor(d / 2) of (page, head, place) at page codes_page + head codes_head + place dim / 2; even d in the low half (strides in bytes,
+ *           multiples of 4 like the addresses)
+ *   scales  pair of (page, head, place) at index page scales_page + head scales_head + place (strides in pairs; addresses multiples of 16, strides of 4) */
+typedef struct oz2_kv4_cache {
+  int64_t pages, page_size, heads, dim;
+  uint8_t *k_codes, *v_codes;
+  int64_t codes_page, codes_head;
+  void *k_scales, *v_scales;
+  int64_t scales_page, scales_head;
+} oz2_kv4_cache;
+
+/* Sequences on a cache: place t of sequence s lies in page table[s ld_table + t / page_size] at t % page_size; lengths[s] places are held, at most
+ * max_pages page_size.  A page number outside 0 .. pages - 1 is no page: its places are seen by nobody, and nothing is written there.
+ * Where a call takes new tokens, cu packs them, and the new tokens of a sequence are its last places: `lengths` counts them already.  (If it counts fewer,
+ * the first of them have no place.)
+ * positions, weights (or NULL): for each (sequence, kv head, place) at s ld_sequence + head ld_head + place, with capacity for max_pages page_size places:
+ * which token of its sequence it holds, and the attention weight that it has received. */
+typedef struct oz2_kv4_sequences {
+  int64_t sequences, max_pages;
+  const int32_t* table;
+  int64_t ld_table;
+  const int32_t* lengths;
+  int64_t tokens;
+  const int32_t* cu;
+  int32_t* positions;
+  int64_t positions_sequence, positions_head;
+  float* weights;
+  int64_t weights_sequence, weights_head;
+} oz2_kv4_sequences;
+
+/* Appends the new tokens k, v (tokens x kv heads x dim, both of one type) to their places: o = the smallest value, s = (largest - smallest) / 15, both rounded
+ * to FP16, c = (x - o) (1 / s) in FP32 rounded to the nearest integer (ties to even) within 0 .. 15, 0 where s is 0.  A key or value with a NaN, an
+ * infinity, or values beyond FP16 is held as one whose values are not finite.
+ * at: NULL, or the position of every new token, stored for all heads (needs positions); weights, if there, are 0 in the new places.  held_k, held_v: NULL, or
+ * where to write what the cache now holds of k and v, rounded to their type (k and v themselves are allowed); of a token without a place too. */
+int oz2_kv4_append(const oz2_kv4_cache* cache, const oz2_kv4_sequences* on, const int32_t* at, const oz2_rows* k, const oz2_rows* v, const oz2_rows* held_k,
+                   const oz2_rows* held_v, void* stream);
+
+/* out := attention of the new tokens q (tokens x heads x dim) over their sequences' places: new token j of n sees the places before lengths - n + j + 1.
+ * The keys and values are what the cache stands for, unrounded; p s is rounded to two bf16 terms (three for FP32 results) before it meets the codes.
+ * weights, if there: weights[s, kv head, t] += sum of p over the new tokens and the query heads of that kv head.
+ * Meant for few new tokens a sequence: the cache is read once for every sixteen pairs of new token and query head of a kv head.  out shares no byte with q.
+ * Workspace (256-byte aligned): oz2_kv4_attention_workspace_bytes, 0 for what is not valid. */
+size_t oz2_kv4_attention_workspace_bytes(const oz2_kv4_cache* cache, int64_t sequences, int64_t max_pages, int64_t tokens, int64_t heads, int weights);
+int oz2_kv4_attention(const oz2_kv4_cache* cache, const oz2_kv4_sequences* on, int64_t heads, float scale, const oz2_rows* q, const oz2_rows* out, void* stream);
+int oz2_context_kv4_attention(oz2_context* ctx, const oz2_kv4_cache* cache, const oz2_kv4_sequences* on, int64_t heads, float scale, const oz2_rows* q,
+                              const oz2_rows* out, void* stream);
+
+/* Evicts from sequences that hold more than `keep` places: of every (sequence, kv head) those with the `recent` newest positions stay (position > newest -
+ * recent), and of the others those with the largest weights (a NaN counts as the largest; of equal ones the lower place), `keep` in all.  Those that stay and lie at
+ * places from `keep` on move into the places below that were given up, the i-th of them into the i-th of these; nothing else moves, since attention asks for
+ * no order.  on: positions and weights needed, cu and tokens not used; to: NULL (in place), or where lengths, positions and weights afterwards go, of the same
+ * shapes (each may be the one of `on`); `to` is written below the new lengths alone.  0 <= recent <= keep.  Heads choose for themselves, so a place then
+ * holds different tokens for different heads.  Pages that two sequences share must not be evicted in. */
+typedef struct oz2_kv4_kept {
+  int32_t* lengths;
+  int32_t* positions;
+  int64_t positions_sequence, positions_head;
+  float* weights;
+  int64_t weights_sequence, weights_head;
+} oz2_kv4_kept;
+size_t oz2_kv4_evict_workspace_bytes(const oz2_kv4_cache* cache, int64_t sequences, int64_t max_pages, int64_t keep);
+int oz2_kv4_evict(const oz2_kv4_cache* cache, const oz2_kv4_sequences* on, int64_t keep, int64_t recent, const oz2_kv4_kept* to, void* stream);
+int oz2_context_kv4_evict(oz2_context* ctx, const oz2_kv4_cache* cache, const oz2_kv4_sequences* on, int64_t keep, int64_t recent, const oz2_kv4_kept* to,
+                          void* stream);
+
 const char* oz2_status_string(int status);
 
 #ifdef __cplusplus

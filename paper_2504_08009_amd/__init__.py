@@ -10,6 +10,7 @@ from .binding import (  # noqa: F401
     oz2_stage1_convert, oz2_stage2_gemm, oz2_stage3_crt, set_workspace, workspace_bytes, workspace_layout,
     oz2_set_gemm_algorithm, oz2_gemm_algorithm_for, workspace_bytes_strassen, workspace_bytes_preferred,
     Workspace, dgemm, Context,
+    attention, KV4Cache, kv4_append, kv4_attention, kv4_attention_workspace_bytes, kv4_evict, kv4_evict_workspace_bytes,
     W4Matrix, MoeLayer, w4_matvec, w4_moe, w4_moe_workspace_bytes, OZ2_F32, OZ2_BF16, OZ2_F16, OZ2_SCORE_SOFTMAX, OZ2_SCORE_SIGMOID, OZ2_ACT_SILU, OZ2_ACT_GELU,
     OZ2_OPT_SHIFT_MODE, OZ2_OPT_PRODUCT_FORMAT, OZ2_OPT_GEMM_ALGORITHM, OZ2_OPT_KBLOCK, OZ2_OPT_BIT_SPLIT, OZ2_OPT_NONFINITE_CHECK,
 )

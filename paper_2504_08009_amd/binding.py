@@ -14,6 +14,8 @@ SYMBOLS = [
     "oz2_context_workspace_bytes", "oz2_context_dgemm", "oz2_context_dsyrk", "oz2_context_dtrmm",
     "oz2_set_kblock", "oz2_set_round_sync", "oz2_set_shift_mode", "oz2_set_product_format", "oz2_set_bit_split", "oz2_set_nonfinite_check", "oz2_set_stage_events", "oz2_calibrate_mfma", "oz2_host_kernel_choice", "oz2_host_route", "oz2_host_crt_element", "oz2_host_crt_element_digits", "oz2_host_crt_element_wide_digits", "oz2_host_residues", "oz2_host_product_residues", "oz2_host_short_product_residues", "oz2_status_string",
     "oz2_w4_matvec", "oz2_w4_moe_workspace_bytes", "oz2_w4_moe", "oz2_context_w4_moe",
+    "oz2_attention", "oz2_kv4_append", "oz2_kv4_attention_workspace_bytes", "oz2_kv4_attention", "oz2_context_kv4_attention",
+    "oz2_kv4_evict_workspace_bytes", "oz2_kv4_evict", "oz2_context_kv4_evict",
 ]
 
 
@@ -87,6 +89,16 @@ def lib():
         L.oz2_w4_moe_workspace_bytes.argtypes = [vp, i64]
         L.oz2_w4_moe.argtypes = [vp, i64, ci, vp, i64, vp, ci, vp, i64, vp, vp, vp]
         L.oz2_context_w4_moe.argtypes = [vp, vp, i64, ci, vp, i64, vp, ci, vp, i64, vp, vp, vp]
+        L.oz2_attention.argtypes = [i64, i64, vp, i64, i64, i64, cf, ci, vp, vp, vp, vp, vp]
+        L.oz2_kv4_append.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp]
+        L.oz2_kv4_attention_workspace_bytes.restype = ctypes.c_size_t
+        L.oz2_kv4_attention_workspace_bytes.argtypes = [vp, i64, i64, i64, i64, ci]
+        L.oz2_kv4_attention.argtypes = [vp, vp, i64, cf, vp, vp, vp]
+        L.oz2_context_kv4_attention.argtypes = [vp, vp, vp, i64, cf, vp, vp, vp]
+        L.oz2_kv4_evict_workspace_bytes.restype = ctypes.c_size_t
+        L.oz2_kv4_evict_workspace_bytes.argtypes = [vp, i64, i64, i64]
+        L.oz2_kv4_evict.argtypes = [vp, vp, i64, i64, vp, vp]
+        L.oz2_context_kv4_evict.argtypes = [vp, vp, vp, i64, i64, vp, vp]
         L.oz2_status_string.restype = ctypes.c_char_p
         L.oz2_status_string.argtypes = [ci]
         _lib = L
@@ -384,6 +396,32 @@ class Context:
         """(y, ids, weights) of a MoeLayer for x (tokens, d); see w4_moe."""
         return _w4_moe(lib().oz2_context_w4_moe, "oz2_context_w4_moe", (self.handle,), layer, x, active, out, ids, weights, stream)
 
+    def allocate_kv4_workspace(self, cache, table, tokens=0, heads=0, weights=False, keep=None):
+        """A workspace on the cache's device for kv4_attention with up to that many new tokens of that many query heads (0: none), with weights if they are wanted,
+        and for kv4_evict with that `keep` (None: none), on a table of that shape; any other that the context had is let go."""
+        import torch
+        sequences, max_pages = table.shape
+        nbytes = []
+        if heads:
+            nbytes.append(int(lib().oz2_kv4_attention_workspace_bytes(cache.ref, sequences, max_pages, tokens, heads, int(bool(weights)))))
+        if keep is not None:
+            nbytes.append(int(lib().oz2_kv4_evict_workspace_bytes(cache.ref, sequences, max_pages, keep)))
+        if not nbytes or 0 in nbytes:
+            raise Oz2Error("invalid cache, table, tokens, heads or keep")
+        buf = torch.empty(max(nbytes) + 256, dtype=torch.uint8, device=cache.device)
+        off = (-buf.data_ptr()) % 256
+        _check(lib().oz2_context_set_workspace(self.handle, buf.data_ptr() + off, max(nbytes)), "oz2_context_set_workspace")
+        self.buf = buf
+        return max(nbytes)
+
+    def kv4_attention(self, cache, q, cu, table, lengths, scale=None, weights=None, out=None, stream=None):
+        """Attention of the new tokens q over the cache; see kv4_attention."""
+        return _kv4_attention(lib().oz2_context_kv4_attention, "oz2_context_kv4_attention", (self.handle,), cache, q, cu, table, lengths, scale, weights, out, stream)
+
+    def kv4_evict(self, cache, table, lengths, positions, weights, keep, recent=0, out=None, stream=None):
+        """(lengths, positions, weights) after an eviction; see kv4_evict."""
+        return _kv4_evict(lib().oz2_context_kv4_evict, "oz2_context_kv4_evict", (self.handle,), cache, table, lengths, positions, weights, keep, recent, out, stream)
+
     def close(self):
         if self.handle:
             lib().oz2_context_destroy(self.handle)
@@ -655,3 +693,216 @@ def w4_moe(layer, x, active=None, out=None, ids=None, weights=None, stream=None)
 def w4_moe_workspace_bytes(layer, tokens):
     """Bytes that w4_moe takes of the registered workspace; 0 for an invalid layer or number of tokens."""
     return int(lib().oz2_w4_moe_workspace_bytes(layer.ref, tokens))
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("ld_token", ctypes.c_int64), ("ld_head", ctypes.c_int64), ("type", ctypes.c_int)]
+
+
+class _Kv4(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_int64) for f in ("pages", "page_size", "heads", "dim")] + [(f, ctypes.c_void_p) for f in ("k_codes", "v_codes")] +
+                [(f, ctypes.c_int64) for f in ("codes_page", "codes_head")] + [(f, ctypes.c_void_p) for f in ("k_scales", "v_scales")] +
+                [(f, ctypes.c_int64) for f in ("scales_page", "scales_head")])
+
+
+class _Sequences(ctypes.Structure):
+    _fields_ = [("sequences", ctypes.c_int64), ("max_pages", ctypes.c_int64), ("table", ctypes.c_void_p), ("ld_table", ctypes.c_int64), ("lengths", ctypes.c_void_p),
+                ("tokens", ctypes.c_int64), ("cu", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("positions_sequence", ctypes.c_int64),
+                ("positions_head", ctypes.c_int64), ("weights", ctypes.c_void_p), ("weights_sequence", ctypes.c_int64), ("weights_head", ctypes.c_int64)]
+
+
+class _Kept(ctypes.Structure):
+    _fields_ = [("lengths", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("positions_sequence", ctypes.c_int64), ("positions_head", ctypes.c_int64),
+                ("weights", ctypes.c_void_p), ("weights_sequence", ctypes.c_int64), ("weights_head", ctypes.c_int64)]
+
+
+def _heads(name, x, index, tokens=None, heads=None, dim=None):
+    """(tokens, heads, dim) tensor on device `index`, its last dimension contiguous, as the library sees it"""
+    shape, strides = x.shape, x.stride()
+    if len(shape) != 3 or (shape[2] > 1 and strides[2] != 1) or (tokens is not None and shape[0] != tokens) or (heads is not None and shape[1] != heads) or (
+            dim is not None and shape[2] != dim):
+        raise Oz2Error("%s is (tokens, heads, dim)%s with the last dimension contiguous, got shape %s" % (
+            name, "" if heads is None and dim is None else " = (%s, %s, %s)" % tuple("." if v is None else v for v in (tokens, heads, dim)), tuple(shape)))
+    if x.get_device() != index or index < 0:
+        raise Oz2Error("%s is on %s: tensors of one call are on one GPU" % (name, x.device))
+    return _Rows(x.data_ptr(), strides[0], strides[1], _type(x.dtype))
+
+
+def _integers(name, x, index, shape):
+    import torch
+    if x.dtype != torch.int32 or x.shape != shape or (x.dim() and x.shape[-1] > 1 and x.stride(-1) != 1):
+        raise Oz2Error("%s is int32 of shape %s, its last dimension contiguous, got %s %s" % (name, tuple(shape), x.dtype, tuple(x.shape)))
+    if x.get_device() != index:
+        raise Oz2Error("%s is on %s: tensors of one call are on one GPU" % (name, x.device))
+    return x.data_ptr()
+
+
+def _refuse_gradients(*tensors):
+    if any(v is not None and v.requires_grad for v in tensors):
+        _refuse_gradient()
+
+
+def _scale(scale, dim):
+    return dim ** -0.5 if scale is None else float(scale)
+
+
+def attention(q, k, v, cu, causal=True, scale=None, out=None, stream=None):
+    """softmax(scale q k) v over packed prompts (include/oz2.h): q (tokens, heads, dim), k and v (tokens, kv_heads, dim) of one type in float32, bfloat16 or float16, cu
+    (sequences + 1) int32 with the first row of every sequence; scale 1 / sqrt(dim) if None.  The result is like `out`, or q where it is None, and belongs to
+    the stream of the call; rows behind the last sequence are left as they were (where the result is made here, they are not set).  There is no gradient:
+    tensors that require one are refused where one would be recorded."""
+    _refuse_gradients(q, k, v, out)
+    index = q.get_device()
+    rows_q = _heads("q", q, index)
+    tokens, heads, dim = q.shape
+    rows_k = _heads("k", k, index, tokens, None, dim)
+    rows_v = _heads("v", v, index, tokens, k.shape[1], dim)
+    if out is None:
+        out = _new(q, q.shape, q.dtype, stream)
+    rows_out = _heads("out", out, index, tokens, heads, dim)
+    if cu.dim() != 1 or not cu.shape[0]:
+        raise Oz2Error("cu is (sequences + 1,) int32")
+    rc = lib().oz2_attention(tokens, cu.shape[0] - 1, _integers("cu", cu, index, cu.shape), heads, k.shape[1], dim, _scale(scale, dim), int(bool(causal)),
+                             ctypes.addressof(rows_q), ctypes.addressof(rows_k), ctypes.addressof(rows_v), ctypes.addressof(rows_out), _stream_on(stream, index))
+    if rc:
+        _check(rc, "oz2_attention")
+    return out
+
+
+class KV4Cache:
+    """A paged cache of keys and values held in 4 bits (include/oz2.h): codes (pages, kv_heads, page_size, dim / 2) uint8 and scales (pages, kv_heads, page_size, 2)
+    float16 of keys and of values, alike in strides, the last two dimensions without gaps.  The object keeps the tensors."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales):
+        import torch
+        if any(v.dim() != 4 for v in (k_codes, k_scales, v_codes, v_scales)):
+            raise Oz2Error("codes are (pages, kv_heads, page_size, dim / 2), scales (pages, kv_heads, page_size, 2)")
+        pages, heads, page_size, half = k_codes.shape
+        for name, v, dtype, last in (("k_codes", k_codes, torch.uint8, half), ("v_codes", v_codes, torch.uint8, half), ("k_scales", k_scales, torch.float16, 2),
+                                     ("v_scales", v_scales, torch.float16, 2)):
+            if v.dtype != dtype or v.shape != (pages, heads, page_size, last):
+                raise Oz2Error("%s is %s of shape %s, got %s %s" % (name, dtype, (pages, heads, page_size, last), v.dtype, tuple(v.shape)))
+            if (last > 1 and v.stride(3) != 1) or (page_size > 1 and v.stride(2) != last):
+                raise Oz2Error("the last two dimensions of %s are without gaps" % name)
+            if v.device != k_codes.device:
+                raise Oz2Error("the parts of the cache are on different devices")
+        for a, b in ((k_codes, v_codes), (k_scales, v_scales)):
+            if any(a.shape[i] > 1 and a.stride(i) != b.stride(i) for i in (0, 1)):
+                raise Oz2Error("keys and values have the same strides")
+        if k_scales.stride(0) % 2 or k_scales.stride(1) % 2:
+            raise Oz2Error("strides of scales are whole pairs")
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self.pages, self.heads, self.page_size, self.dim = pages, heads, page_size, 2 * half
+        self.device, self.index = k_codes.device, k_codes.get_device()
+        self.struct = _Kv4(pages, page_size, heads, 2 * half, k_codes.data_ptr(), v_codes.data_ptr(), k_codes.stride(0), k_codes.stride(1), k_scales.data_ptr(),
+                           v_scales.data_ptr(), k_scales.stride(0) // 2, k_scales.stride(1) // 2)
+        self.ref = ctypes.addressof(self.struct)
+
+    @classmethod
+    def empty(cls, pages, kv_heads, page_size, dim, device="cuda:0"):
+        """A cache of new tensors: its places hold zeros."""
+        import torch
+        make = lambda last, dtype: torch.zeros((pages, kv_heads, page_size, last), dtype=dtype, device=device)
+        return cls(make(dim // 2, torch.uint8), make(2, torch.float16), make(dim // 2, torch.uint8), make(2, torch.float16))
+
+
+def _places(name, x, cache, sequences, capacity, dtype):
+    if x.dtype != dtype or x.dim() != 3 or x.shape[0] != sequences or x.shape[1] != cache.heads or x.shape[2] < capacity or (x.shape[2] > 1 and x.stride(2) != 1):
+        raise Oz2Error("%s is %s of shape (sequences, kv_heads, places) = (%d, %d, at least %d), its last dimension contiguous, got %s %s" % (
+            name, dtype, sequences, cache.heads, capacity, x.dtype, tuple(x.shape)))
+    if x.get_device() != cache.index:
+        raise Oz2Error("%s is on %s: tensors of one call are on one GPU" % (name, x.device))
+    return x.data_ptr(), x.stride(0), x.stride(1)
+
+
+def _sequences(cache, table, lengths, tokens=0, cu=None, positions=None, weights=None):
+    import torch
+    if cache.index < 0:
+        raise Oz2Error("tensors on the GPU wanted, got %s" % cache.device)
+    if table.dim() != 2:
+        raise Oz2Error("table is (sequences, pages) int32")
+    sequences, max_pages = table.shape
+    capacity = max_pages * cache.page_size
+    of_positions = (None, 0, 0) if positions is None else _places("positions", positions, cache, sequences, capacity, torch.int32)
+    of_weights = (None, 0, 0) if weights is None else _places("weights", weights, cache, sequences, capacity, torch.float32)
+    return _Sequences(sequences, max_pages, _integers("table", table, cache.index, table.shape), table.stride(0),
+                      _integers("lengths", lengths, cache.index, (sequences,)), tokens, None if cu is None else _integers("cu", cu, cache.index, (sequences + 1,)),
+                      *of_positions, *of_weights)
+
+
+def kv4_append(cache, k, v, cu, table, lengths, at=None, positions=None, weights=None, held=None, stream=None):
+    """Appends the new tokens k and v (tokens, kv_heads, dim), packed by cu (sequences + 1) int32, to their sequences' last places (include/oz2.h): table (sequences, pages)
+    int32, lengths (sequences) int32 with the new tokens counted.  at (tokens) int32: positions of the new tokens, stored in positions (sequences, kv_heads,
+    places) int32; weights, of that shape in float32: set to 0 in the new places; held: (k, v) like the arguments, for what the cache then holds of them."""
+    held_k, held_v = (None, None) if held is None else held
+    _refuse_gradients(k, v, weights, held_k, held_v)
+    rows_k = _heads("k", k, cache.index, None, cache.heads, cache.dim)
+    tokens = k.shape[0]
+    rows_v = _heads("v", v, cache.index, tokens, cache.heads, cache.dim)
+    on = _sequences(cache, table, lengths, tokens, cu, positions, weights)
+    if (at is None) != (positions is None):
+        raise Oz2Error("at and positions go together")
+    of_held = []
+    for name, x in (("held k", held_k), ("held v", held_v)):
+        of_held.append(None if x is None else _heads(name, x, cache.index, tokens, cache.heads, cache.dim))
+    rc = lib().oz2_kv4_append(cache.ref, ctypes.addressof(on), None if at is None else _integers("at", at, cache.index, (tokens,)), ctypes.addressof(rows_k),
+                              ctypes.addressof(rows_v), *(None if r is None else ctypes.addressof(r) for r in of_held), _stream_on(stream, cache.index))
+    if rc:
+        _check(rc, "oz2_kv4_append")
+
+
+def _kv4_attention(call, name, first, cache, q, cu, table, lengths, scale, weights, out, stream):
+    _refuse_gradients(q, weights, out)
+    rows_q = _heads("q", q, cache.index, None, None, cache.dim)
+    tokens, heads, dim = q.shape
+    if out is None:
+        out = _new(q, q.shape, q.dtype, stream)
+    rows_out = _heads("out", out, cache.index, tokens, heads, dim)
+    on = _sequences(cache, table, lengths, tokens, cu, None, weights)
+    rc = call(*first, cache.ref, ctypes.addressof(on), heads, _scale(scale, dim), ctypes.addressof(rows_q), ctypes.addressof(rows_out),
+              _stream_on(stream, cache.index))
+    if rc:
+        _check(rc, name)
+    return out
+
+
+def kv4_attention(cache, q, cu, table, lengths, scale=None, weights=None, out=None, stream=None):
+    """Attention of the new tokens q (tokens, heads, dim), packed by cu, over their sequences' places (include/oz2.h), in the workspace that set_workspace registered: a
+    sequence's new tokens are its last ones, and each sees the places up to its own.  weights (sequences, kv_heads, places) float32: what every place received is
+    added.  Streams, results and gradients as for attention."""
+    return _kv4_attention(lib().oz2_kv4_attention, "oz2_kv4_attention", (), cache, q, cu, table, lengths, scale, weights, out, stream)
+
+
+def kv4_attention_workspace_bytes(cache, table, tokens, heads, weights=False):
+    """Bytes that kv4_attention takes of the registered workspace on a table of that shape; 0 for what is not valid."""
+    return int(lib().oz2_kv4_attention_workspace_bytes(cache.ref, table.shape[0], table.shape[1], tokens, heads, int(bool(weights))))
+
+
+def _kv4_evict(call, name, first, cache, table, lengths, positions, weights, keep, recent, out, stream):
+    import torch
+    _refuse_gradients(weights, *(out or ()))
+    on = _sequences(cache, table, lengths, 0, None, positions, weights)
+    if positions is None or weights is None:
+        raise Oz2Error("positions and weights are needed")
+    kept = None
+    if out is not None:
+        to_lengths, to_positions, to_weights = out
+        capacity = table.shape[1] * cache.page_size
+        kept = _Kept(_integers("lengths", to_lengths, cache.index, (table.shape[0],)), *_places("positions", to_positions, cache, table.shape[0], capacity, torch.int32),
+                     *_places("weights", to_weights, cache, table.shape[0], capacity, torch.float32))
+    rc = call(*first, cache.ref, ctypes.addressof(on), int(keep), int(recent), None if kept is None else ctypes.addressof(kept), _stream_on(stream, cache.index))
+    if rc:
+        _check(rc, name)
+    return (lengths, positions, weights) if out is None else tuple(out)
+
+
+def kv4_evict(cache, table, lengths, positions, weights, keep, recent=0, out=None, stream=None):
+    """(lengths, positions, weights) with at most `keep` places of every sequence (include/oz2.h): the `recent` newest stay, and of the others those with the largest
+    weights; the cache's tokens move into the first `keep` places.  In place, or where out = (lengths, positions, weights) says; in the workspace that
+    set_workspace registered."""
+    return _kv4_evict(lib().oz2_kv4_evict, "oz2_kv4_evict", (), cache, table, lengths, positions, weights, keep, recent, out, stream)
+
+
+def kv4_evict_workspace_bytes(cache, table, keep):
+    """Bytes that kv4_evict takes of the registered workspace on a table of that shape; 0 for what is not valid."""
+    return int(lib().oz2_kv4_evict_workspace_bytes(cache.ref, table.shape[0], table.shape[1], keep))

@@ -1,10 +1,12 @@
 // C ABI of liboz2 (see include/oz2.h): argument checks, workspace bookkeeping, stage sequencing.
+#include <cmath>
 #include <mutex>
 #include <new>
 
 #include "../../include/oz2.h"
 #include "oz2_bound.h"
 #include "oz2_internal.h"
+#include "oz2_kv4.h"
 #include "oz2_route.h"
 #include "oz2_w4.h"
 
@@ -943,6 +945,169 @@ int oz2_context_w4_moe(oz2_context* ctx, const oz2_moe_layer* layer, int64_t t, 
                        const uint8_t* active, int y_type, void* Y, int64_t ldy, int32_t* ids, float* weights, void* stream) {
   UseContext use(ctx);
   const int rc = oz2_w4_moe(layer, t, x_type, X, ldx, active, y_type, Y, ldy, ids, weights, stream);
+  return rc < 0 ? rc - 1 : rc;
+}
+
+namespace {
+// Rows of width `width` at i step_a + j step_b (i < a, j < b) that do not overlap: the smaller step keeps rows apart, the larger one runs of them.
+bool lattice_ok(int64_t width, int64_t a, int64_t step_a, int64_t b, int64_t step_b) {
+  if ((a > 1 && step_a < width) || (b > 1 && step_b < width)) return false;
+  typedef __int128 wide;
+  if ((a > 1 ? (wide)(a - 1) * step_a : 0) + (b > 1 ? (wide)(b - 1) * step_b : 0) >= (wide)1 << 46) return false;  // (no memory is that large)
+  if (a <= 1 || b <= 1) return true;
+  return step_a < step_b ? step_b - width >= (a - 1) * step_a : step_a - width >= (b - 1) * step_b;
+}
+bool rows_ok(const oz2_rows* r, int64_t tokens, int64_t heads, int64_t dim) {
+  return r && type_ok(r->type) && (tokens == 0 || r->data) && lattice_ok(dim, tokens, r->ld_token, heads, r->ld_head);
+}
+// Whether two tensors of heads have no byte in common, as far as that is easily seen: one lies behind the other, or a token's heads lie between those of the
+// other's tokens, like parts of one packed tensor.
+bool rows_apart(const oz2_rows& a, int64_t heads_a, const oz2_rows& b, int64_t heads_b, int64_t tokens, int64_t dim) {
+  const int64_t size_a = size_of(a.type), size_b = size_of(b.type);
+  // (a stride of a single token or head says nothing)
+  const int64_t token_a = ((heads_a > 1 ? (heads_a - 1) * a.ld_head : 0) + dim) * size_a, token_b = ((heads_b > 1 ? (heads_b - 1) * b.ld_head : 0) + dim) * size_b;
+  const int64_t more_a = tokens > 1 ? (tokens - 1) * a.ld_token * size_a : 0, more_b = tokens > 1 ? (tokens - 1) * b.ld_token * size_b : 0;
+  const int64_t bytes_a = more_a + token_a, bytes_b = more_b + token_b;
+  const uintptr_t pa = (uintptr_t)a.data, pb = (uintptr_t)b.data;
+  if (pa >= pb + bytes_b || pb >= pa + bytes_a) return true;
+  if (tokens == 1) return false;
+  const int64_t step = a.ld_token * size_a;
+  if (step != b.ld_token * size_b || step < token_a || step < token_b) return false;
+  int64_t from = (int64_t)(pb - pa) % step;
+  if (from < 0) from += step;
+  return from >= token_a && from + token_b <= step;
+}
+bool same_rows(const oz2_rows& a, const oz2_rows& b) {
+  return a.data == b.data && a.ld_token == b.ld_token && a.ld_head == b.ld_head && a.type == b.type;
+}
+
+constexpr int64_t kMostRows = (int64_t)1 << 24, kMostSequences = 65535;  // (sequences and heads are grid extents)
+
+bool cache_ok(const oz2_kv4_cache* c) {
+  if (!c || c->pages < 1 || c->pages > INT32_MAX || c->heads < 1 || c->heads > 65535) return false;
+  if (c->page_size < 16 || c->page_size % 16 || c->page_size > ((int64_t)1 << 24) || c->dim < 8 || c->dim % 8 || c->dim > OZ2_ATTENTION_MAX_DIM) return false;
+  if (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales) return false;
+  if (((uintptr_t)c->k_codes | (uintptr_t)c->v_codes) % 4 || ((uintptr_t)c->k_scales | (uintptr_t)c->v_scales) % 16) return false;
+  if ((c->pages > 1 && (c->codes_page % 4 || c->scales_page % 4)) || (c->heads > 1 && (c->codes_head % 4 || c->scales_head % 4))) return false;
+  return lattice_ok(c->page_size * c->dim / 2, c->pages, c->codes_page, c->heads, c->codes_head) &&
+         lattice_ok(c->page_size, c->pages, c->scales_page, c->heads, c->scales_head);
+}
+bool capacity_ok(const oz2_kv4_cache& c, int64_t sequences, int64_t max_pages) {
+  return sequences >= 0 && sequences <= kMostSequences && sequences * c.heads <= ((int64_t)1 << 21) && max_pages >= 0 &&
+         max_pages <= (((int64_t)1 << 31) - 65536) / c.page_size;
+}
+// arrays of (sequence, head, place)
+bool places_ok(const oz2_kv4_cache& c, const oz2_kv4_sequences& on, int64_t sequence, int64_t head) {
+  const int64_t capacity = on.max_pages * c.page_size;
+  return capacity == 0 || lattice_ok(capacity, on.sequences, sequence, c.heads, head);
+}
+bool sequences_ok(const oz2_kv4_cache& c, const oz2_kv4_sequences* on, bool fresh) {
+  if (!on || !capacity_ok(c, on->sequences, on->max_pages)) return false;
+  if (fresh && (on->tokens < 0 || on->tokens * c.heads > ((int64_t)1 << 26))) return false;
+  if (on->sequences == 0) return true;
+  if (!on->lengths || (fresh && !on->cu) || (on->max_pages && !on->table) || (on->sequences > 1 && on->ld_table < on->max_pages)) return false;
+  return (!on->positions || places_ok(c, *on, on->positions_sequence, on->positions_head)) &&
+         (!on->weights || places_ok(c, *on, on->weights_sequence, on->weights_head));
+}
+bool scale_ok(float scale) { return scale > 0.f && std::isfinite(scale); }
+}  // namespace
+
+int oz2_attention(int64_t tokens, int64_t sequences, const int32_t* cu, int64_t heads, int64_t kv_heads, int64_t dim, float scale, int causal,
+                  const oz2_rows* q, const oz2_rows* k, const oz2_rows* v, const oz2_rows* out, void* stream) {
+  if (tokens < 0 || tokens > ((int64_t)1 << 28)) return -1;
+  if (sequences < 0 || sequences > ((int64_t)1 << 20)) return -2;
+  if (heads < 1 || heads > 65535 || tokens * heads > ((int64_t)1 << 28)) return -4;
+  if (kv_heads < 1 || heads % kv_heads) return -5;
+  if (dim < 1 || dim > OZ2_ATTENTION_MAX_DIM) return -6;
+  if (!scale_ok(scale)) return -7;
+  if (!rows_ok(q, tokens, heads, dim)) return -9;
+  if (!rows_ok(k, tokens, kv_heads, dim) || k->type != q->type) return -10;
+  if (!rows_ok(v, tokens, kv_heads, dim) || v->type != q->type) return -11;
+  if (!rows_ok(out, tokens, heads, dim)) return -12;
+  if (tokens == 0 || sequences == 0) return OZ2_OK;
+  if (!cu) return -3;
+  if (!rows_apart(*out, heads, *q, heads, tokens, dim) || !rows_apart(*out, heads, *k, kv_heads, tokens, dim) ||
+      !rows_apart(*out, heads, *v, kv_heads, tokens, dim))
+    return -12;
+  return oz2_launch_attention(tokens, sequences, cu, heads, kv_heads, dim, scale, causal, *q, *k, *v, *out, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? OZ2_OK : OZ2_ERR_HIP;
+}
+
+int oz2_kv4_append(const oz2_kv4_cache* cache, const oz2_kv4_sequences* on, const int32_t* at, const oz2_rows* k, const oz2_rows* v, const oz2_rows* held_k,
+                   const oz2_rows* held_v, void* stream) {
+  if (!cache_ok(cache)) return -1;
+  if (!sequences_ok(*cache, on, true)) return -2;
+  if (at && !on->positions) return -3;
+  const int64_t tokens = on->tokens, heads = cache->heads, dim = cache->dim;
+  if (!rows_ok(k, tokens, heads, dim)) return -4;
+  if (!rows_ok(v, tokens, heads, dim) || v->type != k->type) return -5;
+  if (held_k && (!rows_ok(held_k, tokens, heads, dim) || held_k->type != k->type)) return -6;
+  if (held_v && (!rows_ok(held_v, tokens, heads, dim) || held_v->type != k->type)) return -7;
+  if (tokens == 0 || on->sequences == 0) return OZ2_OK;
+  if (held_k && !((same_rows(*held_k, *k) || rows_apart(*held_k, heads, *k, heads, tokens, dim)) && rows_apart(*held_k, heads, *v, heads, tokens, dim))) return -6;
+  if (held_v && !((same_rows(*held_v, *v) || rows_apart(*held_v, heads, *v, heads, tokens, dim)) && rows_apart(*held_v, heads, *k, heads, tokens, dim))) return -7;
+  if (held_k && held_v && !rows_apart(*held_k, heads, *held_v, heads, tokens, dim)) return -7;
+  return oz2_launch_kv4_append(*cache, *on, at, *k, *v, held_k, held_v, static_cast<hipStream_t>(stream)) == hipSuccess ? OZ2_OK : OZ2_ERR_HIP;
+}
+
+size_t oz2_kv4_attention_workspace_bytes(const oz2_kv4_cache* cache, int64_t sequences, int64_t max_pages, int64_t tokens, int64_t heads, int weights) {
+  if (!cache_ok(cache) || !capacity_ok(*cache, sequences, max_pages) || tokens < 0 || heads < 1 || heads % cache->heads || tokens > kMostRows / heads) return 0;
+  return oz2_kv4_attention_space(*cache, sequences, max_pages, tokens, heads, weights) + 256;
+}
+
+int oz2_kv4_attention(const oz2_kv4_cache* cache, const oz2_kv4_sequences* on, int64_t heads, float scale, const oz2_rows* q, const oz2_rows* out, void* stream) {
+  if (!cache_ok(cache)) return -1;
+  if (!sequences_ok(*cache, on, true)) return -2;
+  const int64_t tokens = on->tokens;
+  if (heads < 1 || heads % cache->heads || tokens > kMostRows / heads) return -3;
+  if (!scale_ok(scale)) return -4;
+  if (!rows_ok(q, tokens, heads, cache->dim)) return -5;
+  if (!rows_ok(out, tokens, heads, cache->dim)) return -6;
+  if (tokens == 0 || on->sequences == 0) return OZ2_OK;
+  if (!rows_apart(*out, heads, *q, heads, tokens, cache->dim)) return -6;
+  State& s = state();
+  std::lock_guard<std::mutex> lock(s.mu);
+  if (!s.ws || s.ws_bytes < oz2_kv4_attention_space(*cache, on->sequences, on->max_pages, tokens, heads, on->weights != nullptr)) return OZ2_ERR_WORKSPACE;
+  return oz2_launch_kv4_attention(*cache, *on, heads, scale, *q, *out, s.ws, static_cast<hipStream_t>(stream)) == hipSuccess ? OZ2_OK : OZ2_ERR_HIP;
+}
+
+int oz2_context_kv4_attention(oz2_context* ctx, const oz2_kv4_cache* cache, const oz2_kv4_sequences* on, int64_t heads, float scale, const oz2_rows* q,
+                              const oz2_rows* out, void* stream) {
+  UseContext use(ctx);
+  const int rc = oz2_kv4_attention(cache, on, heads, scale, q, out, stream);
+  return rc < 0 ? rc - 1 : rc;
+}
+
+size_t oz2_kv4_evict_workspace_bytes(const oz2_kv4_cache* cache, int64_t sequences, int64_t max_pages, int64_t keep) {
+  if (!cache_ok(cache) || !capacity_ok(*cache, sequences, max_pages) || keep < 0) return 0;
+  return oz2_kv4_evict_space(*cache, sequences, max_pages, keep) + 256;
+}
+
+int oz2_kv4_evict(const oz2_kv4_cache* cache, const oz2_kv4_sequences* on, int64_t keep, int64_t recent, const oz2_kv4_kept* to, void* stream) {
+  if (!cache_ok(cache)) return -1;
+  if (!sequences_ok(*cache, on, false) || (on->sequences && (!on->positions || !on->weights))) return -2;
+  if (keep < 0) return -3;
+  if (recent < 0 || recent > keep) return -4;
+  oz2_kv4_kept here = {const_cast<int32_t*>(on->lengths), on->positions, on->positions_sequence, on->positions_head, on->weights, on->weights_sequence, on->weights_head};
+  if (to) {
+    if (on->sequences && (!to->lengths || !to->positions || !to->weights)) return -5;
+    if (!places_ok(*cache, *on, to->positions_sequence, to->positions_head) || !places_ok(*cache, *on, to->weights_sequence, to->weights_head)) return -5;
+    // the same array with other strides would be read and written at once
+    if (to->positions == on->positions && (to->positions_sequence != on->positions_sequence || to->positions_head != on->positions_head)) return -5;
+    if (to->weights == on->weights && (to->weights_sequence != on->weights_sequence || to->weights_head != on->weights_head)) return -5;
+    here = *to;
+  }
+  if (on->sequences == 0) return OZ2_OK;
+  State& s = state();
+  std::lock_guard<std::mutex> lock(s.mu);
+  if (!s.ws || s.ws_bytes < oz2_kv4_evict_space(*cache, on->sequences, on->max_pages, keep)) return OZ2_ERR_WORKSPACE;
+  return oz2_launch_kv4_evict(*cache, *on, keep, recent, here, s.ws, static_cast<hipStream_t>(stream)) == hipSuccess ? OZ2_OK : OZ2_ERR_HIP;
+}
+
+int oz2_context_kv4_evict(oz2_context* ctx, const oz2_kv4_cache* cache, const oz2_kv4_sequences* on, int64_t keep, int64_t recent, const oz2_kv4_kept* to,
+                          void* stream) {
+  UseContext use(ctx);
+  const int rc = oz2_kv4_evict(cache, on, keep, recent, to, stream);
   return rc < 0 ? rc - 1 : rc;
 }
 

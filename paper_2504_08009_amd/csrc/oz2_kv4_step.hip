@@ -1,0 +1,119 @@
+// Attention of a few new tokens over a cache held in 4 bits (oz2_kv4_attention): how the work is cut, and how its parts come together.
+#include "oz2_kv4_step.h"
+
+extern template hipError_t oz2_kv4_step_of<OZ2_F32>(const Kv4Step&, dim3, hipStream_t);
+extern template hipError_t oz2_kv4_step_of<OZ2_BF16>(const Kv4Step&, dim3, hipStream_t);
+extern template hipError_t oz2_kv4_step_of<OZ2_F16>(const Kv4Step&, dim3, hipStream_t);
+
+namespace {
+
+// One wave a row: the parts of its chunks, each with a maximum of its own.
+__global__ void __launch_bounds__(256) kv4_join_kernel(Kv4Step a) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+  const int lane = threadIdx.x % 64;
+  if (row >= a.rows) return;
+  const int64_t token = row / a.heads, query = row % a.heads;
+  const int64_t s = kv_sequence(a.on.cu, a.on.sequences, token);
+  const KvRange r = kv_range(a.on.cu, s, a.on.tokens);
+  if (token < r.begin || token >= r.end) return;
+  const int held = kv_held(a.on.lengths, s, a.capacity);
+  if (held <= a.chunk) return;
+  const int chunks = (held + a.chunk - 1) / a.chunk;
+  float high = -3e38f, total = 0.f;
+  for (int i = lane; i < chunks; i += 64) high = fmaxf(high, a.stats[(i * a.rows + row) * 2]);
+  for (int d = 32; d; d /= 2) high = fmaxf(high, __shfl_xor(high, d));
+  float v[4] = {};
+  for (int i = 0; i < chunks; ++i) {
+    const float f = __builtin_amdgcn_exp2f(a.stats[(i * a.rows + row) * 2] - high);
+    total = fmaf(f, a.stats[(i * a.rows + row) * 2 + 1], total);
+    const float* part = a.part + (i * a.rows + row) * a.dim;
+    for (int j = 0; j < 4; ++j)
+      if (j * 64 + lane < a.dim) v[j] = fmaf(f, part[j * 64 + lane], v[j]);
+  }
+  for (int j = 0; j < 4; ++j)
+    if (j * 64 + lane < a.dim)
+      w4_store(a.out.type, a.out.data, token * a.out.ld_token + query * a.out.ld_head + j * 64 + lane, total == 0.f ? 0.f : v[j] / total);
+}
+
+// What each place received, from the scores and the rows' maxima and sums.
+__global__ void __launch_bounds__(256) kv4_received_kernel(Kv4Step a) {
+  __shared__ float top[64], inverse[64];
+  const int head = blockIdx.y, s = blockIdx.z, place = blockIdx.x * 256 + threadIdx.x;
+  const KvRange r = kv_range(a.on.cu, s, a.on.tokens);
+  const int held = kv_held(a.on.lengths, s, a.capacity), rows = (int)(r.end - r.begin) * a.group;
+  if ((int)blockIdx.x * 256 >= held || rows == 0) return;
+  const int chunks = (held + a.chunk - 1) / a.chunk;
+  float sum = 0.f;
+  for (int r0 = 0; r0 < rows; r0 += 64) {
+    __syncthreads();
+    const int n = min(64, rows - r0);
+    if ((int)threadIdx.x < n) {
+      const int fresh = (r0 + threadIdx.x) / a.group;
+      const int64_t row = (r.begin + fresh) * a.heads + head * a.group + (r0 + threadIdx.x - fresh * a.group);
+      float high = -3e38f, total = 0.f;
+      for (int i = 0; i < chunks; ++i) high = fmaxf(high, a.stats[(i * a.rows + row) * 2]);
+      for (int i = 0; i < chunks; ++i) total = fmaf(__builtin_amdgcn_exp2f(a.stats[(i * a.rows + row) * 2] - high), a.stats[(i * a.rows + row) * 2 + 1], total);
+      top[threadIdx.x] = high;
+      inverse[threadIdx.x] = total == 0.f ? 0.f : 1.f / total;
+    }
+    __syncthreads();
+    if (place < held) {
+      for (int i = 0; i < n; ++i) {
+        const int fresh = (r0 + i) / a.group;
+        const int64_t row = (r.begin + fresh) * a.heads + head * a.group + (r0 + i - fresh * a.group);
+        sum = fmaf(__builtin_amdgcn_exp2f(fmaf(a.scores[row * a.capacity + place], a.scale2, -top[i])), inverse[i], sum);
+      }
+    }
+  }
+  if (place < held) a.on.weights[s * a.on.weights_sequence + head * a.on.weights_head + place] += sum;
+}
+
+int64_t chunk_of(int64_t capacity, int64_t pairs) {
+  const int64_t each = (capacity * pairs + 4095) / 4096;
+  const int64_t chunk = (each + 127) / 128 * 128;
+  return chunk < 128 ? 128 : chunk;
+}
+size_t rounded(int64_t n) { return (size_t)((n + 63) / 64 * 64) * 4; }
+struct Space { size_t part, stats, scores; };
+Space space(int64_t capacity, int64_t chunk, int64_t rows, int64_t dim, bool weights) {
+  const int64_t chunks = (capacity + chunk - 1) / chunk;
+  return {chunks > 1 ? rounded(chunks * rows * dim) : 0, chunks > 1 || weights ? rounded(chunks * rows * 2) : 0, weights ? rounded(rows * capacity) : 0};
+}
+
+}  // namespace
+
+size_t oz2_kv4_attention_space(const oz2_kv4_cache& cache, int64_t sequences, int64_t max_pages, int64_t tokens, int64_t heads, int weights) {
+  const int64_t capacity = max_pages * cache.page_size;
+  const Space n = space(capacity, chunk_of(capacity, sequences * cache.heads), tokens * heads, cache.dim, weights != 0);
+  return n.part + n.stats + n.scores;
+}
+
+hipError_t oz2_launch_kv4_attention(const oz2_kv4_cache& cache, const oz2_kv4_sequences& on, int64_t heads, float scale, const oz2_rows& q,
+                                    const oz2_rows& out, char* ws, hipStream_t st) {
+  const int64_t capacity = on.max_pages * cache.page_size, chunk = chunk_of(capacity, on.sequences * cache.heads), rows = on.tokens * heads;
+  const int64_t chunks = capacity ? (capacity + chunk - 1) / chunk : 1;
+  const Space n = space(capacity, chunk, rows, cache.dim, on.weights != nullptr);
+  Kv4Step a = {};
+  a.c = cache, a.on = on, a.q = q, a.out = out;
+  a.heads = (int)heads, a.group = (int)(heads / cache.heads), a.dim = (int)cache.dim, a.capacity = (int)capacity;
+  a.page_size = (int)cache.page_size, a.chunk = (int)chunk;
+  a.per_page = fast_div((unsigned)cache.page_size), a.per_group = fast_div((unsigned)a.group);
+  a.scale2 = scale * 1.44269504088896340736f;
+  a.part = n.part ? reinterpret_cast<float*>(ws) : nullptr;
+  a.stats = n.stats ? reinterpret_cast<float*>(ws + n.part) : nullptr;
+  a.scores = n.scores ? reinterpret_cast<float*>(ws + n.part + n.stats) : nullptr;
+  a.rows = rows;
+  const dim3 grid((unsigned)chunks, (unsigned)cache.heads, (unsigned)on.sequences);
+  hipError_t rc = q.type == OZ2_F32    ? oz2_kv4_step_of<OZ2_F32>(a, grid, st)
+                  : q.type == OZ2_BF16 ? oz2_kv4_step_of<OZ2_BF16>(a, grid, st)
+                                       : oz2_kv4_step_of<OZ2_F16>(a, grid, st);
+  if (rc == hipSuccess && chunks > 1) {
+    hipLaunchKernelGGL(kv4_join_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a);
+    rc = hipGetLastError();
+  }
+  if (rc == hipSuccess && on.weights && capacity) {
+    hipLaunchKernelGGL(kv4_received_kernel, dim3((unsigned)((capacity + 255) / 256), (unsigned)cache.heads, (unsigned)on.sequences), dim3(256), 0, st, a);
+    rc = hipGetLastError();
+  }
+  return rc;
+}
