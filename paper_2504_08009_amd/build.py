@@ -32,6 +32,8 @@ EXTRA_FLAGS = {
     "oz2_w4_moe_f16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "oz2_w4_moe_down.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "oz2_attention_any.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "oz2_attention_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "oz2_attention_f16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "oz2_kv4_step_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "oz2_kv4_step_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "oz2_kv4_step_f16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],

@@ -1018,6 +1018,7 @@ int oz2_attention(int64_t tokens, int64_t sequences, const int32_t* cu, int64_t 
   if (sequences < 0 || sequences > ((int64_t)1 << 20)) return -2;
   if (heads < 1 || heads > 65535 || tokens * heads > ((int64_t)1 << 28)) return -4;
   if (kv_heads < 1 || heads % kv_heads) return -5;
+  if (sequences * kv_heads > ((int64_t)1 << 22)) return -2;
   if (dim < 1 || dim > OZ2_ATTENTION_MAX_DIM) return -6;
   if (!scale_ok(scale)) return -7;
   if (!rows_ok(q, tokens, heads, dim)) return -9;

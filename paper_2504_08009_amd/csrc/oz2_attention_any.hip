@@ -129,10 +129,3 @@ hipError_t of(const Attention& a, hipStream_t st) {
 hipError_t oz2_attention_any(const Attention& a, hipStream_t st) {
   return a.q.type == OZ2_F32 ? of<OZ2_F32>(a, st) : a.q.type == OZ2_BF16 ? of<OZ2_BF16>(a, st) : of<OZ2_F16>(a, st);
 }
-
-hipError_t oz2_launch_attention(int64_t tokens, int64_t sequences, const int32_t* cu, int64_t heads, int64_t kv_heads, int64_t dim, float scale, int causal,
-                                const oz2_rows& q, const oz2_rows& k, const oz2_rows& v, const oz2_rows& out, hipStream_t st) {
-  Attention a = {cu, q, k, v, out, tokens, sequences, (int)heads, (int)kv_heads, (int)(heads / kv_heads), (int)dim, causal != 0,
-                 scale * 1.44269504088896340736f, fast_div((unsigned)(heads / kv_heads))};
-  return oz2_attention_any(a, st);
-}

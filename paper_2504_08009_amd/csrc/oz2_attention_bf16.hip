@@ -1,0 +1,4 @@
+// oz2_attention in BF16.
+#include "oz2_attention_tile.h"
+
+template hipError_t oz2_attention_tile_of<OZ2_BF16>(const Attention&, hipStream_t);

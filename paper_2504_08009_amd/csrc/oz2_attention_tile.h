@@ -1,0 +1,332 @@
+// Attention over packed prompts in BF16 and FP16 on the matrix cores: the kernel of one type and of dims up to DP.
+//
+// A workgroup of four waves has 128 NQ rows, a wave 32 NQ of them, which are the columns of its products (32 x 32 x 16): keys x rows, then dims x rows.  So
+// a lane has one row (for each of NQ) throughout, maxima and sums stay in lanes, and what it holds of the first product, rounded, is its part of the second one's
+// operand as it is: of sixteen keys the lanes' lower half has 0..3 and 8..11, the upper half 4..7 and 12..15, and the values are read in that order.
+//   Keys and values come through LDS in tiles of 64, in two buffers: global loads at the begin of a stretch of work, stores to LDS at its end, one barrier.
+// Values are wanted with keys along a lane's words: ds_read_b64_tr_b16 turns 4 x 16 of them on their way.
+//   A step takes 32 keys, and works on three of them at once, none of which waits for another: scores of step j + 1 and values of step j - 1 on the matrix cores, the
+// exponentials of step j on the vector units.  m follows the maximum only where a score is more than 2^8 above it, which hardly happens after the
+// first tile; so the sums are hardly ever rescaled.
+#ifndef OZ2_ATTENTION_TILE_H
+#define OZ2_ATTENTION_TILE_H
+
+#include "oz2_attention.h"
+#include "oz2_w4_core.h"
+
+#ifdef __HIPCC__
+
+typedef float at_f16 __attribute__((ext_vector_type(16)));
+typedef short at_s4 __attribute__((ext_vector_type(4)));
+typedef unsigned at_u2 __attribute__((ext_vector_type(2)));
+
+constexpr int kTileKeys = 64;
+
+template <int XT>
+__device__ __forceinline__ at_f16 at_mfma(w4_u4 a, w4_u4 b, at_f16 c) {
+  if constexpr (XT == OZ2_F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(w4_h8, a), __builtin_bit_cast(w4_h8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(w4_bf8, a), __builtin_bit_cast(w4_bf8, b), c, 0, 0, 0);
+}
+template <int XT>
+__device__ __forceinline__ unsigned at_pair(float a, float b) {
+  if constexpr (XT == OZ2_F16) return __builtin_bit_cast(uint16_t, (_Float16)a) | (unsigned)__builtin_bit_cast(uint16_t, (_Float16)b) << 16;
+  else return __builtin_bit_cast(uint16_t, (__bf16)a) | (unsigned)__builtin_bit_cast(uint16_t, (__bf16)b) << 16;
+}
+template <int XT>
+__device__ __forceinline__ float at_value(unsigned w, int upper) {
+  if constexpr (XT == OZ2_F16) return (float)__builtin_bit_cast(_Float16, (uint16_t)(upper ? w >> 16 : w));
+  else return __uint_as_float(upper ? w & 0xffff0000u : w << 16);
+}
+// whether either of a pair is not finite
+template <int XT>
+__device__ __forceinline__ bool at_odd(unsigned w) {
+  constexpr unsigned top = XT == OZ2_F16 ? 0x7c00u : 0x7f80u;
+  return (w & top) == top || (w & top << 16) == top << 16;
+}
+
+template <int XT, int DP, int NQ>
+__global__ void __launch_bounds__(256, 1) attention_tile_kernel(Attention a) {
+  constexpr int E = DP / 16, F = DP / 32, ROW = DP <= 64 ? 128 : DP <= 128 ? 256 : 512;  // bytes of a row in LDS
+  constexpr int ROWS = 128 * NQ, LOADS = kTileKeys * ROW / 4096, TILE = kTileKeys * ROW;
+  __shared__ __attribute__((aligned(16))) char lds[4 * TILE];  // keys, keys, values, values
+  __shared__ int odd[2];                                       // whether a tile of values has one that is not finite
+  __shared__ float weights[4][32][32 * NQ];                    // (where it has)
+
+  const int tiles = (int)((unsigned)gridDim.x / (unsigned)a.kv_heads);
+  const int head = blockIdx.x % a.kv_heads, lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 32, half = lane / 32;
+  const AttentionTile tile = attention_tile(a, tiles - 1 - (int)(blockIdx.x / a.kv_heads), ROWS);
+  const int rows = tile.tokens * a.group;
+  if (tile.first >= rows) return;
+
+  // keys that the wave's rows see at all, and that all of them see; and the workgroup's
+  const int first_row = tile.first + wave * 32 * NQ, last_row = min(first_row + 32 * NQ, rows) - 1;
+  const int end = first_row >= rows ? 0 : a.causal ? last_row / a.per_group + 1 : tile.tokens;
+  const int full = first_row >= rows ? 0 : a.causal ? first_row / a.per_group + 1 : tile.tokens;
+  const int all = a.causal ? min(tile.first + ROWS - 1, rows - 1) / a.per_group + 1 : tile.tokens;
+  const int steps = (end + 31) / 32, groups = (((all + 31) / 32) + 1) / 2;
+
+  int sees[NQ];
+  w4_u4 q[NQ][E];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const int row = min(first_row + 32 * n + col, rows - 1), at = row / a.per_group;
+    const int64_t query = (int64_t)head * a.group + (row - at * a.group);
+    sees[n] = a.causal ? at + 1 : tile.tokens;
+    const uint16_t* from = static_cast<const uint16_t*>(a.q.data) + (tile.begin + at) * a.q.ld_token + query * a.q.ld_head;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int d = 16 * e + 8 * half;
+      q[n][e] = w4_u4{0, 0, 0, 0};
+      if (d < a.dim) q[n][e] = *reinterpret_cast<const w4_u4*>(from + d);
+    }
+  }
+
+  // a thread's pieces of a tile, sixteen bytes each of every PER-th key, and their places in LDS
+  constexpr int PER = 256 / (ROW / 16);
+  const int of_key = threadIdx.x / (ROW / 16), piece = threadIdx.x % (ROW / 16);
+  // (sixteen keys' pieces of one place, and four keys' 64 bytes, lie in all banks)
+  const int to_k = of_key * ROW + (piece ^ (ROW == 128 ? of_key / 2 % 8 : of_key % 16)) * 16;
+  const int to_v = 2 * TILE + of_key * ROW + (piece / 4 ^ (ROW == 128 ? of_key / 2 % 2 : of_key % 4)) * 64 + piece % 4 * 16;
+  static_assert(ROW == 512 || PER % 16 == 0, "a thread's keys have one swizzle");
+  const char* k_from = static_cast<const char*>(a.k.data) + (tile.begin * a.k.ld_token + head * a.k.ld_head) * 2;
+  const char* v_from = static_cast<const char*>(a.v.data) + (tile.begin * a.v.ld_token + head * a.v.ld_head) * 2;
+  const int k_step = (int)(a.k.ld_token * 2), v_step = (int)(a.v.ld_token * 2);
+  auto fetch = [&](const char* from, int step, int64_t first, w4_u4 (&r)[LOADS]) {
+    const int most = (int)min((int64_t)kTileKeys, tile.tokens - first) - 1;
+    from += first * step;
+    const unsigned at = of_key * step + piece * 16;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      r[i] = w4_u4{0, 0, 0, 0};
+      if (of_key + i * PER <= most && piece * 8 < a.dim) r[i] = *reinterpret_cast<const w4_u4*>(from + i * PER * step + at);
+    }
+  };
+  auto store_k = [&](int buffer, const w4_u4 (&r)[LOADS]) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) *reinterpret_cast<w4_u4*>(lds + buffer * TILE + (to_k ^ (ROW == 512 && i % 2 ? 128 : 0)) + i * PER * ROW) = r[i];
+  };
+  auto store_v = [&](int buffer, int first, const w4_u4 (&r)[LOADS]) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) *reinterpret_cast<w4_u4*>(lds + buffer * TILE + to_v + i * PER * ROW) = r[i];
+    // (only where a key may be hidden from a row does it matter)
+    if (a.causal && first + kTileKeys > tile.first / a.per_group + 1) {
+      bool any = false;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) any |= at_odd<XT>(r[i][j]);
+      if (any) odd[buffer] = 1;
+    }
+  };
+
+  // where a lane reads
+  int k_at[E], v_at[F];
+#pragma unroll
+  for (int e = 0; e < E; ++e) k_at[e] = col * ROW + ((2 * e + half) ^ (ROW == 128 ? col / 2 % 8 : col % 16)) * 16;
+#pragma unroll
+  for (int f = 0; f < F; ++f)
+    v_at[f] = 2 * TILE + (4 * half + lane % 16 / 4) * ROW + (f ^ (ROW == 128 ? lane % 16 / 8 : lane % 16 / 4)) * 64 + lane / 16 % 2 * 32 + lane % 4 * 8;
+
+  float m[NQ], l[NQ];
+  at_f16 o[NQ][F], s[2][NQ];
+  w4_u4 p[2][NQ][2];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    m[n] = -3e38f, l[n] = 0.f;
+#pragma unroll
+    for (int f = 0; f < F; ++f)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[n][f][i] = 0.f;
+  }
+
+  auto score = [&](at_f16 (&s)[NQ], int at) {
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const w4_u4 k = *reinterpret_cast<const w4_u4*>(lds + at + k_at[e]);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) s[n] = at_mfma<XT>(k, q[n][e], s[n]);
+    }
+  };
+  auto add = [&](const w4_u4 (&p)[NQ][2], int at) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int f = 0; f < F; ++f) {
+        typedef __attribute__((address_space(3))) at_s4* In;
+        const at_s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((In)(lds + at + v_at[f] + 16 * b * ROW));
+        const at_s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((In)(lds + at + v_at[f] + (16 * b + 8) * ROW));
+        const at_u2 l2 = __builtin_bit_cast(at_u2, lo), h2 = __builtin_bit_cast(at_u2, hi);
+        const w4_u4 v = {l2[0], l2[1], h2[0], h2[1]};
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) o[n][f] = at_mfma<XT>(v, p[n][b], o[n][f]);
+      }
+  };
+  // The same with values that are not finite, for rows that do not see all of them: key by key.
+  auto add_seen = [&](const w4_u4 (&p)[NQ][2], int at, int place) {
+    float(&w)[32][32 * NQ] = weights[wave];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[i / 4 * 8 + i % 4 + 4 * half][32 * n + col] = at_value<XT>(p[n][i / 8][i % 8 / 2], i % 2);
+    for (int key = 0; key < 32; ++key) {
+      const int swizzle = ROW == 128 ? key / 2 % 2 : key % 4;
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        const float x = w[key][32 * n + col];
+        const bool seen = place + key < sees[n];
+#pragma unroll
+        for (int f = 0; f < F; ++f)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {  // dims 32 f + 8 i + 4 half and on
+            const at_u2 v = *reinterpret_cast<const at_u2*>(lds + 2 * TILE + at + key * ROW + (f ^ swizzle) * 64 + i * 16 + half * 8);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float sum = fmaf(x, at_value<XT>(v[j / 2], j % 2), o[n][f][4 * i + j]);
+              o[n][f][4 * i + j] = seen ? sum : o[n][f][4 * i + j];
+            }
+          }
+      }
+    }
+  };
+
+  // step j: exponentials of s into p; scores of step j + 1 from keys at `k`, values of step j - 1 at `v`
+  auto step = [&](int j, at_f16 (&s)[NQ], at_f16 (&next)[NQ], w4_u4 (&p)[NQ][2], const w4_u4 (&before)[NQ][2], int k, int v, bool seen) {
+    if (j * 32 + 32 > full) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (j * 32 + i / 4 * 8 + i % 4 + 4 * half >= sees[n]) s[n][i] = -INFINITY;
+    }
+    float factor[NQ];
+    bool high = false;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      float top = s[n][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[n][i]);
+      high |= fmaf(top, a.scale2, -m[n]) > 8.f;
+      factor[n] = top;
+    }
+    const bool raise = __any(high);
+    if (raise) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        const float top = fmaxf(factor[n], __shfl_xor(factor[n], 32)) * a.scale2, raised = fmaxf(m[n], top);
+        factor[n] = __builtin_amdgcn_exp2f(m[n] - raised);
+        m[n] = raised;
+        l[n] *= factor[n];
+      }
+    }
+    if (j > 0) {
+      if (seen) add_seen(before, v, j * 32 - 32);
+      else add(before, v);
+    }
+    score(next, k);
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float one = __builtin_amdgcn_exp2f(fmaf(s[n][i], a.scale2, -m[n])), two = __builtin_amdgcn_exp2f(fmaf(s[n][i + 1], a.scale2, -m[n]));
+        sum += one + two;
+        p[n][i / 8][i % 8 / 2] = at_pair<XT>(one, two);
+      }
+      l[n] += sum;
+    }
+    if (raise) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int f = 0; f < F; ++f) o[n][f] *= factor[n];
+    }
+  };
+
+  w4_u4 kr[LOADS], vr[LOADS];
+  if (threadIdx.x < 2) odd[threadIdx.x] = 0;
+  fetch(k_from, k_step, 0, kr);
+  fetch(v_from, v_step, 0, vr);
+  __syncthreads();
+  store_k(0, kr);
+  store_v(0, 0, vr);
+  if (all > kTileKeys) {
+    fetch(k_from, k_step, kTileKeys, kr);
+    store_k(1, kr);
+  }
+  __syncthreads();
+  if (steps > 0) {
+    score(s[0], 0);
+    step(0, s[0], s[1], p[0], p[1], 32 * ROW, 0, false);
+  }
+  __syncthreads();
+  // group g: steps 2 g + 1 and 2 g + 2, which take keys of tile g + 1 and values of tile g
+  for (int g = 0; g < groups; ++g) {
+    const int now = g % 2 * TILE, next = TILE - now;
+    const bool more = (g + 1) * kTileKeys < all, more_keys = (g + 2) * kTileKeys < all;
+    if (more_keys) fetch(k_from, k_step, (int64_t)(g + 2) * kTileKeys, kr);
+    if (more) fetch(v_from, v_step, (int64_t)(g + 1) * kTileKeys, vr);
+    const bool seen = odd[g % 2];
+    if (2 * g < steps) {
+      if (2 * g + 1 < steps) step(2 * g + 1, s[1], s[0], p[1], p[0], next, now, seen && 2 * g * 32 + 32 > full);
+      else if (seen && 2 * g * 32 + 32 > full) add_seen(p[0], now, 2 * g * 32);
+      else add(p[0], now);
+    }
+    if (2 * g + 1 < steps) {
+      if (2 * g + 2 < steps) step(2 * g + 2, s[0], s[1], p[0], p[1], next + 32 * ROW, now + 32 * ROW, seen && (2 * g + 1) * 32 + 32 > full);
+      else if (seen && (2 * g + 1) * 32 + 32 > full) add_seen(p[1], now + 32 * ROW, (2 * g + 1) * 32);
+      else add(p[1], now + 32 * ROW);
+    }
+    if (more_keys) store_k(g % 2, kr);
+    if (more) store_v((g + 1) % 2, (g + 1) * kTileKeys, vr);
+    __syncthreads();
+  }
+
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    l[n] += __shfl_xor(l[n], 32);
+    if (first_row + 32 * n + col >= rows) continue;
+    const int row = first_row + 32 * n + col, at = row / a.per_group;
+    const int64_t out_at = (tile.begin + at) * a.out.ld_token + ((int64_t)head * a.group + (row - at * a.group)) * a.out.ld_head;
+    const float inverse = l[n] == 0.f ? 0.f : 1.f / l[n];
+#pragma unroll
+    for (int f = 0; f < F; ++f)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int d = 32 * f + 8 * i + 4 * half;
+        if (d >= a.dim) continue;
+        float r[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] = l[n] == 0.f ? 0.f : o[n][f][4 * i + j] * inverse;
+        if (a.out.type == OZ2_F32)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) static_cast<float*>(a.out.data)[out_at + d + j] = r[j];
+        else if (a.out.type == OZ2_BF16) {
+          const at_u2 w = {at_pair<OZ2_BF16>(r[0], r[1]), at_pair<OZ2_BF16>(r[2], r[3])};
+          *reinterpret_cast<at_u2*>(static_cast<uint16_t*>(a.out.data) + out_at + d) = w;
+        } else {
+          const at_u2 w = {at_pair<OZ2_F16>(r[0], r[1]), at_pair<OZ2_F16>(r[2], r[3])};
+          *reinterpret_cast<at_u2*>(static_cast<uint16_t*>(a.out.data) + out_at + d) = w;
+        }
+      }
+  }
+}
+
+template <int XT, int DP, int NQ>
+hipError_t oz2_attention_tile_launch(const Attention& a, hipStream_t st) {
+  hipLaunchKernelGGL((attention_tile_kernel<XT, DP, NQ>), dim3((unsigned)(attention_tiles(a, 128 * NQ) * a.kv_heads)), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+template <int XT>
+hipError_t oz2_attention_tile_of(const Attention& a, hipStream_t st) {
+  if (a.dim <= 64) return oz2_attention_tile_launch<XT, 64, 2>(a, st);
+  if (a.dim <= 96) return oz2_attention_tile_launch<XT, 96, 2>(a, st);
+  if (a.dim <= 128) return oz2_attention_tile_launch<XT, 128, 2>(a, st);
+  return oz2_attention_tile_launch<XT, 256, 1>(a, st);
+}
+
+#endif
+#endif
