@@ -1,4 +1,5 @@
 // oz2_attention in BF16.
 #include "oz2_attention_tile.h"
 
+extern template hipError_t oz2_attention_wide_of<OZ2_BF16>(const Attention&, hipStream_t);
 template hipError_t oz2_attention_tile_of<OZ2_BF16>(const Attention&, hipStream_t);

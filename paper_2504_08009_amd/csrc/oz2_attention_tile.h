@@ -29,8 +29,11 @@ __device__ __forceinline__ at_f16 at_mfma(w4_u4 a, w4_u4 b, at_f16 c) {
 }
 template <int XT>
 __device__ __forceinline__ unsigned at_pair(float a, float b) {
-  if constexpr (XT == OZ2_F16) return __builtin_bit_cast(uint16_t, (_Float16)a) | (unsigned)__builtin_bit_cast(uint16_t, (_Float16)b) << 16;
-  else return __builtin_bit_cast(uint16_t, (__bf16)a) | (unsigned)__builtin_bit_cast(uint16_t, (__bf16)b) << 16;
+  typedef float Two __attribute__((ext_vector_type(2)));
+  typedef _Float16 Half __attribute__((ext_vector_type(2)));
+  typedef __bf16 Brain __attribute__((ext_vector_type(2)));
+  if constexpr (XT == OZ2_F16) return __builtin_bit_cast(unsigned, __builtin_convertvector((Two{a, b}), Half));
+  else return __builtin_bit_cast(unsigned, __builtin_convertvector((Two{a, b}), Brain));
 }
 template <int XT>
 __device__ __forceinline__ float at_value(unsigned w, int upper) {
@@ -44,13 +47,13 @@ __device__ __forceinline__ bool at_odd(unsigned w) {
   return (w & top) == top || (w & top << 16) == top << 16;
 }
 
-template <int XT, int DP, int NQ>
-__global__ void __launch_bounds__(256, 1) attention_tile_kernel(Attention a) {
+template <int XT, int DP, int NQ, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, WAVES / 4) attention_tile_kernel(Attention a) {
   constexpr int E = DP / 16, F = DP / 32, ROW = DP <= 64 ? 128 : DP <= 128 ? 256 : 512;  // bytes of a row in LDS
-  constexpr int ROWS = 128 * NQ, LOADS = kTileKeys * ROW / 4096, TILE = kTileKeys * ROW;
+  constexpr int THREADS = 64 * WAVES, ROWS = 32 * NQ * WAVES, LOADS = kTileKeys * ROW / 16 / THREADS, TILE = kTileKeys * ROW;
   __shared__ __attribute__((aligned(16))) char lds[4 * TILE];  // keys, keys, values, values
   __shared__ int odd[2];                                       // whether a tile of values has one that is not finite
-  __shared__ float weights[4][32][32 * NQ];                    // (where it has)
+  __shared__ float weights[WAVES][32][32 * NQ];                    // (where it has)
 
   const int tiles = (int)((unsigned)gridDim.x / (unsigned)a.kv_heads);
   const int head = blockIdx.x % a.kv_heads, lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 32, half = lane / 32;
@@ -82,7 +85,7 @@ __global__ void __launch_bounds__(256, 1) attention_tile_kernel(Attention a) {
   }
 
   // a thread's pieces of a tile, sixteen bytes each of every PER-th key, and their places in LDS
-  constexpr int PER = 256 / (ROW / 16);
+  constexpr int PER = THREADS / (ROW / 16);
   const int of_key = threadIdx.x / (ROW / 16), piece = threadIdx.x % (ROW / 16);
   // (sixteen keys' pieces of one place, and four keys' 64 bytes, lie in all banks)
   const int to_k = of_key * ROW + (piece ^ (ROW == 128 ? of_key / 2 % 8 : of_key % 16)) * 16;
@@ -91,21 +94,27 @@ __global__ void __launch_bounds__(256, 1) attention_tile_kernel(Attention a) {
   const char* k_from = static_cast<const char*>(a.k.data) + (tile.begin * a.k.ld_token + head * a.k.ld_head) * 2;
   const char* v_from = static_cast<const char*>(a.v.data) + (tile.begin * a.v.ld_token + head * a.v.ld_head) * 2;
   const int k_step = (int)(a.k.ld_token * 2), v_step = (int)(a.v.ld_token * 2);
+  // (a piece that is not there is loaded from where another one is, and stored as zeros)
   auto fetch = [&](const char* from, int step, int64_t first, w4_u4 (&r)[LOADS]) {
     const int most = (int)min((int64_t)kTileKeys, tile.tokens - first) - 1;
-    from += first * step;
-    const unsigned at = of_key * step + piece * 16;
+    from += first * step + (piece * 8 < a.dim ? piece * 16 : 0);
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      r[i] = w4_u4{0, 0, 0, 0};
-      if (of_key + i * PER <= most && piece * 8 < a.dim) r[i] = *reinterpret_cast<const w4_u4*>(from + i * PER * step + at);
+    for (int i = 0; i < LOADS; ++i) r[i] = *reinterpret_cast<const w4_u4*>(from + (unsigned)(min(of_key + i * PER, most) * step));
+  };
+  auto clear = [&](int first, w4_u4 (&r)[LOADS]) {
+    if (a.dim < ROW / 2 || tile.tokens - first < kTileKeys) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i)
+        if (piece * 8 >= a.dim || first + of_key + i * PER >= tile.tokens) r[i] = w4_u4{0, 0, 0, 0};
     }
   };
-  auto store_k = [&](int buffer, const w4_u4 (&r)[LOADS]) {
+  auto store_k = [&](int buffer, int first, w4_u4 (&r)[LOADS]) {
+    clear(first, r);
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) *reinterpret_cast<w4_u4*>(lds + buffer * TILE + (to_k ^ (ROW == 512 && i % 2 ? 128 : 0)) + i * PER * ROW) = r[i];
   };
-  auto store_v = [&](int buffer, int first, const w4_u4 (&r)[LOADS]) {
+  auto store_v = [&](int buffer, int first, w4_u4 (&r)[LOADS]) {
+    clear(first, r);
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) *reinterpret_cast<w4_u4*>(lds + buffer * TILE + to_v + i * PER * ROW) = r[i];
     // (only where a key may be hidden from a row does it matter)
@@ -193,40 +202,43 @@ __global__ void __launch_bounds__(256, 1) attention_tile_kernel(Attention a) {
     }
   };
 
-  // step j: exponentials of s into p; scores of step j + 1 from keys at `k`, values of step j - 1 at `v`
-  auto step = [&](int j, at_f16 (&s)[NQ], at_f16 (&next)[NQ], w4_u4 (&p)[NQ][2], const w4_u4 (&before)[NQ][2], int k, int v, bool seen) {
-    if (j * 32 + 32 > full) {
+  // What raised the maximum multiplies the sums a step later, when they have the values of all keys before.
+  float factor[NQ];
+  bool pending = false;
+  auto rescale = [&]() {
+    if (pending) {
 #pragma unroll
       for (int n = 0; n < NQ; ++n)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (j * 32 + i / 4 * 8 + i % 4 + 4 * half >= sees[n]) s[n][i] = -INFINITY;
+        for (int f = 0; f < F; ++f) o[n][f] *= factor[n];
+      pending = false;
     }
-    float factor[NQ];
+  };
+  auto maximum = [&](const at_f16 (&s)[NQ]) {
+    float top[NQ];
     bool high = false;
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-      float top = s[n][0];
+      top[n] = s[n][0];
 #pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[n][i]);
-      high |= fmaf(top, a.scale2, -m[n]) > 8.f;
-      factor[n] = top;
+      for (int i = 1; i < 16; ++i) top[n] = fmaxf(top[n], s[n][i]);
+      high |= fmaf(top[n], a.scale2, -m[n]) > 8.f;
     }
-    const bool raise = __any(high);
-    if (raise) {
+    if (pending || __any(high)) {
+      rescale();
+      if (__any(high)) {
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        const float top = fmaxf(factor[n], __shfl_xor(factor[n], 32)) * a.scale2, raised = fmaxf(m[n], top);
-        factor[n] = __builtin_amdgcn_exp2f(m[n] - raised);
-        m[n] = raised;
-        l[n] *= factor[n];
+        for (int n = 0; n < NQ; ++n) {
+          const float raised = fmaxf(m[n], fmaxf(top[n], __shfl_xor(top[n], 32)) * a.scale2);
+          factor[n] = __builtin_amdgcn_exp2f(m[n] - raised);
+          m[n] = raised;
+          l[n] *= factor[n];
+        }
+        pending = true;
       }
     }
-    if (j > 0) {
-      if (seen) add_seen(before, v, j * 32 - 32);
-      else add(before, v);
-    }
-    score(next, k);
+  };
+  auto exponentials = [&](const at_f16 (&s)[NQ], w4_u4 (&p)[NQ][2]) {
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
       float sum = 0.f;
@@ -238,12 +250,31 @@ __global__ void __launch_bounds__(256, 1) attention_tile_kernel(Attention a) {
       }
       l[n] += sum;
     }
-    if (raise) {
+  };
+  // step j: exponentials of s into p; scores of step j + 1 from keys at `k`, values of step j - 1 at `v`.  All rows see all of step j's keys.
+  auto step = [&](at_f16 (&s)[NQ], at_f16 (&next)[NQ], w4_u4 (&p)[NQ][2], const w4_u4 (&before)[NQ][2], int k, int v) {
+    maximum(s);
+    score(next, k);
+    add(before, v);
+    exponentials(s, p);
+  };
+  // the same where they may not, or where step j or j + 1 may not be the wave's
+  auto last_step = [&](int j, at_f16 (&s)[NQ], at_f16 (&next)[NQ], w4_u4 (&p)[NQ][2], const w4_u4 (&before)[NQ][2], int k, int v, bool seen) {
+    if (j < steps) {
+      if (j * 32 + 32 > full) {
 #pragma unroll
-      for (int n = 0; n < NQ; ++n)
+        for (int n = 0; n < NQ; ++n)
 #pragma unroll
-        for (int f = 0; f < F; ++f) o[n][f] *= factor[n];
+          for (int i = 0; i < 16; ++i) s[n][i] = j * 32 + i / 4 * 8 + i % 4 + 4 * half >= sees[n] ? -INFINITY : s[n][i];
+      }
+      maximum(s);
+    } else rescale();
+    if (j > 0 && j <= steps) {
+      if (seen && j * 32 > full) add_seen(before, v, j * 32 - 32);
+      else add(before, v);
     }
+    if (j + 1 < steps) score(next, k);
+    if (j < steps) exponentials(s, p);
   };
 
   w4_u4 kr[LOADS], vr[LOADS];
@@ -251,39 +282,43 @@ __global__ void __launch_bounds__(256, 1) attention_tile_kernel(Attention a) {
   fetch(k_from, k_step, 0, kr);
   fetch(v_from, v_step, 0, vr);
   __syncthreads();
-  store_k(0, kr);
+  store_k(0, 0, kr);
   store_v(0, 0, vr);
   if (all > kTileKeys) {
     fetch(k_from, k_step, kTileKeys, kr);
-    store_k(1, kr);
+    store_k(1, kTileKeys, kr);
   }
   __syncthreads();
-  if (steps > 0) {
-    score(s[0], 0);
-    step(0, s[0], s[1], p[0], p[1], 32 * ROW, 0, false);
-  }
+  if (steps > 0) score(s[0], 0);
+  last_step(0, s[0], s[1], p[0], p[1], 32 * ROW, 0, false);
   __syncthreads();
   // group g: steps 2 g + 1 and 2 g + 2, which take keys of tile g + 1 and values of tile g
-  for (int g = 0; g < groups; ++g) {
+  int g = 0;
+  const int easy = full >= 96 ? (full - 96) / 64 + 1 : 0;  // groups whose steps, and the next one, all rows see
+  for (; g < easy; ++g) {
+    const int now = g % 2 * TILE, next = TILE - now;
+    const bool more = (g + 1) * kTileKeys < all, more_keys = (g + 2) * kTileKeys < all;
+    fetch(k_from, k_step, more_keys ? (int64_t)(g + 2) * kTileKeys : 0, kr);
+    fetch(v_from, v_step, more ? (int64_t)(g + 1) * kTileKeys : 0, vr);
+    step(s[1], s[0], p[1], p[0], next, now);
+    step(s[0], s[1], p[0], p[1], next + 32 * ROW, now + 32 * ROW);
+    if (more_keys) store_k(g % 2, (g + 2) * kTileKeys, kr);
+    if (more) store_v((g + 1) % 2, (g + 1) * kTileKeys, vr);
+    __syncthreads();
+  }
+  for (; g < groups; ++g) {
     const int now = g % 2 * TILE, next = TILE - now;
     const bool more = (g + 1) * kTileKeys < all, more_keys = (g + 2) * kTileKeys < all;
     if (more_keys) fetch(k_from, k_step, (int64_t)(g + 2) * kTileKeys, kr);
     if (more) fetch(v_from, v_step, (int64_t)(g + 1) * kTileKeys, vr);
     const bool seen = odd[g % 2];
-    if (2 * g < steps) {
-      if (2 * g + 1 < steps) step(2 * g + 1, s[1], s[0], p[1], p[0], next, now, seen && 2 * g * 32 + 32 > full);
-      else if (seen && 2 * g * 32 + 32 > full) add_seen(p[0], now, 2 * g * 32);
-      else add(p[0], now);
-    }
-    if (2 * g + 1 < steps) {
-      if (2 * g + 2 < steps) step(2 * g + 2, s[0], s[1], p[0], p[1], next + 32 * ROW, now + 32 * ROW, seen && (2 * g + 1) * 32 + 32 > full);
-      else if (seen && (2 * g + 1) * 32 + 32 > full) add_seen(p[1], now + 32 * ROW, (2 * g + 1) * 32);
-      else add(p[1], now + 32 * ROW);
-    }
-    if (more_keys) store_k(g % 2, kr);
+    last_step(2 * g + 1, s[1], s[0], p[1], p[0], next, now, seen);
+    last_step(2 * g + 2, s[0], s[1], p[0], p[1], next + 32 * ROW, now + 32 * ROW, seen);
+    if (more_keys) store_k(g % 2, (g + 2) * kTileKeys, kr);
     if (more) store_v((g + 1) % 2, (g + 1) * kTileKeys, vr);
     __syncthreads();
   }
+  rescale();
 
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
@@ -315,17 +350,19 @@ __global__ void __launch_bounds__(256, 1) attention_tile_kernel(Attention a) {
   }
 }
 
-template <int XT, int DP, int NQ>
+template <int XT, int DP, int NQ, int WAVES>
 hipError_t oz2_attention_tile_launch(const Attention& a, hipStream_t st) {
-  hipLaunchKernelGGL((attention_tile_kernel<XT, DP, NQ>), dim3((unsigned)(attention_tiles(a, 128 * NQ) * a.kv_heads)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((attention_tile_kernel<XT, DP, NQ, WAVES>), dim3((unsigned)(attention_tiles(a, 32 * NQ * WAVES) * a.kv_heads)), dim3(64 * WAVES), 0, st, a);
   return hipGetLastError();
 }
+// (of 129 to 256 values: the sums take half the registers, so four waves; compiled in a file of its own)
+template <int XT> hipError_t oz2_attention_wide_of(const Attention& a, hipStream_t st);
 template <int XT>
 hipError_t oz2_attention_tile_of(const Attention& a, hipStream_t st) {
-  if (a.dim <= 64) return oz2_attention_tile_launch<XT, 64, 2>(a, st);
-  if (a.dim <= 96) return oz2_attention_tile_launch<XT, 96, 2>(a, st);
-  if (a.dim <= 128) return oz2_attention_tile_launch<XT, 128, 2>(a, st);
-  return oz2_attention_tile_launch<XT, 256, 1>(a, st);
+  if (a.dim <= 64) return oz2_attention_tile_launch<XT, 64, 1, 8>(a, st);
+  if (a.dim <= 96) return oz2_attention_tile_launch<XT, 96, 1, 8>(a, st);
+  if (a.dim <= 128) return oz2_attention_tile_launch<XT, 128, 1, 8>(a, st);
+  return oz2_attention_wide_of<XT>(a, st);
 }
 
 #endif

@@ -1,8 +1,8 @@
 """Attention over packed prompts, against its formula in 64 bits.
 
 Tolerances (u = 2^-24).  A score is a sum of dim exact or FP32 products in FP32, then scaled and taken to base 2: off by at most e = (dim + 16) u scale max_j sum_d |q k_j|,
-so p is off by a factor within 1 +- (2 e + 8 u); sums of n terms add n u.  16-bit types round p once more, by half a step h (2^-8, 2^-11), before it meets v, and its
-sum is taken of what it became: with A = sum p |v| the result is off by at most (2 e + h + (n + 72) u) (A + |out|), times 2 for what is of second order, before the
+so p is off by a factor within 1 +- (2 e + 8 u); sums of n terms add n u.  16-bit types round p once more, by half a step h (2^-8, 2^-11), before it meets v:
+with A = sum p |v| the result is off by at most (2 e + h + (n + 72) u) (A + |out|), times 2 for what is of second order, before the
 one rounding to the type."""
 import math
 
