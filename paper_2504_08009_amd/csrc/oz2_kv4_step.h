@@ -37,7 +37,9 @@ struct Kv4Step {
 template <int XT> constexpr int step_parts() { return XT == OZ2_BF16 ? 1 : XT == OZ2_F16 ? 2 : 3; }
 
 __device__ __forceinline__ unsigned bf16_pair(float a, float b) {
-  return __builtin_bit_cast(uint16_t, (__bf16)a) | (unsigned)__builtin_bit_cast(uint16_t, (__bf16)b) << 16;
+  typedef float Two __attribute__((ext_vector_type(2)));
+  typedef __bf16 Brain __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(unsigned, __builtin_convertvector((Two{a, b}), Brain));
 }
 // the bf16 values of a pair, taken off: what is left of a and b for the next term
 __device__ __forceinline__ unsigned bf16_term(float& a, float& b) {
@@ -45,12 +47,38 @@ __device__ __forceinline__ unsigned bf16_term(float& a, float& b) {
   a -= __uint_as_float(w << 16), b -= __uint_as_float(w & 0xffff0000u);
   return w;
 }
-// codes j and j + 4 of a word as a pair of bf16 16 + c
-__device__ __forceinline__ unsigned code_pair(unsigned w, int j) {
-  return ((j == 0 ? w << 3 : w >> (4 * j - 3)) & 0x00780078u) | 0x41804180u;
+// codes j and j + 4 of a word as a pair of bf16 16 + c.  `mask` is 0x00780078 in a vector register: an and-or takes one constant from elsewhere.
+__device__ __forceinline__ unsigned code_pair(unsigned w, int j, unsigned mask) {
+  return ((j == 0 ? w << 3 : w >> (4 * j - 3)) & mask) | 0x41804180u;
 }
 __device__ __forceinline__ w4_f4 step_mfma(w4_u4 a, w4_u4 b, w4_f4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(w4_bf8, a), __builtin_bit_cast(w4_bf8, b), c, 0, 0, 0);
+}
+// Loads of 4, 8 or 16 bytes at `at` bytes, 32 bits of a lane's own, behind a base that is the same for all lanes: no address is formed by the vector units.
+typedef __amdgpu_buffer_rsrc_t StepBase;
+__device__ __forceinline__ StepBase step_base(const void* p) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, -1, 0x00027000);
+}
+template <int N>
+__device__ __forceinline__ void step_load(StepBase base, unsigned at, unsigned (&w)[N]) {
+  if constexpr (N == 1) w[0] = __builtin_amdgcn_raw_buffer_load_b32(base, at, 0, 0);
+  else if constexpr (N == 2) {
+    const auto x = __builtin_amdgcn_raw_buffer_load_b64(base, at, 0, 0);
+    w[0] = x[0], w[1] = x[1];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      const auto x = __builtin_amdgcn_raw_buffer_load_b128(base, at + 16 * i, 0, 0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[4 * i + j] = x[j];
+    }
+  }
+}
+// (fmaxf has its operands made quiet first, an instruction each)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
 }
 __device__ __forceinline__ float half_of(unsigned w, int upper) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(upper ? w >> 16 : w)); }
 
@@ -64,40 +92,43 @@ struct StepTile {
 };
 
 template <int XT, int DP, bool WIDE>
-__global__ void __launch_bounds__(256) kv4_step_kernel(Kv4Step a) {
+__global__ void __launch_bounds__(256, XT != OZ2_F32 && DP <= 128 ? 3 : 1) kv4_step_kernel(Kv4Step a) {
   constexpr int E = DP / 32, F = DP / 16, PARTS = step_parts<XT>(), TERMS = XT == OZ2_F32 ? 3 : 2;
   __shared__ float merged[kStepWaves][kStepRows][DP + 1];
   __shared__ float merged_m[kStepWaves][kStepRows], merged_l[kStepWaves][kStepRows], merged_c[kStepWaves][kStepRows];
-  const int head = blockIdx.y, s = blockIdx.z, lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int head = blockIdx.x, s = blockIdx.y, lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int col = lane % 16, quarter = lane / 16;
   const KvRange r = kv_range(a.on.cu, s, a.on.tokens);
   const int news = (int)(r.end - r.begin), rows = news * a.group;
   const int held = kv_held(a.on.lengths, s, a.capacity);
-  const int c0 = blockIdx.x * a.chunk;
+  const int c0 = blockIdx.z * a.chunk;
   if (rows == 0 || (c0 >= held && c0 > 0)) return;
   const int c1 = min(held, c0 + a.chunk);
   const bool whole = held <= a.chunk;
-  const int32_t* table = a.on.table + s * a.on.ld_table;
+  // (read by scalar loads: a vector load would have to be waited for, and with it the tiles that were asked for before)
+  typedef const int32_t __attribute__((address_space(4)))* Scalars;
+  const Scalars table = (Scalars)(uintptr_t)(a.on.table + s * a.on.ld_table);
 
+  unsigned mask = 0x00780078u;
+  asm("" : "+v"(mask));
   const int64_t codes_head = head * a.c.codes_head, scales_head = head * a.c.scales_head;
-  const int bytes = a.dim / 2;
-  // where a lane's words are in a row; words past its end are read from its start, and meet zeros of q or are not stored
-  int k_at[E];
-  for (int e = 0; e < E; ++e) {
-    const int word = WIDE ? quarter * E + e : e * 4 + quarter;
-    k_at[e] = word * 4 < bytes ? word * 4 : 0;
+  const int bytes = WIDE ? DP / 2 : a.dim / 2;
+  // where a lane's words are among sixteen rows; words past a row's end are read from its start, and meet zeros of q or are not stored
+  unsigned k_at[WIDE ? 1 : E], v_at[WIDE ? 1 : (DP + 127) / 128];
+  for (int e = 0; e < (WIDE ? 1 : E); ++e) {
+    const int word = WIDE ? quarter * E : e * 4 + quarter;
+    k_at[e] = col * bytes + (word * 4 < bytes ? word * 4 : 0);
   }
-  int v_at[(DP + 127) / 128];
-  for (int u = 0; u < (DP + 127) / 128; ++u) v_at[u] = col * (DP / 32) + 4 * u < bytes ? col * (DP / 32) + 4 * u : 0;
+  for (int u = 0; u < (WIDE ? 1 : (DP + 127) / 128); ++u) v_at[u] = quarter * 4 * bytes + (col * (DP / 32) + 4 * u < bytes ? col * (DP / 32) + 4 * u : 0);
+  const unsigned s_at = quarter * 16;
 
   struct Pages { int id[2]; };
   auto pages = [&](int tile) {
     Pages p;
     for (int i = 0; i < 2; ++i) {
       const int place = tile * kStepTile + 16 * i;
-      const int at = place < c1 ? place : c0;
-      const int id = __builtin_amdgcn_readfirstlane(place < c1 ? table[at / a.per_page] : -1);
-      p.id[i] = id >= 0 && id < a.c.pages ? id : -1;
+      const int id = table[(place < c1 ? place : c0) / a.per_page];
+      p.id[i] = place < c1 && id >= 0 && id < a.c.pages ? id : -1;
     }
     return p;
   };
@@ -108,28 +139,23 @@ __global__ void __launch_bounds__(256) kv4_step_kernel(Kv4Step a) {
       const int64_t page = p.id[i] < 0 ? 0 : p.id[i];
       r.there[i] = p.id[i] >= 0;
       const int64_t codes = page * a.c.codes_page + codes_head + (int64_t)in * bytes, scales = page * a.c.scales_page + scales_head + in;
-      const uint8_t* k = a.c.k_codes + codes;
-      const uint8_t* v = a.c.v_codes + codes;
-      if constexpr (WIDE) {
-        struct __attribute__((packed, aligned(4))) Words { unsigned w[E]; };
-        const Words w = *reinterpret_cast<const Words*>(k + col * bytes + quarter * (E * 4));
-        for (int e = 0; e < E; ++e) r.k[i][e] = w.w[e];
-      } else {
-        for (int e = 0; e < E; ++e) r.k[i][e] = *reinterpret_cast<const unsigned*>(k + col * bytes + k_at[e]);
+      const StepBase k = step_base(a.c.k_codes + codes), v = step_base(a.c.v_codes + codes);
+      if constexpr (WIDE) step_load(k, k_at[0], r.k[i]);
+      else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) r.k[i][e] = __builtin_amdgcn_raw_buffer_load_b32(k, k_at[e], 0, 0);
       }
+#pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint8_t* at = v + (quarter * 4 + j) * bytes;
-        if constexpr (DP == 64) r.v[4 * i + j][0] = *reinterpret_cast<const uint16_t*>(at + v_at[0]);
-        else if constexpr (WIDE) {
-          struct __attribute__((packed, aligned(4))) Words { unsigned w[DP / 128]; };
-          const Words w = *reinterpret_cast<const Words*>(at + v_at[0]);
-          for (int u = 0; u < DP / 128; ++u) r.v[4 * i + j][u] = w.w[u];
-        } else {
-          for (int u = 0; u < DP / 128; ++u) r.v[4 * i + j][u] = *reinterpret_cast<const unsigned*>(at + v_at[u]);
+        if constexpr (DP == 64) r.v[4 * i + j][0] = __builtin_amdgcn_raw_buffer_load_b16(v, v_at[0] + j * bytes, 0, 0);
+        else if constexpr (WIDE) step_load(v, v_at[0] + j * bytes, r.v[4 * i + j]);
+        else {
+#pragma unroll
+          for (int u = 0; u < DP / 128; ++u) r.v[4 * i + j][u] = __builtin_amdgcn_raw_buffer_load_b32(v, v_at[u] + j * bytes, 0, 0);
         }
       }
-      r.ks[i] = *reinterpret_cast<const w4_u4*>(static_cast<const unsigned*>(a.c.k_scales) + scales + quarter * 4);
-      r.vs[i] = *reinterpret_cast<const w4_u4*>(static_cast<const unsigned*>(a.c.v_scales) + scales + quarter * 4);
+      r.ks[i] = __builtin_bit_cast(w4_u4, __builtin_amdgcn_raw_buffer_load_b128(step_base(static_cast<const unsigned*>(a.c.k_scales) + scales), s_at, 0, 0));
+      r.vs[i] = __builtin_bit_cast(w4_u4, __builtin_amdgcn_raw_buffer_load_b128(step_base(static_cast<const unsigned*>(a.c.v_scales) + scales), s_at, 0, 0));
     }
     return r;
   };
@@ -152,91 +178,118 @@ __global__ void __launch_bounds__(256) kv4_step_kernel(Kv4Step a) {
     sum += __shfl_xor(sum, 32);
 
     float m = -3e38f, l = 0.f, c = 0.f;  // m: finite, so that nothing that is not seen becomes a NaN
-    w4_f4 o[F];
+    w4_f4 o[F], off = {0.f, 0.f, 0.f, 0.f};
     for (int f = 0; f < F; ++f) o[f] = w4_f4{0.f, 0.f, 0.f, 0.f};
+
+    // a tile's places: `cut` where some are hidden from some row
+    auto take = [&](int tile, StepTile<DP>& now) {
+      const int begin = tile * kStepTile;
+      const bool cut = begin + kStepTile > held - news || begin + kStepTile > c1 || !now.there[0] || !now.there[1];
+      unsigned hidden = 0;
+      if (cut) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int place = begin + i / 4 * 16 + quarter * 4 + i % 4;
+          const bool hides = place >= sees || place >= c1 || !now.there[i / 4];
+          hidden |= hides ? 1u << i : 0u;
+          // (what is there may be a NaN)
+          now.ks[i / 4][i % 4] = hides ? 0u : now.ks[i / 4][i % 4];
+          now.vs[i / 4][i % 4] = hides ? 0u : now.vs[i / 4][i % 4];
+        }
+      }
+      float t[8];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        w4_f4 acc = {-16.f * sum, -16.f * sum, -16.f * sum, -16.f * sum};
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          w4_u4 k;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) k[j] = code_pair(now.k[i][e], j, mask);
+#pragma unroll
+          for (int x = 0; x < PARTS; ++x) acc = step_mfma(k, q[x][e], acc);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[4 * i + j] = fmaf(half_of(now.ks[i][j], 0), acc[j], fmaf(half_of(now.ks[i][j], 1), sum, 0.f));  // (+ 0: one instruction that takes FP16)
+      }
+      if (cut) {
+        asm volatile("" : "+v"(hidden));  // (a branch: eight selects by conditions that hardly ever hold cost more)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = hidden >> i & 1 ? -INFINITY : t[i];
+      }
+      if (a.scores && row < rows) {
+        float* to = a.scores + (token * a.heads + query) * a.capacity;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int place = begin + i / 4 * 16 + quarter * 4 + i % 4;
+          if (place < c1) to[place] = t[i];
+        }
+      }
+      const float top = max3(max3(max3(t[0], t[1], t[2]), t[3], t[4]), max3(t[5], t[6], t[7]), t[7]);
+      if (__any(fmaf(top, a.scale2, -m) > 8.f)) {
+        float high = fmaxf(top, __shfl_xor(top, 16));
+        high = fmaxf(high, __shfl_xor(high, 32));
+        const float raised = fmaxf(m, high * a.scale2), f = __builtin_amdgcn_exp2f(m - raised);
+        m = raised;
+        l *= f, c *= f, off *= f;
+#pragma unroll
+        for (int i = 0; i < F; ++i) o[i] *= f;
+      }
+      float w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(t[i], a.scale2, -m));
+        l += p;
+        w[i] = fmaf(p, half_of(now.vs[i / 4][i % 4], 0), 0.f);
+        c = fmaf(p, half_of(now.vs[i / 4][i % 4], 1), c);
+      }
+      w4_u4 b[TERMS];
+#pragma unroll
+      for (int x = 0; x < TERMS; ++x)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b[x][j] = bf16_term(w[2 * j], w[2 * j + 1]);
+#pragma unroll
+      for (int x = 0; x < TERMS; ++x) off = step_mfma(w4_u4{0xc180c180u, 0xc180c180u, 0xc180c180u, 0xc180c180u}, b[x], off);  // -16 sum p s, of what the terms are
+#pragma unroll
+      for (int u = 0; u < (DP + 127) / 128; ++u) {
+        unsigned low[4], high[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          low[j] = __builtin_amdgcn_perm(now.v[2 * j + 1][u], now.v[2 * j][u], 0x05040100);
+          high[j] = __builtin_amdgcn_perm(now.v[2 * j + 1][u], now.v[2 * j][u], 0x07060302);
+        }
+#pragma unroll
+        for (int e = 0; e < (DP == 64 ? 4 : 8); ++e) {
+          w4_u4 v;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] = code_pair(e < 4 ? low[j] : high[j], e % 4, mask);
+#pragma unroll
+          for (int x = 0; x < TERMS; ++x) o[u * 8 + e] = step_mfma(v, b[x], o[u * 8 + e]);
+        }
+      }
+    };
 
     const int first = c0 / kStepTile + wave, last = (c1 + kStepTile - 1) / kStepTile;
     if (first < last) {
       Pages p = pages(first);
-      StepTile<DP> next = fetch(first, p);
+      StepTile<DP> one = fetch(first, p), two;
       p = pages(first + kStepWaves);
-      for (int tile = first; tile < last; tile += kStepWaves) {
-        const StepTile<DP> now = next;
-        next = fetch(tile + kStepWaves, p);
+      for (int tile = first;; tile += 2 * kStepWaves) {
+        two = fetch(tile + kStepWaves, p);
         p = pages(tile + 2 * kStepWaves);
-
-        float t[8];
-        for (int i = 0; i < 2; ++i) {
-          w4_f4 acc = {-16.f * sum, -16.f * sum, -16.f * sum, -16.f * sum};
-          for (int e = 0; e < E; ++e) {
-            w4_u4 k;
-            for (int j = 0; j < 4; ++j) k[j] = code_pair(now.k[i][e], j);
-            for (int x = 0; x < PARTS; ++x) acc = step_mfma(k, q[x][e], acc);
-          }
-          for (int j = 0; j < 4; ++j) t[4 * i + j] = fmaf(half_of(now.ks[i][j], 0), acc[j], half_of(now.ks[i][j], 1) * sum);
-        }
-        const bool cut = tile * kStepTile + kStepTile > held - news || tile * kStepTile + kStepTile > c1 || !now.there[0] || !now.there[1];
-        bool hidden[8] = {};
-        if (cut) {
-          for (int i = 0; i < 8; ++i) {
-            const int place = tile * kStepTile + i / 4 * 16 + quarter * 4 + i % 4;
-            hidden[i] = place >= sees || place >= c1 || !now.there[i / 4];
-            if (hidden[i]) t[i] = -INFINITY;
-          }
-        }
-        if (a.scores && row < rows) {
-          float* to = a.scores + (token * a.heads + query) * a.capacity;
-          for (int i = 0; i < 8; ++i) {
-            const int place = tile * kStepTile + i / 4 * 16 + quarter * 4 + i % 4;
-            if (place < c1) to[place] = t[i];
-          }
-        }
-        float x[8], top = -INFINITY;
-        for (int i = 0; i < 8; ++i) {
-          x[i] = fmaf(t[i], a.scale2, -m);
-          top = fmaxf(top, x[i]);
-        }
-        if (__any(top > 8.f)) {
-          float high = -INFINITY;
-          for (int i = 0; i < 8; ++i) high = fmaxf(high, t[i] * a.scale2);
-          high = fmaxf(high, __shfl_xor(high, 16));
-          high = fmaxf(high, __shfl_xor(high, 32));
-          const float raised = fmaxf(m, high), f = __builtin_amdgcn_exp2f(m - raised);
-          m = raised;
-          l *= f, c *= f;
-          for (int i = 0; i < F; ++i) o[i] *= f;
-          for (int i = 0; i < 8; ++i) x[i] = fmaf(t[i], a.scale2, -m);
-        }
-        float w[8];
-        for (int i = 0; i < 8; ++i) {
-          const float p = __builtin_amdgcn_exp2f(x[i]);
-          l += p;
-          w[i] = p * half_of(now.vs[i / 4][i % 4], 0);
-          float shift = p * half_of(now.vs[i / 4][i % 4], 1);
-          if (cut && hidden[i]) w[i] = shift = 0.f;
-          c += fmaf(-16.f, w[i], shift);
-        }
-        w4_u4 b[TERMS];
-        for (int x = 0; x < TERMS; ++x)
-          for (int j = 0; j < 4; ++j) b[x][j] = bf16_term(w[2 * j], w[2 * j + 1]);
-        for (int u = 0; u < (DP + 127) / 128; ++u) {
-          unsigned low[4], high[4];
-          for (int j = 0; j < 4; ++j) {
-            low[j] = __builtin_amdgcn_perm(now.v[2 * j + 1][u], now.v[2 * j][u], 0x05040100);
-            high[j] = __builtin_amdgcn_perm(now.v[2 * j + 1][u], now.v[2 * j][u], 0x07060302);
-          }
-          for (int e = 0; e < (DP == 64 ? 4 : 8); ++e) {
-            w4_u4 v;
-            for (int j = 0; j < 4; ++j) v[j] = code_pair(e < 4 ? low[j] : high[j], e % 4);
-            for (int x = 0; x < TERMS; ++x) o[u * 8 + e] = step_mfma(v, b[x], o[u * 8 + e]);
-          }
-        }
+        take(tile, one);
+        if (tile + kStepWaves >= last) break;
+        one = fetch(tile + 2 * kStepWaves, p);
+        p = pages(tile + 3 * kStepWaves);
+        take(tile + kStepWaves, two);
+        if (tile + 2 * kStepWaves >= last) break;
       }
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     c += __shfl_xor(c, 16);
     c += __shfl_xor(c, 32);
+    c += off[0];
 
     // the waves' results together
     __syncthreads();
@@ -263,11 +316,11 @@ __global__ void __launch_bounds__(256) kv4_step_kernel(Kv4Step a) {
       if (whole) {
         for (int j = 0; j < 8; ++j) w4_store(a.out.type, a.out.data, token * a.out.ld_token + query * a.out.ld_head + d + j, total == 0.f ? 0.f : v[j] / total);
       } else {
-        float* to = a.part + ((int64_t)blockIdx.x * a.rows + row) * a.dim + d;
+        float* to = a.part + ((int64_t)blockIdx.z * a.rows + row) * a.dim + d;
         for (int j = 0; j < 8; ++j) to[j] = v[j];
       }
       if (d == 0 && a.stats) {
-        float* to = a.stats + ((int64_t)blockIdx.x * a.rows + row) * 2;
+        float* to = a.stats + ((int64_t)blockIdx.z * a.rows + row) * 2;
         to[0] = high, to[1] = total;
       }
     }

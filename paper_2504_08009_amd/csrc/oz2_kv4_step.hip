@@ -7,41 +7,60 @@ extern template hipError_t oz2_kv4_step_of<OZ2_F16>(const Kv4Step&, dim3, hipStr
 
 namespace {
 
-// One wave a row: the parts of its chunks, each with a maximum of its own.
-__global__ void __launch_bounds__(256) kv4_join_kernel(Kv4Step a) {
-  const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-  const int lane = threadIdx.x % 64;
-  if (row >= a.rows) return;
-  const int64_t token = row / a.heads, query = row % a.heads;
-  const int64_t s = kv_sequence(a.on.cu, a.on.sequences, token);
+// A workgroup a row: the parts of its chunks, each with a maximum of its own.  A thread has four dims of every 1024 / dim-th chunk.
+__global__ void __launch_bounds__(256) kv4_join_kernel(Kv4Step a, FastDiv per_heads) {
+  __shared__ float factor[256], sums[256][4], most[4], totals[4];
+  const int row = blockIdx.x, at = row / per_heads, query = row - at * a.heads, thread = threadIdx.x, lane = thread % 64, wave = thread / 64;
+  const int64_t token = at, s = kv_sequence(a.on.cu, a.on.sequences, token);
   const KvRange r = kv_range(a.on.cu, s, a.on.tokens);
   if (token < r.begin || token >= r.end) return;
   const int held = kv_held(a.on.lengths, s, a.capacity);
   if (held <= a.chunk) return;
   const int chunks = (held + a.chunk - 1) / a.chunk;
-  float high = -3e38f, total = 0.f;
-  for (int i = lane; i < chunks; i += 64) high = fmaxf(high, a.stats[(i * a.rows + row) * 2]);
+  const float2* stats = reinterpret_cast<const float2*>(a.stats) + row;
+  float high = -3e38f;
+  for (int i = thread; i < chunks; i += 256) high = fmaxf(high, stats[i * a.rows].x);
   for (int d = 32; d; d /= 2) high = fmaxf(high, __shfl_xor(high, d));
-  float v[4] = {};
-  for (int i = 0; i < chunks; ++i) {
-    const float f = __builtin_amdgcn_exp2f(a.stats[(i * a.rows + row) * 2] - high);
-    total = fmaf(f, a.stats[(i * a.rows + row) * 2 + 1], total);
-    const float* part = a.part + (i * a.rows + row) * a.dim;
-    for (int j = 0; j < 4; ++j)
-      if (j * 64 + lane < a.dim) v[j] = fmaf(f, part[j * 64 + lane], v[j]);
+  if (lane == 0) most[wave] = high;
+  __syncthreads();
+  high = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+  const int fours = a.dim / 4, part = thread / fours, parts = 256 / fours, d = thread % fours * 4;
+  float total = 0.f, v[4] = {};
+  for (int c0 = 0; c0 < chunks; c0 += 256) {
+    const int n = min(256, chunks - c0);
+    __syncthreads();
+    if (thread < n) {
+      const float2 own = stats[(c0 + thread) * a.rows];
+      factor[thread] = __builtin_amdgcn_exp2f(own.x - high);
+      total = fmaf(factor[thread], own.y, total);
+    }
+    __syncthreads();
+    if (part < parts) {
+#pragma unroll 4
+      for (int i = part; i < n; i += parts) {
+        const float4 x = *reinterpret_cast<const float4*>(a.part + ((c0 + i) * a.rows + row) * a.dim + d);
+        v[0] = fmaf(factor[i], x.x, v[0]), v[1] = fmaf(factor[i], x.y, v[1]), v[2] = fmaf(factor[i], x.z, v[2]), v[3] = fmaf(factor[i], x.w, v[3]);
+      }
+    }
   }
-  for (int j = 0; j < 4; ++j)
-    if (j * 64 + lane < a.dim)
-      w4_store(a.out.type, a.out.data, token * a.out.ld_token + query * a.out.ld_head + j * 64 + lane, total == 0.f ? 0.f : v[j] / total);
+  for (int i = 32; i; i /= 2) total += __shfl_xor(total, i);
+  if (lane == 0) totals[wave] = total;
+  for (int j = 0; j < 4; ++j) sums[thread][j] = v[j];
+  __syncthreads();
+  if (part) return;
+  total = totals[0] + totals[1] + totals[2] + totals[3];
+  for (int p = 1; p < parts; ++p)
+    for (int j = 0; j < 4; ++j) v[j] += sums[p * fours + thread][j];
+  for (int j = 0; j < 4; ++j) w4_store(a.out.type, a.out.data, token * a.out.ld_token + query * a.out.ld_head + d + j, total == 0.f ? 0.f : v[j] / total);
 }
 
 // What each place received, from the scores and the rows' maxima and sums.
 __global__ void __launch_bounds__(256) kv4_received_kernel(Kv4Step a) {
   __shared__ float top[64], inverse[64];
-  const int head = blockIdx.y, s = blockIdx.z, place = blockIdx.x * 256 + threadIdx.x;
+  const int head = blockIdx.x, s = blockIdx.y, place = blockIdx.z * 256 + threadIdx.x;
   const KvRange r = kv_range(a.on.cu, s, a.on.tokens);
   const int held = kv_held(a.on.lengths, s, a.capacity), rows = (int)(r.end - r.begin) * a.group;
-  if ((int)blockIdx.x * 256 >= held || rows == 0) return;
+  if ((int)blockIdx.z * 256 >= held || rows == 0) return;
   const int chunks = (held + a.chunk - 1) / a.chunk;
   float sum = 0.f;
   for (int r0 = 0; r0 < rows; r0 += 64) {
@@ -68,10 +87,13 @@ __global__ void __launch_bounds__(256) kv4_received_kernel(Kv4Step a) {
   if (place < held) a.on.weights[s * a.on.weights_sequence + head * a.on.weights_head + place] += sum;
 }
 
+// About a thousand workgroups where there are places enough for them, two rounds of the card; up to 4096 places each, since the begin of a workgroup (some 4 us until
+// its first tile is there) is to be spread over enough of them, and no more, since lengths differ.
+// us with 256 / 1024 / 4096 places: 64 sequences of 2048 to 32768 360 / 213 / 183, 16 of 2000 to 8192 47 / 36 / 46, one of 4096 (8 kv heads) 8 / 14 / 36.
 int64_t chunk_of(int64_t capacity, int64_t pairs) {
-  const int64_t each = (capacity * pairs + 4095) / 4096;
+  const int64_t each = (capacity * pairs + 1023) / 1024;
   const int64_t chunk = (each + 127) / 128 * 128;
-  return chunk < 128 ? 128 : chunk;
+  return chunk < 128 ? 128 : chunk < 4096 ? chunk : 4096;
 }
 size_t rounded(int64_t n) { return (size_t)((n + 63) / 64 * 64) * 4; }
 struct Space { size_t part, stats, scores; };
@@ -103,16 +125,18 @@ hipError_t oz2_launch_kv4_attention(const oz2_kv4_cache& cache, const oz2_kv4_se
   a.stats = n.stats ? reinterpret_cast<float*>(ws + n.part) : nullptr;
   a.scores = n.scores ? reinterpret_cast<float*>(ws + n.part + n.stats) : nullptr;
   a.rows = rows;
-  const dim3 grid((unsigned)chunks, (unsigned)cache.heads, (unsigned)on.sequences);
+  // Chunks last: eight dies take workgroups in turn, and with chunks first one of them would get all first chunks, which every sequence has, and another the
+  // eighth, which few have (64 sequences of 2048 to 32768 places, 8 kv heads: 355 us so, 150 with chunks last).
+  const dim3 grid((unsigned)cache.heads, (unsigned)on.sequences, (unsigned)chunks);
   hipError_t rc = q.type == OZ2_F32    ? oz2_kv4_step_of<OZ2_F32>(a, grid, st)
                   : q.type == OZ2_BF16 ? oz2_kv4_step_of<OZ2_BF16>(a, grid, st)
                                        : oz2_kv4_step_of<OZ2_F16>(a, grid, st);
   if (rc == hipSuccess && chunks > 1) {
-    hipLaunchKernelGGL(kv4_join_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(kv4_join_kernel, dim3((unsigned)rows), dim3(256), 0, st, a, fast_div((unsigned)heads));
     rc = hipGetLastError();
   }
   if (rc == hipSuccess && on.weights && capacity) {
-    hipLaunchKernelGGL(kv4_received_kernel, dim3((unsigned)((capacity + 255) / 256), (unsigned)cache.heads, (unsigned)on.sequences), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(kv4_received_kernel, dim3((unsigned)cache.heads, (unsigned)on.sequences, (unsigned)((capacity + 255) / 256)), dim3(256), 0, st, a);
     rc = hipGetLastError();
   }
   return rc;
