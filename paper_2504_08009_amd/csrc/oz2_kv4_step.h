@@ -3,9 +3,11 @@
 // A workgroup has a chunk of places of one sequence and kv head; its four waves take tiles of 32 places in turn, and sixteen rows (pairs of a new token and
 // one of the kv head's query heads) at a time.  For a tile, with c the codes of a key or value, s and o its scale and offset:
 //   t = s sum_d q_d c_d + o sum_d q_d,    p = exp2(scale log2(e) t - m),    numerator_d = sum p s c_d + sum p o,    denominator = sum p
-// Codes go to the matrix cores as bf16 16 + c (bits put under an exponent: a shift and an and-or for two); the 16 comes off again as -16 sum q (what the
-// sums start from) and -16 sum p s.  q is made of one bf16 (bf16), two (f16) or three (f32) exactly, p s of two bf16, or three for FP32 results: an error of 2^-17 or
-// 2^-25 of it.
+// Codes go to the matrix cores as they lie in a word, where the bits of a bf16 below 2^-125 count in steps of 2^-133 from 0 on, with and without an exponent: four
+// bits at the bottom of a half word are c 2^-133, the four above them c 2^-129, and an AND makes operands of two codes.  q is taken times 2^64 (2^60 where
+// it meets the latter) and p times 2^80, so that sums are far from either end of FP32; the powers of two come off again in `scale2` and at the end.
+// Nothing is added to a code and taken off later, so nothing cancels.  q is made of one bf16 (bf16), two (f16) or three (f32) exactly, p s of two bf16, or three for
+// FP32 results: an error of 2^-16 or 2^-24 of it.
 // The products are keys x rows and then dims x rows, so that every lane has one row throughout: what the first product leaves in a lane (four places of each
 // half of the tile) is what it needs as its part of the second's operand, and maxima and sums stay in lanes until the end.  m is raised only
 // where a score is more than 2^8 above it.
@@ -28,7 +30,7 @@ struct Kv4Step {
   oz2_rows q, out;
   int heads, group, dim, capacity, page_size, chunk;
   FastDiv per_page, per_group;
-  float scale2;  // scale log2(e)
+  float scale2;  // scale log2(e) kStepScore
   // of (chunk, row) and, of scores, (row, place); rows are those of q, (token, head)
   float *part, *stats, *scores;
   int64_t rows;
@@ -47,10 +49,10 @@ __device__ __forceinline__ unsigned bf16_term(float& a, float& b) {
   a -= __uint_as_float(w << 16), b -= __uint_as_float(w & 0xffff0000u);
   return w;
 }
-// codes j and j + 4 of a word as a pair of bf16 16 + c.  `mask` is 0x00780078 in a vector register: an and-or takes one constant from elsewhere.
-__device__ __forceinline__ unsigned code_pair(unsigned w, int j, unsigned mask) {
-  return ((j == 0 ? w << 3 : w >> (4 * j - 3)) & mask) | 0x41804180u;
-}
+// codes j and j + 4 of a word (j even: at the bottom of `w` as it comes or shifted by 8 bits; odd: above it), see above
+__device__ __forceinline__ unsigned code_pair(unsigned w, int j) { return (j < 2 ? w : w >> 8) & (j % 2 ? 0x00f000f0u : 0x000f000fu); }
+constexpr float kStepUp = 0x1p64f, kStepUpOdd = 0x1p60f, kStepScore = 0x1p69f;          // q; what brings sums of q c back
+constexpr float kStepShift = 80.f, kStepDown = 0x1p-80f, kStepBack = 0x1p53f, kStepBackOdd = 0x1p49f;  // log2 of p's factor, what takes it off; off sums of p s c
 __device__ __forceinline__ w4_f4 step_mfma(w4_u4 a, w4_u4 b, w4_f4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(w4_bf8, a), __builtin_bit_cast(w4_bf8, b), c, 0, 0, 0);
 }
@@ -109,8 +111,6 @@ __global__ void __launch_bounds__(256, XT != OZ2_F32 && DP <= 128 ? 3 : 1) kv4_s
   typedef const int32_t __attribute__((address_space(4)))* Scalars;
   const Scalars table = (Scalars)(uintptr_t)(a.on.table + s * a.on.ld_table);
 
-  unsigned mask = 0x00780078u;
-  asm("" : "+v"(mask));
   const int64_t codes_head = head * a.c.codes_head, scales_head = head * a.c.scales_head;
   const int bytes = WIDE ? DP / 2 : a.dim / 2;
   // where a lane's words are among sixteen rows; words past a row's end are read from its start, and meet zeros of q or are not stored
@@ -170,15 +170,19 @@ __global__ void __launch_bounds__(256, XT != OZ2_F32 && DP <= 128 ? 3 : 1) kv4_s
       const int word = WIDE ? quarter * E + e : e * 4 + quarter;
       float x[8] = {};
       if (word * 8 < a.dim) kv_load8<XT>(a.q.data, token * a.q.ld_token + query * a.q.ld_head + word * 8, x);
-      for (int j = 0; j < 8; ++j) sum += x[j];
+      for (int j = 0; j < 8; ++j) {
+        sum += x[j];
+        x[j] *= j % 2 ? kStepUpOdd : kStepUp;
+      }
       for (int t = 0; t < PARTS; ++t)
         for (int j = 0; j < 4; ++j) q[t][e][j] = bf16_term(x[j], x[j + 4]);
     }
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
+    sum *= 1.f / kStepScore;
 
     float m = -3e38f, l = 0.f, c = 0.f;  // m: finite, so that nothing that is not seen becomes a NaN
-    w4_f4 o[F], off = {0.f, 0.f, 0.f, 0.f};
+    w4_f4 o[F];
     for (int f = 0; f < F; ++f) o[f] = w4_f4{0.f, 0.f, 0.f, 0.f};
 
     // a tile's places: `cut` where some are hidden from some row
@@ -200,12 +204,12 @@ __global__ void __launch_bounds__(256, XT != OZ2_F32 && DP <= 128 ? 3 : 1) kv4_s
       float t[8];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        w4_f4 acc = {-16.f * sum, -16.f * sum, -16.f * sum, -16.f * sum};
+        w4_f4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           w4_u4 k;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) k[j] = code_pair(now.k[i][e], j, mask);
+          for (int j = 0; j < 4; ++j) k[j] = code_pair(now.k[i][e], j);
 #pragma unroll
           for (int x = 0; x < PARTS; ++x) acc = step_mfma(k, q[x][e], acc);
         }
@@ -226,19 +230,19 @@ __global__ void __launch_bounds__(256, XT != OZ2_F32 && DP <= 128 ? 3 : 1) kv4_s
         }
       }
       const float top = max3(max3(max3(t[0], t[1], t[2]), t[3], t[4]), max3(t[5], t[6], t[7]), t[7]);
-      if (__any(fmaf(top, a.scale2, -m) > 8.f)) {
+      if (__any(fmaf(top, a.scale2, kStepShift - m) > kStepShift + 8.f)) {
         float high = fmaxf(top, __shfl_xor(top, 16));
         high = fmaxf(high, __shfl_xor(high, 32));
         const float raised = fmaxf(m, high * a.scale2), f = __builtin_amdgcn_exp2f(m - raised);
         m = raised;
-        l *= f, c *= f, off *= f;
+        l *= f, c *= f;
 #pragma unroll
         for (int i = 0; i < F; ++i) o[i] *= f;
       }
       float w[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(t[i], a.scale2, -m));
+        const float p = __builtin_amdgcn_exp2f(fmaf(t[i], a.scale2, kStepShift - m));
         l += p;
         w[i] = fmaf(p, half_of(now.vs[i / 4][i % 4], 0), 0.f);
         c = fmaf(p, half_of(now.vs[i / 4][i % 4], 1), c);
@@ -248,8 +252,6 @@ __global__ void __launch_bounds__(256, XT != OZ2_F32 && DP <= 128 ? 3 : 1) kv4_s
       for (int x = 0; x < TERMS; ++x)
 #pragma unroll
         for (int j = 0; j < 4; ++j) b[x][j] = bf16_term(w[2 * j], w[2 * j + 1]);
-#pragma unroll
-      for (int x = 0; x < TERMS; ++x) off = step_mfma(w4_u4{0xc180c180u, 0xc180c180u, 0xc180c180u, 0xc180c180u}, b[x], off);  // -16 sum p s, of what the terms are
 #pragma unroll
       for (int u = 0; u < (DP + 127) / 128; ++u) {
         unsigned low[4], high[4];
@@ -262,7 +264,7 @@ __global__ void __launch_bounds__(256, XT != OZ2_F32 && DP <= 128 ? 3 : 1) kv4_s
         for (int e = 0; e < (DP == 64 ? 4 : 8); ++e) {
           w4_u4 v;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] = code_pair(e < 4 ? low[j] : high[j], e % 4, mask);
+          for (int j = 0; j < 4; ++j) v[j] = code_pair(e < 4 ? low[j] : high[j], e % 4);
 #pragma unroll
           for (int x = 0; x < TERMS; ++x) o[u * 8 + e] = step_mfma(v, b[x], o[u * 8 + e]);
         }
@@ -289,13 +291,13 @@ __global__ void __launch_bounds__(256, XT != OZ2_F32 && DP <= 128 ? 3 : 1) kv4_s
     l += __shfl_xor(l, 32);
     c += __shfl_xor(c, 16);
     c += __shfl_xor(c, 32);
-    c += off[0];
+    l *= kStepDown, c *= kStepDown;
 
     // the waves' results together
     __syncthreads();
     if (quarter == 0) merged_m[wave][col] = m, merged_l[wave][col] = l, merged_c[wave][col] = c;
     for (int f = 0; f < F; ++f)
-      for (int i = 0; i < 4; ++i) merged[wave][col][(quarter * 4 + i) * F + f] = o[f][i];
+      for (int i = 0; i < 4; ++i) merged[wave][col][(quarter * 4 + i) * F + f] = o[f][i] * (f % 2 ? kStepBackOdd : kStepBack);
     __syncthreads();
     for (int at = threadIdx.x; at < kStepRows * (DP / 8); at += 256) {
       const int b = at / (DP / 8), d = at % (DP / 8) * 8;

@@ -1,8 +1,8 @@
 """Caches of keys and values held in 4 bits: appending, attention, evicting, against their formulas in 64 bits.
 
-Tolerances of attention (u = 2^-24).  The kernels sum (16 + c) q with c the codes, and take 16 sum q off again: with B = sum |q| the score's error is at most
+Tolerances of attention (u = 2^-24) allow for sums of (16 + c) q with c the codes, of which 16 sum q is taken off again: with B = sum |q| the score's error is at most
 e = (dim + 48) u scale max (s 47 B + |o| B), and p is off by a factor within 1 +- (2 e + 8 u).  p s is rounded to two bf16 terms, by 2^-16 of it (three for FP32: 2^-24), and
-meets 16 + c, of which 16 sum p s is taken off: with A = sum p (47 s + |o|) a result is off by at most (2 e + r + (n + 72) u) (A + |out|), r = 2^-16 or 2^-24, times 2
+meets 16 + c likewise: with A = sum p (47 s + |o|) a result is off by at most (2 e + r + (n + 72) u) (A + |out|), r = 2^-16 or 2^-24, times 2
 for what is of second order, before the one rounding to its type.  What a place received is a sum of p: off by at most (2 e + (n + 72) u) of it and u of the weight."""
 import math
 
