@@ -6,7 +6,8 @@
 // Codes go to the matrix cores as they lie in a word, where the bits of a bf16 below 2^-125 count in steps of 2^-133 from 0 on, with and without an exponent: four
 // bits at the bottom of a half word are c 2^-133, the four above them c 2^-129, and an AND makes operands of two codes.  q is taken times 2^64 (2^60 where
 // it meets the latter) and p times 2^80, so that sums are far from either end of FP32; the powers of two come off again in `scale2` and at the end.
-// Nothing is added to a code and taken off later, so nothing cancels.  q is made of one bf16 (bf16), two (f16) or three (f32) exactly, p s of two bf16, or three for
+// Nothing has to be added to a code and taken off later.  (FP32 results would show that the matrix cores cut sums off instead of rounding them, in
+// proportion to the sums of codes, which lie on one side of 0: for them operands are 2 (c - 7.5), at four instructions a pair, and the offsets o + 7.5 s.)  q is made of one bf16 (bf16), two (f16) or three (f32) exactly, p s of two bf16, or three for
 // FP32 results: an error of 2^-16 or 2^-24 of it.
 // The products are keys x rows and then dims x rows, so that every lane has one row throughout: what the first product leaves in a lane (four places of each
 // half of the tile) is what it needs as its part of the second's operand, and maxima and sums stay in lanes until the end.  m is raised only
@@ -30,7 +31,7 @@ struct Kv4Step {
   oz2_rows q, out;
   int heads, group, dim, capacity, page_size, chunk;
   FastDiv per_page, per_group;
-  float scale2;  // scale log2(e) kStepScore
+  float scale2;  // scale log2(e) over the factor of the scores
   // of (chunk, row) and, of scores, (row, place); rows are those of q, (token, head)
   float *part, *stats, *scores;
   int64_t rows;
@@ -49,10 +50,22 @@ __device__ __forceinline__ unsigned bf16_term(float& a, float& b) {
   a -= __uint_as_float(w << 16), b -= __uint_as_float(w & 0xffff0000u);
   return w;
 }
-// codes j and j + 4 of a word (j even: at the bottom of `w` as it comes or shifted by 8 bits; odd: above it), see above
-__device__ __forceinline__ unsigned code_pair(unsigned w, int j) { return (j < 2 ? w : w >> 8) & (j % 2 ? 0x00f000f0u : 0x000f000fu); }
-constexpr float kStepUp = 0x1p64f, kStepUpOdd = 0x1p60f, kStepScore = 0x1p69f;          // q; what brings sums of q c back
-constexpr float kStepShift = 80.f, kStepDown = 0x1p-80f, kStepBack = 0x1p53f, kStepBackOdd = 0x1p49f;  // log2 of p's factor, what takes it off; off sums of p s c
+// codes j and j + 4 of a word as bf16 in steps of 2^-133: c itself (j odd: 16 c), or 2 (c - 7.5) = +- (2 m + 1) of a word whose codes step_centred has made
+// (sign, m)
+template <bool CENTRED>
+__device__ __forceinline__ unsigned code_pair(unsigned w, int j) {
+  if constexpr (!CENTRED) return (j < 2 ? w : w >> 8) & (j % 2 ? 0x00f000f0u : 0x000f000fu);
+  else return ((j == 0 ? w << 1 : w >> (4 * j - 1)) & 0x000e000eu) | 0x00010001u | (w << (12 - 4 * j) & 0x80008000u);
+}
+__device__ __forceinline__ unsigned step_centred(unsigned w) {
+  const unsigned sign = ~w & 0x88888888u;
+  return ((w & 0x77777777u) ^ (sign - (sign >> 3))) | sign;
+}
+constexpr float kStepUp = 0x1p64f, kStepFactor = 0x1p80f;  // of q, and of p
+// what brings sums of q c and of p s c back: operands come in steps of 2^-133, or twice that
+template <int XT> constexpr bool step_is_centred() { return XT == OZ2_F32; }
+template <int XT> constexpr float step_score() { return step_is_centred<XT>() ? 0x1p68f : 0x1p69f; }
+template <int XT> constexpr float step_back() { return step_is_centred<XT>() ? 0x1p52f : 0x1p53f; }
 __device__ __forceinline__ w4_f4 step_mfma(w4_u4 a, w4_u4 b, w4_f4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(w4_bf8, a), __builtin_bit_cast(w4_bf8, b), c, 0, 0, 0);
 }
@@ -96,8 +109,11 @@ struct StepTile {
 template <int XT, int DP, bool WIDE>
 __global__ void __launch_bounds__(256, XT != OZ2_F32 && DP <= 128 ? 3 : 1) kv4_step_kernel(Kv4Step a) {
   constexpr int E = DP / 32, F = DP / 16, PARTS = step_parts<XT>(), TERMS = XT == OZ2_F32 ? 3 : 2;
+  // p's factor comes with the exponent, for which that has seven bits less: 2^-18 of p, which FP32 results would show; there p s is multiplied by it
   __shared__ float merged[kStepWaves][kStepRows][DP + 1];
   __shared__ float merged_m[kStepWaves][kStepRows], merged_l[kStepWaves][kStepRows], merged_c[kStepWaves][kStepRows];
+  constexpr bool CENTRED = step_is_centred<XT>();
+  constexpr float SHIFT = XT == OZ2_F32 ? 0.f : 80.f;
   const int head = blockIdx.x, s = blockIdx.y, lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int col = lane % 16, quarter = lane / 16;
   const KvRange r = kv_range(a.on.cu, s, a.on.tokens);
@@ -172,14 +188,14 @@ __global__ void __launch_bounds__(256, XT != OZ2_F32 && DP <= 128 ? 3 : 1) kv4_s
       if (word * 8 < a.dim) kv_load8<XT>(a.q.data, token * a.q.ld_token + query * a.q.ld_head + word * 8, x);
       for (int j = 0; j < 8; ++j) {
         sum += x[j];
-        x[j] *= j % 2 ? kStepUpOdd : kStepUp;
+        x[j] *= !CENTRED && j % 2 ? kStepUp / 16 : kStepUp;
       }
       for (int t = 0; t < PARTS; ++t)
         for (int j = 0; j < 4; ++j) q[t][e][j] = bf16_term(x[j], x[j + 4]);
     }
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    sum *= 1.f / kStepScore;
+    sum *= 1.f / step_score<XT>();
 
     float m = -3e38f, l = 0.f, c = 0.f;  // m: finite, so that nothing that is not seen becomes a NaN
     w4_f4 o[F];
@@ -208,13 +224,15 @@ __global__ void __launch_bounds__(256, XT != OZ2_F32 && DP <= 128 ? 3 : 1) kv4_s
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           w4_u4 k;
+          const unsigned word = CENTRED ? step_centred(now.k[i][e]) : now.k[i][e];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) k[j] = code_pair(now.k[i][e], j);
+          for (int j = 0; j < 4; ++j) k[j] = code_pair<CENTRED>(word, j);
 #pragma unroll
           for (int x = 0; x < PARTS; ++x) acc = step_mfma(k, q[x][e], acc);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) t[4 * i + j] = fmaf(half_of(now.ks[i][j], 0), acc[j], fmaf(half_of(now.ks[i][j], 1), sum, 0.f));  // (+ 0: one instruction that takes FP16)
+        for (int j = 0; j < 4; ++j) t[4 * i + j] = fmaf(half_of(now.ks[i][j], 0), acc[j], (CENTRED ? fmaf(7.5f, half_of(now.ks[i][j], 0), half_of(now.ks[i][j], 1)) * sum
+                                                                           : fmaf(half_of(now.ks[i][j], 1), sum, 0.f)));  // (+ 0: one instruction that takes FP16)
       }
       if (cut) {
         asm volatile("" : "+v"(hidden));  // (a branch: eight selects by conditions that hardly ever hold cost more)
@@ -230,7 +248,7 @@ __global__ void __launch_bounds__(256, XT != OZ2_F32 && DP <= 128 ? 3 : 1) kv4_s
         }
       }
       const float top = max3(max3(max3(t[0], t[1], t[2]), t[3], t[4]), max3(t[5], t[6], t[7]), t[7]);
-      if (__any(fmaf(top, a.scale2, kStepShift - m) > kStepShift + 8.f)) {
+      if (__any(fmaf(top, a.scale2, SHIFT - m) > SHIFT + 8.f)) {
         float high = fmaxf(top, __shfl_xor(top, 16));
         high = fmaxf(high, __shfl_xor(high, 32));
         const float raised = fmaxf(m, high * a.scale2), f = __builtin_amdgcn_exp2f(m - raised);
@@ -242,10 +260,12 @@ __global__ void __launch_bounds__(256, XT != OZ2_F32 && DP <= 128 ? 3 : 1) kv4_s
       float w[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(t[i], a.scale2, kStepShift - m));
+        const float p = __builtin_amdgcn_exp2f(fmaf(t[i], a.scale2, SHIFT - m));
         l += p;
         w[i] = fmaf(p, half_of(now.vs[i / 4][i % 4], 0), 0.f);
-        c = fmaf(p, half_of(now.vs[i / 4][i % 4], 1), c);
+        if constexpr (XT == OZ2_F32) w[i] *= kStepFactor;
+        const float shift = half_of(now.vs[i / 4][i % 4], 1);
+        c = fmaf(p, CENTRED ? fmaf(7.5f, half_of(now.vs[i / 4][i % 4], 0), shift) : shift, c);
       }
       w4_u4 b[TERMS];
 #pragma unroll
@@ -259,12 +279,13 @@ __global__ void __launch_bounds__(256, XT != OZ2_F32 && DP <= 128 ? 3 : 1) kv4_s
         for (int j = 0; j < 4; ++j) {
           low[j] = __builtin_amdgcn_perm(now.v[2 * j + 1][u], now.v[2 * j][u], 0x05040100);
           high[j] = __builtin_amdgcn_perm(now.v[2 * j + 1][u], now.v[2 * j][u], 0x07060302);
+          if constexpr (CENTRED) low[j] = step_centred(low[j]), high[j] = step_centred(high[j]);
         }
 #pragma unroll
         for (int e = 0; e < (DP == 64 ? 4 : 8); ++e) {
           w4_u4 v;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] = code_pair(e < 4 ? low[j] : high[j], e % 4);
+          for (int j = 0; j < 4; ++j) v[j] = code_pair<CENTRED>(e < 4 ? low[j] : high[j], e % 4);
 #pragma unroll
           for (int x = 0; x < TERMS; ++x) o[u * 8 + e] = step_mfma(v, b[x], o[u * 8 + e]);
         }
@@ -291,13 +312,13 @@ __global__ void __launch_bounds__(256, XT != OZ2_F32 && DP <= 128 ? 3 : 1) kv4_s
     l += __shfl_xor(l, 32);
     c += __shfl_xor(c, 16);
     c += __shfl_xor(c, 32);
-    l *= kStepDown, c *= kStepDown;
+    if constexpr (XT != OZ2_F32) l *= 1.f / kStepFactor, c *= 1.f / kStepFactor;
 
     // the waves' results together
     __syncthreads();
     if (quarter == 0) merged_m[wave][col] = m, merged_l[wave][col] = l, merged_c[wave][col] = c;
     for (int f = 0; f < F; ++f)
-      for (int i = 0; i < 4; ++i) merged[wave][col][(quarter * 4 + i) * F + f] = o[f][i] * (f % 2 ? kStepBackOdd : kStepBack);
+      for (int i = 0; i < 4; ++i) merged[wave][col][(quarter * 4 + i) * F + f] = o[f][i] * (!CENTRED && f % 2 ? step_back<XT>() / 16 : step_back<XT>());
     __syncthreads();
     for (int at = threadIdx.x; at < kStepRows * (DP / 8); at += 256) {
       const int b = at / (DP / 8), d = at % (DP / 8) * 8;

@@ -120,7 +120,7 @@ hipError_t oz2_launch_kv4_attention(const oz2_kv4_cache& cache, const oz2_kv4_se
   a.heads = (int)heads, a.group = (int)(heads / cache.heads), a.dim = (int)cache.dim, a.capacity = (int)capacity;
   a.page_size = (int)cache.page_size, a.chunk = (int)chunk;
   a.per_page = fast_div((unsigned)cache.page_size), a.per_group = fast_div((unsigned)a.group);
-  a.scale2 = scale * 1.44269504088896340736f * kStepScore;
+  a.scale2 = (float)(scale * 1.4426950408889634074) * (q.type == OZ2_F32 ? step_score<OZ2_F32>() : step_score<OZ2_BF16>());
   a.part = n.part ? reinterpret_cast<float*>(ws) : nullptr;
   a.stats = n.stats ? reinterpret_cast<float*>(ws + n.part) : nullptr;
   a.scores = n.scores ? reinterpret_cast<float*>(ws + n.part + n.stats) : nullptr;
