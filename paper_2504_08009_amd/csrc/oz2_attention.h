@@ -27,12 +27,10 @@ struct AttentionTile {
   int tokens, first;  // of the sequence, and the tile's first row
 };
 __device__ __forceinline__ AttentionTile attention_tile(const Attention& a, int64_t tile, int size) {
-  int64_t low = 0, high = a.sequences;
-  while (high - low > 1) {
-    const int64_t mid = (low + high) / 2, cu = a.cu[mid];
-    if ((cu < 0 ? 0 : cu) * a.group / size + mid <= tile) low = mid;
-    else high = mid;
-  }
+  const int64_t low = kv_sequence(a.sequences, [&](int64_t i) {
+    const int64_t cu = a.cu[i];
+    return (cu < 0 ? 0 : cu) * a.group / size + i <= tile;
+  });
   const KvRange r = kv_range(a.cu, low, a.tokens);
   const int64_t cu = a.cu[low], first = (tile - ((cu < 0 ? 0 : cu) * a.group / size + low)) * size;
   const int n = (int)(r.end - r.begin);

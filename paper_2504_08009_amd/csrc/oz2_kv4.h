@@ -35,15 +35,18 @@ __device__ __forceinline__ int kv_held(const int32_t* lengths, int64_t s, int ca
   return n < 0 ? 0 : n < capacity ? n : capacity;
 }
 
-// The last sequence that begins at or before a value, of `sequences` whose begins (plus `each` a sequence, times `times`, over `over`) ascend.
-__device__ __forceinline__ int64_t kv_sequence(const int32_t* cu, int64_t sequences, int64_t value) {
-  int64_t low = 0, high = sequences;  // cu[low] <= value < cu[high], if anything is
-  while (high - low > 1) {
-    const int64_t mid = (low + high) / 2;
-    if (cu[mid] <= value) low = mid;
-    else high = mid;
+// The last of `sequences` that has begun, where begun(i) holds up to one and for none behind it (begun(0) is not asked).  Same arguments in all lanes, which ask
+// for 64 sequences at a time.
+template <class Begun>
+__device__ __forceinline__ int64_t kv_sequence(int64_t sequences, Begun begun) {
+  int64_t first = 0, n = sequences;
+  while (n > 1) {
+    const int64_t step = (n + 63) / 64, i = (threadIdx.x % 64 + 1) * step;
+    const int64_t k = __popcll(__ballot(i < n && begun(first + i)));
+    first += k * step;
+    n = n - k * step < step ? n - k * step : step;
   }
-  return low;
+  return first;
 }
 
 // Eight values beside each other of a row, in FP32.

@@ -11,7 +11,7 @@ namespace {
 __global__ void __launch_bounds__(256) kv4_join_kernel(Kv4Step a, FastDiv per_heads) {
   __shared__ float factor[256], sums[256][4], most[4], totals[4];
   const int row = blockIdx.x, at = row / per_heads, query = row - at * a.heads, thread = threadIdx.x, lane = thread % 64, wave = thread / 64;
-  const int64_t token = at, s = kv_sequence(a.on.cu, a.on.sequences, token);
+  const int64_t token = at, s = kv_sequence(a.on.sequences, [&](int64_t i) { return a.on.cu[i] <= token; });
   const KvRange r = kv_range(a.on.cu, s, a.on.tokens);
   if (token < r.begin || token >= r.end) return;
   const int held = kv_held(a.on.lengths, s, a.capacity);
@@ -49,42 +49,42 @@ __global__ void __launch_bounds__(256) kv4_join_kernel(Kv4Step a, FastDiv per_he
   __syncthreads();
   if (part) return;
   total = totals[0] + totals[1] + totals[2] + totals[3];
+  if (thread == 0) const_cast<float2*>(stats)[0] = {high, total};  // the whole row's, in the place of its first chunk's: kv4_received_kernel reads them
   for (int p = 1; p < parts; ++p)
     for (int j = 0; j < 4; ++j) v[j] += sums[p * fours + thread][j];
   for (int j = 0; j < 4; ++j) w4_store(a.out.type, a.out.data, token * a.out.ld_token + query * a.out.ld_head + d + j, total == 0.f ? 0.f : v[j] / total);
 }
 
-// What each place received, from the scores and the rows' maxima and sums.
+// What each place received, from the scores and the rows' maxima and sums, which are in the places of their first chunks.
 __global__ void __launch_bounds__(256) kv4_received_kernel(Kv4Step a) {
   __shared__ float top[64], inverse[64];
+  __shared__ const float* scores[64];
   const int head = blockIdx.x, s = blockIdx.y, place = blockIdx.z * 256 + threadIdx.x;
+  const int held = kv_held(a.on.lengths, s, a.capacity);
+  if ((int)blockIdx.z * 256 >= held) return;
   const KvRange r = kv_range(a.on.cu, s, a.on.tokens);
-  const int held = kv_held(a.on.lengths, s, a.capacity), rows = (int)(r.end - r.begin) * a.group;
-  if ((int)blockIdx.z * 256 >= held || rows == 0) return;
-  const int chunks = (held + a.chunk - 1) / a.chunk;
+  const int rows = (int)(r.end - r.begin) * a.group;
+  float* to = a.on.weights + s * a.on.weights_sequence + head * a.on.weights_head + place;
+  const float had = rows && place < held ? *to : 0.f;
   float sum = 0.f;
   for (int r0 = 0; r0 < rows; r0 += 64) {
     __syncthreads();
     const int n = min(64, rows - r0);
     if ((int)threadIdx.x < n) {
-      const int fresh = (r0 + threadIdx.x) / a.group;
-      const int64_t row = (r.begin + fresh) * a.heads + head * a.group + (r0 + threadIdx.x - fresh * a.group);
-      float high = -3e38f, total = 0.f;
-      for (int i = 0; i < chunks; ++i) high = fmaxf(high, a.stats[(i * a.rows + row) * 2]);
-      for (int i = 0; i < chunks; ++i) total = fmaf(__builtin_amdgcn_exp2f(a.stats[(i * a.rows + row) * 2] - high), a.stats[(i * a.rows + row) * 2 + 1], total);
-      top[threadIdx.x] = high;
+      const int fresh = (int)(r0 + threadIdx.x) / a.per_group;
+      const int64_t row = (r.begin + fresh) * a.heads + head * a.group + (r0 + (int)threadIdx.x - fresh * a.group);
+      const float total = a.stats[row * 2 + 1];
+      top[threadIdx.x] = a.stats[row * 2];
       inverse[threadIdx.x] = total == 0.f ? 0.f : 1.f / total;
+      scores[threadIdx.x] = a.scores + row * a.capacity;
     }
     __syncthreads();
     if (place < held) {
-      for (int i = 0; i < n; ++i) {
-        const int fresh = (r0 + i) / a.group;
-        const int64_t row = (r.begin + fresh) * a.heads + head * a.group + (r0 + i - fresh * a.group);
-        sum = fmaf(__builtin_amdgcn_exp2f(fmaf(a.scores[row * a.capacity + place], a.scale2, -top[i])), inverse[i], sum);
-      }
+#pragma unroll 4
+      for (int i = 0; i < n; ++i) sum = fmaf(__builtin_amdgcn_exp2f(fmaf(scores[i][place], a.scale2, -top[i])), inverse[i], sum);
     }
   }
-  if (place < held) a.on.weights[s * a.on.weights_sequence + head * a.on.weights_head + place] += sum;
+  if (rows && place < held) *to = had + sum;
 }
 
 // About a thousand workgroups where there are places enough for them, two rounds of the card; up to 4096 places each, since the begin of a workgroup (some 4 us until
