@@ -1,7 +1,7 @@
 // New tokens' keys and values into a cache held in 4 bits (oz2_kv4_append): a vector of dim values becomes dim codes with a scale and an offset.
 //
 // A vector belongs to the smallest power of two of lanes that have eight values each, which is one word of codes a lane; smallest and largest value are found
-// by shuffles.  Bound by the bytes of k and v.
+// across lanes.  Bound by the bytes of k and v.
 #include "oz2_kv4.h"
 #include "oz2_fast_div.h"
 #include "oz2_w4_core.h"
@@ -13,7 +13,7 @@ struct Append {
   oz2_kv4_sequences on;
   const int32_t* at;
   oz2_rows x[2], held[2];
-  int capacity, heads, page_size, lanes, vectors, total;  // vectors: a workgroup's
+  int capacity, heads, page_size, lanes, total;
   FastDiv per_heads, per_page;
 };
 
@@ -31,62 +31,102 @@ __device__ __forceinline__ float over(float v, int lanes, Op op) {
   return v;
 }
 
-template <int XT>
+// The last sequence from s on that begins at or before a token: mostly s, so in strides that double, then halve.
+__device__ __forceinline__ int64_t behind(const Append& a, int64_t s, int token) {
+  int64_t stride = 1;
+  for (; s + stride < a.on.sequences && a.on.cu[s + stride] <= token; stride *= 2) s += stride;
+  for (; stride > 1;) {
+    stride /= 2;
+    if (s + stride < a.on.sequences && a.on.cu[s + stride] <= token) s += stride;
+  }
+  return s;
+}
+
+// N vectors a lane: their loads are under way together.  With one, a workgroup has all heads of some tokens; with more, runs of tokens of one head, which it
+// writes beside each other.
+template <int XT, int N>
 __global__ void __launch_bounds__(256) kv4_append_kernel(Append a) {
   const int which = blockIdx.y;  // 0: keys, 1: values
-  const int lane = threadIdx.x % a.lanes, first = blockIdx.x * a.vectors;
-  const int vector = min(first + (int)threadIdx.x / a.lanes, a.total - 1), token = vector / a.per_heads, head = vector - token * a.heads;
+  const int lane = threadIdx.x % a.lanes, step = 256 / a.lanes;
+  // N == 1: vectors by tokens, then heads; else blocks of tokens, then heads, then tokens
+  const int block = blockIdx.x / a.per_heads, first = N == 1 ? (int)blockIdx.x * step : block * N * step;
   const int d = lane * 8;
   const oz2_rows& x = a.x[which];
-  float v[8];
-  const bool mine = first + (int)threadIdx.x / a.lanes < a.total && d < a.c.dim;
-  if (mine) kv_load8<XT>(x.data, token * x.ld_token + head * x.ld_head + d, v);
+  float v[N][8];
+  int token[N], head[N];
+  bool mine[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int i = first + n * step + (int)threadIdx.x / a.lanes, count = N == 1 ? a.total : (int)a.on.tokens, at = min(i, count - 1);
+    mine[n] = i < count && d < a.c.dim;
+    token[n] = N == 1 ? at / a.per_heads : at;
+    head[n] = N == 1 ? at - token[n] * a.heads : (int)blockIdx.x - block * a.heads;
+    if (mine[n]) kv_load8<XT>(x.data, token[n] * x.ld_token + head[n] * x.ld_head + d, v[n]);
+  }
 
-  // where it goes: the sequence of the workgroup's first token, or one behind it
-  const int begin = first / a.per_heads;
+  // where they go: the sequence of the workgroup's first token, or one behind it
+  const int begin = N == 1 ? first / a.per_heads : first;
   int64_t s = kv_sequence(a.on.sequences, [&](int64_t i) { return a.on.cu[i] <= begin; });
-  while (s + 1 < a.on.sequences && a.on.cu[s + 1] <= token) ++s;
-  const KvRange r = kv_range(a.on.cu, s, a.on.tokens);
-  const bool packed = mine && token >= r.begin && token < r.end;  // rows behind the last sequence are nobody's
-  const int place = kv_held(a.on.lengths, s, a.capacity) - (int)(r.end - token);
-  const int at = place / a.per_page;
-  int page = -1;
-  if (packed && place >= 0) page = a.on.table[s * a.on.ld_table + at];
-  const bool goes = page >= 0 && page < a.c.pages;
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    s = behind(a, s, token[n]);
+    const KvRange r = kv_range(a.on.cu, s, a.on.tokens);
+    const bool packed = mine[n] && token[n] >= r.begin && token[n] < r.end;  // rows behind the last sequence are nobody's
+    const int place = kv_held(a.on.lengths, s, a.capacity) - (int)(r.end - token[n]);
+    const int at = place / a.per_page;
+    int page = -1;
+    if (packed && place >= 0) page = a.on.table[s * a.on.ld_table + at];
+    const bool goes = page >= 0 && page < a.c.pages;
 
-  float low = INFINITY, high = -INFINITY, finite = 0.f;
-  if (mine) {
+    // (minimum and maximum keep a NaN)
+    float low = v[n][0], high = low;
+    if (mine[n]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) low = fminf(low, v[j]), high = fmaxf(high, v[j]), finite = fmaf(v[j], 0.f, finite);
-  }
-  low = over(low, a.lanes, [](float p, float q) { return fminf(p, q); });
-  high = over(high, a.lanes, [](float p, float q) { return fmaxf(p, q); });
-  finite = over(finite, a.lanes, [](float p, float q) { return p + q; });  // 0, or a NaN where a value is a NaN or an infinity
-  const _Float16 scale = (_Float16)((high - low) / 15.f + finite), offset = (_Float16)low;
-  const float s32 = (float)scale, o32 = (float)offset, inverse = 1.f / s32;
-  unsigned word = 0;
-  if (mine) {
+      for (int j = 1; j < 8; ++j) low = __builtin_elementwise_minimum(low, v[n][j]), high = __builtin_elementwise_maximum(high, v[n][j]);
+    } else low = INFINITY, high = -INFINITY;
+    low = over(low, a.lanes, [](float p, float q) { return __builtin_elementwise_minimum(p, q); });
+    high = over(high, a.lanes, [](float p, float q) { return __builtin_elementwise_maximum(p, q); });
+    // The quotient by 15 and the reciprocal, rounded correctly: what an approximation leaves is exact in an FMA, and once corrected by it is the nearest value
+    // (Markstein; neither 15 nor an FP16 value has a significand of ones alone).  Where the range is infinite they are NaNs.
+    const float range = high - low, part = range * (1.f / 15.f), fifteenth = fmaf(fmaf(-15.f, part, range), 1.f / 15.f, part);
+    const _Float16 scale = (_Float16)fifteenth, offset = (_Float16)low;
+    const float s32 = (float)scale, o32 = (float)offset, near = __builtin_amdgcn_rcpf(s32);
+    const float inverse = s32 == 0.f ? 0.f : fmaf(fmaf(-s32, near, 1.f), near, near);
+    unsigned word = 0;
+    if (mine[n]) {
+      float c[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      // (fmaxf and fminf take the other operand for a NaN: a code is 0 .. 15 whatever the value)
-      const float c = s32 == 0.f ? 0.f : fminf(fmaxf(rintf((v[j] - o32) * inverse), 0.f), 15.f);
-      word |= (unsigned)c << (4 * j);
-      v[j] = fmaf(s32, c, o32);
+      for (int j = 0; j < 8; ++j) {
+        c[j] = __builtin_amdgcn_fmed3f(rintf((v[n][j] - o32) * inverse), 0.f, 15.f);  // (of a NaN: 0)
+        v[n][j] = fmaf(s32, c[j], o32);
+      }
+      auto four = [&](int i) { return (unsigned)fmaf(fmaf(c[i + 3], 16.f, c[i + 2]), 256.f, fmaf(c[i + 1], 16.f, c[i])); };
+      word = four(0) | four(4) << 16;
     }
-  }
-  if (goes) {
-    const int in = place - at * a.page_size;
-    uint8_t* codes = which ? a.c.v_codes : a.c.k_codes;
-    *reinterpret_cast<unsigned*>(codes + page * a.c.codes_page + head * a.c.codes_head + (int64_t)in * (a.c.dim / 2) + d / 2) = word;
-    if (lane == 0) {
-      unsigned* scales = static_cast<unsigned*>(which ? a.c.v_scales : a.c.k_scales);
-      scales[page * a.c.scales_page + head * a.c.scales_head + in] = __builtin_bit_cast(uint16_t, scale) | (unsigned)__builtin_bit_cast(uint16_t, offset) << 16;
-      if (!which && a.at) a.on.positions[s * a.on.positions_sequence + head * a.on.positions_head + place] = a.at[token];
-      if (!which && a.on.weights) a.on.weights[s * a.on.weights_sequence + head * a.on.weights_head + place] = 0.f;
+    if (goes) {
+      const int in = place - at * a.page_size;
+      uint8_t* codes = which ? a.c.v_codes : a.c.k_codes;
+      *reinterpret_cast<unsigned*>(codes + page * a.c.codes_page + head[n] * a.c.codes_head + (int64_t)in * (a.c.dim / 2) + d / 2) = word;
+      if (lane == 0) {
+        unsigned* scales = static_cast<unsigned*>(which ? a.c.v_scales : a.c.k_scales);
+        scales[page * a.c.scales_page + head[n] * a.c.scales_head + in] = __builtin_bit_cast(uint16_t, scale) | (unsigned)__builtin_bit_cast(uint16_t, offset) << 16;
+        if (!which && a.at) a.on.positions[s * a.on.positions_sequence + head[n] * a.on.positions_head + place] = a.at[token[n]];
+        if (!which && a.on.weights) a.on.weights[s * a.on.weights_sequence + head[n] * a.on.weights_head + place] = 0.f;
+      }
     }
+    const oz2_rows& h = a.held[which];
+    if (h.data && packed) kv_store8<XT>(h.data, token[n] * h.ld_token + head[n] * h.ld_head + d, v[n]);
   }
-  const oz2_rows& h = a.held[which];
-  if (h.data && packed) kv_store8<XT>(h.data, token * h.ld_token + head * h.ld_head + d, v);
+}
+
+template <int XT>
+hipError_t append(const Append& a, hipStream_t st) {
+  const int step = 256 / a.lanes;
+  const int64_t once = (a.total + step - 1) / step, blocks = (a.on.tokens + 4 * step - 1) / (4 * step);
+  // (four at once where that leaves every compute unit eight workgroups: 54200 tokens of 8 heads of 128 values 67 us one by one, 55 so)
+  if (once >= 4 * 1024) hipLaunchKernelGGL((kv4_append_kernel<XT, 4>), dim3((unsigned)(blocks * a.heads), 2), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((kv4_append_kernel<XT, 1>), dim3((unsigned)once, 2), dim3(256), 0, st, a);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -94,12 +134,7 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(Append a) {
 hipError_t oz2_launch_kv4_append(const oz2_kv4_cache& cache, const oz2_kv4_sequences& on, const int32_t* at, const oz2_rows& k, const oz2_rows& v,
                                  const oz2_rows* held_k, const oz2_rows* held_v, hipStream_t st) {
   Append a = {cache, on, at, {k, v}, {held_k ? *held_k : oz2_rows{}, held_v ? *held_v : oz2_rows{}}, (int)(on.max_pages * cache.page_size), (int)cache.heads,
-              (int)cache.page_size, 1, 256, (int)(on.tokens * cache.heads), fast_div((unsigned)cache.heads), fast_div((unsigned)cache.page_size)};
+              (int)cache.page_size, 1, (int)(on.tokens * cache.heads), fast_div((unsigned)cache.heads), fast_div((unsigned)cache.page_size)};
   while (a.lanes * 8 < cache.dim) a.lanes *= 2;
-  a.vectors = 256 / a.lanes;
-  const dim3 grid((unsigned)((a.total + a.vectors - 1) / a.vectors), 2);
-  if (k.type == OZ2_F32) hipLaunchKernelGGL(kv4_append_kernel<OZ2_F32>, grid, dim3(256), 0, st, a);
-  else if (k.type == OZ2_BF16) hipLaunchKernelGGL(kv4_append_kernel<OZ2_BF16>, grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(kv4_append_kernel<OZ2_F16>, grid, dim3(256), 0, st, a);
-  return hipGetLastError();
+  return k.type == OZ2_F32 ? append<OZ2_F32>(a, st) : k.type == OZ2_BF16 ? append<OZ2_BF16>(a, st) : append<OZ2_F16>(a, st);
 }
