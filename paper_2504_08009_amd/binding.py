@@ -1,6 +1,7 @@
 """ctypes binding of liboz2.so.  Function names follow include/oz2.h; arguments are marshalled only."""
 import ctypes
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "liboz2.so")
@@ -505,12 +506,18 @@ class _Moe(ctypes.Structure):
 
 
 _types = {}
+_dtypes = []
+
+
+def _type_table():
+    import torch
+    _dtypes[:] = [torch.int32, torch.float32]
+    _types.update({torch.float32: OZ2_F32, torch.bfloat16: OZ2_BF16, torch.float16: OZ2_F16})
 
 
 def _type(dtype):
     if not _types:
-        import torch
-        _types.update({torch.float32: OZ2_F32, torch.bfloat16: OZ2_BF16, torch.float16: OZ2_F16})
+        _type_table()
     if dtype not in _types:
         raise Oz2Error("float32, bfloat16 or float16 wanted, got %s" % dtype)
     return _types[dtype]
@@ -695,55 +702,44 @@ def w4_moe_workspace_bytes(layer, tokens):
     return int(lib().oz2_w4_moe_workspace_bytes(layer.ref, tokens))
 
 
-class _Rows(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("ld_token", ctypes.c_int64), ("ld_head", ctypes.c_int64), ("type", ctypes.c_int)]
-
-
 class _Kv4(ctypes.Structure):
     _fields_ = ([(f, ctypes.c_int64) for f in ("pages", "page_size", "heads", "dim")] + [(f, ctypes.c_void_p) for f in ("k_codes", "v_codes")] +
                 [(f, ctypes.c_int64) for f in ("codes_page", "codes_head")] + [(f, ctypes.c_void_p) for f in ("k_scales", "v_scales")] +
                 [(f, ctypes.c_int64) for f in ("scales_page", "scales_head")])
 
 
-class _Sequences(ctypes.Structure):
-    _fields_ = [("sequences", ctypes.c_int64), ("max_pages", ctypes.c_int64), ("table", ctypes.c_void_p), ("ld_table", ctypes.c_int64), ("lengths", ctypes.c_void_p),
-                ("tokens", ctypes.c_int64), ("cu", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("positions_sequence", ctypes.c_int64),
-                ("positions_head", ctypes.c_int64), ("weights", ctypes.c_void_p), ("weights_sequence", ctypes.c_int64), ("weights_head", ctypes.c_int64)]
+# oz2_rows, oz2_kv4_sequences and oz2_kv4_kept as bytes: objects of ctypes structures take several times as long to make
+_pack_rows, _pack_sequences, _pack_kept = (struct.Struct(f).pack for f in ("Pqqi4x", "qqPqPqPPqqPqq", "PPqqPqq"))
 
 
-class _Kept(ctypes.Structure):
-    _fields_ = [("lengths", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("positions_sequence", ctypes.c_int64), ("positions_head", ctypes.c_int64),
-                ("weights", ctypes.c_void_p), ("weights_sequence", ctypes.c_int64), ("weights_head", ctypes.c_int64)]
-
-
-def _heads(name, x, index, tokens=None, heads=None, dim=None):
-    """(tokens, heads, dim) tensor on device `index`, its last dimension contiguous, as the library sees it"""
-    shape, strides = x.shape, x.stride()
-    if len(shape) != 3 or (shape[2] > 1 and strides[2] != 1) or (tokens is not None and shape[0] != tokens) or (heads is not None and shape[1] != heads) or (
-            dim is not None and shape[2] != dim):
-        raise Oz2Error("%s is (tokens, heads, dim)%s with the last dimension contiguous, got shape %s" % (
-            name, "" if heads is None and dim is None else " = (%s, %s, %s)" % tuple("." if v is None else v for v in (tokens, heads, dim)), tuple(shape)))
+def _heads(name, x, index, shape):
+    """(tokens, heads, dim) tensor of that shape on device `index`, its last dimension contiguous, as the library sees it"""
+    strides = x.stride()
+    if x.shape != shape or len(strides) != 3 or (strides[2] != 1 and shape[2] > 1):
+        raise Oz2Error("%s is (tokens, heads, dim) = %s with the last dimension contiguous, got shape %s" % (name, tuple(shape), tuple(x.shape)))
     if x.get_device() != index or index < 0:
         raise Oz2Error("%s is on %s: tensors of one call are on one GPU" % (name, x.device))
-    return _Rows(x.data_ptr(), strides[0], strides[1], _type(x.dtype))
+    return _pack_rows(x.data_ptr(), strides[0], strides[1], _type(x.dtype))
 
 
 def _integers(name, x, index, shape):
-    import torch
-    if x.dtype != torch.int32 or x.shape != shape or (x.dim() and x.shape[-1] > 1 and x.stride(-1) != 1):
+    if x.dtype is not _int32() or x.shape != shape or (x.stride()[-1] != 1 and shape[-1] > 1):
         raise Oz2Error("%s is int32 of shape %s, its last dimension contiguous, got %s %s" % (name, tuple(shape), x.dtype, tuple(x.shape)))
     if x.get_device() != index:
         raise Oz2Error("%s is on %s: tensors of one call are on one GPU" % (name, x.device))
     return x.data_ptr()
 
 
+def _int32():
+    if not _types:
+        _type_table()
+    return _dtypes[0]
+
+
 def _refuse_gradients(*tensors):
-    if any(v is not None and v.requires_grad for v in tensors):
-        _refuse_gradient()
-
-
-def _scale(scale, dim):
-    return dim ** -0.5 if scale is None else float(scale)
+    for v in tensors:
+        if v is not None and v.requires_grad:
+            _refuse_gradient()
 
 
 def attention(q, k, v, cu, causal=True, scale=None, out=None, stream=None):
@@ -752,18 +748,19 @@ def attention(q, k, v, cu, causal=True, scale=None, out=None, stream=None):
     the stream of the call; rows behind the last sequence are left as they were (where the result is made here, they are not set).  There is no gradient:
     tensors that require one are refused where one would be recorded."""
     _refuse_gradients(q, k, v, out)
-    index = q.get_device()
-    rows_q = _heads("q", q, index)
-    tokens, heads, dim = q.shape
-    rows_k = _heads("k", k, index, tokens, None, dim)
-    rows_v = _heads("v", v, index, tokens, k.shape[1], dim)
+    index, shape, of_kv = q.get_device(), q.shape, k.shape
+    rows_q = _heads("q", q, index, shape)
+    tokens, heads, dim = shape
+    if len(of_kv) != 3 or of_kv[0] != tokens or of_kv[2] != dim:
+        raise Oz2Error("k and v are (tokens, kv_heads, dim) = (%d, ., %d), got shape %s" % (tokens, dim, tuple(of_kv)))
+    rows_k, rows_v = _heads("k", k, index, of_kv), _heads("v", v, index, of_kv)
     if out is None:
-        out = _new(q, q.shape, q.dtype, stream)
-    rows_out = _heads("out", out, index, tokens, heads, dim)
-    if cu.dim() != 1 or not cu.shape[0]:
+        out = _new(q, shape, q.dtype, stream)
+    rows_out, of_cu = _heads("out", out, index, shape), cu.shape
+    if len(of_cu) != 1 or not of_cu[0]:
         raise Oz2Error("cu is (sequences + 1,) int32")
-    rc = lib().oz2_attention(tokens, cu.shape[0] - 1, _integers("cu", cu, index, cu.shape), heads, k.shape[1], dim, _scale(scale, dim), int(bool(causal)),
-                             ctypes.addressof(rows_q), ctypes.addressof(rows_k), ctypes.addressof(rows_v), ctypes.addressof(rows_out), _stream_on(stream, index))
+    rc = lib().oz2_attention(tokens, of_cu[0] - 1, _integers("cu", cu, index, of_cu), heads, of_kv[1], dim, dim ** -0.5 if scale is None else scale,
+                             bool(causal), rows_q, rows_k, rows_v, rows_out, _stream_on(stream, index))
     if rc:
         _check(rc, "oz2_attention")
     return out
@@ -807,60 +804,66 @@ class KV4Cache:
 
 
 def _places(name, x, cache, sequences, capacity, dtype):
-    if x.dtype != dtype or x.dim() != 3 or x.shape[0] != sequences or x.shape[1] != cache.heads or x.shape[2] < capacity or (x.shape[2] > 1 and x.stride(2) != 1):
+    shape, strides = x.shape, x.stride()
+    if x.dtype is not dtype or len(shape) != 3 or shape[0] != sequences or shape[1] != cache.heads or shape[2] < capacity or (strides[2] != 1 and shape[2] > 1):
         raise Oz2Error("%s is %s of shape (sequences, kv_heads, places) = (%d, %d, at least %d), its last dimension contiguous, got %s %s" % (
-            name, dtype, sequences, cache.heads, capacity, x.dtype, tuple(x.shape)))
+            name, dtype, sequences, cache.heads, capacity, x.dtype, tuple(shape)))
     if x.get_device() != cache.index:
         raise Oz2Error("%s is on %s: tensors of one call are on one GPU" % (name, x.device))
-    return x.data_ptr(), x.stride(0), x.stride(1)
+    return x.data_ptr(), strides[0], strides[1]
+
+
+_nowhere = (0, 0, 0)
 
 
 def _sequences(cache, table, lengths, tokens=0, cu=None, positions=None, weights=None):
-    import torch
-    if cache.index < 0:
+    index, shape = cache.index, table.shape
+    if index < 0:
         raise Oz2Error("tensors on the GPU wanted, got %s" % cache.device)
-    if table.dim() != 2:
+    if len(shape) != 2:
         raise Oz2Error("table is (sequences, pages) int32")
-    sequences, max_pages = table.shape
-    capacity = max_pages * cache.page_size
-    of_positions = (None, 0, 0) if positions is None else _places("positions", positions, cache, sequences, capacity, torch.int32)
-    of_weights = (None, 0, 0) if weights is None else _places("weights", weights, cache, sequences, capacity, torch.float32)
-    return _Sequences(sequences, max_pages, _integers("table", table, cache.index, table.shape), table.stride(0),
-                      _integers("lengths", lengths, cache.index, (sequences,)), tokens, None if cu is None else _integers("cu", cu, cache.index, (sequences + 1,)),
-                      *of_positions, *of_weights)
+    sequences, max_pages = shape
+    capacity, int32 = max_pages * cache.page_size, _int32()
+    of_positions = _nowhere if positions is None else _places("positions", positions, cache, sequences, capacity, int32)
+    of_weights = _nowhere if weights is None else _places("weights", weights, cache, sequences, capacity, _dtypes[1])
+    return _pack_sequences(sequences, max_pages, _integers("table", table, index, shape), table.stride()[0], _integers("lengths", lengths, index, (sequences,)),
+                           tokens, 0 if cu is None else _integers("cu", cu, index, (sequences + 1,)), *of_positions, *of_weights)
 
 
 def kv4_append(cache, k, v, cu, table, lengths, at=None, positions=None, weights=None, held=None, stream=None):
     """Appends the new tokens k and v (tokens, kv_heads, dim), packed by cu (sequences + 1) int32, to their sequences' last places (include/oz2.h): table (sequences, pages)
     int32, lengths (sequences) int32 with the new tokens counted.  at (tokens) int32: positions of the new tokens, stored in positions (sequences, kv_heads,
     places) int32; weights, of that shape in float32: set to 0 in the new places; held: (k, v) like the arguments, for what the cache then holds of them."""
-    held_k, held_v = (None, None) if held is None else held
+    held_k, held_v = _none if held is None else held
     _refuse_gradients(k, v, weights, held_k, held_v)
-    rows_k = _heads("k", k, cache.index, None, cache.heads, cache.dim)
-    tokens = k.shape[0]
-    rows_v = _heads("v", v, cache.index, tokens, cache.heads, cache.dim)
+    index, shape = cache.index, k.shape
+    if len(shape) != 3 or shape[1] != cache.heads or shape[2] != cache.dim:
+        raise Oz2Error("k and v are (tokens, kv_heads, dim) = (., %d, %d), got shape %s" % (cache.heads, cache.dim, tuple(shape)))
+    rows_k, rows_v, tokens = _heads("k", k, index, shape), _heads("v", v, index, shape), shape[0]
     on = _sequences(cache, table, lengths, tokens, cu, positions, weights)
     if (at is None) != (positions is None):
         raise Oz2Error("at and positions go together")
-    of_held = []
-    for name, x in (("held k", held_k), ("held v", held_v)):
-        of_held.append(None if x is None else _heads(name, x, cache.index, tokens, cache.heads, cache.dim))
-    rc = lib().oz2_kv4_append(cache.ref, ctypes.addressof(on), None if at is None else _integers("at", at, cache.index, (tokens,)), ctypes.addressof(rows_k),
-                              ctypes.addressof(rows_v), *(None if r is None else ctypes.addressof(r) for r in of_held), _stream_on(stream, cache.index))
+    rc = lib().oz2_kv4_append(cache.ref, on, None if at is None else _integers("at", at, index, (tokens,)), rows_k, rows_v,
+                              None if held_k is None else _heads("held k", held_k, index, shape), None if held_v is None else _heads("held v", held_v, index, shape),
+                              _stream_on(stream, index))
     if rc:
         _check(rc, "oz2_kv4_append")
 
 
+_none = (None, None)
+
+
 def _kv4_attention(call, name, first, cache, q, cu, table, lengths, scale, weights, out, stream):
     _refuse_gradients(q, weights, out)
-    rows_q = _heads("q", q, cache.index, None, None, cache.dim)
-    tokens, heads, dim = q.shape
+    index, shape = cache.index, q.shape
+    if len(shape) != 3 or shape[2] != cache.dim:
+        raise Oz2Error("q is (tokens, heads, dim) = (., ., %d), got shape %s" % (cache.dim, tuple(shape)))
+    rows_q = _heads("q", q, index, shape)
     if out is None:
-        out = _new(q, q.shape, q.dtype, stream)
-    rows_out = _heads("out", out, cache.index, tokens, heads, dim)
-    on = _sequences(cache, table, lengths, tokens, cu, None, weights)
-    rc = call(*first, cache.ref, ctypes.addressof(on), heads, _scale(scale, dim), ctypes.addressof(rows_q), ctypes.addressof(rows_out),
-              _stream_on(stream, cache.index))
+        out = _new(q, shape, q.dtype, stream)
+    rows_out = _heads("out", out, index, shape)
+    on = _sequences(cache, table, lengths, shape[0], cu, None, weights)
+    rc = call(*first, cache.ref, on, shape[1], shape[2] ** -0.5 if scale is None else scale, rows_q, rows_out, _stream_on(stream, index))
     if rc:
         _check(rc, name)
     return out
@@ -879,18 +882,18 @@ def kv4_attention_workspace_bytes(cache, table, tokens, heads, weights=False):
 
 
 def _kv4_evict(call, name, first, cache, table, lengths, positions, weights, keep, recent, out, stream):
-    import torch
     _refuse_gradients(weights, *(out or ()))
-    on = _sequences(cache, table, lengths, 0, None, positions, weights)
     if positions is None or weights is None:
         raise Oz2Error("positions and weights are needed")
+    on = _sequences(cache, table, lengths, 0, None, positions, weights)
     kept = None
     if out is not None:
         to_lengths, to_positions, to_weights = out
-        capacity = table.shape[1] * cache.page_size
-        kept = _Kept(_integers("lengths", to_lengths, cache.index, (table.shape[0],)), *_places("positions", to_positions, cache, table.shape[0], capacity, torch.int32),
-                     *_places("weights", to_weights, cache, table.shape[0], capacity, torch.float32))
-    rc = call(*first, cache.ref, ctypes.addressof(on), int(keep), int(recent), None if kept is None else ctypes.addressof(kept), _stream_on(stream, cache.index))
+        sequences, max_pages = table.shape
+        capacity = max_pages * cache.page_size
+        kept = _pack_kept(_integers("lengths", to_lengths, cache.index, (sequences,)), *_places("positions", to_positions, cache, sequences, capacity, _dtypes[0]),
+                          *_places("weights", to_weights, cache, sequences, capacity, _dtypes[1]))
+    rc = call(*first, cache.ref, on, keep, recent, kept, _stream_on(stream, cache.index))
     if rc:
         _check(rc, name)
     return (lengths, positions, weights) if out is None else tuple(out)

@@ -6,11 +6,28 @@ import pytest
 torch = pytest.importorskip("torch")
 
 import paper_2504_08009_amd as oz
-from paper_2504_08009_amd.binding import _Kept, _Kv4, _Rows, _Sequences
+from paper_2504_08009_amd import binding
+from paper_2504_08009_amd.binding import _Kv4
 
 P = 1 << 20  # an address that nobody reads
 F32, BF16, F16 = oz.OZ2_F32, oz.OZ2_BF16, oz.OZ2_F16
 INT64 = 2 ** 63 - 1
+
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("ld_token", ctypes.c_int64), ("ld_head", ctypes.c_int64), ("type", ctypes.c_int)]
+
+
+class _Sequences(ctypes.Structure):
+    _fields_ = [("sequences", ctypes.c_int64), ("max_pages", ctypes.c_int64), ("table", ctypes.c_void_p), ("ld_table", ctypes.c_int64), ("lengths", ctypes.c_void_p),
+                ("tokens", ctypes.c_int64), ("cu", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("positions_sequence", ctypes.c_int64),
+                ("positions_head", ctypes.c_int64), ("weights", ctypes.c_void_p), ("weights_sequence", ctypes.c_int64), ("weights_head", ctypes.c_int64)]
+
+
+class _Kept(ctypes.Structure):
+    _fields_ = [("lengths", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("positions_sequence", ctypes.c_int64), ("positions_head", ctypes.c_int64),
+                ("weights", ctypes.c_void_p), ("weights_sequence", ctypes.c_int64), ("weights_head", ctypes.c_int64)]
 
 
 def ref(s):
@@ -163,3 +180,9 @@ def test_workspaces_grow_with_what_is_asked():
     evict = lambda s, p, keep: L.oz2_kv4_evict_workspace_bytes(ref(c), s, p, keep)
     assert 0 < evict(1, 10, 0) <= evict(1, 10, 640) < evict(1, 10, 320) and evict(1, 10, 10 ** 12) > 0
     assert evict(1, 1, -1) == 0
+
+
+def test_bytes_are_laid_out_like_the_structures():
+    kinds = ((_Rows, binding._pack_rows, (P, 5, 6, 2)), (_Sequences, binding._pack_sequences, tuple(range(1, 14))), (_Kept, binding._pack_kept, tuple(range(1, 8))))
+    for kind, pack, values in kinds:
+        assert bytes(kind(*values)) == pack(*values) and len(pack(*values)) == ctypes.sizeof(kind)
