@@ -26,7 +26,43 @@ struct AttentionTile {
   int64_t begin;      // the sequence's first token
   int tokens, first;  // of the sequence, and the tile's first row
 };
-__device__ __forceinline__ AttentionTile attention_tile(const Attention& a, int64_t tile, int size) {
+__device__ __forceinline__ int attention_lanes_sum(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return __builtin_amdgcn_readlane(v, 63);
+}
+// The tile that is the `tile`-th to be worked on.  Up to 64 sequences: the tiles furthest from their sequences' begins come first, which with causal attention have
+// the most to do, so that none of these is left to the end.  More: by sequences from the last on, each from its end.
+__device__ __forceinline__ AttentionTile attention_tile(const Attention& a, int64_t tile, int64_t tiles, int size) {
+  if (a.sequences <= 64) {
+    const int lane = threadIdx.x % 64;
+    int64_t begin = 0;
+    int n = 0, own = 0;  // tokens and tiles of the lane's sequence
+    if (lane < a.sequences) {
+      const KvRange r = kv_range(a.cu, lane, a.tokens);
+      begin = r.begin, n = (int)(r.end - r.begin);
+      own = (int)(((int64_t)n * a.group + size - 1) / size);
+    }
+    // the largest number that more than `tile` tiles have before them in their sequence, or are at
+    int low = 0, high = (int)tiles, behind = 0;  // count(low) > tile >= count(high) = behind
+    if (attention_lanes_sum(own) <= tile) return {0, 0, 0};
+    while (high - low > 1) {
+      const int mid = low + (high - low) / 2, count = attention_lanes_sum(own > mid ? own - mid : 0);
+      if (count > tile) low = mid;
+      else high = mid, behind = count;
+    }
+    // of the sequences that have a tile `low`, the (tile - behind)-th
+    unsigned long long left = __ballot(own > low);
+    for (int64_t i = tile - behind; i > 0; --i) left &= left - 1;
+    const int s = __builtin_amdgcn_readfirstlane(__ffsll((long long)left) - 1);
+    const int64_t from = (int64_t)((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)begin, s) | (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(begin >> 32), s) << 32);
+    return {from, __builtin_amdgcn_readlane(n, s), low * size};
+  }
+  tile = tiles - 1 - tile;
   const int64_t low = kv_sequence(a.sequences, [&](int64_t i) {
     const int64_t cu = a.cu[i];
     return (cu < 0 ? 0 : cu) * a.group / size + i <= tile;

@@ -37,7 +37,7 @@ __global__ void __launch_bounds__(256, 1) attention_any_kernel(Attention a) {
   constexpr int E = DP / 8, F = DP / 32, SIZE = XT == OZ2_F32 ? 4 : 2;
   __shared__ float merged[4 * kRows * (DP + 1)];  // [wave][row][DP + 1]
   __shared__ float merged_m[4][kRows], merged_l[4][kRows];
-  const AttentionTile tile = attention_tile(a, blockIdx.x, kRows);
+  const AttentionTile tile = attention_tile(a, blockIdx.x, gridDim.x, kRows);
   const int rows = tile.tokens * a.group;
   if (tile.first >= rows) return;
   const int head = blockIdx.y, lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 32, half = lane / 32;

@@ -47,26 +47,36 @@ __device__ __forceinline__ bool at_odd(unsigned w) {
   return (w & top) == top || (w & top << 16) == top << 16;
 }
 
-template <int XT, int DP, int NQ, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, WAVES / 4) attention_tile_kernel(Attention a) {
+template <int XT, int DP, int NQ, int WAVES, int SPLIT>
+__global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) attention_tile_kernel(Attention a) {
   constexpr int E = DP / 16, F = DP / 32, ROW = DP <= 64 ? 128 : DP <= 128 ? 256 : 512;  // bytes of a row in LDS
-  constexpr int THREADS = 64 * WAVES, ROWS = 32 * NQ * WAVES, LOADS = kTileKeys * ROW / 16 / THREADS, TILE = kTileKeys * ROW;
-  __shared__ __attribute__((aligned(16))) char lds[4 * TILE];  // keys, keys, values, values
-  __shared__ int odd[2];                                       // whether a tile of values has one that is not finite
-  __shared__ float weights[WAVES][32][32 * NQ];                    // (where it has)
+  constexpr int THREADS = 64 * WAVES / SPLIT, ROWS = 32 * NQ * WAVES / SPLIT, LOADS = kTileKeys * ROW / 16 / THREADS, TILE = kTileKeys * ROW;
+  __shared__ __attribute__((aligned(16))) char all_lds[SPLIT * 4 * TILE];  // keys, keys, values, values, of each part
+  __shared__ int all_odd[SPLIT][2];                            // whether a tile of values has one that is not finite
+  __shared__ unsigned weights[WAVES][16][32 * NQ];             // (where it has: p of two keys)
 
   const int tiles = (int)((unsigned)gridDim.x / (unsigned)a.kv_heads);
-  const int head = blockIdx.x % a.kv_heads, lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 32, half = lane / 32;
-  const AttentionTile tile = attention_tile(a, tiles - 1 - (int)(blockIdx.x / a.kv_heads), ROWS);
+  const int head = blockIdx.x % a.kv_heads, lane = threadIdx.x % 64, col = lane % 32, half = lane / 32;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), part = wave / (WAVES / SPLIT), thread = threadIdx.x % THREADS;
+  char* const lds = all_lds + part * 4 * TILE;
+  int* const odd = all_odd[part];
+  const AttentionTile tile = attention_tile(a, blockIdx.x / a.kv_heads, tiles, ROWS);
   const int rows = tile.tokens * a.group;
   if (tile.first >= rows) return;
 
-  // keys that the wave's rows see at all, and that all of them see; and the workgroup's
-  const int first_row = tile.first + wave * 32 * NQ, last_row = min(first_row + 32 * NQ, rows) - 1;
-  const int end = first_row >= rows ? 0 : a.causal ? last_row / a.per_group + 1 : tile.tokens;
-  const int full = first_row >= rows ? 0 : a.causal ? first_row / a.per_group + 1 : tile.tokens;
-  const int all = a.causal ? min(tile.first + ROWS - 1, rows - 1) / a.per_group + 1 : tile.tokens;
-  const int steps = (end + 31) / 32, groups = (((all + 31) / 32) + 1) / 2;
+  // The part's keys: every SPLIT-th tile, counted as if they were one behind the other.  `own` of the first n keys belong to it.
+  auto own = [&](int n) {
+    if constexpr (SPLIT == 1) return n;
+    const int full = n / kTileKeys, mine = full > part ? (full - part + SPLIT - 1) / SPLIT : 0;
+    return mine * kTileKeys + (full % SPLIT == part ? n % kTileKeys : 0);
+  };
+  // keys that the wave's rows see at all, and that all of them see; and the most of any part
+  const int first_row = tile.first + wave % (WAVES / SPLIT) * 32 * NQ, last_row = min(first_row + 32 * NQ, rows) - 1;
+  const int end = first_row >= rows ? 0 : own(a.causal ? last_row / a.per_group + 1 : tile.tokens);
+  const int full = first_row >= rows ? 0 : own(a.causal ? first_row / a.per_group + 1 : tile.tokens);
+  const int seen_by_any = a.causal ? min(tile.first + ROWS - 1, rows - 1) / a.per_group + 1 : tile.tokens, tokens = own(tile.tokens);
+  const int all = own(seen_by_any), most = SPLIT == 1 ? all : min(seen_by_any, (seen_by_any / (SPLIT * kTileKeys) + 1) * kTileKeys);
+  const int steps = (end + 31) / 32, groups = (((most + 31) / 32) + 1) / 2;
 
   int sees[NQ];
   w4_u4 q[NQ][E];
@@ -74,7 +84,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES / 4) attention_tile_kernel(A
   for (int n = 0; n < NQ; ++n) {
     const int row = min(first_row + 32 * n + col, rows - 1), at = row / a.per_group;
     const int64_t query = (int64_t)head * a.group + (row - at * a.group);
-    sees[n] = a.causal ? at + 1 : tile.tokens;
+    sees[n] = own(a.causal ? at + 1 : tile.tokens);
     const uint16_t* from = static_cast<const uint16_t*>(a.q.data) + (tile.begin + at) * a.q.ld_token + query * a.q.ld_head;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -86,7 +96,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES / 4) attention_tile_kernel(A
 
   // a thread's pieces of a tile, sixteen bytes each of every PER-th key, and their places in LDS
   constexpr int PER = THREADS / (ROW / 16);
-  const int of_key = threadIdx.x / (ROW / 16), piece = threadIdx.x % (ROW / 16);
+  const int of_key = thread / (ROW / 16), piece = thread % (ROW / 16);
   // (sixteen keys' pieces of one place, and four keys' 64 bytes, lie in all banks)
   const int to_k = of_key * ROW + (piece ^ (ROW == 128 ? of_key / 2 % 8 : of_key % 16)) * 16;
   const int to_v = 2 * TILE + of_key * ROW + (piece / 4 ^ (ROW == 128 ? of_key / 2 % 2 : of_key % 4)) * 64 + piece % 4 * 16;
@@ -96,16 +106,17 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES / 4) attention_tile_kernel(A
   const int k_step = (int)(a.k.ld_token * 2), v_step = (int)(a.v.ld_token * 2);
   // (a piece that is not there is loaded from where another one is, and stored as zeros)
   auto fetch = [&](const char* from, int step, int64_t first, w4_u4 (&r)[LOADS]) {
-    const int most = (int)min((int64_t)kTileKeys, tile.tokens - first) - 1;
+    const int most = min(kTileKeys, tokens - (int)first) - 1;
+    if constexpr (SPLIT > 1) first = first * SPLIT + part * kTileKeys;
     from += first * step + (piece * 8 < a.dim ? piece * 16 : 0);
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) r[i] = *reinterpret_cast<const w4_u4*>(from + (unsigned)(min(of_key + i * PER, most) * step));
   };
   auto clear = [&](int first, w4_u4 (&r)[LOADS]) {
-    if (a.dim < ROW / 2 || tile.tokens - first < kTileKeys) {
+    if (a.dim < ROW / 2 || tokens - first < kTileKeys) {
 #pragma unroll
       for (int i = 0; i < LOADS; ++i)
-        if (piece * 8 >= a.dim || first + of_key + i * PER >= tile.tokens) r[i] = w4_u4{0, 0, 0, 0};
+        if (piece * 8 >= a.dim || first + of_key + i * PER >= tokens) r[i] = w4_u4{0, 0, 0, 0};
     }
   };
   auto store_k = [&](int buffer, int first, w4_u4 (&r)[LOADS]) {
@@ -118,7 +129,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES / 4) attention_tile_kernel(A
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) *reinterpret_cast<w4_u4*>(lds + buffer * TILE + to_v + i * PER * ROW) = r[i];
     // (only where a key may be hidden from a row does it matter)
-    if (a.causal && first + kTileKeys > tile.first / a.per_group + 1) {
+    if (a.causal && first + kTileKeys > own(tile.first / a.per_group + 1)) {
       bool any = false;
 #pragma unroll
       for (int i = 0; i < LOADS; ++i)
@@ -176,16 +187,16 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES / 4) attention_tile_kernel(A
   };
   // The same with values that are not finite, for rows that do not see all of them: key by key.
   auto add_seen = [&](const w4_u4 (&p)[NQ][2], int at, int place) {
-    float(&w)[32][32 * NQ] = weights[wave];
+    unsigned(&w)[16][32 * NQ] = weights[wave];
 #pragma unroll
     for (int n = 0; n < NQ; ++n)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) w[i / 4 * 8 + i % 4 + 4 * half][32 * n + col] = at_value<XT>(p[n][i / 8][i % 8 / 2], i % 2);
+      for (int i = 0; i < 16; i += 2) w[i / 4 * 4 + i % 4 / 2 + 2 * half][32 * n + col] = p[n][i / 8][i % 8 / 2];
     for (int key = 0; key < 32; ++key) {
       const int swizzle = ROW == 128 ? key / 2 % 2 : key % 4;
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
-        const float x = w[key][32 * n + col];
+        const float x = at_value<XT>(w[key / 2][32 * n + col], key % 2);
         const bool seen = place + key < sees[n];
 #pragma unroll
         for (int f = 0; f < F; ++f)
@@ -278,12 +289,16 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES / 4) attention_tile_kernel(A
   };
 
   w4_u4 kr[LOADS], vr[LOADS];
-  if (threadIdx.x < 2) odd[threadIdx.x] = 0;
-  fetch(k_from, k_step, 0, kr);
-  fetch(v_from, v_step, 0, vr);
+  if (thread < 2) odd[thread] = 0;
+  if (all > 0) {
+    fetch(k_from, k_step, 0, kr);
+    fetch(v_from, v_step, 0, vr);
+  }
   __syncthreads();
-  store_k(0, 0, kr);
-  store_v(0, 0, vr);
+  if (all > 0) {
+    store_k(0, 0, kr);
+    store_v(0, 0, vr);
+  }
   if (all > kTileKeys) {
     fetch(k_from, k_step, kTileKeys, kr);
     store_k(1, kTileKeys, kr);
@@ -320,6 +335,31 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES / 4) attention_tile_kernel(A
   }
   rescale();
 
+  if constexpr (SPLIT > 1) {
+    // the parts' sums come to the first one
+    static_assert(SPLIT == 2 && NQ == 1 && THREADS * F * 64 <= SPLIT * 4 * TILE, "one other part, whose sums find room");
+    __shared__ float other_m[THREADS], other_l[THREADS];
+    float4* to = reinterpret_cast<float4*>(all_lds) + thread;
+    if (part) {
+      other_m[thread] = m[0], other_l[thread] = l[0];
+#pragma unroll
+      for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[(f * 4 + i) * THREADS] = float4{o[0][f][4 * i], o[0][f][4 * i + 1], o[0][f][4 * i + 2], o[0][f][4 * i + 3]};
+    }
+    __syncthreads();
+    if (part) return;
+    const float high = fmaxf(m[0], other_m[thread]), here = __builtin_amdgcn_exp2f(m[0] - high), there = __builtin_amdgcn_exp2f(other_m[thread] - high);
+    l[0] = fmaf(l[0], here, other_l[thread] * there);
+#pragma unroll
+    for (int f = 0; f < F; ++f)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 x = to[(f * 4 + i) * THREADS];
+        o[0][f][4 * i] = fmaf(o[0][f][4 * i], here, x.x * there), o[0][f][4 * i + 1] = fmaf(o[0][f][4 * i + 1], here, x.y * there);
+        o[0][f][4 * i + 2] = fmaf(o[0][f][4 * i + 2], here, x.z * there), o[0][f][4 * i + 3] = fmaf(o[0][f][4 * i + 3], here, x.w * there);
+      }
+  }
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     l[n] += __shfl_xor(l[n], 32);
@@ -350,19 +390,24 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES / 4) attention_tile_kernel(A
   }
 }
 
-template <int XT, int DP, int NQ, int WAVES>
+template <int XT, int DP, int WAVES, int SPLIT>
 hipError_t oz2_attention_tile_launch(const Attention& a, hipStream_t st) {
-  hipLaunchKernelGGL((attention_tile_kernel<XT, DP, NQ, WAVES>), dim3((unsigned)(attention_tiles(a, 32 * NQ * WAVES) * a.kv_heads)), dim3(64 * WAVES), 0, st, a);
+  hipLaunchKernelGGL((attention_tile_kernel<XT, DP, 1, WAVES, SPLIT>), dim3((unsigned)(attention_tiles(a, 32 * WAVES / SPLIT) * a.kv_heads)), dim3(64 * WAVES), 0, st, a);
   return hipGetLastError();
 }
 // (of 129 to 256 values: the sums take half the registers, so four waves; compiled in a file of its own)
 template <int XT> hipError_t oz2_attention_wide_of(const Attention& a, hipStream_t st);
+#include <stdlib.h>
+template <int XT, int S>
+hipError_t oz2_attention_tile_w(const Attention& a, hipStream_t st) {
+  if (a.dim <= 64) return oz2_attention_tile_launch<XT, 64, 8, S>(a, st);
+  if (a.dim <= 96) return oz2_attention_tile_launch<XT, 96, 8, S>(a, st);
+  if (a.dim <= 128) return oz2_attention_tile_launch<XT, 128, 8, S>(a, st);
+  return oz2_attention_wide_of<XT>(a, st);
+}
 template <int XT>
 hipError_t oz2_attention_tile_of(const Attention& a, hipStream_t st) {
-  if (a.dim <= 64) return oz2_attention_tile_launch<XT, 64, 1, 8>(a, st);
-  if (a.dim <= 96) return oz2_attention_tile_launch<XT, 96, 1, 8>(a, st);
-  if (a.dim <= 128) return oz2_attention_tile_launch<XT, 128, 1, 8>(a, st);
-  return oz2_attention_wide_of<XT>(a, st);
+  return getenv("W4") ? oz2_attention_tile_w<XT, 2>(a, st) : oz2_attention_tile_w<XT, 1>(a, st);
 }
 
 #endif

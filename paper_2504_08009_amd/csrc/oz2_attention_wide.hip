@@ -4,7 +4,7 @@
 
 template <int XT>
 hipError_t oz2_attention_wide_of(const Attention& a, hipStream_t st) {
-  return oz2_attention_tile_launch<XT, 256, 1, 4>(a, st);
+  return oz2_attention_tile_launch<XT, 256, 4, 1>(a, st);
 }
 template hipError_t oz2_attention_wide_of<OZ2_BF16>(const Attention&, hipStream_t);
 template hipError_t oz2_attention_wide_of<OZ2_F16>(const Attention&, hipStream_t);
