@@ -12,6 +12,7 @@
 #define OZ2_ATTENTION_TILE_H
 
 #include "oz2_attention.h"
+#include "oz2_gemm.h"
 #include "oz2_w4_core.h"
 
 #ifdef __HIPCC__
@@ -48,18 +49,19 @@ __device__ __forceinline__ bool at_odd(unsigned w) {
 }
 
 template <int XT, int DP, int NQ, int WAVES, int SPLIT>
-__global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) attention_tile_kernel(Attention a) {
+__global__ void __launch_bounds__(64 * WAVES, DP <= 128 && NQ == 1 ? 2 : 1) attention_tile_kernel(Attention a) {
   constexpr int E = DP / 16, F = DP / 32, ROW = DP <= 64 ? 128 : DP <= 128 ? 256 : 512;  // bytes of a row in LDS
-  constexpr int THREADS = 64 * WAVES / SPLIT, ROWS = 32 * NQ * WAVES / SPLIT, LOADS = kTileKeys * ROW / 16 / THREADS, TILE = kTileKeys * ROW;
-  __shared__ __attribute__((aligned(16))) char all_lds[SPLIT * 4 * TILE];  // keys, keys, values, values, of each part
-  __shared__ int all_odd[SPLIT][2];                            // whether a tile of values has one that is not finite
-  __shared__ unsigned weights[WAVES][16][32 * NQ];             // (where it has: p of two keys)
+  constexpr int THREADS = 64 * WAVES / SPLIT, ROWS = 32 * NQ * WAVES / SPLIT, TILE = kTileKeys * ROW;
+  constexpr int LOADS = TILE / 16 / THREADS, LDS = 4 * TILE;  // keys, keys, values, values
+  __shared__ __attribute__((aligned(16))) char all_lds[SPLIT * LDS];  // of each part
+  __shared__ int all_odd[SPLIT];                               // whether the tile of values has one that is not finite
+  __shared__ unsigned weights[WAVES][8][32 * NQ];              // (where it has: p of two keys)
 
   const int tiles = (int)((unsigned)gridDim.x / (unsigned)a.kv_heads);
   const int head = blockIdx.x % a.kv_heads, lane = threadIdx.x % 64, col = lane % 32, half = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), part = wave / (WAVES / SPLIT), thread = threadIdx.x % THREADS;
-  char* const lds = all_lds + part * 4 * TILE;
-  int* const odd = all_odd[part];
+  char* const lds = all_lds + part * LDS;
+  int& odd = all_odd[part];
   const AttentionTile tile = attention_tile(a, blockIdx.x / a.kv_heads, tiles, ROWS);
   const int rows = tile.tokens * a.group;
   if (tile.first >= rows) return;
@@ -77,6 +79,10 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) attention_tile_
   const int seen_by_any = a.causal ? min(tile.first + ROWS - 1, rows - 1) / a.per_group + 1 : tile.tokens, tokens = own(tile.tokens);
   const int all = own(seen_by_any), most = SPLIT == 1 ? all : min(seen_by_any, (seen_by_any / (SPLIT * kTileKeys) + 1) * kTileKeys);
   const int steps = (end + 31) / 32, groups = (((most + 31) / 32) + 1) / 2;
+  // groups whose steps, and the next one, all rows of the workgroup see: of the last part, which has the fewest keys
+  const int seen_by_all = a.causal ? tile.first / a.per_group + 1 : tile.tokens;
+  const int least = SPLIT == 1 ? seen_by_all : seen_by_all / (SPLIT * kTileKeys) * kTileKeys;
+  const int easy = least >= 96 ? (least - 96) / 64 + 1 : 0;
 
   int sees[NQ];
   w4_u4 q[NQ][E];
@@ -94,58 +100,34 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) attention_tile_
     }
   }
 
-  // a thread's pieces of a tile, sixteen bytes each of every PER-th key, and their places in LDS
-  constexpr int PER = THREADS / (ROW / 16);
-  const int of_key = thread / (ROW / 16), piece = thread % (ROW / 16);
-  // (sixteen keys' pieces of one place, and four keys' 64 bytes, lie in all banks)
-  const int to_k = of_key * ROW + (piece ^ (ROW == 128 ? of_key / 2 % 8 : of_key % 16)) * 16;
-  const int to_v = 2 * TILE + of_key * ROW + (piece / 4 ^ (ROW == 128 ? of_key / 2 % 2 : of_key % 4)) * 64 + piece % 4 * 16;
-  static_assert(ROW == 512 || PER % 16 == 0, "a thread's keys have one swizzle");
+  // Copies of tiles into LDS: sixteen bytes a lane, a wave's 1024 beside each other.  Pieces of sixteen bytes change places within a row, so that sixteen keys' pieces, and
+  // four values' 64 bytes, lie in all banks: which piece comes to a place is chosen by what the lane loads.  Rows behind the last token are copies of it, pieces
+  // behind the last dim of the first piece: what they meet is not seen, a 0 of q, or not stored.
+  constexpr int PIECES = ROW / 16, PER = THREADS / PIECES;
+  const int of_key = thread / PIECES, place = thread % PIECES;
+  auto piece_at = [&](int swizzled) { return (swizzled * 8 < a.dim ? swizzled : 0) * 16; };
+  int k_piece[ROW == 512 ? 2 : 1];  // (of even and odd loads, where a thread's keys do not have one exchange)
+#pragma unroll
+  for (int i = 0; i < (ROW == 512 ? 2 : 1); ++i) k_piece[i] = piece_at(place ^ (ROW == 128 ? of_key / 2 % 8 : (of_key + i * PER) % 16));
+  static_assert(ROW == 512 ? PER == 8 : PER % 16 == 0, "a thread's keys have one exchange of pieces, or two in turn");
+  const int v_piece = piece_at(place ^ (ROW == 128 ? of_key / 2 % 2 : of_key % 4) * 4);
   const char* k_from = static_cast<const char*>(a.k.data) + (tile.begin * a.k.ld_token + head * a.k.ld_head) * 2;
   const char* v_from = static_cast<const char*>(a.v.data) + (tile.begin * a.v.ld_token + head * a.v.ld_head) * 2;
   const int k_step = (int)(a.k.ld_token * 2), v_step = (int)(a.v.ld_token * 2);
-  // (a piece that is not there is loaded from where another one is, and stored as zeros)
-  auto fetch = [&](const char* from, int step, int64_t first, w4_u4 (&r)[LOADS]) {
-    const int most = min(kTileKeys, tokens - (int)first) - 1;
-    if constexpr (SPLIT > 1) first = first * SPLIT + part * kTileKeys;
-    from += first * step + (piece * 8 < a.dim ? piece * 16 : 0);
+  const unsigned lds_at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave % (WAVES / SPLIT) * 1024;
+  auto fetch = [&](const char* from, int step, int first, int at, const int* piece, int pieces) {
+    const int last = min(kTileKeys, tokens - first) - 1;
+    from += (int64_t)(SPLIT > 1 ? first * SPLIT + part * kTileKeys : first) * step;
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) r[i] = *reinterpret_cast<const w4_u4*>(from + (unsigned)(min(of_key + i * PER, most) * step));
+    for (int i = 0; i < LOADS; ++i)
+      load_to_lds_16(reinterpret_cast<const int8_t*>(from), (unsigned)(min(of_key + i * PER, last) * step + piece[i % pieces]), lds_at + at + i * THREADS * 16);
   };
-  auto clear = [&](int first, w4_u4 (&r)[LOADS]) {
-    if (a.dim < ROW / 2 || tokens - first < kTileKeys) {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i)
-        if (piece * 8 >= a.dim || first + of_key + i * PER >= tokens) r[i] = w4_u4{0, 0, 0, 0};
-    }
-  };
-  auto store_k = [&](int buffer, int first, w4_u4 (&r)[LOADS]) {
-    clear(first, r);
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) *reinterpret_cast<w4_u4*>(lds + buffer * TILE + (to_k ^ (ROW == 512 && i % 2 ? 128 : 0)) + i * PER * ROW) = r[i];
-  };
-  auto store_v = [&](int buffer, int first, w4_u4 (&r)[LOADS]) {
-    clear(first, r);
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) *reinterpret_cast<w4_u4*>(lds + buffer * TILE + to_v + i * PER * ROW) = r[i];
-    // (only where a key may be hidden from a row does it matter)
-    if (a.causal && first + kTileKeys > own(tile.first / a.per_group + 1)) {
-      bool any = false;
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) any |= at_odd<XT>(r[i][j]);
-      if (any) odd[buffer] = 1;
-    }
-  };
+  auto fetch_keys = [&](int number) { fetch(k_from, k_step, number * kTileKeys, number % 2 * TILE, k_piece, ROW == 512 ? 2 : 1); };
+  auto fetch_values = [&](int number) { fetch(v_from, v_step, number * kTileKeys, (2 + number % 2) * TILE, &v_piece, 1); };
 
-  // where a lane reads
-  int k_at[E], v_at[F];
-#pragma unroll
-  for (int e = 0; e < E; ++e) k_at[e] = col * ROW + ((2 * e + half) ^ (ROW == 128 ? col / 2 % 8 : col % 16)) * 16;
-#pragma unroll
-  for (int f = 0; f < F; ++f)
-    v_at[f] = 2 * TILE + (4 * half + lane % 16 / 4) * ROW + (f ^ (ROW == 128 ? lane % 16 / 8 : lane % 16 / 4)) * 64 + lane / 16 % 2 * 32 + lane % 4 * 8;
+  // where a lane reads: pieces of keys and 64 bytes of values at these with bits exchanged
+  const int k_at = col * ROW + (half ^ (ROW == 128 ? col / 2 % 8 : col % 16)) * 16;
+  const int v_at = 2 * TILE + (4 * half + lane % 16 / 4) * ROW + (ROW == 128 ? lane % 16 / 8 : lane % 16 / 4) * 64 + lane / 16 % 2 * 32 + lane % 4 * 8;
 
   float m[NQ], l[NQ];
   at_f16 o[NQ][F], s[2][NQ];
@@ -159,56 +141,67 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) attention_tile_
       for (int i = 0; i < 16; ++i) o[n][f][i] = 0.f;
   }
 
-  auto score = [&](at_f16 (&s)[NQ], int at) {
+  // (at: bytes from the first tile of keys, or of values)
+  auto key_piece = [&](int at, int e) { return *reinterpret_cast<const w4_u4*>(lds + ((at + k_at) ^ (e * 32))); };
+  auto value_piece = [&](int at, int b, int f) {
+    typedef __attribute__((address_space(3))) at_s4* In;
+    const char* from = lds + ((at + v_at) ^ (f * 64));
+    const at_s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((In)(from + 16 * b * ROW));
+    const at_s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((In)(from + (16 * b + 8) * ROW));
+    const at_u2 l2 = __builtin_bit_cast(at_u2, lo), h2 = __builtin_bit_cast(at_u2, hi);
+    return w4_u4{l2[0], l2[1], h2[0], h2[1]};
+  };
+  auto clear_scores = [&](at_f16 (&s)[NQ]) {
 #pragma unroll
     for (int n = 0; n < NQ; ++n)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
+  };
+  auto score_with = [&](at_f16 (&s)[NQ], int at, int e) {
+    const w4_u4 k = key_piece(at, e);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const w4_u4 k = *reinterpret_cast<const w4_u4*>(lds + at + k_at[e]);
+    for (int n = 0; n < NQ; ++n) s[n] = at_mfma<XT>(k, q[n][e], s[n]);
+  };
+  auto add_with = [&](const w4_u4 (&p)[NQ][2], int at, int b, int f) {
+    const w4_u4 v = value_piece(at, b, f);
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) s[n] = at_mfma<XT>(k, q[n][e], s[n]);
-    }
+    for (int n = 0; n < NQ; ++n) o[n][f] = at_mfma<XT>(v, p[n][b], o[n][f]);
+  };
+  auto score = [&](at_f16 (&s)[NQ], int at) {
+    clear_scores(s);
+#pragma unroll
+    for (int e = 0; e < E; ++e) score_with(s, at, e);
   };
   auto add = [&](const w4_u4 (&p)[NQ][2], int at) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int f = 0; f < F; ++f) {
-        typedef __attribute__((address_space(3))) at_s4* In;
-        const at_s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((In)(lds + at + v_at[f] + 16 * b * ROW));
-        const at_s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((In)(lds + at + v_at[f] + (16 * b + 8) * ROW));
-        const at_u2 l2 = __builtin_bit_cast(at_u2, lo), h2 = __builtin_bit_cast(at_u2, hi);
-        const w4_u4 v = {l2[0], l2[1], h2[0], h2[1]};
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) o[n][f] = at_mfma<XT>(v, p[n][b], o[n][f]);
-      }
+    for (int i = 0; i < 2 * F; ++i) add_with(p, at, i / F, i % F);
   };
   // The same with values that are not finite, for rows that do not see all of them: key by key.
   auto add_seen = [&](const w4_u4 (&p)[NQ][2], int at, int place) {
-    unsigned(&w)[16][32 * NQ] = weights[wave];
+    unsigned(&w)[8][32 * NQ] = weights[wave];
 #pragma unroll
-    for (int n = 0; n < NQ; ++n)
+    for (int b = 0; b < 2; ++b) {
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) w[i / 4 * 4 + i % 4 / 2 + 2 * half][32 * n + col] = p[n][i / 8][i % 8 / 2];
-    for (int key = 0; key < 32; ++key) {
-      const int swizzle = ROW == 128 ? key / 2 % 2 : key % 4;
+      for (int n = 0; n < NQ; ++n)
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        const float x = at_value<XT>(w[key / 2][32 * n + col], key % 2);
-        const bool seen = place + key < sees[n];
+        for (int i = 0; i < 8; i += 2) w[i / 4 * 4 + i % 4 / 2 + 2 * half][32 * n + col] = p[n][b][i / 2];
+      for (int key = 0; key < 16; ++key) {
 #pragma unroll
-        for (int f = 0; f < F; ++f)
+        for (int n = 0; n < NQ; ++n) {
+          const float x = at_value<XT>(w[key / 2][32 * n + col], key % 2);
+          const bool seen = place + 16 * b + key < sees[n];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {  // dims 32 f + 8 i + 4 half and on
-            const at_u2 v = *reinterpret_cast<const at_u2*>(lds + 2 * TILE + at + key * ROW + (f ^ swizzle) * 64 + i * 16 + half * 8);
+          for (int f = 0; f < F; ++f)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float sum = fmaf(x, at_value<XT>(v[j / 2], j % 2), o[n][f][4 * i + j]);
-              o[n][f][4 * i + j] = seen ? sum : o[n][f][4 * i + j];
+            for (int i = 0; i < 4; ++i) {  // dims 32 f + 8 i + 4 half and on
+              const at_u2 v = *reinterpret_cast<const at_u2*>(lds + 2 * TILE + at + (16 * b + key) * ROW + (f ^ (ROW == 128 ? key / 2 % 2 : key % 4)) * 64 + i * 16 + half * 8);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const float sum = fmaf(x, at_value<XT>(v[j / 2], j % 2), o[n][f][4 * i + j]);
+                o[n][f][4 * i + j] = seen ? sum : o[n][f][4 * i + j];
+              }
             }
-          }
+        }
       }
     }
   };
@@ -249,25 +242,36 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) attention_tile_
       }
     }
   };
-  auto exponentials = [&](const at_f16 (&s)[NQ], w4_u4 (&p)[NQ][2]) {
+  // pairs first .. last - 1 of the sixteen scores of a row that a lane has
+  auto exponentials = [&](const at_f16 (&s)[NQ], w4_u4 (&p)[NQ][2], int first, int last) {
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      float sum = 0.f;
+    for (int n = 0; n < NQ; ++n)
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        const float one = __builtin_amdgcn_exp2f(fmaf(s[n][i], a.scale2, -m[n])), two = __builtin_amdgcn_exp2f(fmaf(s[n][i + 1], a.scale2, -m[n]));
-        sum += one + two;
-        p[n][i / 8][i % 8 / 2] = at_pair<XT>(one, two);
+      for (int i = first; i < last; ++i) {
+        const float one = __builtin_amdgcn_exp2f(fmaf(s[n][2 * i], a.scale2, -m[n])), two = __builtin_amdgcn_exp2f(fmaf(s[n][2 * i + 1], a.scale2, -m[n]));
+        l[n] += one + two;
+        p[n][i / 4][i % 4] = at_pair<XT>(one, two);
       }
-      l[n] += sum;
-    }
   };
-  // step j: exponentials of s into p; scores of step j + 1 from keys at `k`, values of step j - 1 at `v`.  All rows see all of step j's keys.
+  // step j: exponentials of s into p; scores of step j + 1 from keys at `k`, values of step j - 1 at `v`.  All rows see all of step j's keys.  Operands are read from
+  // LDS two pairs of products ahead, and a part of the exponentials follows each pair; in this order, to which the compiler is held.
   auto step = [&](at_f16 (&s)[NQ], at_f16 (&next)[NQ], w4_u4 (&p)[NQ][2], const w4_u4 (&before)[NQ][2], int k, int v) {
+    w4_u4 keys[3], values[3];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) keys[i] = key_piece(k, i), values[i] = value_piece(v, i / F, i % F);
     maximum(s);
-    score(next, k);
-    add(before, v);
-    exponentials(s, p);
+    clear_scores(next);
+#pragma unroll
+    for (int i = 0; i < E; ++i) {  // (E == 2 F)
+      if (i + 2 < E) keys[(i + 2) % 3] = key_piece(k, i + 2), values[(i + 2) % 3] = value_piece(v, (i + 2) / F, (i + 2) % F);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        next[n] = at_mfma<XT>(keys[i % 3], q[n][i], next[n]);
+        o[n][i % F] = at_mfma<XT>(values[i % 3], before[n][i / F], o[n][i % F]);
+      }
+      exponentials(s, p, 8 * i / E, 8 * (i + 1) / E);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
   // the same where they may not, or where step j or j + 1 may not be the wave's
   auto last_step = [&](int j, at_f16 (&s)[NQ], at_f16 (&next)[NQ], w4_u4 (&p)[NQ][2], const w4_u4 (&before)[NQ][2], int k, int v, bool seen) {
@@ -285,59 +289,56 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) attention_tile_
       else add(before, v);
     }
     if (j + 1 < steps) score(next, k);
-    if (j < steps) exponentials(s, p);
+    if (j < steps) exponentials(s, p, 0, 8);
   };
 
-  w4_u4 kr[LOADS], vr[LOADS];
-  if (thread < 2) odd[thread] = 0;
-  if (all > 0) {
-    fetch(k_from, k_step, 0, kr);
-    fetch(v_from, v_step, 0, vr);
-  }
-  __syncthreads();
-  if (all > 0) {
-    store_k(0, 0, kr);
-    store_v(0, 0, vr);
-  }
-  if (all > kTileKeys) {
-    fetch(k_from, k_step, kTileKeys, kr);
-    store_k(1, kTileKeys, kr);
-  }
-  __syncthreads();
+  // What is under way when a group begins is there when it ends: the wait is for all of a wave's copies, the barrier for the others'.
+  auto arrived = [&]() {
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+    __syncthreads();
+  };
+  if (all > 0) fetch_keys(0), fetch_values(0);
+  if (all > kTileKeys) fetch_keys(1);
+  arrived();
   if (steps > 0) score(s[0], 0);
   last_step(0, s[0], s[1], p[0], p[1], 32 * ROW, 0, false);
   __syncthreads();
   // group g: steps 2 g + 1 and 2 g + 2, which take keys of tile g + 1 and values of tile g
   int g = 0;
-  const int easy = full >= 96 ? (full - 96) / 64 + 1 : 0;  // groups whose steps, and the next one, all rows see
   for (; g < easy; ++g) {
-    const int now = g % 2 * TILE, next = TILE - now;
-    const bool more = (g + 1) * kTileKeys < all, more_keys = (g + 2) * kTileKeys < all;
-    fetch(k_from, k_step, more_keys ? (int64_t)(g + 2) * kTileKeys : 0, kr);
-    fetch(v_from, v_step, more ? (int64_t)(g + 1) * kTileKeys : 0, vr);
-    step(s[1], s[0], p[1], p[0], next, now);
-    step(s[0], s[1], p[0], p[1], next + 32 * ROW, now + 32 * ROW);
-    if (more_keys) store_k(g % 2, (g + 2) * kTileKeys, kr);
-    if (more) store_v((g + 1) % 2, (g + 1) * kTileKeys, vr);
-    __syncthreads();
+    const int keys = (g + 1) % 2 * TILE, values = g % 2 * TILE;
+    if ((g + 2) * kTileKeys < all) fetch_keys(g + 2);
+    if ((g + 1) * kTileKeys < all) fetch_values(g + 1);
+    step(s[1], s[0], p[1], p[0], keys, values);
+    step(s[0], s[1], p[0], p[1], keys + 32 * ROW, values + 32 * ROW);
+    arrived();
   }
   for (; g < groups; ++g) {
-    const int now = g % 2 * TILE, next = TILE - now;
-    const bool more = (g + 1) * kTileKeys < all, more_keys = (g + 2) * kTileKeys < all;
-    if (more_keys) fetch(k_from, k_step, (int64_t)(g + 2) * kTileKeys, kr);
-    if (more) fetch(v_from, v_step, (int64_t)(g + 1) * kTileKeys, vr);
-    const bool seen = odd[g % 2];
-    last_step(2 * g + 1, s[1], s[0], p[1], p[0], next, now, seen);
-    last_step(2 * g + 2, s[0], s[1], p[0], p[1], next + 32 * ROW, now + 32 * ROW, seen);
-    if (more_keys) store_k(g % 2, (g + 2) * kTileKeys, kr);
-    if (more) store_v((g + 1) % 2, (g + 1) * kTileKeys, vr);
+    const int keys = (g + 1) % 2 * TILE, values = g % 2 * TILE;
+    // values that some row may not see: whether one of them is not finite
+    if (thread == 0) odd = 0;
     __syncthreads();
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const w4_u4 v = *reinterpret_cast<const w4_u4*>(lds + 2 * TILE + values + (i * THREADS + thread) * 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) any |= at_odd<XT>(v[j]);
+    }
+    if (any) odd = 1;
+    __syncthreads();
+    const bool seen = odd;
+    if ((g + 2) * kTileKeys < all) fetch_keys(g + 2);
+    if ((g + 1) * kTileKeys < all) fetch_values(g + 1);
+    last_step(2 * g + 1, s[1], s[0], p[1], p[0], keys, values, seen);
+    last_step(2 * g + 2, s[0], s[1], p[0], p[1], keys + 32 * ROW, values + 32 * ROW, seen);
+    arrived();
   }
   rescale();
 
   if constexpr (SPLIT > 1) {
     // the parts' sums come to the first one
-    static_assert(SPLIT == 2 && NQ == 1 && THREADS * F * 64 <= SPLIT * 4 * TILE, "one other part, whose sums find room");
+    static_assert(SPLIT == 2 && NQ == 1 && THREADS * F * 64 <= SPLIT * LDS, "one other part, whose sums find room");
     __shared__ float other_m[THREADS], other_l[THREADS];
     float4* to = reinterpret_cast<float4*>(all_lds) + thread;
     if (part) {
