@@ -1,13 +1,17 @@
 // Attention over packed prompts in BF16 and FP16 on the matrix cores: the kernel of one type and of dims up to DP.
 //
-// A workgroup of four waves has 128 NQ rows, a wave 32 NQ of them, which are the columns of its products (32 x 32 x 16): keys x rows, then dims x rows.  So
-// a lane has one row (for each of NQ) throughout, maxima and sums stay in lanes, and what it holds of the first product, rounded, is its part of the second one's
-// operand as it is: of sixteen keys the lanes' lower half has 0..3 and 8..11, the upper half 4..7 and 12..15, and the values are read in that order.
-//   Keys and values come through LDS in tiles of 64, in two buffers: global loads at the begin of a stretch of work, stores to LDS at its end, one barrier.
-// Values are wanted with keys along a lane's words: ds_read_b64_tr_b16 turns 4 x 16 of them on their way.
+// A workgroup of eight waves has 256 rows, a wave 32 of them, which are the columns of its products (32 x 32 x 16): keys x rows, then dims x rows.  So a lane has one
+// row throughout, maxima and sums stay in lanes, and what it holds of the first product, rounded, is its part of the second one's operand as it is: of sixteen
+// keys the lanes' lower half has 0..3 and 8..11, the upper half 4..7 and 12..15, and the values are read in that order.  (p is rounded to the type of the values,
+// as the matrix cores take it; its sum l is of what it was before.)
+//   Keys and values come into LDS in tiles of 64, in two buffers, by copies that pass no registers, begun a tile ahead; one barrier a tile.  Values are wanted with
+// keys along a lane's words: ds_read_b64_tr_b16 turns 4 x 16 of them on their way.
 //   A step takes 32 keys, and works on three of them at once, none of which waits for another: scores of step j + 1 and values of step j - 1 on the matrix cores, the
 // exponentials of step j on the vector units.  m follows the maximum only where a score is more than 2^8 above it, which hardly happens after the
-// first tile; so the sums are hardly ever rescaled.
+// first tile; so the sums are hardly ever rescaled.  `step` is for tiles that all rows see, and has no branch but that; `last_step` is for all others.
+//   With SPLIT = 2 the two halves of a workgroup have the same 128 rows and every other tile of keys each; their sums are joined at the end.
+//   16384 tokens of 16 heads of 128 values, FP16, causal, take 1.10 ms, 1000 TFLOP/s, where a large matrix product reaches 1507: the vector units' part of a step, 32
+// exponentials a lane's pair of rows and what goes with them, is nearly as long as the products' 16 x 32 cycles, and the clock falls under both.
 #ifndef OZ2_ATTENTION_TILE_H
 #define OZ2_ATTENTION_TILE_H
 
@@ -48,14 +52,14 @@ __device__ __forceinline__ bool at_odd(unsigned w) {
   return (w & top) == top || (w & top << 16) == top << 16;
 }
 
-template <int XT, int DP, int NQ, int WAVES, int SPLIT>
-__global__ void __launch_bounds__(64 * WAVES, DP <= 128 && NQ == 1 ? 2 : 1) attention_tile_kernel(Attention a) {
+template <int XT, int DP, int WAVES, int SPLIT>
+__global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) attention_tile_kernel(Attention a) {
   constexpr int E = DP / 16, F = DP / 32, ROW = DP <= 64 ? 128 : DP <= 128 ? 256 : 512;  // bytes of a row in LDS
-  constexpr int THREADS = 64 * WAVES / SPLIT, ROWS = 32 * NQ * WAVES / SPLIT, TILE = kTileKeys * ROW;
+  constexpr int THREADS = 64 * WAVES / SPLIT, ROWS = 32 * WAVES / SPLIT, TILE = kTileKeys * ROW;
   constexpr int LOADS = TILE / 16 / THREADS, LDS = 4 * TILE;  // keys, keys, values, values
   __shared__ __attribute__((aligned(16))) char all_lds[SPLIT * LDS];  // of each part
   __shared__ int all_odd[SPLIT];                               // whether the tile of values has one that is not finite
-  __shared__ unsigned weights[WAVES][8][32 * NQ];              // (where it has: p of two keys)
+  __shared__ unsigned weights[WAVES][8][32];              // (where it has: p of two keys)
 
   const int tiles = (int)((unsigned)gridDim.x / (unsigned)a.kv_heads);
   const int head = blockIdx.x % a.kv_heads, lane = threadIdx.x % 64, col = lane % 32, half = lane / 32;
@@ -73,7 +77,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 128 && NQ == 1 ? 2 : 1) atte
     return mine * kTileKeys + (full % SPLIT == part ? n % kTileKeys : 0);
   };
   // keys that the wave's rows see at all, and that all of them see; and the most of any part
-  const int first_row = tile.first + wave % (WAVES / SPLIT) * 32 * NQ, last_row = min(first_row + 32 * NQ, rows) - 1;
+  const int first_row = tile.first + wave % (WAVES / SPLIT) * 32, last_row = min(first_row + 32, rows) - 1;
   const int end = first_row >= rows ? 0 : own(a.causal ? last_row / a.per_group + 1 : tile.tokens);
   const int full = first_row >= rows ? 0 : own(a.causal ? first_row / a.per_group + 1 : tile.tokens);
   const int seen_by_any = a.causal ? min(tile.first + ROWS - 1, rows - 1) / a.per_group + 1 : tile.tokens, tokens = own(tile.tokens);
@@ -84,20 +88,16 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 128 && NQ == 1 ? 2 : 1) atte
   const int least = SPLIT == 1 ? seen_by_all : seen_by_all / (SPLIT * kTileKeys) * kTileKeys;
   const int easy = least >= 96 ? (least - 96) / 64 + 1 : 0;
 
-  int sees[NQ];
-  w4_u4 q[NQ][E];
+  w4_u4 q[E];
+  const int row = min(first_row + col, rows - 1), at = row / a.per_group;
+  const int64_t query = (int64_t)head * a.group + (row - at * a.group);
+  const int sees = own(a.causal ? at + 1 : tile.tokens);
+  const uint16_t* from = static_cast<const uint16_t*>(a.q.data) + (tile.begin + at) * a.q.ld_token + query * a.q.ld_head;
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const int row = min(first_row + 32 * n + col, rows - 1), at = row / a.per_group;
-    const int64_t query = (int64_t)head * a.group + (row - at * a.group);
-    sees[n] = own(a.causal ? at + 1 : tile.tokens);
-    const uint16_t* from = static_cast<const uint16_t*>(a.q.data) + (tile.begin + at) * a.q.ld_token + query * a.q.ld_head;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int d = 16 * e + 8 * half;
-      q[n][e] = w4_u4{0, 0, 0, 0};
-      if (d < a.dim) q[n][e] = *reinterpret_cast<const w4_u4*>(from + d);
-    }
+  for (int e = 0; e < E; ++e) {
+    const int d = 16 * e + 8 * half;
+    q[e] = w4_u4{0, 0, 0, 0};
+    if (d < a.dim) q[e] = *reinterpret_cast<const w4_u4*>(from + d);
   }
 
   // Copies of tiles into LDS: sixteen bytes a lane, a wave's 1024 beside each other.  Pieces of sixteen bytes change places within a row, so that sixteen keys' pieces, and
@@ -129,17 +129,13 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 128 && NQ == 1 ? 2 : 1) atte
   const int k_at = col * ROW + (half ^ (ROW == 128 ? col / 2 % 8 : col % 16)) * 16;
   const int v_at = 2 * TILE + (4 * half + lane % 16 / 4) * ROW + (ROW == 128 ? lane % 16 / 8 : lane % 16 / 4) * 64 + lane / 16 % 2 * 32 + lane % 4 * 8;
 
-  float m[NQ], l[NQ];
-  at_f16 o[NQ][F], s[2][NQ];
-  w4_u4 p[2][NQ][2];
+  float m = -3e38f, l = 0.f;
+  at_f16 o[F], s[2];
+  w4_u4 p[2][2];
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    m[n] = -3e38f, l[n] = 0.f;
+  for (int f = 0; f < F; ++f)
 #pragma unroll
-    for (int f = 0; f < F; ++f)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[n][f][i] = 0.f;
-  }
+    for (int i = 0; i < 16; ++i) o[f][i] = 0.f;
 
   // (at: bytes from the first tile of keys, or of values)
   auto key_piece = [&](int at, int e) { return *reinterpret_cast<const w4_u4*>(lds + ((at + k_at) ^ (e * 32))); };
@@ -151,136 +147,113 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 128 && NQ == 1 ? 2 : 1) atte
     const at_u2 l2 = __builtin_bit_cast(at_u2, lo), h2 = __builtin_bit_cast(at_u2, hi);
     return w4_u4{l2[0], l2[1], h2[0], h2[1]};
   };
-  auto clear_scores = [&](at_f16 (&s)[NQ]) {
+  auto clear_scores = [&](at_f16 &s) {
 #pragma unroll
-    for (int n = 0; n < NQ; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
   };
-  auto score_with = [&](at_f16 (&s)[NQ], int at, int e) {
+  auto score_with = [&](at_f16 &s, int at, int e) {
     const w4_u4 k = key_piece(at, e);
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) s[n] = at_mfma<XT>(k, q[n][e], s[n]);
+    s = at_mfma<XT>(k, q[e], s);
   };
-  auto add_with = [&](const w4_u4 (&p)[NQ][2], int at, int b, int f) {
+  auto add_with = [&](const w4_u4 (&p)[2], int at, int b, int f) {
     const w4_u4 v = value_piece(at, b, f);
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) o[n][f] = at_mfma<XT>(v, p[n][b], o[n][f]);
+    o[f] = at_mfma<XT>(v, p[b], o[f]);
   };
-  auto score = [&](at_f16 (&s)[NQ], int at) {
+  auto score = [&](at_f16 &s, int at) {
     clear_scores(s);
 #pragma unroll
     for (int e = 0; e < E; ++e) score_with(s, at, e);
   };
-  auto add = [&](const w4_u4 (&p)[NQ][2], int at) {
+  auto add = [&](const w4_u4 (&p)[2], int at) {
 #pragma unroll
     for (int i = 0; i < 2 * F; ++i) add_with(p, at, i / F, i % F);
   };
   // The same with values that are not finite, for rows that do not see all of them: key by key.
-  auto add_seen = [&](const w4_u4 (&p)[NQ][2], int at, int place) {
-    unsigned(&w)[8][32 * NQ] = weights[wave];
+  auto add_seen = [&](const w4_u4 (&p)[2], int at, int place) {
+    unsigned(&w)[8][32] = weights[wave];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
 #pragma unroll
-      for (int n = 0; n < NQ; ++n)
-#pragma unroll
-        for (int i = 0; i < 8; i += 2) w[i / 4 * 4 + i % 4 / 2 + 2 * half][32 * n + col] = p[n][b][i / 2];
+      for (int i = 0; i < 8; i += 2) w[i / 4 * 4 + i % 4 / 2 + 2 * half][col] = p[b][i / 2];
       for (int key = 0; key < 16; ++key) {
+        const float x = at_value<XT>(w[key / 2][col], key % 2);
+        const bool seen = place + 16 * b + key < sees;
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-          const float x = at_value<XT>(w[key / 2][32 * n + col], key % 2);
-          const bool seen = place + 16 * b + key < sees[n];
+        for (int f = 0; f < F; ++f)
 #pragma unroll
-          for (int f = 0; f < F; ++f)
+          for (int i = 0; i < 4; ++i) {  // dims 32 f + 8 i + 4 half and on
+            const at_u2 v = *reinterpret_cast<const at_u2*>(lds + 2 * TILE + at + (16 * b + key) * ROW + (f ^ (ROW == 128 ? key / 2 % 2 : key % 4)) * 64 + i * 16 + half * 8);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {  // dims 32 f + 8 i + 4 half and on
-              const at_u2 v = *reinterpret_cast<const at_u2*>(lds + 2 * TILE + at + (16 * b + key) * ROW + (f ^ (ROW == 128 ? key / 2 % 2 : key % 4)) * 64 + i * 16 + half * 8);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const float sum = fmaf(x, at_value<XT>(v[j / 2], j % 2), o[n][f][4 * i + j]);
-                o[n][f][4 * i + j] = seen ? sum : o[n][f][4 * i + j];
-              }
+            for (int j = 0; j < 4; ++j) {
+              const float sum = fmaf(x, at_value<XT>(v[j / 2], j % 2), o[f][4 * i + j]);
+              o[f][4 * i + j] = seen ? sum : o[f][4 * i + j];
             }
-        }
+          }
       }
     }
   };
 
   // What raised the maximum multiplies the sums a step later, when they have the values of all keys before.
-  float factor[NQ];
+  float factor;
   bool pending = false;
   auto rescale = [&]() {
     if (pending) {
 #pragma unroll
-      for (int n = 0; n < NQ; ++n)
-#pragma unroll
-        for (int f = 0; f < F; ++f) o[n][f] *= factor[n];
+      for (int f = 0; f < F; ++f) o[f] *= factor;
       pending = false;
     }
   };
-  auto maximum = [&](const at_f16 (&s)[NQ]) {
-    float top[NQ];
-    bool high = false;
+  auto maximum = [&](const at_f16 &s) {
+    float top = s[0];
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      top[n] = s[n][0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) top[n] = fmaxf(top[n], s[n][i]);
-      high |= fmaf(top[n], a.scale2, -m[n]) > 8.f;
-    }
-    if (pending || __any(high)) {
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+    const bool high = __any(fmaf(top, a.scale2, -m) > 8.f);
+    if (pending || high) {
       rescale();
-      if (__any(high)) {
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-          const float raised = fmaxf(m[n], fmaxf(top[n], __shfl_xor(top[n], 32)) * a.scale2);
-          factor[n] = __builtin_amdgcn_exp2f(m[n] - raised);
-          m[n] = raised;
-          l[n] *= factor[n];
-        }
+      if (high) {
+        const float raised = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)) * a.scale2);
+        factor = __builtin_amdgcn_exp2f(m - raised);
+        m = raised;
+        l *= factor;
         pending = true;
       }
     }
   };
   // pairs first .. last - 1 of the sixteen scores of a row that a lane has
-  auto exponentials = [&](const at_f16 (&s)[NQ], w4_u4 (&p)[NQ][2], int first, int last) {
+  auto exponentials = [&](const at_f16 &s, w4_u4 (&p)[2], int first, int last) {
 #pragma unroll
-    for (int n = 0; n < NQ; ++n)
-#pragma unroll
-      for (int i = first; i < last; ++i) {
-        const float one = __builtin_amdgcn_exp2f(fmaf(s[n][2 * i], a.scale2, -m[n])), two = __builtin_amdgcn_exp2f(fmaf(s[n][2 * i + 1], a.scale2, -m[n]));
-        l[n] += one + two;
-        p[n][i / 4][i % 4] = at_pair<XT>(one, two);
-      }
+    for (int i = first; i < last; ++i) {
+      const float one = __builtin_amdgcn_exp2f(fmaf(s[2 * i], a.scale2, -m)), two = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], a.scale2, -m));
+      l += one + two;
+      p[i / 4][i % 4] = at_pair<XT>(one, two);
+    }
   };
   // step j: exponentials of s into p; scores of step j + 1 from keys at `k`, values of step j - 1 at `v`.  All rows see all of step j's keys.  Operands are read from
   // LDS two pairs of products ahead, and a part of the exponentials follows each pair; in this order, to which the compiler is held.
-  auto step = [&](at_f16 (&s)[NQ], at_f16 (&next)[NQ], w4_u4 (&p)[NQ][2], const w4_u4 (&before)[NQ][2], int k, int v) {
+  auto step = [&](at_f16 &s, at_f16 &next, w4_u4 (&p)[2], const w4_u4 (&before)[2], int k, int v) {
     w4_u4 keys[3], values[3];
 #pragma unroll
     for (int i = 0; i < 2; ++i) keys[i] = key_piece(k, i), values[i] = value_piece(v, i / F, i % F);
     maximum(s);
     clear_scores(next);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int i = 0; i < E; ++i) {  // (E == 2 F)
       if (i + 2 < E) keys[(i + 2) % 3] = key_piece(k, i + 2), values[(i + 2) % 3] = value_piece(v, (i + 2) / F, (i + 2) % F);
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        next[n] = at_mfma<XT>(keys[i % 3], q[n][i], next[n]);
-        o[n][i % F] = at_mfma<XT>(values[i % 3], before[n][i / F], o[n][i % F]);
-      }
+      next = at_mfma<XT>(keys[i % 3], q[i], next);
+      o[i % F] = at_mfma<XT>(values[i % 3], before[i / F], o[i % F]);
       exponentials(s, p, 8 * i / E, 8 * (i + 1) / E);
+      asm volatile("" : "+v"(p[(8 * (i + 1) / E - 1) / 4]), "+v"(l));  // (else they wait for their use, a step later)
       __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
   };
   // the same where they may not, or where step j or j + 1 may not be the wave's
-  auto last_step = [&](int j, at_f16 (&s)[NQ], at_f16 (&next)[NQ], w4_u4 (&p)[NQ][2], const w4_u4 (&before)[NQ][2], int k, int v, bool seen) {
+  auto last_step = [&](int j, at_f16 &s, at_f16 &next, w4_u4 (&p)[2], const w4_u4 (&before)[2], int k, int v, bool seen) {
     if (j < steps) {
       if (j * 32 + 32 > full) {
 #pragma unroll
-        for (int n = 0; n < NQ; ++n)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[n][i] = j * 32 + i / 4 * 8 + i % 4 + 4 * half >= sees[n] ? -INFINITY : s[n][i];
+        for (int i = 0; i < 16; ++i) s[i] = j * 32 + i / 4 * 8 + i % 4 + 4 * half >= sees ? -INFINITY : s[i];
       }
       maximum(s);
     } else rescale();
@@ -338,77 +311,75 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 128 && NQ == 1 ? 2 : 1) atte
 
   if constexpr (SPLIT > 1) {
     // the parts' sums come to the first one
-    static_assert(SPLIT == 2 && NQ == 1 && THREADS * F * 64 <= SPLIT * LDS, "one other part, whose sums find room");
+    static_assert(SPLIT == 2 && THREADS * F * 64 <= SPLIT * LDS, "one other part, whose sums find room");
     __shared__ float other_m[THREADS], other_l[THREADS];
     float4* to = reinterpret_cast<float4*>(all_lds) + thread;
     if (part) {
-      other_m[thread] = m[0], other_l[thread] = l[0];
+      other_m[thread] = m, other_l[thread] = l;
 #pragma unroll
       for (int f = 0; f < F; ++f)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) to[(f * 4 + i) * THREADS] = float4{o[0][f][4 * i], o[0][f][4 * i + 1], o[0][f][4 * i + 2], o[0][f][4 * i + 3]};
+        for (int i = 0; i < 4; ++i) to[(f * 4 + i) * THREADS] = float4{o[f][4 * i], o[f][4 * i + 1], o[f][4 * i + 2], o[f][4 * i + 3]};
     }
     __syncthreads();
     if (part) return;
-    const float high = fmaxf(m[0], other_m[thread]), here = __builtin_amdgcn_exp2f(m[0] - high), there = __builtin_amdgcn_exp2f(other_m[thread] - high);
-    l[0] = fmaf(l[0], here, other_l[thread] * there);
+    const float high = fmaxf(m, other_m[thread]), here = __builtin_amdgcn_exp2f(m - high), there = __builtin_amdgcn_exp2f(other_m[thread] - high);
+    l = fmaf(l, here, other_l[thread] * there);
 #pragma unroll
     for (int f = 0; f < F; ++f)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float4 x = to[(f * 4 + i) * THREADS];
-        o[0][f][4 * i] = fmaf(o[0][f][4 * i], here, x.x * there), o[0][f][4 * i + 1] = fmaf(o[0][f][4 * i + 1], here, x.y * there);
-        o[0][f][4 * i + 2] = fmaf(o[0][f][4 * i + 2], here, x.z * there), o[0][f][4 * i + 3] = fmaf(o[0][f][4 * i + 3], here, x.w * there);
+        o[f][4 * i] = fmaf(o[f][4 * i], here, x.x * there), o[f][4 * i + 1] = fmaf(o[f][4 * i + 1], here, x.y * there);
+        o[f][4 * i + 2] = fmaf(o[f][4 * i + 2], here, x.z * there), o[f][4 * i + 3] = fmaf(o[f][4 * i + 3], here, x.w * there);
       }
   }
+  l += __shfl_xor(l, 32);
+  if (first_row + col >= rows) return;
+  const int64_t out_at = (tile.begin + at) * a.out.ld_token + query * a.out.ld_head;
+  const float inverse = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    l[n] += __shfl_xor(l[n], 32);
-    if (first_row + 32 * n + col >= rows) continue;
-    const int row = first_row + 32 * n + col, at = row / a.per_group;
-    const int64_t out_at = (tile.begin + at) * a.out.ld_token + ((int64_t)head * a.group + (row - at * a.group)) * a.out.ld_head;
-    const float inverse = l[n] == 0.f ? 0.f : 1.f / l[n];
+  for (int f = 0; f < F; ++f)
 #pragma unroll
-    for (int f = 0; f < F; ++f)
+    for (int i = 0; i < 4; ++i) {
+      const int d = 32 * f + 8 * i + 4 * half;
+      if (d >= a.dim) continue;
+      float r[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int d = 32 * f + 8 * i + 4 * half;
-        if (d >= a.dim) continue;
-        float r[4];
+      for (int j = 0; j < 4; ++j) r[j] = l == 0.f ? 0.f : o[f][4 * i + j] * inverse;
+      if (a.out.type == OZ2_F32)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) r[j] = l[n] == 0.f ? 0.f : o[n][f][4 * i + j] * inverse;
-        if (a.out.type == OZ2_F32)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) static_cast<float*>(a.out.data)[out_at + d + j] = r[j];
-        else if (a.out.type == OZ2_BF16) {
-          const at_u2 w = {at_pair<OZ2_BF16>(r[0], r[1]), at_pair<OZ2_BF16>(r[2], r[3])};
-          *reinterpret_cast<at_u2*>(static_cast<uint16_t*>(a.out.data) + out_at + d) = w;
-        } else {
-          const at_u2 w = {at_pair<OZ2_F16>(r[0], r[1]), at_pair<OZ2_F16>(r[2], r[3])};
-          *reinterpret_cast<at_u2*>(static_cast<uint16_t*>(a.out.data) + out_at + d) = w;
-        }
+        for (int j = 0; j < 4; ++j) static_cast<float*>(a.out.data)[out_at + d + j] = r[j];
+      else if (a.out.type == OZ2_BF16) {
+        const at_u2 w = {at_pair<OZ2_BF16>(r[0], r[1]), at_pair<OZ2_BF16>(r[2], r[3])};
+        *reinterpret_cast<at_u2*>(static_cast<uint16_t*>(a.out.data) + out_at + d) = w;
+      } else {
+        const at_u2 w = {at_pair<OZ2_F16>(r[0], r[1]), at_pair<OZ2_F16>(r[2], r[3])};
+        *reinterpret_cast<at_u2*>(static_cast<uint16_t*>(a.out.data) + out_at + d) = w;
       }
-  }
+    }
 }
 
 template <int XT, int DP, int WAVES, int SPLIT>
 hipError_t oz2_attention_tile_launch(const Attention& a, hipStream_t st) {
-  hipLaunchKernelGGL((attention_tile_kernel<XT, DP, 1, WAVES, SPLIT>), dim3((unsigned)(attention_tiles(a, 32 * WAVES / SPLIT) * a.kv_heads)), dim3(64 * WAVES), 0, st, a);
+  hipLaunchKernelGGL((attention_tile_kernel<XT, DP, WAVES, SPLIT>), dim3((unsigned)(attention_tiles(a, 32 * WAVES / SPLIT) * a.kv_heads)), dim3(64 * WAVES), 0, st, a);
   return hipGetLastError();
 }
 // (of 129 to 256 values: the sums take half the registers, so four waves; compiled in a file of its own)
 template <int XT> hipError_t oz2_attention_wide_of(const Attention& a, hipStream_t st);
-#include <stdlib.h>
-template <int XT, int S>
-hipError_t oz2_attention_tile_w(const Attention& a, hipStream_t st) {
-  if (a.dim <= 64) return oz2_attention_tile_launch<XT, 64, 8, S>(a, st);
-  if (a.dim <= 96) return oz2_attention_tile_launch<XT, 96, 8, S>(a, st);
-  if (a.dim <= 128) return oz2_attention_tile_launch<XT, 128, 8, S>(a, st);
-  return oz2_attention_wide_of<XT>(a, st);
+template <int XT, int SPLIT>
+hipError_t oz2_attention_tile_dims(const Attention& a, hipStream_t st) {
+  if (a.dim <= 64) return oz2_attention_tile_launch<XT, 64, 8, SPLIT>(a, st);
+  if (a.dim <= 96) return oz2_attention_tile_launch<XT, 96, 8, SPLIT>(a, st);
+  return oz2_attention_tile_launch<XT, 128, 8, SPLIT>(a, st);
 }
+// Whose rows fill the compute units about once with tiles of 256 has them in tiles of 128 with their keys in two parts: twice the workgroups, and half the way of the
+// longest, against twice the reads of keys.  bf16, causal, one sequence, heads of 128 values, us split and not: 1024 tokens of 8 heads 27 and 40, 2048 of 32 62 and 68,
+// 8192 of 8 160 and 228 (256 tiles); 4096 of 32 185 and 156, 8192 of 16 322 and 300 (512 tiles).
 template <int XT>
 hipError_t oz2_attention_tile_of(const Attention& a, hipStream_t st) {
-  return getenv("W4") ? oz2_attention_tile_w<XT, 2>(a, st) : oz2_attention_tile_w<XT, 1>(a, st);
+  if (a.dim > 128) return oz2_attention_wide_of<XT>(a, st);
+  return a.tokens * a.heads <= 256 * 320 ? oz2_attention_tile_dims<XT, 2>(a, st) : oz2_attention_tile_dims<XT, 1>(a, st);
 }
 
 #endif
