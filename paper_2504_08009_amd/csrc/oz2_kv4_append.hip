@@ -88,7 +88,9 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(Append a) {
     high = over(high, a.lanes, [](float p, float q) { return __builtin_elementwise_maximum(p, q); });
     // The quotient by 15 and the reciprocal, rounded correctly: what an approximation leaves is exact in an FMA, and once corrected by it is the nearest value
     // (Markstein; neither 15 nor an FP16 value has a significand of ones alone).  Where the range is infinite they are NaNs.
-    const float range = high - low, part = range * (1.f / 15.f), fifteenth = fmaf(fmaf(-15.f, part, range), 1.f / 15.f, part);
+    const float range = high - low, part = range * (1.f / 15.f);
+    float fifteenth = fmaf(fmaf(-15.f, part, range), 1.f / 15.f, part);
+    asm("" : "+v"(fifteenth));  // (an FP32 value, not an FMA rounded straight to FP16, which differs in one of 20000)
     const _Float16 scale = (_Float16)fifteenth, offset = (_Float16)low;
     const float s32 = (float)scale, o32 = (float)offset, near = __builtin_amdgcn_rcpf(s32);
     const float inverse = s32 == 0.f ? 0.f : fmaf(fmaf(-s32, near, 1.f), near, near);
