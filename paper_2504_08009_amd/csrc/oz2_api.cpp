@@ -960,22 +960,24 @@ bool lattice_ok(int64_t width, int64_t a, int64_t step_a, int64_t b, int64_t ste
 bool rows_ok(const oz2_rows* r, int64_t tokens, int64_t heads, int64_t dim) {
   return r && type_ok(r->type) && (tokens == 0 || r->data) && lattice_ok(dim, tokens, r->ld_token, heads, r->ld_head);
 }
-// Whether two tensors of heads have no byte in common, as far as that is easily seen: one lies behind the other, or a token's heads lie between those of the
-// other's tokens, like parts of one packed tensor.
+// Whether two tensors of heads have no byte in common, as far as that is easily seen: one lies behind the other, or what one has of a token (or, where these are
+// further apart, of a head) lies between what the other has of two, like parts of one packed tensor.
 bool rows_apart(const oz2_rows& a, int64_t heads_a, const oz2_rows& b, int64_t heads_b, int64_t tokens, int64_t dim) {
   const int64_t size_a = size_of(a.type), size_b = size_of(b.type);
   // (a stride of a single token or head says nothing)
-  const int64_t token_a = ((heads_a > 1 ? (heads_a - 1) * a.ld_head : 0) + dim) * size_a, token_b = ((heads_b > 1 ? (heads_b - 1) * b.ld_head : 0) + dim) * size_b;
-  const int64_t more_a = tokens > 1 ? (tokens - 1) * a.ld_token * size_a : 0, more_b = tokens > 1 ? (tokens - 1) * b.ld_token * size_b : 0;
-  const int64_t bytes_a = more_a + token_a, bytes_b = more_b + token_b;
+  const int64_t tokens_a = tokens > 1 ? (tokens - 1) * a.ld_token * size_a : 0, tokens_b = tokens > 1 ? (tokens - 1) * b.ld_token * size_b : 0;
+  const int64_t all_a = heads_a > 1 ? (heads_a - 1) * a.ld_head * size_a : 0, all_b = heads_b > 1 ? (heads_b - 1) * b.ld_head * size_b : 0;
   const uintptr_t pa = (uintptr_t)a.data, pb = (uintptr_t)b.data;
-  if (pa >= pb + bytes_b || pb >= pa + bytes_a) return true;
-  if (tokens == 1) return false;
-  const int64_t step = a.ld_token * size_a;
-  if (step != b.ld_token * size_b || step < token_a || step < token_b) return false;
-  int64_t from = (int64_t)(pb - pa) % step;
-  if (from < 0) from += step;
-  return from >= token_a && from + token_b <= step;
+  if (pa >= pb + tokens_b + all_b + dim * size_b || pb >= pa + tokens_a + all_a + dim * size_a) return true;
+  auto between = [&](int64_t step_a, int64_t step_b, int64_t inner_a, int64_t inner_b) {
+    const int64_t step = step_a ? step_a : step_b, bytes_a = inner_a + dim * size_a, bytes_b = inner_b + dim * size_b;
+    if (!step || (step_a && step_b && step_a != step_b) || step < bytes_a || step < bytes_b) return false;
+    int64_t from = (int64_t)(pb - pa) % step;
+    if (from < 0) from += step;
+    return from >= bytes_a && from + bytes_b <= step;
+  };
+  return between(tokens > 1 ? a.ld_token * size_a : 0, tokens > 1 ? b.ld_token * size_b : 0, all_a, all_b) ||
+         between(heads_a > 1 ? a.ld_head * size_a : 0, heads_b > 1 ? b.ld_head * size_b : 0, tokens_a, tokens_b);
 }
 bool same_rows(const oz2_rows& a, const oz2_rows& b) {
   return a.data == b.data && a.ld_token == b.ld_token && a.ld_head == b.ld_head && a.type == b.type;
@@ -1003,7 +1005,7 @@ bool places_ok(const oz2_kv4_cache& c, const oz2_kv4_sequences& on, int64_t sequ
 }
 bool sequences_ok(const oz2_kv4_cache& c, const oz2_kv4_sequences* on, bool fresh) {
   if (!on || !capacity_ok(c, on->sequences, on->max_pages)) return false;
-  if (fresh && (on->tokens < 0 || on->tokens * c.heads > ((int64_t)1 << 26))) return false;
+  if (fresh && (on->tokens < 0 || on->tokens > ((int64_t)1 << 26) / c.heads)) return false;
   if (on->sequences == 0) return true;
   if (!on->lengths || (fresh && !on->cu) || (on->max_pages && !on->table) || (on->sequences > 1 && on->ld_table < on->max_pages)) return false;
   return (!on->positions || places_ok(c, *on, on->positions_sequence, on->positions_head)) &&
