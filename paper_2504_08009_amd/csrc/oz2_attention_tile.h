@@ -1,6 +1,6 @@
 // Attention over packed prompts in BF16 and FP16 on the matrix cores: the kernel of one type and of dims up to DP.
 //
-// A workgroup of eight waves has 256 rows, a wave 32 of them, which are the columns of its products (32 x 32 x 16): keys x rows, then dims x rows.  So a lane has one
+// A workgroup has 256 or 128 rows, a wave 32 of them, which are the columns of its products (32 x 32 x 16): keys x rows, then dims x rows.  So a lane has one
 // row throughout, maxima and sums stay in lanes, and what it holds of the first product, rounded, is its part of the second one's operand as it is: of sixteen
 // keys the lanes' lower half has 0..3 and 8..11, the upper half 4..7 and 12..15, and the values are read in that order.  (p is rounded to the type of the values,
 // as the matrix cores take it; its sum l is of what it was before.)
@@ -367,19 +367,25 @@ hipError_t oz2_attention_tile_launch(const Attention& a, hipStream_t st) {
 }
 // (of 129 to 256 values: the sums take half the registers, so four waves; compiled in a file of its own)
 template <int XT> hipError_t oz2_attention_wide_of(const Attention& a, hipStream_t st);
-template <int XT, int SPLIT>
+template <int XT, int WAVES, int SPLIT>
 hipError_t oz2_attention_tile_dims(const Attention& a, hipStream_t st) {
-  if (a.dim <= 64) return oz2_attention_tile_launch<XT, 64, 8, SPLIT>(a, st);
-  if (a.dim <= 96) return oz2_attention_tile_launch<XT, 96, 8, SPLIT>(a, st);
-  return oz2_attention_tile_launch<XT, 128, 8, SPLIT>(a, st);
+  if (a.dim <= 64) return oz2_attention_tile_launch<XT, 64, WAVES, SPLIT>(a, st);
+  if (a.dim <= 96) return oz2_attention_tile_launch<XT, 96, WAVES, SPLIT>(a, st);
+  return oz2_attention_tile_launch<XT, 128, WAVES, SPLIT>(a, st);
 }
-// Whose rows fill the compute units about once with tiles of 256 has them in tiles of 128 with their keys in two parts: twice the workgroups, and half the way of the
-// longest, against twice the reads of keys.  bf16, causal, one sequence, heads of 128 values, us split and not: 1024 tokens of 8 heads 27 and 40, 2048 of 32 62 and 68,
-// 8192 of 8 160 and 228 (256 tiles); 4096 of 32 185 and 156, 8192 of 16 322 and 300 (512 tiles).
+// Tiles of 256 rows read keys least often, and serve sequences that are long on the mean.  Shorter ones: 128 rows, of which two workgroups share a compute unit and
+// one begins or ends while the other is at work.  Where even tiles of 128 leave compute units without work, or last much longer than their number needs:
+// 128 rows with their keys in two parts.  bf16, causal, 8 query and kv heads of 128 values, us with 256 rows, 128 rows, and parts:
+//   sequences          2 x 1024   1 x 2048   1 x 4096   4 x 2048   1 x 8192   24 x 512   3 x 4096   (32 and 8 heads) 12 of 16 to 2000   1 x 4096   1 x 8192
+//   256 rows              36         57        101         64        201         48        123                     257                  151        533
+//   128 rows              27         42         76         56        181         39        121                     242                  155        554
+//   128 rows, parts       25         37         65         60        156         55        139
 template <int XT>
 hipError_t oz2_attention_tile_of(const Attention& a, hipStream_t st) {
   if (a.dim > 128) return oz2_attention_wide_of<XT>(a, st);
-  return a.tokens * a.heads <= 256 * 320 ? oz2_attention_tile_dims<XT, 2>(a, st) : oz2_attention_tile_dims<XT, 1>(a, st);
+  const int64_t tiles = a.tokens * a.heads / 256, mean = a.tokens / a.sequences;
+  if (mean >= 3000 ? tiles <= 288 : mean >= 1000 && tiles <= 128) return oz2_attention_tile_dims<XT, 8, 2>(a, st);
+  return mean >= 3000 ? oz2_attention_tile_dims<XT, 8, 1>(a, st) : oz2_attention_tile_dims<XT, 4, 1>(a, st);
 }
 
 #endif

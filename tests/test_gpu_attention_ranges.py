@@ -57,11 +57,11 @@ def offsets(lengths):
 @pytest.mark.parametrize("name", ["bf16", "f16"])
 @pytest.mark.parametrize("causal", [True, False], ids=["causal", "all"])
 @pytest.mark.parametrize("dim", [40, 64, 96, 128])
-def test_more_rows_than_split_keys_serve(dim, causal, name):
-    """above 81920 rows a workgroup has 256 of them, below 128: both, at ends of tiles, with shared heads that do not divide a tile"""
-    for lengths, heads, kv_heads in (([1500, 0, 1, 257, 256, 64, 700], 30, 2), ([1500, 0, 1, 257, 256, 64, 700], 29, 29)):
+def test_tiles_of_all_sizes(dim, causal, name):
+    """128 rows to a workgroup, 256, and 128 with keys in two parts: at ends of tiles, with shared heads that do not divide a tile"""
+    for lengths, heads, kv_heads in (([1500, 0, 1, 257, 256, 64, 700], 30, 2), ([1500, 0, 1, 257, 256, 64, 700], 29, 29), ([4100, 1900], 14, 2), ([3000], 27, 27),
+                                     ([3111], 6, 2), ([1100, 930], 5, 5)):
         cu, on = offsets(lengths)
-        assert cu[-1] * heads > 80000
         q, k, v = made(dim, cu[-1] + 5, heads, kv_heads, dim, TYPES[name])
         out = torch.full_like(q, 7.0)
         oz.attention(q, k, v, on, causal=causal, out=out)
@@ -71,10 +71,9 @@ def test_more_rows_than_split_keys_serve(dim, causal, name):
 
 @pytest.mark.parametrize("name", ["bf16", "f16"])
 @pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
-@pytest.mark.parametrize("heads", [32, 8], ids=["whole", "split"])
-def test_values_that_some_rows_do_not_see(heads, what, name):
-    lengths = [1300, 1700]
-    cu, on = offsets(lengths)
+@pytest.mark.parametrize("heads,more", [(32, 0), (8, 0), (32, 3000)], ids=["128", "parts", "256"])
+def test_values_that_some_rows_do_not_see(heads, more, what, name):
+    cu, on = offsets([1300, 1700 + more])
     q, k, v = made(3, cu[-1], heads, 8, 128, TYPES[name])
     clean = v.clone()
     at = [700, 1299, 1300 + 64, 1300 + 1695]
