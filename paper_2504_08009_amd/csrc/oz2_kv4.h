@@ -49,6 +49,17 @@ __device__ __forceinline__ int64_t kv_sequence(int64_t sequences, Begun begun) {
   return first;
 }
 
+// The last sequence from s on that begins at or before a token: mostly s, so in strides that double, then halve.
+__device__ __forceinline__ int64_t kv_behind(const oz2_kv4_sequences& on, int64_t s, int64_t token) {
+  int64_t stride = 1;
+  for (; s + stride < on.sequences && on.cu[s + stride] <= token; stride *= 2) s += stride;
+  for (; stride > 1;) {
+    stride /= 2;
+    if (s + stride < on.sequences && on.cu[s + stride] <= token) s += stride;
+  }
+  return s;
+}
+
 // Eight values beside each other of a row, in FP32.
 template <int XT>
 __device__ __forceinline__ void kv_load8(const void* p, int64_t i, float (&x)[8]) {

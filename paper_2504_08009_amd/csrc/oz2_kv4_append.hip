@@ -31,17 +31,6 @@ __device__ __forceinline__ float over(float v, int lanes, Op op) {
   return v;
 }
 
-// The last sequence from s on that begins at or before a token: mostly s, so in strides that double, then halve.
-__device__ __forceinline__ int64_t behind(const Append& a, int64_t s, int token) {
-  int64_t stride = 1;
-  for (; s + stride < a.on.sequences && a.on.cu[s + stride] <= token; stride *= 2) s += stride;
-  for (; stride > 1;) {
-    stride /= 2;
-    if (s + stride < a.on.sequences && a.on.cu[s + stride] <= token) s += stride;
-  }
-  return s;
-}
-
 // N vectors a lane: their loads are under way together.  With one, a workgroup has all heads of some tokens; with more, runs of tokens of one head, which it
 // writes beside each other.
 template <int XT, int N>
@@ -69,7 +58,7 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(Append a) {
   int64_t s = kv_sequence(a.on.sequences, [&](int64_t i) { return a.on.cu[i] <= begin; });
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    s = behind(a, s, token[n]);
+    s = kv_behind(a.on, s, token[n]);
     const KvRange r = kv_range(a.on.cu, s, a.on.tokens);
     const bool packed = mine[n] && token[n] >= r.begin && token[n] < r.end;  // rows behind the last sequence are nobody's
     const int place = kv_held(a.on.lengths, s, a.capacity) - (int)(r.end - token[n]);
@@ -125,7 +114,8 @@ template <int XT>
 hipError_t append(const Append& a, hipStream_t st) {
   const int step = 256 / a.lanes;
   const int64_t once = (a.total + step - 1) / step, blocks = (a.on.tokens + 4 * step - 1) / (4 * step);
-  // (four at once where that leaves every compute unit eight workgroups: 54200 tokens of 8 heads of 128 values 67 us one by one, 55 so)
+  // (four at once where that leaves every compute unit eight workgroups: BF16, 54200 tokens of 8 heads of 128 values, 89 us one by one,
+  // 82 so; 16384 of 8 28 and 27; FP32 is as fast either way)
   if (once >= 4 * 1024) hipLaunchKernelGGL((kv4_append_kernel<XT, 4>), dim3((unsigned)(blocks * a.heads), 2), dim3(256), 0, st, a);
   else hipLaunchKernelGGL((kv4_append_kernel<XT, 1>), dim3((unsigned)once, 2), dim3(256), 0, st, a);
   return hipGetLastError();
