@@ -495,7 +495,7 @@ typedef struct oz2_kv4_cache {
 } oz2_kv4_cache;
 
 /* Sequences on a cache: place t of sequence s lies in page table[s ld_table + t / page_size] at t % page_size; lengths[s] places are held, at most
- * max_pages page_size.  A page number outside 0 .. pages - 1 is no page: its places are seen by nobody, and nothing is written there.
+ * max_pages page_size (below 2^28).  A page number outside 0 .. pages - 1 is no page: its places are seen by nobody, and nothing is written there.
  * Where a call takes new tokens, cu packs them, and the new tokens of a sequence are its last places: `lengths` counts them already.  (If it counts fewer,
  * the first of them have no place.)
  * positions, weights (or NULL): for each (sequence, kv head, place) at s ld_sequence + head ld_head + place, with capacity for max_pages page_size places:

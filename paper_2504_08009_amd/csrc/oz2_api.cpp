@@ -996,7 +996,7 @@ bool cache_ok(const oz2_kv4_cache* c) {
 }
 bool capacity_ok(const oz2_kv4_cache& c, int64_t sequences, int64_t max_pages) {
   return sequences >= 0 && sequences <= kMostSequences && sequences * c.heads <= ((int64_t)1 << 21) && max_pages >= 0 &&
-         max_pages <= (((int64_t)1 << 31) - 65536) / c.page_size;
+         max_pages <= 65535 * (int64_t)4096 / c.page_size;  // (65535 chunks of 4096 places, a grid's extent)
 }
 // arrays of (sequence, head, place)
 bool places_ok(const oz2_kv4_cache& c, const oz2_kv4_sequences& on, int64_t sequence, int64_t head) {

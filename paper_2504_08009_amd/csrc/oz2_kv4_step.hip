@@ -7,22 +7,29 @@ extern template hipError_t oz2_kv4_step_of<OZ2_F16>(const Kv4Step&, dim3, hipStr
 
 namespace {
 
-// The parts of a row's chunks, each with a maximum of its own, come together: a thread has four dims of every `parts`-th chunk of a row, with a maximum and sums that
+// Rows joined: the parts of a row's chunks, each with a maximum of its own, come together: a thread has four dims of every `parts`-th chunk of a row, with a maximum and sums that
 // follow as it goes, so that no load waits for another; then the row's `parts` threads of a dim do.  Bound by its waits: the begin, the sequence, the chunks.
 // us with all of 256 threads on one row, their maximum looked for first, and so: 4096 rows of up to 8 chunks 12.2 and 6.4, 512 of 8 5.4 and 4.8, 32 of 32 4.6 and 3.9.
-__global__ void __launch_bounds__(256) kv4_join_kernel(Kv4Step a, FastDiv per_heads, int shift) {
-  const int parts = 1 << shift;
-  __shared__ float sums[256][4], tops[256], totals[256];
-  const int fours = a.dim / 4, thread = threadIdx.x, of = thread / fours, d = (thread - of * fours) * 4, slots = 256 / fours >> shift;
-  const int slot = of >> shift, part = of & (parts - 1);
+struct Finish {
+  Kv4Step a;
+  FastDiv per_heads, per_pair;
+  int shift;              // of the threads that share a row's chunks
+  unsigned joins, turns;  // workgroups that join rows; of the others, those of a (sequence, kv head)
+};
+struct Joining { float sums[256][4], tops[256], totals[256]; };
+__device__ __forceinline__ void join(const Finish& f, Joining& sh) {
+  const Kv4Step& a = f.a;
+  const int parts = 1 << f.shift;
+  const int fours = a.dim / 4, thread = threadIdx.x, of = thread / fours, d = (thread - of * fours) * 4, slots = 256 / fours >> f.shift;
+  const int slot = of >> f.shift, part = of & (parts - 1);
   const int64_t first = (int64_t)blockIdx.x * slots, row = min(first + slot, a.rows - 1);
-  const int begin = (int)first / per_heads, at = (int)row / per_heads, query = (int)row - at * a.heads;
+  const int begin = (int)first / f.per_heads, at = (int)row / f.per_heads, query = (int)row - at * a.heads;
   const int64_t s = kv_behind(a.on, kv_sequence(a.on.sequences, [&](int64_t i) { return a.on.cu[i] <= begin; }), at);
   const KvRange r = kv_range(a.on.cu, s, a.on.tokens);
   const int held = kv_held(a.on.lengths, s, a.capacity);
   const bool mine = slot < slots && first + slot < a.rows && at >= r.begin && at < r.end && held > a.chunk;
   const int chunks = mine ? (held + a.chunk - 1) / a.chunk : 0;
-  float2* stats = reinterpret_cast<float2*>(a.stats) + row;
+  const float2* stats = reinterpret_cast<const float2*>(a.stats) + row;
   float high = -3e38f, total = 0.f, v[4] = {};
 #pragma unroll 4
   for (int i = part; i < chunks; i += parts) {
@@ -33,58 +40,83 @@ __global__ void __launch_bounds__(256) kv4_join_kernel(Kv4Step a, FastDiv per_he
     v[0] = fmaf(now, x.x, v[0] * before), v[1] = fmaf(now, x.y, v[1] * before), v[2] = fmaf(now, x.z, v[2] * before), v[3] = fmaf(now, x.w, v[3] * before);
     high = raised;
   }
-  tops[thread] = high, totals[thread] = total;
-  for (int j = 0; j < 4; ++j) sums[thread][j] = v[j];
-  __syncthreads();
-  if (!mine || part) return;
   if (parts > 1) {
+    sh.tops[thread] = high, sh.totals[thread] = total;
+    for (int j = 0; j < 4; ++j) sh.sums[thread][j] = v[j];
+    __syncthreads();
+    if (!mine || part) return;
     float most = high;
-    for (int p = 1; p < parts; ++p) most = fmaxf(most, tops[thread + p * fours]);
+    for (int p = 1; p < parts; ++p) most = fmaxf(most, sh.tops[thread + p * fours]);
     float factor = __builtin_amdgcn_exp2f(high - most);
     total *= factor;
     for (int j = 0; j < 4; ++j) v[j] *= factor;
     for (int p = 1; p < parts; ++p) {
       const int from = thread + p * fours;
-      factor = __builtin_amdgcn_exp2f(tops[from] - most);
-      total = fmaf(factor, totals[from], total);
-      for (int j = 0; j < 4; ++j) v[j] = fmaf(factor, sums[from][j], v[j]);
+      factor = __builtin_amdgcn_exp2f(sh.tops[from] - most);
+      total = fmaf(factor, sh.totals[from], total);
+      for (int j = 0; j < 4; ++j) v[j] = fmaf(factor, sh.sums[from][j], v[j]);
     }
-    high = most;
   }
+  if (!mine) return;
   for (int j = 0; j < 4; ++j) w4_store(a.out.type, a.out.data, at * a.out.ld_token + query * a.out.ld_head + d + j, total == 0.f ? 0.f : v[j] / total);
-  if (d == 0 && a.scores) *stats = {high, total};  // the whole row's, in the place of its first chunk's: kv4_received_kernel reads them
 }
 
-// What each place received, from the scores and the rows' maxima and sums, which are in the places of their first chunks.
-__global__ void __launch_bounds__(256) kv4_received_kernel(Kv4Step a) {
-  __shared__ float top[64], inverse[64];
-  __shared__ const float* scores[64];
-  const int head = blockIdx.x, s = blockIdx.y, place = blockIdx.z * 256 + threadIdx.x;
-  const int held = kv_held(a.on.lengths, s, a.capacity);
-  if ((int)blockIdx.z * 256 >= held) return;
+// What each place received, from the scores and the maxima and sums of its rows, 64 rows at a time and four threads to the chunks of one.
+struct Receiving { float top[64], inverse[64]; const float* scores[64]; };
+__device__ __forceinline__ void receive(const Finish& f, Receiving& sh) {
+  const Kv4Step& a = f.a;
+  const unsigned i = blockIdx.x - f.joins, pairs = (unsigned)(a.on.sequences * a.c.heads), turn = i / f.per_pair, pair = i - turn * pairs;
+  const int s = (int)(pair / (unsigned)a.c.heads), head = (int)(pair - s * (unsigned)a.c.heads), thread = threadIdx.x;
+  const int held = kv_held(a.on.lengths, s, a.capacity), chunks = (held + a.chunk - 1) / a.chunk;
+  if ((int64_t)turn * 256 >= held) return;
   const KvRange r = kv_range(a.on.cu, s, a.on.tokens);
   const int rows = (int)(r.end - r.begin) * a.group;
-  float* to = a.on.weights + s * a.on.weights_sequence + head * a.on.weights_head + place;
-  const float had = rows && place < held ? *to : 0.f;
-  float sum = 0.f;
-  for (int r0 = 0; r0 < rows; r0 += 64) {
-    __syncthreads();
-    const int n = min(64, rows - r0);
-    if ((int)threadIdx.x < n) {
-      const int fresh = (int)(r0 + threadIdx.x) / a.per_group;
-      const int64_t row = (r.begin + fresh) * a.heads + head * a.group + (r0 + (int)threadIdx.x - fresh * a.group);
-      const float total = a.stats[row * 2 + 1];
-      top[threadIdx.x] = a.stats[row * 2];
-      inverse[threadIdx.x] = total == 0.f ? 0.f : 1.f / total;
-      scores[threadIdx.x] = a.scores + row * a.capacity;
-    }
-    __syncthreads();
-    if (place < held) {
+  if (!rows) return;
+  float* to = a.on.weights + s * a.on.weights_sequence + head * a.on.weights_head;
+  for (int64_t first = (int64_t)turn * 256; first < held; first += (int64_t)f.turns * 256) {
+    const int place = (int)first + thread;
+    const float had = place < held ? to[place] : 0.f;
+    float sum = 0.f;
+    for (int r0 = 0; r0 < rows; r0 += 64) {
+      const int n = min(64, rows - r0), own = r0 + min(thread / 4, n - 1), fresh = own / a.per_group;
+      const int64_t row = (r.begin + fresh) * a.heads + head * a.group + (own - fresh * a.group);
+      const float2* stats = reinterpret_cast<const float2*>(a.stats) + row;
+      float high = -3e38f, total = 0.f;
+      auto with = [&](float top, float part) {
+        const float raised = fmaxf(high, top);
+        total = fmaf(total, __builtin_amdgcn_exp2f(high - raised), part * __builtin_amdgcn_exp2f(top - raised));
+        high = raised;
+      };
 #pragma unroll 4
-      for (int i = 0; i < n; ++i) sum = fmaf(__builtin_amdgcn_exp2f(fmaf(scores[i][place], a.scale2, -top[i])), inverse[i], sum);
+      for (int c = thread % 4; c < chunks; c += 4) {
+        const float2 x = stats[c * a.rows];
+        with(x.x, x.y);
+      }
+      for (int d = 1; d < 4; d *= 2) {
+        const float top = __shfl_xor(high, d), part = __shfl_xor(total, d);
+        with(top, part);
+      }
+      __syncthreads();
+      if (thread % 4 == 0 && thread / 4 < n) {
+        sh.top[thread / 4] = high;
+        sh.inverse[thread / 4] = total == 0.f ? 0.f : 1.f / total;
+        sh.scores[thread / 4] = a.scores + row * a.capacity;
+      }
+      __syncthreads();
+      if (place < held) {
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) sum = fmaf(__builtin_amdgcn_exp2f(fmaf(sh.scores[j][place], a.scale2, -sh.top[j])), sh.inverse[j], sum);
+      }
     }
+    if (place < held) to[place] = had + sum;
   }
-  if (rows && place < held) *to = had + sum;
+}
+
+// Both in one launch, side by side: 16 sequences of 2000 to 8192 places and 4 rows, 10.7 us one after the other, 8.3 so.
+__global__ void __launch_bounds__(256) kv4_finish_kernel(Finish f) {
+  __shared__ union { Joining join; Receiving receive; } sh;
+  if (blockIdx.x < f.joins) join(f, sh.join);
+  else receive(f, sh.receive);
 }
 
 // About a thousand workgroups where there are places enough for them, two rounds of the card; up to 4096 places each, since the begin of a workgroup (some 4 us until
@@ -131,17 +163,22 @@ hipError_t oz2_launch_kv4_attention(const oz2_kv4_cache& cache, const oz2_kv4_se
   hipError_t rc = q.type == OZ2_F32    ? oz2_kv4_step_of<OZ2_F32>(a, grid, st)
                   : q.type == OZ2_BF16 ? oz2_kv4_step_of<OZ2_BF16>(a, grid, st)
                                        : oz2_kv4_step_of<OZ2_F16>(a, grid, st);
-  if (rc == hipSuccess && chunks > 1) {
+  Finish f = {a, fast_div((unsigned)heads), fast_div((unsigned)(on.sequences * cache.heads)), 0, 0, 1};
+  if (chunks > 1) {
     // (of rows with few chunks several in a workgroup: about eight chunks for a thread)
     const int64_t most = 256 / (cache.dim / 4);
-    int shift = 0;
-    while ((2 << shift) <= most && chunks > 8 << shift) ++shift;
-    const int64_t slots = most >> shift;
-    hipLaunchKernelGGL(kv4_join_kernel, dim3((unsigned)((rows + slots - 1) / slots)), dim3(256), 0, st, a, fast_div((unsigned)heads), shift);
-    rc = hipGetLastError();
+    while ((2 << f.shift) <= most && chunks > 8 << f.shift) ++f.shift;
+    const int64_t slots = most >> f.shift;
+    f.joins = (unsigned)((rows + slots - 1) / slots);
   }
-  if (rc == hipSuccess && on.weights && capacity) {
-    hipLaunchKernelGGL(kv4_received_kernel, dim3((unsigned)cache.heads, (unsigned)on.sequences, (unsigned)((capacity + 255) / 256)), dim3(256), 0, st, a);
+  int64_t blocks = f.joins;
+  if (on.weights && capacity) {
+    const int64_t pairs = on.sequences * cache.heads, turns = (capacity + 255) / 256, most = ((int64_t)1 << 30) / pairs;
+    f.turns = (unsigned)(turns < most ? turns : most);
+    blocks += pairs * f.turns;
+  }
+  if (rc == hipSuccess && blocks) {
+    hipLaunchKernelGGL(kv4_finish_kernel, dim3((unsigned)blocks), dim3(256), 0, st, f);
     rc = hipGetLastError();
   }
   return rc;

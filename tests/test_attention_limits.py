@@ -28,3 +28,11 @@ def test_results_between_heads_that_are_not_apart():
     for by in (1278, 200 - 4096 * 3, -200):  # (one kv head, whose tokens do not lie between two heads of the result)
         assert attention(tokens=5, kv_heads=1, q=rows(P << 6), k=major(P), v=rows(P << 4, 256), out=major(P + by)) == -12
     assert attention(tokens=5, q=major(P), out=rows(P + 1280, 128, 2049), **far) == -12
+
+
+def test_more_places_than_a_grid_has_chunks_of():
+    c = cache(page_size=4096, codes_head=4096 * 32, codes_page=2 * 4096 * 32, scales_head=4096, scales_page=2 * 4096)
+    far = dict(table=P, ld_table=1 << 20, positions=None, weights=None)
+    assert oz.lib().oz2_kv4_attention(ref(c), ref(sequences(max_pages=65536, **far)), 8, 0.1, ref(rows(P, 512, 64)), ref(rows(P << 1, 512, 64)), None) == -2
+    assert oz.lib().oz2_kv4_attention_workspace_bytes(ref(c), 1, 65535, 1, 2, 1) > 0 and oz.lib().oz2_kv4_attention_workspace_bytes(ref(c), 1, 65536, 1, 2, 1) == 0
+    assert oz.lib().oz2_kv4_evict_workspace_bytes(ref(c), 1, 65535, 100) > 0 and oz.lib().oz2_kv4_evict_workspace_bytes(ref(c), 1, 65536, 100) == 0

@@ -168,3 +168,21 @@ def test_contexts_side_by_side():
             graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(s[4], w[0]) and torch.equal(s[5], w[1]) for s, w in zip(sets, want))
+
+
+def test_a_sequence_of_as_many_places_as_there_may_be():
+    """65535 chunks, of which the first and the last have pages; a place that nobody sees receives nothing"""
+    rng = np.random.default_rng(10)
+    n = 65535 * 4096
+    held = Held(rng, [3 * 4096], 1, 64, 4096, spare=0)
+    table = torch.full((1, 65535), -1, dtype=torch.int32)
+    table[0, 0], table[0, 65533], table[0, 65534] = (int(x) for x in held.table[0])
+    q = torch.from_numpy(rng.standard_normal((1, 2, 64))).bfloat16()
+    ctx, weights = oz.Context(), torch.zeros((1, 1, n), device="cuda")
+    ctx.allocate_kv4_workspace(held.cache, table.cuda(), tokens=1, heads=2, weights=True)
+    out = ctx.kv4_attention(held.cache, q.cuda(), ints([0, 1]), table.cuda(), ints([n]), weights=weights)
+    want = formula(held, q.double().numpy(), [0, 1], 0.125)
+    close(out, want, "bf16", 64)
+    got = torch.cat((weights[0, 0, :4096], weights[0, 0, 65533 * 4096 :])).double().cpu().numpy()
+    assert (np.abs(got - want[4][0, 0]) <= 2 * want[5][0, 0] + 2 * U * want[4][0, 0]).all()
+    assert not weights[0, 0, 4096 : 65533 * 4096].any()
