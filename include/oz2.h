@@ -467,7 +467,9 @@ int oz2_context_w4_moe(oz2_context* ctx, const oz2_moe_layer* layer, int64_t t, 
  * lies outside 0 .. tokens is cut off).  Rows behind the last sequence are left as they were.  `heads` query heads share `kv_heads` heads of keys and values
  * in order: query head h reads kv head h / (heads / kv_heads).
  * Sums, maxima and sums of exponentials are FP32; results are rounded once to their type.  A row that sees no key, or none with a score above
- * -infinity, is 0; a NaN among the scores that it sees makes it NaN.  What a row does not see never reaches it, whatever it holds.  Equal calls give equal bits. */
+ * -infinity, is 0; a NaN among the scores that it sees makes it NaN.  What a row does not see never reaches it, whatever it holds.  Equal calls give equal bits.
+ * scale: finite and above 0.  A result lies behind or before its inputs, or between what they have of two tokens or two heads (parts of one packed tensor): other
+ * arrangements are refused, also where they share no byte.  tokens heads <= 2^28, 2^24 (new tokens) on a cache; sequences <= 2^20, 65535 on a cache. */
 typedef struct oz2_rows {
   void* data;
   int64_t ld_token, ld_head;
@@ -516,6 +518,7 @@ typedef struct oz2_kv4_sequences {
 /* Appends the new tokens k, v (tokens x kv heads x dim, both of one type) to their places: o = the smallest value, s = (largest - smallest) / 15, both rounded
  * to FP16, c = (x - o) (1 / s) in FP32 rounded to the nearest integer (ties to even) within 0 .. 15, 0 where s is 0.  A key or value with a NaN, an
  * infinity, or values beyond FP16 is held as one whose values are not finite.
+ * Two new tokens must not have one place (a page that two sequences share).
  * at: NULL, or the position of every new token, stored for all heads (needs positions); weights, if there, are 0 in the new places.  held_k, held_v: NULL, or
  * where to write what the cache now holds of k and v, rounded to their type (k and v themselves are allowed); of a token without a place too. */
 int oz2_kv4_append(const oz2_kv4_cache* cache, const oz2_kv4_sequences* on, const int32_t* at, const oz2_rows* k, const oz2_rows* v, const oz2_rows* held_k,
@@ -523,6 +526,7 @@ int oz2_kv4_append(const oz2_kv4_cache* cache, const oz2_kv4_sequences* on, cons
 
 /* out := attention of the new tokens q (tokens x heads x dim) over their sequences' places: new token j of n sees the places before lengths - n + j + 1.
  * The keys and values are what the cache stands for, unrounded; p s is rounded to two bf16 terms (three for FP32 results) before it meets the codes.
+ * Elements of q from 2^63 on count as infinities.
  * weights, if there: weights[s, kv head, t] += sum of p over the new tokens and the query heads of that kv head.
  * Meant for few new tokens a sequence: the cache is read once for every sixteen pairs of new token and query head of a kv head.  out shares no byte with q.
  * Workspace (256-byte aligned): oz2_kv4_attention_workspace_bytes, 0 for what is not valid. */
@@ -535,7 +539,7 @@ int oz2_context_kv4_attention(oz2_context* ctx, const oz2_kv4_cache* cache, cons
  * recent), and of the others those with the largest weights (a NaN counts as the largest; of equal ones the lower place), `keep` in all.  Those that stay and lie at
  * places from `keep` on move into the places below that were given up, the i-th of them into the i-th of these; nothing else moves, since attention asks for
  * no order.  on: positions and weights needed, cu and tokens not used; to: NULL (in place), or where lengths, positions and weights afterwards go, of the same
- * shapes (each may be the one of `on`); `to` is written below the new lengths alone.  0 <= recent <= keep.  Heads choose for themselves, so a place then
+ * shapes (each may be the one of `on`, and shares no byte with it else); `to` is written below the new lengths alone.  0 <= recent <= keep.  Heads choose for themselves, so a place then
  * holds different tokens for different heads.  Pages that two sequences share must not be evicted in. */
 typedef struct oz2_kv4_kept {
   int32_t* lengths;

@@ -1,8 +1,9 @@
-// Eviction from a cache held in 4 bits (oz2_kv4_evict), in two launches: a workgroup chooses for each sequence and kv head, then many move tokens.
+// Eviction from a cache held in 4 bits (oz2_kv4_evict): a workgroup chooses for each sequence and kv head, then many move tokens, or the same one where they are few.
 //
 // The choice: an unsigned key that orders weights as oz2.h says; the keep-th largest key by three passes over its bits from the top, with a histogram of 2048
 // bins in LDS; places with that key itself are taken from the lowest on.  Places below `keep` that were given up and places from `keep` on that stay are then
-// listed in order, by ranks from the lanes' votes.  Bound by the waits between these steps: a workgroup reads 8 bytes a place once.
+// listed in order, by ranks from the lanes' votes.  Bound by the waits between these steps, and by what one compute unit reads, 8 bytes a place: of 64 heads with up to
+// 32768 places and 4096 to keep, 8 us until the keys are there, 2 for the recent ones, 8 for the passes, 7 for the ranks; the moves, rows of 64 bytes from anywhere, 20.
 #include "oz2_kv4.h"
 #include "oz2_fast_div.h"
 
