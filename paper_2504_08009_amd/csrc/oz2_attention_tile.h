@@ -58,14 +58,15 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) attention_tile_
   constexpr int THREADS = 64 * WAVES / SPLIT, ROWS = 32 * WAVES / SPLIT, TILE = kTileKeys * ROW;
   constexpr int LOADS = TILE / 16 / THREADS, LDS = 4 * TILE;  // keys, keys, values, values
   __shared__ __attribute__((aligned(16))) char all_lds[SPLIT * LDS];  // of each part
-  __shared__ int all_odd[SPLIT];                               // whether the tile of values has one that is not finite
+  __shared__ int all_odd[SPLIT][2];                            // whether the tile of values has one that is not finite, of even and odd tiles
   __shared__ unsigned weights[WAVES][8][32];              // (where it has: p of two keys)
 
   const int tiles = (int)((unsigned)gridDim.x / (unsigned)a.kv_heads);
   const int head = blockIdx.x % a.kv_heads, lane = threadIdx.x % 64, col = lane % 32, half = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), part = wave / (WAVES / SPLIT), thread = threadIdx.x % THREADS;
   char* const lds = all_lds + part * LDS;
-  int& odd = all_odd[part];
+  int* const odd = all_odd[part];
+  if (thread < 2) odd[thread] = 0;
   const AttentionTile tile = attention_tile(a, blockIdx.x / a.kv_heads, tiles, ROWS);
   const int rows = tile.tokens * a.group;
   if (tile.first >= rows) return;
@@ -289,18 +290,20 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) attention_tile_
   for (; g < groups; ++g) {
     const int keys = (g + 1) % 2 * TILE, values = g % 2 * TILE;
     // values that some row may not see: whether one of them is not finite
-    if (thread == 0) odd = 0;
-    __syncthreads();
-    bool any = false;
+    bool seen = false;
+    if (least < (g + 1) * kTileKeys) {
+      bool any = false;
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const w4_u4 v = *reinterpret_cast<const w4_u4*>(lds + 2 * TILE + values + (i * THREADS + thread) * 16);
+      for (int i = 0; i < LOADS; ++i) {
+        const w4_u4 v = *reinterpret_cast<const w4_u4*>(lds + 2 * TILE + values + (i * THREADS + thread) * 16);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) any |= at_odd<XT>(v[j]);
+        for (int j = 0; j < 4; ++j) any |= at_odd<XT>(v[j]);
+      }
+      if (any) odd[g % 2] = 1;
+      if (thread == 0) odd[(g + 1) % 2] = 0;  // (which is read no more)
+      __syncthreads();
+      seen = odd[g % 2];
     }
-    if (any) odd = 1;
-    __syncthreads();
-    const bool seen = odd;
     if ((g + 2) * kTileKeys < all) fetch_keys(g + 2);
     if ((g + 1) * kTileKeys < all) fetch_values(g + 1);
     last_step(2 * g + 1, s[1], s[0], p[1], p[0], keys, values, seen);
