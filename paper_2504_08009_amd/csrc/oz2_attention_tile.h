@@ -53,7 +53,7 @@ __device__ __forceinline__ bool at_odd(unsigned w) {
 }
 
 template <int XT, int DP, int WAVES, int SPLIT>
-__global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) attention_tile_kernel(Attention a) {
+__global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) attention_tile_kernel(Attention a) {
   constexpr int E = DP / 16, F = DP / 32, ROW = DP <= 64 ? 128 : DP <= 128 ? 256 : 512;  // bytes of a row in LDS
   constexpr int THREADS = 64 * WAVES / SPLIT, ROWS = 32 * WAVES / SPLIT, TILE = kTileKeys * ROW;
   constexpr int LOADS = TILE / 16 / THREADS, LDS = 4 * TILE;  // keys, keys, values, values

@@ -197,10 +197,10 @@ __global__ void __launch_bounds__(kThreads) kv4_choose_kernel(Evict a) {
   int newest = INT32_MIN;
   int32_t p[TURNS][4];
   float w[TURNS][4];
-  // (the arrays have room for `capacity` places, a multiple of 16, whatever is held: all loads are made, and none waits for another)
+  // (all loads are made, and none waits for another: behind what is held those of its last four places, since there is room for `capacity`, a multiple of 16)
 #pragma unroll
   for (int i = 0; i < TURNS; ++i) {
-    const int t = min((i * kThreads + thread) * 4, a.capacity - 4);
+    const int t = min((i * kThreads + thread) * 4, (held - 1) / 4 * 4);
     four(positions + t, p[i]);
     four(weights + t, w[i]);
   }
