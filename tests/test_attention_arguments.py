@@ -69,8 +69,8 @@ def test_results_over_inputs_are_refused():
         assert attention(tokens=5, out=rows(at)) == -12
     # heads of one packed tensor q, k, v, out: no byte in common, yet one after the other
     packed = dict(q=rows(P, 2560), k=rows(P + 2048, 2560), v=rows(P + 2560, 2560))
-    assert attention(tokens=0, out=rows(P + 3072, 2560), **packed) == 0
-    assert attention(tokens=5, out=rows(P + 3070, 2560), **packed) == -12  # (the last of a token's values is the next one's first)
+    assert attention(tokens=0, out=rows(P + 2560 + 512, 2560), **packed) == 0
+    assert attention(tokens=5, out=rows(P + 2560 + 510, 2560), **packed) == -12  # (the last of a token's values is the next one's first)
 
 
 def cache(**more):
