@@ -469,7 +469,7 @@ int oz2_context_w4_moe(oz2_context* ctx, const oz2_moe_layer* layer, int64_t t, 
  * Sums, maxima and sums of exponentials are FP32; results are rounded once to their type.  A row that sees no key, or none with a score above
  * -infinity, is 0; a NaN among the scores that it sees makes it NaN.  What a row does not see never reaches it, whatever it holds.  Equal calls give equal bits.
  * scale: finite and above 0.  A result lies behind or before its inputs, or between what they have of two tokens or two heads (parts of one packed tensor): other
- * arrangements are refused, also where they share no byte.  tokens heads <= 2^28, 2^24 (new tokens) on a cache; sequences <= 2^20, 65535 on a cache. */
+ * arrangements are refused, also where they share no byte.  tokens heads <= 2^28, 2^23 (new tokens) on a cache; sequences <= 2^20, 65535 on a cache. */
 typedef struct oz2_rows {
   void* data;
   int64_t ld_token, ld_head;

@@ -983,7 +983,7 @@ bool same_rows(const oz2_rows& a, const oz2_rows& b) {
   return a.data == b.data && a.ld_token == b.ld_token && a.ld_head == b.ld_head && a.type == b.type;
 }
 
-constexpr int64_t kMostRows = (int64_t)1 << 24, kMostSequences = 65535;  // (sequences and heads are grid extents)
+constexpr int64_t kMostRows = (int64_t)1 << 23, kMostSequences = 65535;  // (grid extents; a grid has fewer than 2^32 threads)
 
 bool cache_ok(const oz2_kv4_cache* c) {
   if (!c || c->pages < 1 || c->pages > INT32_MAX || c->heads < 1 || c->heads > 65535) return false;

@@ -173,7 +173,7 @@ hipError_t oz2_launch_kv4_attention(const oz2_kv4_cache& cache, const oz2_kv4_se
   }
   int64_t blocks = f.joins;
   if (on.weights && capacity) {
-    const int64_t pairs = on.sequences * cache.heads, turns = (capacity + 255) / 256, most = ((int64_t)1 << 30) / pairs;
+    const int64_t pairs = on.sequences * cache.heads, turns = (capacity + 255) / 256, most = ((int64_t)1 << 22) / pairs;  // (a grid has fewer than 2^32 threads)
     f.turns = (unsigned)(turns < most ? turns : most);
     blocks += pairs * f.turns;
   }

@@ -36,3 +36,11 @@ def test_more_places_than_a_grid_has_chunks_of():
     assert oz.lib().oz2_kv4_attention(ref(c), ref(sequences(max_pages=65536, **far)), 8, 0.1, ref(rows(P, 512, 64)), ref(rows(P << 1, 512, 64)), None) == -2
     assert oz.lib().oz2_kv4_attention_workspace_bytes(ref(c), 1, 65535, 1, 2, 1) > 0 and oz.lib().oz2_kv4_attention_workspace_bytes(ref(c), 1, 65536, 1, 2, 1) == 0
     assert oz.lib().oz2_kv4_evict_workspace_bytes(ref(c), 1, 65535, 100) > 0 and oz.lib().oz2_kv4_evict_workspace_bytes(ref(c), 1, 65536, 100) == 0
+
+
+def test_more_rows_over_a_cache_than_a_grid_has_workgroups_for():
+    q = lambda heads: ref(rows(P, 64 * heads, 64))
+    for tokens, heads, rc in ((1 << 22, 4, -3), ((1 << 22) + 1, 2, -3), (3, 1 << 22, -3)):
+        assert oz.lib().oz2_kv4_attention(ref(cache()), ref(sequences(tokens=tokens)), heads, 0.1, q(heads), q(heads), None) == rc
+        assert oz.lib().oz2_kv4_attention_workspace_bytes(ref(cache()), 3, 4, tokens, heads, 0) == 0
+    assert oz.lib().oz2_kv4_attention_workspace_bytes(ref(cache()), 3, 4, 1 << 22, 2, 0) > 0

@@ -186,3 +186,27 @@ def test_a_sequence_of_as_many_places_as_there_may_be():
     got = torch.cat((weights[0, 0, :4096], weights[0, 0, 65533 * 4096 :])).double().cpu().numpy()
     assert (np.abs(got - want[4][0, 0]) <= 2 * want[5][0, 0] + 2 * U * want[4][0, 0]).all()
     assert not weights[0, 0, 4096 : 65533 * 4096].any()
+
+
+def test_more_rows_than_a_launch_has_workgroups_for_weights():
+    """many sequences and heads of a long table: places are received in turns"""
+    rng = np.random.default_rng(11)
+    sequences, kv_heads, page, places = 600, 1000, 16, 2048  # 600000 pairs, 8 turns each of which 6 go to a workgroup
+    cache = oz.KV4Cache.empty(2, kv_heads, page, 8)
+    cache.k_scales.fill_(0.25), cache.v_scales.fill_(0.5)
+    cache.k_codes.copy_(torch.from_numpy(rng.integers(0, 256, cache.k_codes.shape, dtype=np.uint8)))
+    cache.v_codes.copy_(torch.from_numpy(rng.integers(0, 256, cache.v_codes.shape, dtype=np.uint8)))
+    table = np.full((sequences, places // page), -1, dtype=np.int32)
+    table[:, 0], table[::3, 100] = 0, 1
+    lengths = np.where(np.arange(sequences) % 3 == 0, 1616, 16)
+    weights = torch.zeros((sequences, kv_heads, places), device="cuda")
+    q = torch.from_numpy(rng.standard_normal((1, kv_heads, 8))).bfloat16().expand(sequences, -1, -1).contiguous()
+    ctx = oz.Context()
+    ctx.allocate_kv4_workspace(cache, ints(table), tokens=sequences, heads=kv_heads, weights=True)
+    out = ctx.kv4_attention(cache, q.cuda(), ints(np.arange(sequences + 1)), ints(table), ints(lengths), weights=weights)
+    for first in (0, 1):  # sequences are alike by threes
+        same = torch.arange(first, sequences, 3, device="cuda")
+        assert torch.equal(out[same], out[first].expand(len(same), -1, -1)) and torch.equal(weights[same], weights[first].expand(len(same), -1, -1))
+    total = weights[:2].double().sum(2).cpu().numpy()
+    assert (np.abs(total - 1) <= (40 + 72) * U * 2).all()
+    assert not weights[0, :, 16:1600].any() and not weights[0, :, 1616:].any() and (weights[0, :, 1600:1616] > 0).all() and not weights[1, :, 16:].any()
