@@ -18,6 +18,7 @@ struct Attention {
   int heads, kv_heads, group, dim, causal;
   float scale2;  // scale log2(e)
   FastDiv per_group;
+  bool wide_out;  // the result's rows are 16-bit values in pieces of 16 bytes
 };
 
 inline int64_t attention_tiles(const Attention& a, int64_t size) { return a.tokens * a.group / size + a.sequences; }

@@ -20,7 +20,7 @@ bool fours(const oz2_rows& r, int64_t heads) {
 hipError_t oz2_launch_attention(int64_t tokens, int64_t sequences, const int32_t* cu, int64_t heads, int64_t kv_heads, int64_t dim, float scale, int causal,
                                 const oz2_rows& q, const oz2_rows& k, const oz2_rows& v, const oz2_rows& out, hipStream_t st) {
   Attention a = {cu, q, k, v, out, tokens, sequences, (int)heads, (int)kv_heads, (int)(heads / kv_heads), (int)dim, causal != 0,
-                 scale * 1.44269504088896340736f, fast_div((unsigned)(heads / kv_heads))};
+                 scale * 1.44269504088896340736f, fast_div((unsigned)(heads / kv_heads)), out.type != OZ2_F32 && pieces(out, heads)};
   if (q.type != OZ2_F32 && dim % 8 == 0 && pieces(q, heads) && pieces(k, kv_heads) && pieces(v, kv_heads) && fours(out, heads))
     return q.type == OZ2_BF16 ? oz2_attention_tile_of<OZ2_BF16>(a, st) : oz2_attention_tile_of<OZ2_F16>(a, st);
   return oz2_attention_any(a, st);

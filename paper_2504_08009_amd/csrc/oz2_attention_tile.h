@@ -338,9 +338,39 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) 
       }
   }
   l += __shfl_xor(l, 32);
+  const float inverse = l == 0.f ? 0.f : 1.f / l;
+  auto result = [&](int f, int i) { return l == 0.f ? 0.f : o[f][i] * inverse; };
+  if (a.wide_out) {
+    // Rows in pieces of 16 bytes, which come together in LDS, where keys and values (or the parts' sums) have been: a store has whole rows, not 16 bytes of 32 of them.
+    char* const to = all_lds + (SPLIT - 1) * LDS + wave * 32 * ROW;
+    static_assert(WAVES / SPLIT * 32 * ROW <= LDS, "room for all waves' rows");
+    auto place_of = [&](int r, int piece) { return r * ROW + (piece ^ r % (ROW == 128 ? 8 : 16)) * 16; };
+#pragma unroll
+    for (int f = 0; f < F; ++f)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        at_u2 w;
+        const float r[4] = {result(f, 4 * i), result(f, 4 * i + 1), result(f, 4 * i + 2), result(f, 4 * i + 3)};
+        if (a.out.type == OZ2_BF16) w = at_u2{at_pair<OZ2_BF16>(r[0], r[1]), at_pair<OZ2_BF16>(r[2], r[3])};
+        else w = at_u2{at_pair<OZ2_F16>(r[0], r[1]), at_pair<OZ2_F16>(r[2], r[3])};
+        *reinterpret_cast<at_u2*>(to + place_of(col, 4 * f + i) + half * 8) = w;
+      }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    constexpr int EACH = 64 / PIECES;  // rows of a store
+    const int piece = lane % PIECES;
+#pragma unroll
+    for (int i = 0; i < 32 / EACH; ++i) {
+      const int r = i * EACH + lane / PIECES, row = first_row + r, at = row / a.per_group;
+      const int64_t out_at = (tile.begin + at) * a.out.ld_token + ((int64_t)head * a.group + (row - at * a.group)) * a.out.ld_head;
+      const w4_u4 w = *reinterpret_cast<const w4_u4*>(to + place_of(r, piece));
+      if (row < rows && piece * 8 < a.dim) *reinterpret_cast<w4_u4*>(static_cast<uint16_t*>(a.out.data) + out_at + piece * 8) = w;
+    }
+    return;
+  }
   if (first_row + col >= rows) return;
   const int64_t out_at = (tile.begin + at) * a.out.ld_token + query * a.out.ld_head;
-  const float inverse = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int f = 0; f < F; ++f)
 #pragma unroll
@@ -349,7 +379,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) 
       if (d >= a.dim) continue;
       float r[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) r[j] = l == 0.f ? 0.f : o[f][4 * i + j] * inverse;
+      for (int j = 0; j < 4; ++j) r[j] = result(f, 4 * i + j);
       if (a.out.type == OZ2_F32)
 #pragma unroll
         for (int j = 0; j < 4; ++j) static_cast<float*>(a.out.data)[out_at + d + j] = r[j];
