@@ -10,8 +10,8 @@
 // exponentials of step j on the vector units.  m follows the maximum only where a score is more than 2^8 above it, which hardly happens after the
 // first tile; so the sums are hardly ever rescaled.  `step` is for tiles that all rows see, and has no branch but that; `last_step` is for all others.
 //   With SPLIT = 2 the two halves of a workgroup have the same 128 rows and every other tile of keys each; their sums are joined at the end.
-//   16384 tokens of 16 heads of 128 values, FP16, causal, take 1.10 ms, 1000 TFLOP/s, where a large matrix product reaches 1507: the vector units' part of a step, 32
-// exponentials a lane's pair of rows and what goes with them, is nearly as long as the products' 16 x 32 cycles, and the clock falls under both.
+//   16384 tokens of 16 heads of 128 values, FP16, causal, take 1.03 to 1.10 ms, 1000 to 1070 TFLOP/s, where a large matrix product reaches 1507: the vector units' part of
+// a step, sixteen exponentials a lane and what goes with them, is nearly as long as the products' 16 x 32 cycles, and the clock falls under both.
 #ifndef OZ2_ATTENTION_TILE_H
 #define OZ2_ATTENTION_TILE_H
 
