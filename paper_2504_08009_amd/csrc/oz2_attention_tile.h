@@ -410,9 +410,9 @@ hipError_t oz2_attention_tile_dims(const Attention& a, hipStream_t st) {
 // one begins or ends while the other is at work.  Where even tiles of 128 leave compute units without work, or last much longer than their number needs:
 // 128 rows with their keys in two parts.  bf16, causal, 8 query and kv heads of 128 values, us with 256 rows, 128 rows, and parts:
 //   sequences          2 x 1024   1 x 2048   1 x 4096   4 x 2048   1 x 8192   24 x 512   3 x 4096   (32 and 8 heads) 12 of 16 to 2000   1 x 4096   1 x 8192
-//   256 rows              36         57        101         64        201         48        123                     257                  151        533
-//   128 rows              27         42         76         56        181         39        121                     242                  155        554
-//   128 rows, parts       25         37         65         60        156         55        139
+//   256 rows              35         56        100         62        194         44        117                     155                  135        497
+//   128 rows              27         43         79         55        174         35        113                     148                  142        511
+//   128 rows, parts       25         38         66         58        155         52        133                     204                  162        569
 template <int XT>
 hipError_t oz2_attention_tile_of(const Attention& a, hipStream_t st) {
   if (a.dim > 128) return oz2_attention_wide_of<XT>(a, st);
