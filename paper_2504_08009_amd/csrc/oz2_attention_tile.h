@@ -1,6 +1,6 @@
 // Attention over packed prompts in BF16 and FP16 on the matrix cores: the kernel of one type and of dims up to DP.
 //
-// A workgroup has 256 or 128 rows, a wave 32 of them, which are the columns of its products (32 x 32 x 16): keys x rows, then dims x rows.  So a lane has one
+// A workgroup has 256, 128 or 64 rows, a wave 32 of them, which are the columns of its products (32 x 32 x 16): keys x rows, then dims x rows.  So a lane has one
 // row throughout, maxima and sums stay in lanes, and what it holds of the first product, rounded, is its part of the second one's operand as it is: of sixteen
 // keys the lanes' lower half has 0..3 and 8..11, the upper half 4..7 and 12..15, and the values are read in that order.  (p is rounded to the type of the values,
 // as the matrix cores take it; its sum l is of what it was before.)
@@ -9,7 +9,7 @@
 //   A step takes 32 keys, and works on three of them at once, none of which waits for another: scores of step j + 1 and values of step j - 1 on the matrix cores, the
 // exponentials of step j on the vector units.  m follows the maximum only where a score is more than 2^8 above it, which hardly happens after the
 // first tile; so the sums are hardly ever rescaled.  `step` is for tiles that all rows see, and has no branch but that; `last_step` is for all others.
-//   With SPLIT = 2 the two halves of a workgroup have the same 128 rows and every other tile of keys each; their sums are joined at the end.
+//   With SPLIT = 2 the two halves of a workgroup have the same rows and every other tile of keys each; their sums are joined at the end.
 //   16384 tokens of 16 heads of 128 values, FP16, causal, take 1.03 to 1.10 ms, 1000 to 1070 TFLOP/s, where a large matrix product reaches 1507: the vector units' part of
 // a step, sixteen exponentials a lane and what goes with them, is nearly as long as the products' 16 x 32 cycles, and the clock falls under both.
 #ifndef OZ2_ATTENTION_TILE_H
@@ -104,13 +104,13 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) 
   // Copies of tiles into LDS: sixteen bytes a lane, a wave's 1024 beside each other.  Pieces of sixteen bytes change places within a row, so that sixteen keys' pieces, and
   // four values' 64 bytes, lie in all banks: which piece comes to a place is chosen by what the lane loads.  Rows behind the last token are copies of it, pieces
   // behind the last dim of the first piece: what they meet is not seen, a 0 of q, or not stored.
-  constexpr int PIECES = ROW / 16, PER = THREADS / PIECES;
+  constexpr int PIECES = ROW / 16, PER = THREADS / PIECES, TURNS = PER % 16 ? 2 : 1;
   const int of_key = thread / PIECES, place = thread % PIECES;
   auto piece_at = [&](int swizzled) { return (swizzled * 8 < a.dim ? swizzled : 0) * 16; };
-  int k_piece[ROW == 512 ? 2 : 1];  // (of even and odd loads, where a thread's keys do not have one exchange)
+  int k_piece[TURNS];  // (of even and odd loads, where a thread's keys do not have one exchange)
 #pragma unroll
-  for (int i = 0; i < (ROW == 512 ? 2 : 1); ++i) k_piece[i] = piece_at(place ^ (ROW == 128 ? of_key / 2 % 8 : (of_key + i * PER) % 16));
-  static_assert(ROW == 512 ? PER == 8 : PER % 16 == 0, "a thread's keys have one exchange of pieces, or two in turn");
+  for (int i = 0; i < TURNS; ++i) k_piece[i] = piece_at(place ^ (ROW == 128 ? (of_key + i * PER) / 2 % 8 : (of_key + i * PER) % 16));
+  static_assert(PER % 8 == 0, "a thread's keys have one exchange of pieces, or two in turn");
   const int v_piece = piece_at(place ^ (ROW == 128 ? of_key / 2 % 2 : of_key % 4) * 4);
   const char* k_from = static_cast<const char*>(a.k.data) + (tile.begin * a.k.ld_token + head * a.k.ld_head) * 2;
   const char* v_from = static_cast<const char*>(a.v.data) + (tile.begin * a.v.ld_token + head * a.v.ld_head) * 2;
@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) 
     for (int i = 0; i < LOADS; ++i)
       load_to_lds_16(reinterpret_cast<const int8_t*>(from), (unsigned)(min(of_key + i * PER, last) * step + piece[i % pieces]), lds_at + at + i * THREADS * 16);
   };
-  auto fetch_keys = [&](int number) { fetch(k_from, k_step, number * kTileKeys, number % 2 * TILE, k_piece, ROW == 512 ? 2 : 1); };
+  auto fetch_keys = [&](int number) { fetch(k_from, k_step, number * kTileKeys, number % 2 * TILE, k_piece, TURNS); };
   auto fetch_values = [&](int number) { fetch(v_from, v_step, number * kTileKeys, (2 + number % 2) * TILE, &v_piece, 1); };
 
   // where a lane reads: pieces of keys and 64 bytes of values at these with bits exchanged
@@ -413,10 +413,15 @@ hipError_t oz2_attention_tile_dims(const Attention& a, hipStream_t st) {
 //   256 rows              35         56        100         62        194         44        117                     155                  135        497
 //   128 rows              27         43         79         55        174         35        113                     148                  142        511
 //   128 rows, parts       25         38         66         58        155         52        133                     204                  162        569
+// Few rows: 64 of them with their keys in two parts, of which 65 to 128 dims leave room for one workgroup a compute unit, up to 64 for two.
+//   us with 128 rows, 128 in parts, 64 in parts       1 x 512   1 x 1024   1 x 2048   (one head) 1 x 4096   1 x 16384   4 x 512   8 x 512
+//   8 heads of 128 values                            17 17 15   26 24 20   42 36 31           74 59 48     269 206 167  18 18 16  20 20 26
+//   8 heads of 64                                    13 12 11   19 16 14   30 24 21           53 40 33     191 135 108  13 13 11  14 13 13
 template <int XT>
 hipError_t oz2_attention_tile_of(const Attention& a, hipStream_t st) {
   if (a.dim > 128) return oz2_attention_wide_of<XT>(a, st);
   const int64_t tiles = a.tokens * a.heads / 256, mean = a.tokens / a.sequences;
+  if (mean >= 500 && tiles <= (a.dim <= 64 ? 128 : 64)) return oz2_attention_tile_dims<XT, 4, 2>(a, st);
   if (mean >= 3000 ? tiles <= 288 : mean >= 1000 && tiles <= 128) return oz2_attention_tile_dims<XT, 8, 2>(a, st);
   return mean >= 3000 ? oz2_attention_tile_dims<XT, 8, 1>(a, st) : oz2_attention_tile_dims<XT, 4, 1>(a, st);
 }

@@ -58,9 +58,9 @@ def offsets(lengths):
 @pytest.mark.parametrize("causal", [True, False], ids=["causal", "all"])
 @pytest.mark.parametrize("dim", [40, 64, 96, 128])
 def test_tiles_of_all_sizes(dim, causal, name):
-    """128 rows to a workgroup, 256, and 128 with keys in two parts: at ends of tiles, with shared heads that do not divide a tile"""
+    """128 rows to a workgroup, 256, and 128 and 64 with keys in two parts: at ends of tiles, with shared heads that do not divide a tile"""
     for lengths, heads, kv_heads in (([1500, 0, 1, 257, 256, 64, 700], 30, 2), ([1500, 0, 1, 257, 256, 64, 700], 29, 29), ([4100, 1900], 14, 2), ([3000], 27, 27),
-                                     ([3111], 6, 2), ([1100, 930], 5, 5)):
+                                     ([3111], 6, 2), ([1100, 930], 5, 5), ([1000, 35], 14, 2), ([513, 511, 640], 3, 3), ([2900], 5, 1), ([1111, 1, 900], 2, 1)):
         cu, on = offsets(lengths)
         q, k, v = made(dim, cu[-1] + 5, heads, kv_heads, dim, TYPES[name])
         out = torch.full_like(q, 7.0)
@@ -71,10 +71,10 @@ def test_tiles_of_all_sizes(dim, causal, name):
 
 @pytest.mark.parametrize("name", ["bf16", "f16"])
 @pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
-@pytest.mark.parametrize("heads,more", [(32, 0), (8, 0), (32, 3000)], ids=["128", "parts", "256"])
-def test_values_that_some_rows_do_not_see(heads, more, what, name):
+@pytest.mark.parametrize("heads,kv_heads,more", [(32, 8, 0), (8, 8, 0), (32, 8, 3000), (4, 2, 0)], ids=["128", "128_parts", "256", "64_parts"])
+def test_values_that_some_rows_do_not_see(heads, kv_heads, more, what, name):
     cu, on = offsets([1300, 1700 + more])
-    q, k, v = made(3, cu[-1], heads, 8, 128, TYPES[name])
+    q, k, v = made(3, cu[-1], heads, kv_heads, 128, TYPES[name])
     clean = v.clone()
     at = [700, 1299, 1300 + 64, 1300 + 1695]
     for t in at:
