@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) 
     const int keys = (g + 1) % 2 * TILE, values = g % 2 * TILE;
     // values that some row may not see: whether one of them is not finite
     bool seen = false;
-    if (least < (g + 1) * kTileKeys) {
+    if (DP > 128 || least < (g + 1) * kTileKeys) {  // (with more dims the condition has addresses of the loop above spilled: 4096 tokens of 16 heads of 256 254 us, 200 so)
       bool any = false;
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
