@@ -82,11 +82,14 @@ __global__ void __launch_bounds__(256, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) attenti
 
   const char* k_from = static_cast<const char*>(a.k.data) + (tile.begin * a.k.ld_token + head * a.k.ld_head) * SIZE;
   const char* v_from = static_cast<const char*>(a.v.data) + (tile.begin * a.v.ld_token + head * a.v.ld_head) * SIZE;
-  // (a dim that is not there: of keys another one, which meets a 0 of q; of values another one, whose sum is not stored.  A token behind the last one is the last one.)
+  // (a dim that is not there: of keys another one is read and 0 taken, since an infinity would make a NaN of the 0 of q that it meets; of values another one, whose sum
+  // is not stored.  A token behind the last one is the last one.)
   Piece k[AHEAD];
   unsigned v[AHEAD][F];
   const char* k_row;
   auto read_keys = [&](int e) { k[e % AHEAD].read(k_row, 8 * e + 4 * half, a.dim); };
+  int dims = a.dim - 4 * half;
+  auto key = [&](int e, int j) { return 8 * e + (FOURS ? 0 : j) < dims ? k[e % AHEAD][j] : 0.f; };
   auto read_values = [&](int k0, int i) {
     const char* from = v_from + min(k0 + i / 4 * 8 + i % 4 + 4 * half, tile.tokens - 1) * a.v.ld_token * SIZE;
 #pragma unroll
@@ -117,12 +120,13 @@ __global__ void __launch_bounds__(256, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) attenti
   auto step = [&](int k0, auto all) {
     constexpr bool ALL = decltype(all)::value;
     f16v s;
+    asm volatile("" : "+v"(dims));  // (else all comparisons with it are made ahead of the loop, and their results spilled)
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e % AHEAD][j], q[e][j], s, 0, 0, 0);
+      for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_32x32x2f32(key(e, j), q[e][j], s, 0, 0, 0);
       if (e + AHEAD < E) read_keys(e + AHEAD);
       else read_values(k0, e + AHEAD - E);
       __builtin_amdgcn_sched_barrier(0);

@@ -102,29 +102,46 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) 
   }
 
   // Copies of tiles into LDS: sixteen bytes a lane, a wave's 1024 beside each other.  Pieces of sixteen bytes change places within a row, so that sixteen keys' pieces, and
-  // four values' 64 bytes, lie in all banks: which piece comes to a place is chosen by what the lane loads.  Rows behind the last token are copies of it, pieces
-  // behind the last dim of the first piece: what they meet is not seen, a 0 of q, or not stored.
+  // four values' 64 bytes, lie in all banks: which piece comes to a place is chosen by what the lane loads.  Rows behind the last token are copies of it, which no row
+  // sees.  Pieces behind the last dim: of keys 0 from the beginning on, and not copied to (they meet a 0 of q, which an infinity would make a NaN); of values the first
+  // piece, whose sums are not stored.
   constexpr int PIECES = ROW / 16, PER = THREADS / PIECES, TURNS = PER % 16 ? 2 : 1;
   const int of_key = thread / PIECES, place = thread % PIECES;
-  auto piece_at = [&](int swizzled) { return (swizzled * 8 < a.dim ? swizzled : 0) * 16; };
   int k_piece[TURNS];  // (of even and odd loads, where a thread's keys do not have one exchange)
+  unsigned long long k_lanes[TURNS];
 #pragma unroll
-  for (int i = 0; i < TURNS; ++i) k_piece[i] = piece_at(place ^ (ROW == 128 ? (of_key + i * PER) / 2 % 8 : (of_key + i * PER) % 16));
+  for (int t = 0; t < TURNS; ++t) {
+    k_piece[t] = place ^ (ROW == 128 ? (of_key + t * PER) / 2 % 8 : (of_key + t * PER) % 16);
+    k_lanes[t] = __ballot(k_piece[t] * 8 < a.dim);
+  }
   static_assert(PER % 8 == 0, "a thread's keys have one exchange of pieces, or two in turn");
-  const int v_piece = piece_at(place ^ (ROW == 128 ? of_key / 2 % 2 : of_key % 4) * 4);
+  const int v_swizzled = place ^ (ROW == 128 ? of_key / 2 % 2 : of_key % 4) * 4, v_piece = v_swizzled * 8 < a.dim ? v_swizzled : 0;
   const char* k_from = static_cast<const char*>(a.k.data) + (tile.begin * a.k.ld_token + head * a.k.ld_head) * 2;
   const char* v_from = static_cast<const char*>(a.v.data) + (tile.begin * a.v.ld_token + head * a.v.ld_head) * 2;
   const int k_step = (int)(a.k.ld_token * 2), v_step = (int)(a.v.ld_token * 2);
   const unsigned lds_at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave % (WAVES / SPLIT) * 1024;
-  auto fetch = [&](const char* from, int step, int first, int at, const int* piece, int pieces) {
+  auto fetch = [&](const char* from, int step, int first, auto load) {
     const int last = min(kTileKeys, tokens - first) - 1;
     from += (int64_t)(SPLIT > 1 ? first * SPLIT + part * kTileKeys : first) * step;
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i)
-      load_to_lds_16(reinterpret_cast<const int8_t*>(from), (unsigned)(min(of_key + i * PER, last) * step + piece[i % pieces]), lds_at + at + i * THREADS * 16);
+    for (int i = 0; i < LOADS; ++i) load(reinterpret_cast<const int8_t*>(from), min(of_key + i * PER, last) * step, i);
   };
-  auto fetch_keys = [&](int number) { fetch(k_from, k_step, number * kTileKeys, number % 2 * TILE, k_piece, TURNS); };
-  auto fetch_values = [&](int number) { fetch(v_from, v_step, number * kTileKeys, (2 + number % 2) * TILE, &v_piece, 1); };
+  auto fetch_keys = [&](int number) {
+    fetch(k_from, k_step, number * kTileKeys, [&](const int8_t* from, int at, int i) {
+      load_to_lds_16(from, (unsigned)(at + k_piece[i % TURNS] * 16), lds_at + number % 2 * TILE + i * THREADS * 16, k_lanes[i % TURNS]);
+    });
+  };
+  auto fetch_values = [&](int number) {
+    fetch(v_from, v_step, number * kTileKeys, [&](const int8_t* from, int at, int i) {
+      load_to_lds_16(from, (unsigned)(at + v_piece * 16), lds_at + (2 + number % 2) * TILE + i * THREADS * 16);
+    });
+  };
+#pragma unroll
+  for (int t = 0; t < TURNS; ++t)
+    if (k_piece[t] * 8 >= a.dim)
+#pragma unroll
+      for (int i = t; i < 2 * LOADS; i += TURNS) *reinterpret_cast<w4_u4*>(lds + (i * THREADS + thread) * 16) = w4_u4{0, 0, 0, 0};
+  static_assert(LOADS % TURNS == 0, "both tiles of keys have the same turns");
 
   // where a lane reads: pieces of keys and 64 bytes of values at these with bits exchanged
   const int k_at = col * ROW + (half ^ (ROW == 128 ? col / 2 % 8 : col % 16)) * 16;
