@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(256, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) attenti
 #pragma unroll
       for (int j = 0; j < 4; ++j) q[e][j] = 8 * e + 4 * half + j < a.dim ? raw[e][j] : 0.f;
   }
-  float m = -3e38f, l = 0.f;
+  float m = kNoScore, l = 0.f;
   f16v o[F];
 #pragma unroll
   for (int f = 0; f < F; ++f)

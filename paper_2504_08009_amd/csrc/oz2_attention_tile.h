@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) 
   const int k_at = col * ROW + (half ^ (ROW == 128 ? col / 2 % 8 : col % 16)) * 16;
   const int v_at = 2 * TILE + (4 * half + lane % 16 / 4) * ROW + (ROW == 128 ? lane % 16 / 8 : lane % 16 / 4) * 64 + lane / 16 % 2 * 32 + lane % 4 * 8;
 
-  float m = -3e38f, l = 0.f;
+  float m = kNoScore, l = 0.f, scale2 = a.scale2;
   at_f16 o[F], s[2];
   w4_u4 p[2][2];
 #pragma unroll
@@ -225,11 +225,13 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) 
     float top = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-    const bool high = __any(fmaf(top, a.scale2, -m) > 8.f);
+    const bool high = __any(fmaf(top, scale2, -m) > 8.f);
     if (pending || high) {
       rescale();
       if (high) {
-        const float raised = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)) * a.scale2);
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float with = kv_scale_of(top, a.scale2), raised = fmaxf(m, top * with);
+        scale2 = raised > m ? with : scale2;
         factor = __builtin_amdgcn_exp2f(m - raised);
         m = raised;
         l *= factor;
@@ -241,7 +243,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) 
   auto exponentials = [&](const at_f16 &s, w4_u4 (&p)[2], int first, int last) {
 #pragma unroll
     for (int i = first; i < last; ++i) {
-      const float one = __builtin_amdgcn_exp2f(fmaf(s[2 * i], a.scale2, -m)), two = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], a.scale2, -m));
+      const float one = __builtin_amdgcn_exp2f(fmaf(s[2 * i], scale2, -m)), two = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], scale2, -m));
       l += one + two;
       p[i / 4][i % 4] = at_pair<XT>(one, two);
     }

@@ -23,6 +23,13 @@ hipError_t oz2_launch_kv4_evict(const oz2_kv4_cache& cache, const oz2_kv4_sequen
 #ifdef __HIPCC__
 #include "oz2_w4.h"
 
+// Softmax weights are exp2(score scale2 - m), one FMA: m is a row's largest product, rounded, and what its rounding left is part of every weight alike.  From 2^31 on that
+// would be 2^128 of them or none.  So a product beyond kLarge is formed with the power of two above scale2 instead, which leaves nothing: m is then a function of the score
+// that still rises with it, and differences count up to twice, where neighbouring FP32 numbers are 4 apart and more.
+constexpr float kLarge = 0x1p25f, kNoScore = -3.402823466e38f;  // (and the m of a row without a score: no product is below it)
+__device__ __forceinline__ float kv_power_above(float x) { return __uint_as_float((__float_as_uint(x) + 0x7fffff) & 0x7f800000); }
+__device__ __forceinline__ float kv_scale_of(float score, float scale2) { return fabsf(score * scale2) > kLarge ? kv_power_above(scale2) : scale2; }
+
 // Rows of sequence s among `tokens` packed ones, and how many places it holds: whatever cu and lengths say, within what there is.
 struct KvRange { int64_t begin, end; };
 __device__ __forceinline__ KvRange kv_range(const int32_t* cu, int64_t s, int64_t tokens) {

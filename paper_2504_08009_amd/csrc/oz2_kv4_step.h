@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(256, XT != OZ2_F32 && DP <= 128 ? 3 : 1) kv4_s
     sum += __shfl_xor(sum, 32);
     sum *= 1.f / step_score<XT>();
 
-    float m = -3e38f, l = 0.f, c = 0.f;  // m: finite, so that nothing that is not seen becomes a NaN
+    float m = kNoScore, l = 0.f, c = 0.f;  // (finite, so that nothing that is not seen becomes a NaN)
     w4_f4 o[F];
     for (int f = 0; f < F; ++f) o[f] = w4_f4{0.f, 0.f, 0.f, 0.f};
 
@@ -250,19 +250,26 @@ __global__ void __launch_bounds__(256, XT != OZ2_F32 && DP <= 128 ? 3 : 1) kv4_s
         }
       }
       const float top = max3(max3(max3(t[0], t[1], t[2]), t[3], t[4]), max3(t[5], t[6], t[7]), t[7]);
-      if (__any(fmaf(top, a.scale2, SHIFT - m) > SHIFT + 8.f)) {
+      // (a row of large scores, and one without any: m is taken off ahead of the exponent, where SHIFT would be lost in it)
+      float shift = SHIFT - (fabsf(m) > kLarge ? 0.f : m);
+      if (__any(fabsf(m) > kLarge || fmaf(top, a.scale2, shift) > SHIFT + 8.f)) {
         float high = fmaxf(top, __shfl_xor(top, 16));
         high = fmaxf(high, __shfl_xor(high, 32));
-        const float raised = fmaxf(m, high * a.scale2), f = __builtin_amdgcn_exp2f(m - raised);
+        const float raised = fmaxf(m, high * kv_scale_of(high, a.scale2)), f = __builtin_amdgcn_exp2f(m - raised);
         m = raised;
         l *= f, c *= f;
 #pragma unroll
         for (int i = 0; i < F; ++i) o[i] *= f;
+        const bool large = fabsf(m) > kLarge;
+        const float above = kv_power_above(a.scale2), back = __builtin_amdgcn_rcpf(a.scale2);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = large ? fmaf(t[i], above, -m) * back : t[i];
+        shift = SHIFT - (large ? 0.f : m);
       }
       float w[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(t[i], a.scale2, SHIFT - m));
+        const float p = __builtin_amdgcn_exp2f(fmaf(t[i], a.scale2, shift));
         l += p;
         w[i] = fmaf(p, half_of(now.vs[i / 4][i % 4], 0), 0.f);
         if constexpr (XT == OZ2_F32) w[i] *= kStepFactor;

@@ -30,7 +30,7 @@ __device__ __forceinline__ void join(const Finish& f, Joining& sh) {
   const bool mine = slot < slots && first + slot < a.rows && at >= r.begin && at < r.end && held > a.chunk;
   const int chunks = mine ? (held + a.chunk - 1) / a.chunk : 0;
   const float2* stats = reinterpret_cast<const float2*>(a.stats) + row;
-  float high = -3e38f, total = 0.f, v[4] = {};
+  float high = kNoScore, total = 0.f, v[4] = {};
 #pragma unroll 4
   for (int i = part; i < chunks; i += parts) {
     const float2 own = stats[i * a.rows];
@@ -62,7 +62,7 @@ __device__ __forceinline__ void join(const Finish& f, Joining& sh) {
 }
 
 // What each place received, from the scores and the maxima and sums of its rows, 64 rows at a time and four threads to the chunks of one.
-struct Receiving { float top[64], inverse[64]; const float* scores[64]; };
+struct Receiving { float top[64], scale2[64], inverse[64]; const float* scores[64]; };
 __device__ __forceinline__ void receive(const Finish& f, Receiving& sh) {
   const Kv4Step& a = f.a;
   const unsigned i = blockIdx.x - f.joins, pairs = (unsigned)(a.on.sequences * a.c.heads), turn = i / f.per_pair, pair = i - turn * pairs;
@@ -81,7 +81,7 @@ __device__ __forceinline__ void receive(const Finish& f, Receiving& sh) {
       const int n = min(64, rows - r0), own = r0 + min(thread / 4, n - 1), fresh = own / a.per_group;
       const int64_t row = (r.begin + fresh) * a.heads + head * a.group + (own - fresh * a.group);
       const float2* stats = reinterpret_cast<const float2*>(a.stats) + row;
-      float high = -3e38f, total = 0.f;
+      float high = kNoScore, total = 0.f;
       auto with = [&](float top, float part) {
         const float raised = fmaxf(high, top);
         total = fmaf(total, __builtin_amdgcn_exp2f(high - raised), part * __builtin_amdgcn_exp2f(top - raised));
@@ -99,13 +99,14 @@ __device__ __forceinline__ void receive(const Finish& f, Receiving& sh) {
       __syncthreads();
       if (thread % 4 == 0 && thread / 4 < n) {
         sh.top[thread / 4] = high;
+        sh.scale2[thread / 4] = fabsf(high) > kLarge ? kv_power_above(a.scale2) : a.scale2;
         sh.inverse[thread / 4] = total == 0.f ? 0.f : 1.f / total;
         sh.scores[thread / 4] = a.scores + row * a.capacity;
       }
       __syncthreads();
       if (place < held) {
 #pragma unroll 4
-        for (int j = 0; j < n; ++j) sum = fmaf(__builtin_amdgcn_exp2f(fmaf(sh.scores[j][place], a.scale2, -sh.top[j])), sh.inverse[j], sum);
+        for (int j = 0; j < n; ++j) sum = fmaf(__builtin_amdgcn_exp2f(fmaf(sh.scores[j][place], sh.scale2[j], -sh.top[j])), sh.inverse[j], sum);
       }
     }
     if (place < held) to[place] = had + sum;
