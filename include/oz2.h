@@ -480,8 +480,9 @@ typedef struct oz2_rows {
 #define OZ2_ATTENTION_MAX_DIM 256
 
 /* out_i := sum_j p_ij v_j,  p_i = softmax over j of  scale q_i k_j,  over the tokens j of i's own sequence, up to i itself if causal != 0.
- * q, out: tokens x heads x dim; k, v: tokens x kv_heads x dim, of q's type; dim <= OZ2_ATTENTION_MAX_DIM.  For 16-bit types p is rounded to that type before
- * it meets v; its sum is taken unrounded.  out shares no byte with q, k or v.  Uses no workspace; may be captured. */
+ * q, out: tokens x heads x dim; k, v: tokens x kv_heads x dim, of q's type; dim <= OZ2_ATTENTION_MAX_DIM.  For 16-bit types with a dim in eights, and rows that
+ * start at multiples of 16 bytes, p is rounded to that type before it meets v (FP16: by 2^-11 of it, or 2^-32 of the row's largest where that is more); its sum is
+ * taken unrounded.  out shares no byte with q, k or v.  Uses no workspace; may be captured. */
 int oz2_attention(int64_t tokens, int64_t sequences, const int32_t* cu, int64_t heads, int64_t kv_heads, int64_t dim, float scale, int causal,
                   const oz2_rows* q, const oz2_rows* k, const oz2_rows* v, const oz2_rows* out, void* stream);
 

@@ -3,11 +3,11 @@
 // A workgroup has 256, 128 or 64 rows, a wave 32 of them, which are the columns of its products (32 x 32 x 16): keys x rows, then dims x rows.  So a lane has one
 // row throughout, maxima and sums stay in lanes, and what it holds of the first product, rounded, is its part of the second one's operand as it is: of sixteen
 // keys the lanes' lower half has 0..3 and 8..11, the upper half 4..7 and 12..15, and the values are read in that order.  (p is rounded to the type of the values,
-// as the matrix cores take it; its sum l is of what it was before.)
+// as the matrix cores take it; its sum l is of what it was before.  In FP16 that is half a step, 2^-11 of p, or 2^-32 of the largest p where that is more.)
 //   Keys and values come into LDS in tiles of 64, in two buffers, by copies that pass no registers, begun a tile ahead; one barrier a tile.  Values are wanted with
 // keys along a lane's words: ds_read_b64_tr_b16 turns 4 x 16 of them on their way.
 //   A step takes 32 keys, and works on three of them at once, none of which waits for another: scores of step j + 1 and values of step j - 1 on the matrix cores, the
-// exponentials of step j on the vector units.  m follows the maximum only where a score is more than 2^8 above it, which hardly happens after the
+// exponentials of step j on the vector units.  m follows the maximum only where a score is more than 8 above it (to base 2), which hardly happens after the
 // first tile; so the sums are hardly ever rescaled.  `step` is for tiles that all rows see, and has no branch but that; `last_step` is for all others.
 //   With SPLIT = 2 the two halves of a workgroup have the same rows and every other tile of keys each; their sums are joined at the end.
 //   16384 tokens of 16 heads of 128 values, FP16, causal, take 1.03 to 1.10 ms, 1000 to 1070 TFLOP/s, where a large matrix product reaches 1507: the vector units' part of
@@ -57,6 +57,8 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) 
   constexpr int E = DP / 16, F = DP / 32, ROW = DP <= 64 ? 128 : DP <= 128 ? 256 : 512;  // bytes of a row in LDS
   constexpr int THREADS = 64 * WAVES / SPLIT, ROWS = 32 * WAVES / SPLIT, TILE = kTileKeys * ROW;
   constexpr int LOADS = TILE / 16 / THREADS, LDS = 4 * TILE;  // keys, keys, values, values
+  // m is the maximum less UP: in FP16, where normal numbers end at 2^-14, p goes up to 2^15, and many keys far below one count
+  constexpr float UP = XT == OZ2_F16 ? 7.f : 0.f;
   __shared__ __attribute__((aligned(16))) char all_lds[SPLIT * LDS];  // of each part
   __shared__ int all_odd[SPLIT][2];                            // whether the tile of values has one that is not finite, of even and odd tiles
   __shared__ unsigned weights[WAVES][8][32];              // (where it has: p of two keys)
@@ -225,12 +227,12 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) 
     float top = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-    const bool high = __any(fmaf(top, scale2, -m) > 8.f);
+    const bool high = __any(fmaf(top, scale2, -m) > UP + 8.f);
     if (pending || high) {
       rescale();
       if (high) {
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float with = kv_scale_of(top, a.scale2), raised = fmaxf(m, top * with);
+        const float with = kv_scale_of(top, a.scale2), raised = fmaxf(m, fmaf(top, with, -UP));
         scale2 = raised > m ? with : scale2;
         factor = __builtin_amdgcn_exp2f(m - raised);
         m = raised;
