@@ -109,38 +109,42 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) 
   // piece, whose sums are not stored.
   constexpr int PIECES = ROW / 16, PER = THREADS / PIECES, TURNS = PER % 16 ? 2 : 1;
   const int of_key = thread / PIECES, place = thread % PIECES;
-  int k_piece[TURNS];  // (of even and odd loads, where a thread's keys do not have one exchange)
+  static_assert(TURNS == 1 || PER % 16 == 8, "a thread's keys have one exchange of pieces, or two in turn");
+  const int k_piece = place ^ (ROW == 128 ? of_key / 2 % 8 : of_key % 16);  // (of odd loads with two turns: k_piece ^ 8)
   unsigned long long k_lanes[TURNS];
 #pragma unroll
-  for (int t = 0; t < TURNS; ++t) {
-    k_piece[t] = place ^ (ROW == 128 ? (of_key + t * PER) / 2 % 8 : (of_key + t * PER) % 16);
-    k_lanes[t] = __ballot(k_piece[t] * 8 < a.dim);
-  }
-  static_assert(PER % 8 == 0, "a thread's keys have one exchange of pieces, or two in turn");
-  const int v_swizzled = place ^ (ROW == 128 ? of_key / 2 % 2 : of_key % 4) * 4, v_piece = v_swizzled * 8 < a.dim ? v_swizzled : 0;
+  for (int t = 0; t < TURNS; ++t) k_lanes[t] = __ballot((k_piece ^ t * 8) * 8 < a.dim);
+  const int v_swizzled = place ^ (ROW == 128 ? of_key / 2 % 2 : of_key % 4) * 4;
+  unsigned pieces = k_piece * 16 | (v_swizzled * 8 < a.dim ? v_swizzled : 0) << 20;  // (bytes of both in one register, which is short of others' in the loops)
   const char* k_from = static_cast<const char*>(a.k.data) + (tile.begin * a.k.ld_token + head * a.k.ld_head) * 2;
   const char* v_from = static_cast<const char*>(a.v.data) + (tile.begin * a.v.ld_token + head * a.v.ld_head) * 2;
   const int k_step = (int)(a.k.ld_token * 2), v_step = (int)(a.v.ld_token * 2);
   const unsigned lds_at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave % (WAVES / SPLIT) * 1024;
-  auto fetch = [&](const char* from, int step, int first, auto load) {
+  auto fetch = [&](const char* from, int step, int first, auto load) {  // (steps below 2^24)
     const int last = min(kTileKeys, tokens - first) - 1;
+    int key = of_key;
+    if constexpr (DP <= 128) asm volatile("" : "+v"(key), "+v"(pieces));  // (else what follows from them is held in registers across the loops)
     from += (int64_t)(SPLIT > 1 ? first * SPLIT + part * kTileKeys : first) * step;
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) load(reinterpret_cast<const int8_t*>(from), min(of_key + i * PER, last) * step, i);
+    for (int i = 0; i < LOADS; ++i) {
+      const int at = min(key + i * PER, last);
+      // (of more dims a piece of q was spilled in FP16 with the one product or the other line, which every step then waited for: 4096 tokens of 16 heads of 256 213 us, 190 so)
+      load(reinterpret_cast<const int8_t*>(from), DP <= 128 ? __umul24(at, step) : (unsigned)(at * step), i);
+    }
   };
   auto fetch_keys = [&](int number) {
-    fetch(k_from, k_step, number * kTileKeys, [&](const int8_t* from, int at, int i) {
-      load_to_lds_16(from, (unsigned)(at + k_piece[i % TURNS] * 16), lds_at + number % 2 * TILE + i * THREADS * 16, k_lanes[i % TURNS]);
+    fetch(k_from, k_step, number * kTileKeys, [&](const int8_t* from, unsigned at, int i) {
+      load_to_lds_16(from, at + ((pieces & 0xffff) ^ i % TURNS * 128), lds_at + number % 2 * TILE + i * THREADS * 16, k_lanes[i % TURNS]);
     });
   };
   auto fetch_values = [&](int number) {
-    fetch(v_from, v_step, number * kTileKeys, [&](const int8_t* from, int at, int i) {
-      load_to_lds_16(from, (unsigned)(at + v_piece * 16), lds_at + (2 + number % 2) * TILE + i * THREADS * 16);
+    fetch(v_from, v_step, number * kTileKeys, [&](const int8_t* from, unsigned at, int i) {
+      load_to_lds_16(from, at + (pieces >> 16), lds_at + (2 + number % 2) * TILE + i * THREADS * 16);
     });
   };
 #pragma unroll
   for (int t = 0; t < TURNS; ++t)
-    if (k_piece[t] * 8 >= a.dim)
+    if ((k_piece ^ t * 8) * 8 >= a.dim)
 #pragma unroll
       for (int i = t; i < 2 * LOADS; i += TURNS) *reinterpret_cast<w4_u4*>(lds + (i * THREADS + thread) * 16) = w4_u4{0, 0, 0, 0};
   static_assert(LOADS % TURNS == 0, "both tiles of keys have the same turns");
