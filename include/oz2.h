@@ -530,7 +530,7 @@ int oz2_kv4_append(const oz2_kv4_cache* cache, const oz2_kv4_sequences* on, cons
 /* out := attention of the new tokens q (tokens x heads x dim) over their sequences' places: new token j of n sees the places before lengths - n + j + 1.
  * The keys and values are what the cache stands for, unrounded; p s is rounded to two bf16 terms (three for FP32 results) before it meets the codes.
  * Elements of q from 2^63 on count as infinities.
- * weights, if there: weights[s, kv head, t] += sum of p over the new tokens and the query heads of that kv head.
+ * weights, if there: weights[s, kv head, t] += sum of p over the new tokens that see the place and the query heads of that kv head.
  * Meant for few new tokens a sequence: the cache is read once for every sixteen pairs of new token and query head of a kv head.  out shares no byte with q.
  * Workspace (256-byte aligned): oz2_kv4_attention_workspace_bytes, 0 for what is not valid. */
 size_t oz2_kv4_attention_workspace_bytes(const oz2_kv4_cache* cache, int64_t sequences, int64_t max_pages, int64_t tokens, int64_t heads, int weights);

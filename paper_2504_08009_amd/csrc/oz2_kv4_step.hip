@@ -61,8 +61,11 @@ __device__ __forceinline__ void join(const Finish& f, Joining& sh) {
   for (int j = 0; j < 4; ++j) w4_store(a.out.type, a.out.data, at * a.out.ld_token + query * a.out.ld_head + d + j, total == 0.f ? 0.f : v[j] / total);
 }
 
-// What each place received, from the scores and the maxima and sums of its rows, 64 rows at a time and four threads to the chunks of one.
-struct Receiving { float top[64], scale2[64], inverse[64]; const float* scores[64]; };
+// What each place received, from the scores and the maxima and sums of its rows, 64 rows at a time and four threads to the chunks of one.  Places that a row does not
+// see are passed over, and those on pages that are none altogether: a weight of 0 would be a NaN of a row that is one.
+struct Receiving {
+  struct alignas(16) Row { float top, scale2, inverse; int sees; const float* scores; } rows[64];
+};
 __device__ __forceinline__ void receive(const Finish& f, Receiving& sh) {
   const Kv4Step& a = f.a;
   const unsigned i = blockIdx.x - f.joins, pairs = (unsigned)(a.on.sequences * a.c.heads), turn = i / f.per_pair, pair = i - turn * pairs;
@@ -70,12 +73,14 @@ __device__ __forceinline__ void receive(const Finish& f, Receiving& sh) {
   const int held = kv_held(a.on.lengths, s, a.capacity), chunks = (held + a.chunk - 1) / a.chunk;
   if ((int64_t)turn * 256 >= held) return;
   const KvRange r = kv_range(a.on.cu, s, a.on.tokens);
-  const int rows = (int)(r.end - r.begin) * a.group;
+  const int news = (int)(r.end - r.begin), rows = news * a.group;
   if (!rows) return;
+  const int32_t* table = a.on.table + s * a.on.ld_table;
   float* to = a.on.weights + s * a.on.weights_sequence + head * a.on.weights_head;
   for (int64_t first = (int64_t)turn * 256; first < held; first += (int64_t)f.turns * 256) {
-    const int place = (int)first + thread;
+    const int place = (int)first + thread, page = place < held ? table[place / a.per_page] : -1;
     const float had = place < held ? to[place] : 0.f;
+    const bool there = page >= 0 && page < a.c.pages;
     float sum = 0.f;
     for (int r0 = 0; r0 < rows; r0 += 64) {
       const int n = min(64, rows - r0), own = r0 + min(thread / 4, n - 1), fresh = own / a.per_group;
@@ -98,18 +103,19 @@ __device__ __forceinline__ void receive(const Finish& f, Receiving& sh) {
       }
       __syncthreads();
       if (thread % 4 == 0 && thread / 4 < n) {
-        sh.top[thread / 4] = high;
-        sh.scale2[thread / 4] = fabsf(high) > kLarge ? kv_power_above(a.scale2) : a.scale2;
-        sh.inverse[thread / 4] = total == 0.f ? 0.f : 1.f / total;
-        sh.scores[thread / 4] = a.scores + row * a.capacity;
+        sh.rows[thread / 4] = {high, fabsf(high) > kLarge ? kv_power_above(a.scale2) : a.scale2, total == 0.f ? 0.f : 1.f / total, held - news + fresh + 1, a.scores + row * a.capacity};
       }
       __syncthreads();
-      if (place < held) {
+      if (there) {
 #pragma unroll 4
-        for (int j = 0; j < n; ++j) sum = fmaf(__builtin_amdgcn_exp2f(fmaf(sh.scores[j][place], sh.scale2[j], -sh.top[j])), sh.inverse[j], sum);
+        for (int j = 0; j < n; ++j) {
+          const Receiving::Row& x = sh.rows[j];
+          const float more = fmaf(__builtin_amdgcn_exp2f(fmaf(x.scores[place], x.scale2, -x.top)), x.inverse, sum);
+          sum = place < x.sees ? more : sum;
+        }
       }
     }
-    if (place < held) to[place] = had + sum;
+    if (there) to[place] = had + sum;
   }
 }
 
