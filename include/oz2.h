@@ -470,7 +470,7 @@ int oz2_context_w4_moe(oz2_context* ctx, const oz2_moe_layer* layer, int64_t t, 
  * -infinity, is 0; a NaN or +infinity among the scores that it sees makes it NaN.  What a row does not see never reaches it, whatever it holds.  Equal calls give equal bits.
  * Scores are taken to base 2: scale log2(e) q k beyond 2^126 in size counts as infinite, and beyond 2^25, where FP32 numbers are 4 apart, differences of scores may count up
  * to twice.
- * scale: finite and above 0.  A result lies behind or before its inputs, or between what they have of two tokens or two heads (parts of one packed tensor): other
+ * scale: above 0, up to 2^126, on a cache up to 2^55.  A result lies behind or before its inputs, or between what they have of two tokens or two heads (parts of one packed tensor): other
  * arrangements are refused, also where they share no byte.  tokens heads <= 2^28, 2^23 (new tokens) on a cache; sequences <= 2^20, 65535 on a cache. */
 typedef struct oz2_rows {
   void* data;

@@ -1,5 +1,4 @@
 // C ABI of liboz2 (see include/oz2.h): argument checks, workspace bookkeeping, stage sequencing.
-#include <cmath>
 #include <mutex>
 #include <new>
 
@@ -1011,7 +1010,8 @@ bool sequences_ok(const oz2_kv4_cache& c, const oz2_kv4_sequences* on, bool fres
   return (!on->positions || places_ok(c, *on, on->positions_sequence, on->positions_head)) &&
          (!on->weights || places_ok(c, *on, on->weights_sequence, on->weights_head));
 }
-bool scale_ok(float scale) { return scale > 0.f && std::isfinite(scale); }
+// (most: kernels take it times log2(e), on a cache times 2^69 too, and the power of two above that, or its reciprocal)
+bool scale_ok(float scale, float most) { return scale > 0.f && scale <= most; }
 }  // namespace
 
 int oz2_attention(int64_t tokens, int64_t sequences, const int32_t* cu, int64_t heads, int64_t kv_heads, int64_t dim, float scale, int causal,
@@ -1022,7 +1022,7 @@ int oz2_attention(int64_t tokens, int64_t sequences, const int32_t* cu, int64_t 
   if (kv_heads < 1 || heads % kv_heads) return -5;
   if (sequences * kv_heads > ((int64_t)1 << 22)) return -2;
   if (dim < 1 || dim > OZ2_ATTENTION_MAX_DIM) return -6;
-  if (!scale_ok(scale)) return -7;
+  if (!scale_ok(scale, 0x1p126f)) return -7;
   if (!rows_ok(q, tokens, heads, dim)) return -9;
   if (!rows_ok(k, tokens, kv_heads, dim) || k->type != q->type) return -10;
   if (!rows_ok(v, tokens, kv_heads, dim) || v->type != q->type) return -11;
@@ -1063,7 +1063,7 @@ int oz2_kv4_attention(const oz2_kv4_cache* cache, const oz2_kv4_sequences* on, i
   if (!sequences_ok(*cache, on, true)) return -2;
   const int64_t tokens = on->tokens;
   if (heads < 1 || heads % cache->heads || tokens > kMostRows / heads) return -3;
-  if (!scale_ok(scale)) return -4;
+  if (!scale_ok(scale, 0x1p55f)) return -4;
   if (!rows_ok(q, tokens, heads, cache->dim)) return -5;
   if (!rows_ok(out, tokens, heads, cache->dim)) return -6;
   if (tokens == 0 || on->sequences == 0) return OZ2_OK;

@@ -134,3 +134,23 @@ def test_large_scores_over_a_cache(n, dim, name):
                 assert (off <= (2.0 ** -16 + 64 * U) * size + HALF[name] * np.abs(v[best]).max()).all(), (power, sign)
                 got = received[s, 0].double().cpu().numpy()
                 assert (np.abs(got[best] - 2 / len(best)) <= 64 * U).all() and not np.delete(got, best).any(), (power, sign)
+
+
+@pytest.mark.parametrize("name", TYPES)
+def test_scores_of_zero_at_the_largest_scales(name):
+    """a query of zeros weighs all keys alike"""
+    rng = np.random.default_rng(5)
+    held = Held(rng, [300], 1, 64, 16)
+    ctx = oz.Context()
+    ctx.allocate_kv4_workspace(held.cache, held.gpu_table, tokens=1, heads=2, weights=True)
+    q, received = torch.zeros((1, 2, 64), dtype=TYPES[name], device="cuda"), torch.zeros(held.weights.shape, device="cuda")
+    out = ctx.kv4_attention(held.cache, q, ints([0, 1]), held.gpu_table, held.gpu_lengths, scale=2.0 ** 55, weights=received)
+    v, vs, vo, _ = held.row("v", 0, 0)
+    size = np.mean(15 * vs + np.abs(vo))
+    assert (np.abs(out[0].double().cpu().numpy() - v.mean(0)) <= (2.0 ** -16 + 400 * U) * size + HALF[name] * np.abs(v.mean(0))).all()
+    assert (np.abs(received[0, 0, :300].double().cpu().numpy() - 2 / 300) <= 400 * U * 2 / 300).all()
+    x = torch.from_numpy(rng.standard_normal((50, 1, 64))).to(TYPES[name])
+    got = oz.attention(torch.zeros_like(x).cuda(), x.cuda(), x.cuda(), ints([0, 50]), scale=2.0 ** 126, causal=False)
+    mean = x.double().numpy().mean(0)
+    size = np.abs(x.double().numpy()).mean(0)
+    assert (np.abs(got.double().cpu().numpy() - mean) <= 400 * U * size + HALF[name] * np.abs(mean)).all()
