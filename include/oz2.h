@@ -542,7 +542,8 @@ int oz2_context_kv4_attention(oz2_context* ctx, const oz2_kv4_cache* cache, cons
  * recent), and of the others those with the largest weights (a NaN counts as the largest; of equal ones the lower place), `keep` in all.  Those that stay and lie at
  * places from `keep` on move into the places below that were given up, the i-th of them into the i-th of these; nothing else moves, since attention asks for
  * no order.  on: positions and weights needed, cu and tokens not used; to: NULL (in place), or where lengths, positions and weights afterwards go, of the same
- * shapes (each may be the one of `on`, and shares no byte with it else); `to` is written below the new lengths alone.  0 <= recent <= keep.  Heads choose for themselves, so a place then
+ * shapes (each may be the one of `on`; other arrangements than behind one another, or with equal strides between one another's sequences or heads, are refused, also where
+ * they share no byte); `to` is written below the new lengths alone.  0 <= recent <= keep.  Heads choose for themselves, so a place then
  * holds different tokens for different heads.  Pages that two sequences share must not be evicted in. */
 typedef struct oz2_kv4_kept {
   int32_t* lengths;

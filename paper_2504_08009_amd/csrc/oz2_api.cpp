@@ -1010,6 +1010,53 @@ bool sequences_ok(const oz2_kv4_cache& c, const oz2_kv4_sequences* on, bool fres
   return (!on->positions || places_ok(c, *on, on->positions_sequence, on->positions_head)) &&
          (!on->weights || places_ok(c, *on, on->weights_sequence, on->weights_head));
 }
+bool apart(const void* p, int64_t bytes_p, const void* q, int64_t bytes_q) {
+  return (uintptr_t)p + bytes_p <= (uintptr_t)q || (uintptr_t)q + bytes_q <= (uintptr_t)p;
+}
+// Arrays of (sequence, head, place) of 4 bytes, and whether two of them have no byte in common, as far as that is easily seen: one lies behind the other, or with the same
+// strides what one has of a sequence or a head lies between what the other has of two.
+struct Places { const void* data; int64_t sequence, head; };
+int64_t places_bytes(const Places& a, int64_t sequences, int64_t heads, int64_t capacity) {
+  return 4 * ((sequences > 1 ? (sequences - 1) * a.sequence : 0) + (heads > 1 ? (heads - 1) * a.head : 0) + capacity);
+}
+bool places_apart(const Places& a, const Places& b, int64_t sequences, int64_t heads, int64_t capacity) {
+  const int64_t bytes = places_bytes(a, sequences, heads, capacity);
+  if (apart(a.data, bytes, b.data, places_bytes(b, sequences, heads, capacity))) return true;
+  if ((sequences > 1 && a.sequence != b.sequence) || (heads > 1 && a.head != b.head)) return false;
+  // rows of `width` at `inner` steps, which repeat at `outer` ones (0: there is but one)
+  const int64_t s = sequences > 1 ? 4 * a.sequence : 0, h = heads > 1 ? 4 * a.head : 0, inner = s && h ? (s < h ? s : h) : s + h, outer = s && h ? (s < h ? h : s) : 0;
+  const int64_t width = 4 * capacity, by = (int64_t)((uintptr_t)b.data - (uintptr_t)a.data);
+  auto between = [](int64_t by, int64_t step, int64_t width) {
+    const int64_t from = (by % step + step) % step;
+    return from >= width && from + width <= step;
+  };
+  if (!inner) return false;
+  if (!outer) return between(by, inner, width);
+  if (between(by, outer, bytes - (outer == s ? (sequences - 1) * s : (heads - 1) * h))) return true;
+  const int64_t from = (by % outer + outer) % outer;
+  return between(from, inner, width) && between(from - outer, inner, width);
+}
+// Whether what an eviction writes is in each case the array that it reads the same of, or apart from all others.
+bool kept_ok(const oz2_kv4_cache& c, const oz2_kv4_sequences& on, const oz2_kv4_kept& to) {
+  const int64_t n = on.sequences, capacity = on.max_pages * c.page_size;
+  const Places read[2] = {{on.positions, on.positions_sequence, on.positions_head}, {on.weights, on.weights_sequence, on.weights_head}};
+  const Places write[2] = {{to.positions, to.positions_sequence, to.positions_head}, {to.weights, to.weights_sequence, to.weights_head}};
+  if (to.lengths != on.lengths && !apart(to.lengths, 4 * n, on.lengths, 4 * n)) return false;
+  if (!capacity) return true;
+  const int64_t ld = on.ld_table < ((int64_t)1 << 40) ? on.ld_table : (int64_t)1 << 40, table = 4 * ((n > 1 ? (n - 1) * ld : 0) + on.max_pages);  // (no memory is larger)
+  if (!apart(to.lengths, 4 * n, on.table, table)) return false;
+  for (int i = 0; i < 2; ++i) {
+    const int64_t bytes = places_bytes(write[i], n, c.heads, capacity);
+    if (!apart(write[i].data, bytes, to.lengths, 4 * n) || !apart(write[i].data, bytes, on.lengths, 4 * n) || !apart(write[i].data, bytes, on.table, table)) return false;
+    if (to.lengths != on.lengths && !apart(to.lengths, 4 * n, read[i].data, places_bytes(read[i], n, c.heads, capacity))) return false;
+    for (int j = 0; j < 2; ++j) {
+      // (the same array with other strides would be read and written at once)
+      const bool same = i == j && write[i].data == read[j].data && (n <= 1 || write[i].sequence == read[j].sequence) && (c.heads <= 1 || write[i].head == read[j].head);
+      if (!same && !places_apart(write[i], read[j], n, c.heads, capacity)) return false;
+    }
+  }
+  return places_apart(write[0], write[1], n, c.heads, capacity);
+}
 // (most: kernels take it times log2(e), on a cache times 2^69 too, and the power of two above that, or its reciprocal)
 bool scale_ok(float scale, float most) { return scale > 0.f && scale <= most; }
 }  // namespace
@@ -1095,9 +1142,7 @@ int oz2_kv4_evict(const oz2_kv4_cache* cache, const oz2_kv4_sequences* on, int64
   if (to) {
     if (on->sequences && (!to->lengths || !to->positions || !to->weights)) return -5;
     if (!places_ok(*cache, *on, to->positions_sequence, to->positions_head) || !places_ok(*cache, *on, to->weights_sequence, to->weights_head)) return -5;
-    // the same array with other strides would be read and written at once
-    if (to->positions == on->positions && (to->positions_sequence != on->positions_sequence || to->positions_head != on->positions_head)) return -5;
-    if (to->weights == on->weights && (to->weights_sequence != on->weights_sequence || to->weights_head != on->weights_head)) return -5;
+    if (on->sequences && !kept_ok(*cache, *on, *to)) return -5;
     here = *to;
   }
   if (on->sequences == 0) return OZ2_OK;
