@@ -578,6 +578,18 @@ def _refuse_gradient():
         raise Oz2Error("a tensor requires a gradient, which these products do not form: call them under torch.no_grad(), or with detached tensors")
 
 
+_forward = None
+
+
+def _refuse_tangents(*tensors):
+    """Tensors with a tangent require no gradient, and their tangents would be lost.  There are none but inside a level of forward-mode differentiation."""
+    global _forward
+    if _forward is None:
+        import torch.autograd.forward_ad as _forward
+    if getattr(_forward, "_current_level", 0) >= 0 and any(v is not None and _forward.unpack_dual(v).tangent is not None for v in tensors):
+        raise Oz2Error("a tensor has a tangent, which these products do not form: call them with the primal of it")
+
+
 _raw_stream = _current_device = None
 
 
@@ -609,9 +621,11 @@ def _new(x, shape, dtype, stream):
 
 def w4_matvec(W, x, alpha=1.0, beta=0.0, c=None, out=None, stream=None):
     """alpha W x + beta c for every row of x (tokens, k), as (tokens, n) in the type of `out`, or of x where it is None; c is like the result.
-    A result that is made here belongs to the stream of the call.  There is no gradient: tensors that require one are refused where one would be recorded."""
+    A result that is made here belongs to the stream of the call.  There is no gradient: tensors that require one are refused where one would be recorded, and those with a
+    tangent everywhere."""
     if x.requires_grad or W.scales.requires_grad or (c is not None and c.requires_grad) or (out is not None and out.requires_grad):
         _refuse_gradient()
+    _refuse_tangents(x, W.scales, c, out)
     if out is None:
         out = _new(x, (x.shape[0], W.n), x.dtype, stream)
     index = x.get_device()
@@ -664,6 +678,7 @@ def _w4_moe(call, name, first, layer, x, active, out, ids, weights, stream):
     t, index = x.shape[0], x.get_device()
     if any(v is not None and v.requires_grad for v in (x, out, weights, *layer.with_gradient)):
         _refuse_gradient()
+    _refuse_tangents(x, out, weights, *layer.with_gradient)
     if out is None:
         out = _new(x, (t, layer.d), x.dtype, stream)
     if ids is None:
@@ -740,13 +755,14 @@ def _refuse_gradients(*tensors):
     for v in tensors:
         if v is not None and v.requires_grad:
             _refuse_gradient()
+    _refuse_tangents(*tensors)
 
 
 def attention(q, k, v, cu, causal=True, scale=None, out=None, stream=None):
     """softmax(scale q k) v over packed prompts (include/oz2.h): q (tokens, heads, dim), k and v (tokens, kv_heads, dim) of one type in float32, bfloat16 or float16, cu
     (sequences + 1) int32 with the first row of every sequence; scale 1 / sqrt(dim) if None.  The result is like `out`, or q where it is None, and belongs to
     the stream of the call; rows behind the last sequence are left as they were (where the result is made here, they are not set).  There is no gradient:
-    tensors that require one are refused where one would be recorded."""
+    tensors that require one are refused where one would be recorded, and those with a tangent everywhere."""
     _refuse_gradients(q, k, v, out)
     index, shape, of_kv = q.get_device(), q.shape, k.shape
     rows_q = _heads("q", q, index, shape)
