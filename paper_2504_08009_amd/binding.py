@@ -775,7 +775,7 @@ def attention(q, k, v, cu, causal=True, scale=None, out=None, stream=None):
     rows_out, of_cu = _heads("out", out, index, shape), cu.shape
     if len(of_cu) != 1 or not of_cu[0]:
         raise Oz2Error("cu is (sequences + 1,) int32")
-    rc = lib().oz2_attention(tokens, of_cu[0] - 1, _integers("cu", cu, index, of_cu), heads, of_kv[1], dim, dim ** -0.5 if scale is None else scale,
+    rc = lib().oz2_attention(tokens, of_cu[0] - 1, _integers("cu", cu, index, of_cu), heads, of_kv[1], dim, max(dim, 1) ** -0.5 if scale is None else scale,
                              bool(causal), rows_q, rows_k, rows_v, rows_out, _stream_on(stream, index))
     if rc:
         _check(rc, "oz2_attention")
