@@ -851,7 +851,7 @@ def kv4_append(cache, k, v, cu, table, lengths, at=None, positions=None, weights
     int32, lengths (sequences) int32 with the new tokens counted.  at (tokens) int32: positions of the new tokens, stored in positions (sequences, kv_heads,
     places) int32; weights, of that shape in float32: set to 0 in the new places; held: (k, v) like the arguments, for what the cache then holds of them."""
     held_k, held_v = _none if held is None else held
-    _refuse_gradients(k, v, weights, held_k, held_v)
+    _refuse_gradients(k, v, weights, held_k, held_v, cache.k_scales, cache.v_scales)
     index, shape = cache.index, k.shape
     if len(shape) != 3 or shape[1] != cache.heads or shape[2] != cache.dim:
         raise Oz2Error("k and v are (tokens, kv_heads, dim) = (., %d, %d), got shape %s" % (cache.heads, cache.dim, tuple(shape)))
@@ -870,7 +870,7 @@ _none = (None, None)
 
 
 def _kv4_attention(call, name, first, cache, q, cu, table, lengths, scale, weights, out, stream):
-    _refuse_gradients(q, weights, out)
+    _refuse_gradients(q, weights, out, cache.k_scales, cache.v_scales)
     index, shape = cache.index, q.shape
     if len(shape) != 3 or shape[2] != cache.dim:
         raise Oz2Error("q is (tokens, heads, dim) = (., ., %d), got shape %s" % (cache.dim, tuple(shape)))
@@ -898,7 +898,7 @@ def kv4_attention_workspace_bytes(cache, table, tokens, heads, weights=False):
 
 
 def _kv4_evict(call, name, first, cache, table, lengths, positions, weights, keep, recent, out, stream):
-    _refuse_gradients(weights, *(out or ()))
+    _refuse_gradients(weights, cache.k_scales, cache.v_scales, *(out or ()))
     if positions is None or weights is None:
         raise Oz2Error("positions and weights are needed")
     on = _sequences(cache, table, lengths, 0, None, positions, weights)
