@@ -192,6 +192,12 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) 
 #pragma unroll
     for (int i = 0; i < 2 * F; ++i) add_with(p, at, i / F, i % F);
   };
+  // what lanes of a wave have written is there for its others, and what they have read may be written over
+  auto exchanged = [&]() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
   // The same with values that are not finite, for rows that do not see all of them: key by key.
   auto add_seen = [&](const w4_u4 (&p)[2], int at, int place) {
     unsigned(&w)[8][32] = weights[wave];
@@ -199,6 +205,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) 
     for (int b = 0; b < 2; ++b) {
 #pragma unroll
       for (int i = 0; i < 8; i += 2) w[i / 4 * 4 + i % 4 / 2 + 2 * half][col] = p[b][i / 2];
+      exchanged();
       for (int key = 0; key < 16; ++key) {
         const float x = at_value<XT>(w[key / 2][col], key % 2);
         const bool seen = place + 16 * b + key < sees;
@@ -214,6 +221,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) 
             }
           }
       }
+      exchanged();
     }
   };
 
@@ -380,9 +388,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) 
         else w = at_u2{at_pair<OZ2_F16>(r[0], r[1]), at_pair<OZ2_F16>(r[2], r[3])};
         *reinterpret_cast<at_u2*>(to + place_of(col, 4 * f + i) + half * 8) = w;
       }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    exchanged();
     constexpr int EACH = 64 / PIECES;  // rows of a store
     const int piece = lane % PIECES;
 #pragma unroll
