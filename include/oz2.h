@@ -519,8 +519,8 @@ typedef struct oz2_kv4_sequences {
 } oz2_kv4_sequences;
 
 /* Appends the new tokens k, v (tokens x kv heads x dim, both of one type) to their places: o = the smallest value, s = (largest - smallest) / 15, both rounded
- * to FP16, c = (x - o) (1 / s) in FP32 rounded to the nearest integer (ties to even) within 0 .. 15, 0 where s is 0.  A key or value with a NaN, an
- * infinity, or values beyond FP16 is held as one whose values are not finite.
+ * to FP16, c = (x - o) (1 / s) in FP32 rounded to the nearest integer (ties to even) within 0 .. 15, 0 where s is 0.  A key or value with a NaN or an
+ * infinity, or whose s or o is beyond FP16, is held as one whose values are not finite.
  * Two new tokens must not have one place (a page that two sequences share).
  * at: NULL, or the position of every new token, stored for all heads (needs positions); weights, if there, are 0 in the new places.  held_k, held_v: NULL, or
  * where to write what the cache now holds of k and v, rounded to their type (k and v themselves are allowed); of a token without a place too. */
@@ -528,8 +528,8 @@ int oz2_kv4_append(const oz2_kv4_cache* cache, const oz2_kv4_sequences* on, cons
                    const oz2_rows* held_v, void* stream);
 
 /* out := attention of the new tokens q (tokens x heads x dim) over their sequences' places: new token j of n sees the places before lengths - n + j + 1.
- * The keys and values are what the cache stands for, unrounded; p s is rounded to two bf16 terms (three for FP32 results) before it meets the codes.
- * Elements of q from 2^63 on count as infinities.
+ * The keys and values are what the cache stands for, unrounded; p s is rounded to two bf16 terms (three for FP32 queries) before it meets the codes.
+ * Elements of q from 2^63 on count as infinities, and a row with an infinity may be NaN where its scores, formed at once, would be -infinity.
  * weights, if there: weights[s, kv head, t] += sum of p over the new tokens that see the place and the query heads of that kv head.
  * Meant for few new tokens a sequence: the cache is read once for every sixteen pairs of new token and query head of a kv head.  out shares no byte with q.
  * Workspace (256-byte aligned): oz2_kv4_attention_workspace_bytes, 0 for what is not valid. */
