@@ -80,7 +80,6 @@ __device__ __forceinline__ void receive(const Finish& f, Receiving& sh) {
   for (int64_t first = (int64_t)turn * 256; first < held; first += (int64_t)f.turns * 256) {
     const int place = (int)first + thread, page = place < held ? table[place / a.per_page] : -1;
     const float had = place < held ? to[place] : 0.f;
-    const bool there = page >= 0 && page < a.c.pages;
     float sum = 0.f;
     for (int r0 = 0; r0 < rows; r0 += 64) {
       const int n = min(64, rows - r0), own = r0 + min(thread / 4, n - 1), fresh = own / a.per_group;
@@ -106,7 +105,7 @@ __device__ __forceinline__ void receive(const Finish& f, Receiving& sh) {
         sh.rows[thread / 4] = {high, fabsf(high) > kLarge ? kv_power_above(a.scale2) : a.scale2, total == 0.f ? 0.f : 1.f / total, held - news + fresh + 1, a.scores + row * a.capacity};
       }
       __syncthreads();
-      if (there) {
+      if (place < held) {  // (without a look at the page, so that scores do not wait for it)
 #pragma unroll 4
         for (int j = 0; j < n; ++j) {
           const Receiving::Row& x = sh.rows[j];
@@ -115,7 +114,7 @@ __device__ __forceinline__ void receive(const Finish& f, Receiving& sh) {
         }
       }
     }
-    if (there) to[place] = had + sum;
+    if (page >= 0 && page < a.c.pages) to[place] = had + sum;
   }
 }
 
