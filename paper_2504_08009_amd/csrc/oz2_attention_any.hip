@@ -3,9 +3,9 @@
 // A workgroup has 32 rows; its four waves take tiles of 32 keys in turn, each with sums and a maximum of its own, which come together at the end.  Products are
 // keys x rows and dims x rows on the FP32 matrix cores (32 x 32 x 2), so that a lane has one row throughout, and what it holds of the first product is what the
 // second one wants of it: places 8 (i / 4) + i % 4 and, in the upper half of the lanes, four further on.  Keys and values are read by the lanes that need
-// them, from the caches, a few products ahead: so two waves fit a SIMD with 128 dims, three with 64.  m follows the maximum only where a score is more than 2^8 above it.
-//   The matrix cores bound it where it is long: 4096 tokens of 16 query and 4 kv heads in FP32, causal, take 655 us with 128 dims (105 TFLOP/s; a large matrix product
-// reaches 153), 405 with 64 (85; exponentials are more of it), 2050 with 256 (67; one wave a SIMD).  Few rows are bound by the tiles' number: a compute unit that
+// them, from the caches, a few products ahead: so two waves fit a SIMD with 128 dims, three with 64.  m follows the maximum only where a score is more than 8 above it (to base 2).
+//   The matrix cores bound it where it is long: 4096 tokens of 16 query and 4 kv heads in FP32, causal, take 648 us with 128 dims (106 TFLOP/s; a large matrix product
+// reaches 153), 343 with 64 (100; exponentials are more of it), 2010 with 256 (68; one wave a SIMD).  Few rows are bound by the tiles' number: a compute unit that
 // gets two where others have one takes twice as long.
 #include "oz2_attention.h"
 

@@ -11,7 +11,7 @@
 // made of one bf16 (bf16), two (f16) or three (f32) exactly, p s of two bf16, or three for FP32 results: an error of 2^-16 or 2^-24 of it.
 // The products are keys x rows and then dims x rows, so that every lane has one row throughout: what the first product leaves in a lane (four places of each
 // half of the tile) is what it needs as its part of the second's operand, and maxima and sums stay in lanes until the end.  m is raised only
-// where a score is more than 2^8 above it.
+// where a score is more than 8 above it (to base 2).
 // Nothing goes through LDS but the four waves' results.  A lane reads of keys the codes of one place (a quarter of the row), of values those of eight places
 // (a sixteenth of each row): a tile's words are in registers before the previous tile is done with.
 //   Bound by the bytes of the cache where sequences are long: 64 of 2048 to 32768 places, 8 kv heads of 128, BF16, are read at 4.8 TB/s (163 to 180 us, where a copy

@@ -127,7 +127,8 @@ __global__ void __launch_bounds__(256) kv4_finish_kernel(Finish f) {
 
 // About a thousand workgroups where there are places enough for them, two rounds of the card; up to 4096 places each, since the begin of a workgroup (some 4 us until
 // its first tile is there) is to be spread over enough of them, and no more, since lengths differ.
-// us with 256 / 1024 / 4096 places: 64 sequences of 2048 to 32768 360 / 213 / 183, 16 of 2000 to 8192 47 / 36 / 46, one of 4096 (8 kv heads) 8 / 14 / 36.
+// us a call with 256 / 1024 / 4096 places (BF16, 8 kv heads of 128): 64 sequences of 2048 to 32768 283 / 188 / 174, 16 of 2000 to 8192 40 / 27 / 40, one of 4096
+// 12.3 / 16.7 / 35.7.  What counts is the table's width, which the host knows, not what is held: on one of 131072 places the last two take 39 and 16.9 us instead of 27 and 11.9.
 int64_t chunk_of(int64_t capacity, int64_t pairs) {
   const int64_t each = (capacity * pairs + 1023) / 1024;
   const int64_t chunk = (each + 127) / 128 * 128;
@@ -164,7 +165,7 @@ hipError_t oz2_launch_kv4_attention(const oz2_kv4_cache& cache, const oz2_kv4_se
   a.scores = n.scores ? reinterpret_cast<float*>(ws + n.part + n.stats) : nullptr;
   a.rows = rows;
   // Chunks last: eight dies take workgroups in turn, and with chunks first one of them would get all first chunks, which every sequence has, and another the
-  // eighth, which few have (64 sequences of 2048 to 32768 places, 8 kv heads: 355 us so, 150 with chunks last).
+  // eighth, which few have (64 sequences of 2048 to 32768 places, 8 kv heads: 292 us a call so, 174 with chunks last, 6 of either to join the parts).
   const dim3 grid((unsigned)cache.heads, (unsigned)on.sequences, (unsigned)chunks);
   hipError_t rc = q.type == OZ2_F32    ? oz2_kv4_step_of<OZ2_F32>(a, grid, st)
                   : q.type == OZ2_BF16 ? oz2_kv4_step_of<OZ2_BF16>(a, grid, st)

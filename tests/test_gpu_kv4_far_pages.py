@@ -1,7 +1,7 @@
 """Caches whose pages begin behind 2^32 bytes: results that show which page was read.
 
 Every token has a direction of its own as key, and queries point at some of them so that each has nearly all weight: then the result is that token's value, in which every
-element is its own.  Tolerances: test_kv4_error_bounds derives an error below 2^-17 of sum p s c, with FP32 queries less; 2^-12 of the values' size is far above that,
+element is its own.  Tolerances: errors of a result are below 2^-16 of sum p s c, with FP32 queries less (test_kv4_error_bounds); 2^-12 of the values' size is far above that,
 and far below what another token's value differs by."""
 import numpy as np
 import pytest

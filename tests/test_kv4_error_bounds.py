@@ -2,7 +2,8 @@
 
 Scores are s sum q c + o sum q in FP32, or with c - 7.5 and o + 7.5 s for FP32 queries: sums of terms up to twice those of q (s c + o), of which the matrix cores cut off what
 FP32 does not hold instead of rounding it, twice the error of a plain evaluation again.  So errors are up to 4 times those of the formula in FP32 (root of mean squares over
-the elements of a call), and beside these p s is rounded to two bf16, with FP32 queries to three: by at most r = 2^-17 or 2^-25 of it, each place's by itself: r sqrt(sum (p s c)^2).
+the elements of a call), and beside these p s is rounded to two bf16, with FP32 queries to three: by at most 2^-16 or 2^-24 of it, which is below r = 2^-17 or 2^-25 in the root
+of mean squares, each place's by itself: r sqrt(sum (p s c)^2).
 Weights of places have the first part alone.  Queries are chosen that their last bf16 term counts: as large as it can be, with the sign of the value, and some keys
 have large codes where it is positive and small ones where not.  Or queries and keys are small whole numbers, whose scores are exact: what is left are the
 terms of p s."""
