@@ -52,6 +52,19 @@ __device__ __forceinline__ bool at_odd(unsigned w) {
   return (w & top) == top || (w & top << 16) == top << 16;
 }
 
+// load_to_lds_16 for the lanes of `lanes` alone; what others would have written is left as it was.
+__device__ __forceinline__ void at_load_of(const int8_t* base, unsigned voff, unsigned lds_addr, unsigned long long lanes) {
+  unsigned long long all;
+  asm volatile(
+      "s_mov_b32 m0, %3\n\t"
+      "s_and_saveexec_b64 %0, %4\n\t"
+      "global_load_lds_dwordx4 %1, %2\n\t"
+      "s_mov_b64 exec, %0"
+      : "=&s"(all)
+      : "v"(voff), "s"(base), "s"(lds_addr), "s"(lanes)
+      : "memory", "m0", "scc");
+}
+
 template <int XT, int DP, int WAVES, int SPLIT>
 __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) attention_tile_kernel(Attention a) {
   constexpr int E = DP / 16, F = DP / 32, ROW = DP <= 64 ? 128 : DP <= 128 ? 256 : 512;  // bytes of a row in LDS
@@ -134,7 +147,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) 
   };
   auto fetch_keys = [&](int number) {
     fetch(k_from, k_step, number * kTileKeys, [&](const int8_t* from, unsigned at, int i) {
-      load_to_lds_16(from, at + ((pieces & 0xffff) ^ i % TURNS * 128), lds_at + number % 2 * TILE + i * THREADS * 16, k_lanes[i % TURNS]);
+      at_load_of(from, at + ((pieces & 0xffff) ^ i % TURNS * 128), lds_at + number % 2 * TILE + i * THREADS * 16, k_lanes[i % TURNS]);
     });
   };
   auto fetch_values = [&](int number) {

@@ -19,20 +19,7 @@ __device__ __forceinline__ void load_to_lds_16(const int8_t* base, unsigned voff
       : "memory", "m0");
 }
 
-// The same for the lanes of `lanes` alone; what others would have written is left as it was.
-__device__ __forceinline__ void load_to_lds_16(const int8_t* base, unsigned voff, unsigned lds_addr, unsigned long long lanes) {
-  unsigned long long all;
-  asm volatile(
-      "s_mov_b32 m0, %3\n\t"
-      "s_and_saveexec_b64 %0, %4\n\t"
-      "global_load_lds_dwordx4 %1, %2\n\t"
-      "s_mov_b64 exec, %0"
-      : "=&s"(all)
-      : "v"(voff), "s"(base), "s"(lds_addr), "s"(lanes)
-      : "memory", "m0", "scc");
-}
-
-// The first in two steps, for several loads to one place: M0 once, then loads whose OFFSET counts for the source and for the target.
+// The same in two steps, for several loads to one place: M0 once, then loads whose OFFSET counts for the source and for the target.
 // Nothing else in the kernel may use M0 between them (build.py looks).
 __device__ __forceinline__ void set_lds_target(unsigned lds_addr) { asm volatile("s_mov_b32 m0, %0" : : "s"(lds_addr) : "m0"); }
 template <int OFFSET>
