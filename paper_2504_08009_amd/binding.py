@@ -562,7 +562,7 @@ class W4Matrix:
 def _rows(name, x, width):
     """leading dimension of a two-dimensional tensor with rows of that width, which are contiguous and do not overlap (an expanded one's do)"""
     shape, strides = x.shape, x.stride()  # (whole: each single one asked for costs as much)
-    if len(shape) != 2 or shape[1] != width or (width > 1 and strides[1] != 1):
+    if len(shape) != 2 or shape[1] != width or (width > 1 and strides[1] != 1 and shape[0]):  # (strides of no rows say nothing)
         raise Oz2Error("%s is two-dimensional with contiguous rows of %d, got shape %s" % (name, width, tuple(shape)))
     pitch = strides[0]
     if pitch >= width:
@@ -730,7 +730,7 @@ _pack_rows, _pack_sequences, _pack_kept = (struct.Struct(f).pack for f in ("Pqqi
 def _heads(name, x, index, shape):
     """(tokens, heads, dim) tensor of that shape on device `index`, its last dimension contiguous, as the library sees it"""
     strides = x.stride()
-    if x.shape != shape or len(strides) != 3 or (strides[2] != 1 and shape[2] > 1):
+    if x.shape != shape or len(strides) != 3 or (strides[2] != 1 and shape[2] > 1 and shape[0]):
         raise Oz2Error("%s is (tokens, heads, dim) = %s with the last dimension contiguous, got shape %s" % (name, tuple(shape), tuple(x.shape)))
     if x.get_device() != index or index < 0:
         raise Oz2Error("%s is on %s: tensors of one call are on one GPU" % (name, x.device))
@@ -738,7 +738,7 @@ def _heads(name, x, index, shape):
 
 
 def _integers(name, x, index, shape):
-    if x.dtype is not _int32() or x.shape != shape or (x.stride()[-1] != 1 and shape[-1] > 1):
+    if x.dtype is not _int32() or x.shape != shape or (x.stride()[-1] != 1 and shape[-1] > 1 and x.numel()):
         raise Oz2Error("%s is int32 of shape %s, its last dimension contiguous, got %s %s" % (name, tuple(shape), x.dtype, tuple(x.shape)))
     if x.get_device() != index:
         raise Oz2Error("%s is on %s: tensors of one call are on one GPU" % (name, x.device))
@@ -821,7 +821,7 @@ class KV4Cache:
 
 def _places(name, x, cache, sequences, capacity, dtype):
     shape, strides = x.shape, x.stride()
-    if x.dtype is not dtype or len(shape) != 3 or shape[0] != sequences or shape[1] != cache.heads or shape[2] < capacity or (strides[2] != 1 and shape[2] > 1):
+    if x.dtype is not dtype or len(shape) != 3 or shape[0] != sequences or shape[1] != cache.heads or shape[2] < capacity or (strides[2] != 1 and shape[2] > 1 and sequences):
         raise Oz2Error("%s is %s of shape (sequences, kv_heads, places) = (%d, %d, at least %d), its last dimension contiguous, got %s %s" % (
             name, dtype, sequences, cache.heads, capacity, x.dtype, tuple(shape)))
     if x.get_device() != cache.index:

@@ -957,7 +957,7 @@ bool lattice_ok(int64_t width, int64_t a, int64_t step_a, int64_t b, int64_t ste
   return step_a < step_b ? step_b - width >= (a - 1) * step_a : step_a - width >= (b - 1) * step_b;
 }
 bool rows_ok(const oz2_rows* r, int64_t tokens, int64_t heads, int64_t dim) {
-  return r && type_ok(r->type) && (tokens == 0 || r->data) && lattice_ok(dim, tokens, r->ld_token, heads, r->ld_head);
+  return r && type_ok(r->type) && (tokens == 0 || (r->data && lattice_ok(dim, tokens, r->ld_token, heads, r->ld_head)));  // (strides of no tokens say nothing)
 }
 // Whether two tensors of heads have no byte in common, as far as that is easily seen: one lies behind the other, or what one has of a token (or, where these are
 // further apart, of a head) lies between what the other has of two, like parts of one packed tensor.
@@ -1141,7 +1141,7 @@ int oz2_kv4_evict(const oz2_kv4_cache* cache, const oz2_kv4_sequences* on, int64
   oz2_kv4_kept here = {const_cast<int32_t*>(on->lengths), on->positions, on->positions_sequence, on->positions_head, on->weights, on->weights_sequence, on->weights_head};
   if (to) {
     if (on->sequences && (!to->lengths || !to->positions || !to->weights)) return -5;
-    if (!places_ok(*cache, *on, to->positions_sequence, to->positions_head) || !places_ok(*cache, *on, to->weights_sequence, to->weights_head)) return -5;
+    if (on->sequences && (!places_ok(*cache, *on, to->positions_sequence, to->positions_head) || !places_ok(*cache, *on, to->weights_sequence, to->weights_head))) return -5;
     if (on->sequences && !kept_ok(*cache, *on, *to)) return -5;
     here = *to;
   }
