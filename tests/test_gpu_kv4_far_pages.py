@@ -46,7 +46,7 @@ def test_values_of_far_pages():
             assert ((want - other).abs().amax(2) > 0.25).all() and (want.abs().amax(2) > 0.25).all()
 
     some = lambda n: torch.from_numpy(rng.integers(0, n, (2, 8))).cuda()
-    ends = [torch.tensor([[0, 1023, 1024, 2047, 2048, 3071, 3072, 3499], [0, 1023, 1024, 2047, 2048, 2049, 2099, 5]], device="cuda")]
+    ends = [torch.tensor([[0, 1023, 1024, 2047, 2048, 3 * PAGE - 1, 3 * PAGE, 3499], [0, 1023, 1024, 2047, 2048, 2049, 2099, 5]], device="cuda")]
     check(ends + [torch.stack((some(3500)[0], some(2100)[1])) for _ in range(4)])
 
     # weights that are known: every third place is worth little

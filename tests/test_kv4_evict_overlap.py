@@ -10,7 +10,8 @@ torch = pytest.importorskip("torch")
 import paper_2504_08009_amd as oz
 from test_attention_arguments import P, _Kept, cache, ref, sequences
 
-# sequences(): 3 of up to 4 pages of 32 places, 2 heads; arrays of (3, 2, 128) with strides 256 and 128: 3072 bytes, lengths 12, the table 48
+# sequences(): 3 of up to 4 pages of 32 places, 2 heads; arrays of (3, 2, 128) with strides 256 and 128: 768 elements, lengths 12 bytes, the table 48
+BYTES = 4 * 768
 LENGTHS, POSITIONS, WEIGHTS, TABLE = P << 3, P << 4, P << 5, P << 6
 FREE = dict(lengths=P << 7, positions=P << 8, positions_sequence=256, positions_head=128, weights=P << 9, weights_sequence=256, weights_head=128)
 
@@ -32,13 +33,13 @@ def test_apart_or_the_same():
     for n in (1, 2, 3):
         for names in itertools.combinations(same, n):
             assert evict({k: same[k] for k in names}) == 1
-    for name, size, on in (("lengths", 12, LENGTHS), ("positions", 3072, POSITIONS), ("weights", 3072, WEIGHTS)):
+    for name, size, on in (("lengths", 12, LENGTHS), ("positions", BYTES, POSITIONS), ("weights", BYTES, WEIGHTS)):
         for at in (on - size, on + size):
             assert evict({name: at}) == 1
 
 
-SIZES = dict(lengths=12, positions=3072, weights=3072)
-INPUTS = dict(lengths=(LENGTHS, 12), positions=(POSITIONS, 3072), weights=(WEIGHTS, 3072), table=(TABLE, 48))
+SIZES = dict(lengths=12, positions=BYTES, weights=BYTES)
+INPUTS = dict(lengths=(LENGTHS, 12), positions=(POSITIONS, BYTES), weights=(WEIGHTS, BYTES), table=(TABLE, 48))
 
 
 @pytest.mark.parametrize("to", SIZES)
@@ -65,7 +66,7 @@ def test_other_strides_over_the_same_array():
 
 def test_parts_of_one_packed_array():
     """(3, 2, 4, 128): old and new positions and weights, head by head; (3, 4, 2, 128): sequence by sequence; (4, 3, 2, 128): all of each behind all of another"""
-    for sequence, head, step in ((1024, 512, 512), (1024, 128, 1024), (256, 128, 3072)):
+    for sequence, head, step in ((1024, 512, 512), (1024, 128, 1024), (256, 128, BYTES)):
         at = [P << 10 | i * step for i in range(4)]
         strides = dict(positions_sequence=sequence, positions_head=head, weights_sequence=sequence, weights_head=head)
         assert evict(dict(positions=at[2], weights=at[3], **strides), positions=at[0], weights=at[1], **strides) == 1
