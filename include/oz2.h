@@ -468,7 +468,7 @@ int oz2_context_w4_moe(oz2_context* ctx, const oz2_moe_layer* layer, int64_t t, 
  * in order: query head h reads kv head h / (heads / kv_heads).
  * Sums, maxima and sums of exponentials are FP32; results are rounded once to their type.  A row that sees no key, or none with a score above
  * -infinity, is 0; a NaN or +infinity among the scores that it sees makes it NaN.  What a row does not see never reaches it, whatever it holds.  Equal calls give equal bits.
- * Scores are taken to base 2: scale log2(e) q k beyond 2^126 in size counts as infinite, and beyond 2^25, where FP32 numbers are 4 apart, differences of scores may count up
+ * Scores are taken to base 2: scale log2(e) q k beyond 2^126 in size may count as infinite, and beyond 2^25, where FP32 numbers are 4 apart, differences of scores may count up
  * to twice.
  * scale: above 0, up to 2^126, on a cache up to 2^55.  A result lies behind or before its inputs, or between what they have of two tokens or two heads (parts of one packed tensor): other
  * arrangements are refused, also where they share no byte.  tokens heads <= 2^28, 2^23 (new tokens) on a cache; sequences <= 2^20, 65535 on a cache. */

@@ -154,3 +154,19 @@ def test_scores_of_zero_at_the_largest_scales(name):
     mean = x.double().numpy().mean(0)
     size = np.abs(x.double().numpy()).mean(0)
     assert (np.abs(got.double().cpu().numpy() - mean) <= 400 * U * size + HALF[name] * np.abs(mean)).all()
+
+
+@pytest.mark.parametrize("dim", [64, 100, 255])
+def test_scores_near_the_lowest_number(dim):
+    """in FP32, to base 2 -3.2e38 and 2 % below: the larger ones have all weight"""
+    n = 90
+    rng = np.random.default_rng(dim)
+    large = rng.random(n) < 0.3
+    large[0] = True
+    q, k = torch.zeros((n, 1, dim)), torch.zeros((n, 1, dim))
+    q[:, 0, 0] = -(2.0 ** 70)
+    k[:, 0, 0] = torch.from_numpy(np.where(large, 1.0, 1.02) * 3.2e38 / LOG2E / 2.0 ** 70).float()
+    v = torch.from_numpy(rng.standard_normal((n, 1, dim))).float()
+    got = oz.attention(q.cuda(), k.cuda(), v.cuda(), ints([0, n]), scale=1.0, causal=False).double().cpu().numpy()
+    want, size = v.double().numpy()[large].mean(0), v.abs().double().numpy()[large].mean(0)
+    assert (np.abs(got - want) <= (n + 16) * U * size).all()
