@@ -578,15 +578,16 @@ def _refuse_gradient():
         raise Oz2Error("a tensor requires a gradient, which these products do not form: call them under torch.no_grad(), or with detached tensors")
 
 
-_forward = None
+_forward = None  # torch.autograd.forward_ad, whose _current_level is -1 where no tensor has a tangent
 
 
 def _refuse_tangents(*tensors):
-    """Tensors with a tangent require no gradient, and their tangents would be lost.  There are none but inside a level of forward-mode differentiation."""
+    """Tensors with a tangent require no gradient, and their tangents would be lost.  Called first of all, and inside a level of forward-mode
+    differentiation."""
     global _forward
     if _forward is None:
         import torch.autograd.forward_ad as _forward
-    if getattr(_forward, "_current_level", 0) >= 0 and any(v is not None and _forward.unpack_dual(v).tangent is not None for v in tensors):
+    if any(v is not None and _forward.unpack_dual(v).tangent is not None for v in tensors):
         raise Oz2Error("a tensor has a tangent, which these products do not form: call them with the primal of it")
 
 
@@ -625,7 +626,8 @@ def w4_matvec(W, x, alpha=1.0, beta=0.0, c=None, out=None, stream=None):
     tangent everywhere."""
     if x.requires_grad or W.scales.requires_grad or (c is not None and c.requires_grad) or (out is not None and out.requires_grad):
         _refuse_gradient()
-    _refuse_tangents(x, W.scales, c, out)
+    if _forward is None or _forward._current_level >= 0:
+        _refuse_tangents(x, W.scales, c, out)
     if out is None:
         out = _new(x, (x.shape[0], W.n), x.dtype, stream)
     index = x.get_device()
@@ -678,7 +680,8 @@ def _w4_moe(call, name, first, layer, x, active, out, ids, weights, stream):
     t, index = x.shape[0], x.get_device()
     if any(v is not None and v.requires_grad for v in (x, out, weights, *layer.with_gradient)):
         _refuse_gradient()
-    _refuse_tangents(x, out, weights, *layer.with_gradient)
+    if _forward is None or _forward._current_level >= 0:
+        _refuse_tangents(x, out, weights, *layer.with_gradient)
     if out is None:
         out = _new(x, (t, layer.d), x.dtype, stream)
     if ids is None:
@@ -755,7 +758,8 @@ def _refuse_gradients(*tensors):
     for v in tensors:
         if v is not None and v.requires_grad:
             _refuse_gradient()
-    _refuse_tangents(*tensors)
+    if _forward is None or _forward._current_level >= 0:
+        _refuse_tangents(*tensors)
 
 
 def attention(q, k, v, cu, causal=True, scale=None, out=None, stream=None):
